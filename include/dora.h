@@ -57,7 +57,8 @@ typedef enum {
   DORA_ERR_CAPACITY = -6,    /* an output capacity cannot be represented            */
   DORA_ERR_HIP = -7,         /* the HIP runtime reported an error at launch         */
   DORA_ERR_WORKSPACE = -8,   /* workspace NULL, misaligned or smaller than required */
-  DORA_ERR_STATIC_LIMIT = -9 /* sizes need more than the library's static workspace */
+  DORA_ERR_STATIC_LIMIT = -9, /* sizes need more than the library's static workspace */
+  DORA_ERR_OVERLAP = -10     /* an output overlaps another tensor of the call          */
 } dora_status;
 
 /* Bits OR-ed into *dev_status by the kernels. */
@@ -69,11 +70,15 @@ typedef enum {
 #define DORA_DEV_PLAN 0x10       /* execute called with a workspace not planned for these sizes    */
 #define DORA_DEV_ACTOR 0x20      /* actor decode: a gate-on image without a legal budget or logit row;
                                     it was left unpruned                                           */
+#define DORA_DEV_ACTION 0x40     /* log-probability or policy loss: a row's action is not among its legal
+                                    ones, or none is open; the row was left out                     */
 
 /* Limits of this library. */
 #define DORA_MAX_ROW_TOKENS 2048     /* dora_select_pack: N (tokens per image, CLS included)  */
 #define DORA_MAX_SEQLEN 16384        /* dora_varlen_attn: max_seqlen                          */
 #define DORA_HEAD_DIM 64             /* dora_varlen_attn: D                                   */
+#define DORA_MAX_DECISIONS 16777216  /* dora_action_logprob, dora_policy_loss: T (rows)       */
+#define DORA_MAX_ACTIONS 1048576     /* dora_action_logprob, dora_policy_loss: V (choices)    */
 
 /*
  * dora_select_pack -- hard deletion + packing (Sec. 3.1 Eq. (1); Sec. 3.2
@@ -474,6 +479,162 @@ int dora_varlen_attn_noalloc(const void* q, const void* k, const void* v, const 
                              int32_t B, int32_t H, int32_t D, int32_t max_seqlen, int64_t total,
                              float softmax_scale, dora_dtype dtype, void* out, int32_t* dev_status,
                              void* stream);
+
+/*
+ * dora_action_logprob -- log-probability of the action that each row chose,
+ * and the entropy of its choice, from logits (Sec. 3.2 "Sampling and
+ * deployment": the gate and the budget are categorical choices, the budget
+ * masked to the legal ones).  What scores a rollout under the old and the
+ * reference policy; any head with up to DORA_MAX_ACTIONS choices, a language
+ * model's vocabulary among them.
+ *
+ * Row t, with n = legal[t] open choices (V without `legal`), the first n of
+ * its logits x, and p = softmax over them:
+ *   logprob_out[t] = log p[actions[t]],  entropy_out[t] = -sum p log p
+ * Sums in fp32, the row's own figures in 64 bits; a -inf logit is a choice of
+ * probability 0; infinities and NaN among the n otherwise as in fp32
+ * arithmetic.  Logits at n and past it are not looked at.
+ *
+ *   logits      dtype, T rows of V elements, ld elements apart (ld >= V);
+ *               aligned to the element.
+ *   actions     int32 [T], 0 <= actions[t] < n.
+ *   legal       NULL or int32 [T], 1 <= legal[t] <= V.
+ *   weight      NULL or fp32 [T]: a row of weight 0 is padding.  Nothing else
+ *               of it is looked at; its log-probability and entropy are 0.
+ *   T           1 .. DORA_MAX_DECISIONS; V 1 .. DORA_MAX_ACTIONS.
+ *   logprob_out fp32 [T]; entropy_out NULL or fp32 [T].
+ *   workspace   NULL, or device memory of dora_policy_workspace_size(T, V)
+ *               bytes, 256-byte aligned, no required contents: few long rows
+ *               are then split over several workgroups.  Calls that share a
+ *               workspace must not overlap in time.
+ *   dev_status  DORA_DEV_ACTION for a row whose action or legal count is out
+ *               of range, or whose open logits are all -inf: log-probability
+ *               and entropy NaN.
+ *
+ * Returns DORA_OK or a negative dora_status; enqueues one kernel, or two when
+ * rows are split.
+ */
+size_t dora_policy_workspace_size(int32_t T, int32_t V);  /* 0 when T or V is out of range */
+int dora_action_logprob(const void* logits, int64_t ld, const int32_t* actions, const int32_t* legal,
+                        const float* weight, int32_t T, int32_t V, dora_dtype dtype, float* logprob_out,
+                        float* entropy_out, void* workspace, size_t workspace_bytes, int32_t* dev_status,
+                        void* stream);
+
+/*
+ * dora_policy_loss -- the clipped policy loss with a KL term and an entropy
+ * bonus, and its gradient with respect to the logits, in one call (App. D:
+ * clipped updates of the gate and the budget).
+ *
+ * Row t, with logp and H as dora_action_logprob gives them (here in 64 bits),
+ * A = advantage[t], w = weight[t] (1 without `weight`):
+ *   r    = exp(logp - old_logprob[t])
+ *   gain = min(r A, clip(r, 1 - clip_low, 1 + clip_high) A)
+ *   kl   = exp(ref - logp) - (ref - logp) - 1,  ref = ref_logprob[t] (0 without)
+ *   loss = sum over rows of w (-gain + kl_coef kl - entropy_coef H)
+ *   dlogits[t, j] = d loss / d x_j, rounded once to dtype; 0 for j >= n
+ * The mean over tokens, sequences or images is the weights' matter (1 / count
+ * in each).  old_logprob, ref_logprob and advantage are constants of the
+ * derivative; at coefficient 0 the KL and entropy terms count for nothing
+ * whatever their value.
+ *
+ *   logits, ld, actions, legal, weight, T, V, dtype  as for
+ *               dora_action_logprob.
+ *   old_logprob, advantage  fp32 [T]; ref_logprob NULL (then kl_coef must be
+ *               0) or fp32 [T].
+ *   clip_low    0 .. 1; clip_high >= 0; kl_coef, entropy_coef finite.
+ *   dlogits     dtype, T rows of V elements ld_grad elements apart; may be
+ *               the logits themselves (same address and ld).  Elements between
+ *               rows are left as they were.
+ *   logprob_out fp32 [T].
+ *   stats_out   fp32 [6]: the sums over rows of loss, w gain, w kl, w H,
+ *               w [the clip binds], w.
+ *   workspace   as for dora_action_logprob, but not NULL.
+ *   dev_status  DORA_DEV_ACTION as for dora_action_logprob: log-probability
+ *               NaN, gradient 0, no share in the sums.
+ * Results do not depend on timing: the rows' terms are added in 64 bits in a
+ * fixed order.
+ *
+ * Returns DORA_OK or a negative dora_status (DORA_ERR_OVERLAP when dlogits
+ * overlaps the logits otherwise than above); enqueues two kernels.
+ */
+int dora_policy_loss(const void* logits, int64_t ld, const int32_t* actions, const int32_t* legal,
+                     const float* old_logprob, const float* ref_logprob, const float* advantage, const float* weight,
+                     int32_t T, int32_t V, dora_dtype dtype, float clip_low, float clip_high, float kl_coef,
+                     float entropy_coef, void* dlogits, int64_t ld_grad, float* logprob_out, float* stats_out,
+                     void* workspace, size_t workspace_bytes, int32_t* dev_status, void* stream);
+
+/*
+ * dora_pl_policy_loss -- the clipped policy loss of ordered Plackett-Luce
+ * draws, and its gradient with respect to the removal scores (App. A.3, Eq.
+ * (app-actor-pl); App. D: clipped updates of the selector).
+ *
+ * Image b: logp is the ordered log-probability of its draws (dora_pl_logprob,
+ * here in 64 bits); loss, gain and kl from it as in dora_policy_loss, without
+ * an entropy term.  With S_t the sum of exp over the tokens left before draw t:
+ *   dscores_j = d loss / d logp ([j drawn] - exp(s_j) sum_{t <= tau_j} 1 / S_t)
+ * tau_j the draw that takes j (the last one for a token never drawn), and 0
+ * for CLS and where nothing is drawn.  Scores however far apart keep their
+ * share of the gradient.
+ *
+ *   scores, order, cu_order, cu_in, total_in, B, N  as for dora_pl_logprob.
+ *   old_logprob, ref_logprob, advantage, weight, clip_low, clip_high, kl_coef
+ *               as for dora_policy_loss, one entry per image; an image of
+ *               weight 0 has log-probability 0 and gradient 0, and its scores
+ *               and draws are not looked at.
+ *   dscores     fp32 in the scores' layout, which it may share; rows outside
+ *               every segment are left as they were.
+ *   logprob_out fp32 [B]; stats_out fp32 [6] as for dora_policy_loss.
+ *   workspace   device, 256-byte aligned, dora_pl_policy_workspace_size(B)
+ *               bytes, no required contents; calls that share it must not
+ *               overlap in time.
+ *   dev_status  as for dora_pl_logprob; such an image has log-probability
+ *               NaN, gradient 0 (not written for an invalid segment) and no
+ *               share in the sums.
+ *
+ * Returns DORA_OK or a negative dora_status; enqueues two kernels.
+ */
+size_t dora_pl_policy_workspace_size(int32_t B);  /* 0 when B is out of range */
+int dora_pl_policy_loss(const float* scores, const int32_t* order, const int32_t* cu_order, const int32_t* cu_in,
+                        int64_t total_in, const float* old_logprob, const float* ref_logprob, const float* advantage,
+                        const float* weight, int32_t B, int32_t N, float clip_low, float clip_high, float kl_coef,
+                        float* dscores, float* logprob_out, float* stats_out, void* workspace, size_t workspace_bytes,
+                        int32_t* dev_status, void* stream);
+
+/* One tensor of a list: numel elements of dtype from data on (aligned to the element). */
+typedef struct {
+  void* data;
+  int64_t numel; /* 0: nothing, data may be NULL */
+  int32_t dtype; /* dora_dtype */
+  int32_t reserved;
+} dora_span;
+
+/*
+ * dora_grad_clip -- global norm of many gradient tensors, and clipping by it
+ * (App. D: the actor's gradients are clipped at a global norm).
+ *   norm = sqrt(sum over tensors and elements of g^2)
+ *   c    = min(1, max_norm / (norm + eps)), 1 for norm 0
+ *   out  = c g, rounded once to the tensor's dtype
+ * The squares are added in 64 bits in a fixed order.  NaN or infinite
+ * gradients give a norm that is, and outputs as the formula gives them.
+ *
+ *   grads      HOST array of n spans, read during the call; types may be mixed.
+ *   out        HOST array of n spans with the gradients' sizes and types, or
+ *              NULL: in place.  An output may be its own input and overlaps
+ *              no other tensor (in place, no tensor may be given twice).
+ *   n          1 .. 65536.
+ *   max_norm   >= 0; infinity: only the norm is formed, out is ignored.
+ *   eps        >= 0.
+ *   norm_out   device fp32 [1].
+ *   workspace  device, 256-byte aligned, dora_grad_clip_workspace_size(n)
+ *              bytes, no required contents; calls that share it must not
+ *              overlap in time.
+ *
+ * Returns DORA_OK or a negative dora_status (DORA_ERR_OVERLAP for tensors that
+ * overlap otherwise); enqueues two kernels per 96 tensors.
+ */
+size_t dora_grad_clip_workspace_size(int32_t n); /* 0 when n is out of range */
+int dora_grad_clip(const dora_span* grads, const dora_span* out, int32_t n, float max_norm, float eps,
+                   float* norm_out, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Human-readable name of a dora_status value (static string). */
 const char* dora_status_string(int status);

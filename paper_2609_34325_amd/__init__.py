@@ -39,6 +39,7 @@ DORA_ERR_CAPACITY = -6
 DORA_ERR_HIP = -7
 DORA_ERR_WORKSPACE = -8
 DORA_ERR_STATIC_LIMIT = -9
+DORA_ERR_OVERLAP = -10
 
 DORA_DEV_KEEP_RANGE = 0x1
 DORA_DEV_CAPACITY = 0x2
@@ -47,9 +48,12 @@ DORA_DEV_CU_SEQLENS = 0x8
 DORA_DEV_PLAN = 0x10
 
 DORA_DEV_ACTOR = 0x20
+DORA_DEV_ACTION = 0x40
 DORA_MAX_ROW_TOKENS = 2048
 DORA_MAX_SEQLEN = 16384
 DORA_HEAD_DIM = 64
+DORA_MAX_DECISIONS = 1 << 24
+DORA_MAX_ACTIONS = 1 << 20
 DORA_NOALLOC_WORKSPACE_BYTES = 4 << 20
 
 EXPORTS = (
@@ -68,6 +72,13 @@ EXPORTS = (
     "dora_varlen_attn_execute",
     "dora_varlen_attn",
     "dora_varlen_attn_noalloc",
+    "dora_policy_workspace_size",
+    "dora_action_logprob",
+    "dora_policy_loss",
+    "dora_pl_policy_workspace_size",
+    "dora_pl_policy_loss",
+    "dora_grad_clip_workspace_size",
+    "dora_grad_clip",
     "dora_status_string",
 )
 
@@ -79,6 +90,10 @@ _PACK_OUT = (("idx_out", _I32), ("cu_out", _I32), ("packed_out", _ANY), None)
 _STATUS = (("dev_status", _I32), None)
 _ATTN = (("q", _ANY), ("k", _ANY), ("v", _ANY), ("cu_seqlens", _I32)) + (None,) * 7 + \
     (("out", _ANY), ("workspace", _ANY), None) + _STATUS
+# The rows of logits go by address and leading dimension (strided views are allowed).
+_LOGITS = (None, None, ("actions", _I32), ("legal", _I32))
+_DECISIONS = (("old_logprob", _F32), ("ref_logprob", _F32), ("advantage", _F32), ("weight", _F32))
+_LOSS_OUT = (("logprob_out", _F32), ("stats_out", _F32), ("workspace", _ANY), None) + _STATUS
 _ENTRIES = (
     ("dora_select_pack", _PACK + (("cu_in", _I32),) + (None,) * 5 + _PACK_OUT + _STATUS),
     ("dora_select_pack_plan", _PACK + (("cu_in", _I32),) + (None,) * 5 + _PACK_OUT + (None,) * 3 +
@@ -98,19 +113,33 @@ _ENTRIES = (
     ("dora_varlen_attn_plan", (("cu_seqlens", _I32), None, None, None, None, ("workspace", _ANY), None) + _STATUS),
     ("dora_varlen_attn_execute", _ATTN),
     ("dora_varlen_attn", _ATTN),
+    ("dora_action_logprob", _LOGITS + (("weight", _F32), None, None, None, ("logprob_out", _F32),
+                                       ("entropy_out", _F32), ("workspace", _ANY), None) + _STATUS),
+    ("dora_policy_loss", _LOGITS + _DECISIONS + (None,) * 9 + _LOSS_OUT),
+    ("dora_pl_policy_loss", (("scores", _F32), ("order", _I32), ("cu_order", _I32), ("cu_in", _I32), None) +
+     _DECISIONS + (None,) * 5 + (("dscores", _F32),) + _LOSS_OUT),
+    ("dora_grad_clip", (None,) * 5 + (("norm_out", _F32), ("workspace", _ANY), None, None)),
 )
 _INDEX = {name: i for i, (name, _) in enumerate(_ENTRIES)}
 
-_OPTIONAL = ("cu_in", "budget_logits", "removal_scores", "scores_out", "workspace")
+_OPTIONAL = ("cu_in", "budget_logits", "removal_scores", "scores_out", "workspace", "legal", "weight", "ref_logprob",
+             "entropy_out")
 
 _lib = None
 _native_call = None
+_native_spans = None
 
 
 class FlopsConfig(ctypes.Structure):
     """dora_flops_config of include/dora.h."""
     _fields_ = [(name, ctypes.c_int32) for name in
                 ("d", "L", "N0", "patch", "in_chans", "classes", "head_inputs", "mlp_ratio", "M", "actor")]
+
+
+class Span(ctypes.Structure):
+    """dora_span of include/dora.h."""
+    _fields_ = [("data", ctypes.c_void_p), ("numel", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
 
 
 class DoraError(RuntimeError):
@@ -125,7 +154,7 @@ def _leave_to_ctypes(*args):
 
 def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     """Load libdora.so (built in-tree by ``paper_2609_34325_amd.build``)."""
-    global _lib, _native_call
+    global _lib, _native_call, _native_spans
     if _lib is not None and path is None:
         return _lib
     p = path or LIB_PATH
@@ -169,16 +198,33 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.dora_varlen_attn.argtypes = lib.dora_varlen_attn_execute.argtypes
     lib.dora_varlen_attn_noalloc.restype = ctypes.c_int
     lib.dora_varlen_attn_noalloc.argtypes = lib.dora_varlen_attn_execute.argtypes[:12] + [vp, vp]
+    f32 = ctypes.c_float
+    lib.dora_policy_workspace_size.restype = sz
+    lib.dora_policy_workspace_size.argtypes = [i32, i32]
+    lib.dora_action_logprob.restype = ctypes.c_int
+    lib.dora_action_logprob.argtypes = [vp, i64, vp, vp, vp, i32, i32, ctypes.c_int, vp, vp, vp, sz, vp, vp]
+    lib.dora_policy_loss.restype = ctypes.c_int
+    lib.dora_policy_loss.argtypes = [vp, i64, vp, vp, vp, vp, vp, vp, i32, i32, ctypes.c_int, f32, f32, f32, f32, vp,
+                                     i64, vp, vp, vp, sz, vp, vp]
+    lib.dora_pl_policy_workspace_size.restype = sz
+    lib.dora_pl_policy_workspace_size.argtypes = [i32]
+    lib.dora_pl_policy_loss.restype = ctypes.c_int
+    lib.dora_pl_policy_loss.argtypes = [vp, vp, vp, vp, i64, vp, vp, vp, vp, i32, i32, f32, f32, f32, vp, vp, vp, vp,
+                                        sz, vp, vp]
+    lib.dora_grad_clip_workspace_size.restype = sz
+    lib.dora_grad_clip_workspace_size.argtypes = [i32]
+    lib.dora_grad_clip.restype = ctypes.c_int
+    lib.dora_grad_clip.argtypes = [vp, vp, i32, f32, f32, vp, vp, sz, vp]
     lib.dora_status_string.restype = ctypes.c_char_p
     lib.dora_status_string.argtypes = [ctypes.c_int]
     lib.addresses = tuple(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name, _ in _ENTRIES)
     if _native_call is None:
         try:
-            from ._host_call import call as _native_call
+            from ._host_call import call as _native_call, spans as _native_spans
         except ImportError as e:  # not built, or for another Python or torch
             warnings.warn(f"calls are marshalled by ctypes, about 5 us slower each: {e}; build the native marshalling "
                           "with `python -m paper_2609_34325_amd.build`")
-            _native_call = _leave_to_ctypes
+            _native_call = _native_spans = _leave_to_ctypes
     if path is None:
         _lib = lib
     return lib
@@ -588,3 +634,216 @@ def dora_varlen_attn_noalloc(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, 
         _dev(dev_status, "dev_status", torch.int32), _stream(stream))
     _check("dora_varlen_attn_noalloc", rc)
     return out
+
+
+def _one_device(*tensors) -> None:
+    """The tensors of a call share a device, the current one (whose stream runs it)."""
+    first = tensors[0].device
+    for t in tensors:
+        if t is not None and t.device != first:
+            raise ValueError(f"tensors on {first} and {t.device}")
+    if first.type == "cuda" and first.index != torch._C._cuda_getDevice():
+        raise ValueError(f"tensors on {first}, which is not the current device")
+
+
+def _rows(t: torch.Tensor, name: str):
+    """Address and leading dimension of rows whose elements are adjacent."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor")
+    if t.dim() != 2:
+        raise ValueError(f"{name} must be [T, V]")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be on the GPU")
+    T, V = t.shape
+    ld, one = t.stride()
+    if T <= 1:
+        ld = V
+    if (V > 1 and one != 1) or ld < V:
+        raise ValueError(f"{name} must have adjacent elements in each row, and rows apart")
+    return t.data_ptr(), ld
+
+
+def _per_row(n: int, **tensors) -> None:
+    for name, t in tensors.items():
+        if t is not None and tuple(t.shape) != (n,):
+            raise ValueError(f"{name} must be [{n}]")
+
+
+def _room(t: Optional[torch.Tensor], shape, dtype, device, name: str) -> torch.Tensor:
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+        raise ValueError(f"{name} must be {list(shape)} {dtype}")
+    return t
+
+
+def _bytes(workspace: Optional[torch.Tensor]) -> int:
+    return 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
+def _new_bytes(fn: str, n: int, device) -> torch.Tensor:
+    if n == 0:
+        raise DoraError(fn, DORA_ERR_SHAPE)
+    return torch.empty(n, dtype=torch.uint8, device=device or "cuda")
+
+
+def dora_policy_workspace_size(T: int, V: int) -> int:
+    return int(load_library().dora_policy_workspace_size(int(T), int(V)))
+
+
+def new_policy_workspace(T: int, V: int, device=None) -> torch.Tensor:
+    """A workspace for dora_policy_loss and dora_action_logprob (no required contents)."""
+    return _new_bytes("dora_policy_workspace_size", dora_policy_workspace_size(T, V), device)
+
+
+def dora_action_logprob(logits: torch.Tensor, actions: torch.Tensor, weight: Optional[torch.Tensor] = None,
+                        legal: Optional[torch.Tensor] = None, logprob_out: Optional[torch.Tensor] = None,
+                        entropy_out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                        single: bool = False, dev_status: Optional[torch.Tensor] = None, stream=None):
+    """Log-probability of each row's action, and the entropy of its choice.
+
+    logits: [T, V] bf16 or fp32, elements of a row adjacent, rows any distance
+    apart; actions: int32 [T]; legal: int32 [T], the first legal[t] choices are
+    open; weight: fp32 [T], rows of weight 0 are padding (results 0).  With a
+    workspace (a new one when None) few long rows may be split over several
+    workgroups; single=True passes none.  Returns (logprob [T], entropy [T],
+    dev_status)."""
+    address, ld = _rows(logits, "logits")
+    T, V = (int(n) for n in logits.shape)
+    dev = logits.device
+    _per_row(T, actions=actions, weight=weight, legal=legal)
+    logprob_out = _room(logprob_out, (T,), torch.float32, dev, "logprob_out")
+    entropy_out = _room(entropy_out, (T,), torch.float32, dev, "entropy_out")
+    if single:
+        workspace = None
+    elif workspace is None:
+        workspace = new_policy_workspace(T, V, dev)
+    dev_status = new_status(dev) if dev_status is None else dev_status
+    _one_device(logits, actions, weight, legal, logprob_out, entropy_out, workspace, dev_status)
+    _call("dora_action_logprob", stream, address, ld, actions, legal, weight, T, V, _dtype_code(logits), logprob_out,
+          entropy_out, workspace, _bytes(workspace), dev_status)
+    return logprob_out, entropy_out, dev_status
+
+
+def dora_policy_loss(logits: torch.Tensor, actions: torch.Tensor, old_logprob: torch.Tensor, advantage: torch.Tensor,
+                     ref_logprob: Optional[torch.Tensor] = None, weight: Optional[torch.Tensor] = None,
+                     legal: Optional[torch.Tensor] = None, clip_low: float = 0.2, clip_high: float = 0.2,
+                     kl_coef: float = 0.0, entropy_coef: float = 0.0, dlogits: Optional[torch.Tensor] = None,
+                     logprob_out: Optional[torch.Tensor] = None, stats_out: Optional[torch.Tensor] = None,
+                     workspace: Optional[torch.Tensor] = None, dev_status: Optional[torch.Tensor] = None, stream=None):
+    """The clipped policy loss of T decisions and its gradient.
+
+    logits, actions, weight and legal as for dora_action_logprob; old_logprob,
+    advantage and ref_logprob (needed for kl_coef != 0): fp32 [T].  The loss is
+    the sum over rows of weight * (-min(r A, clip(r) A) + kl_coef * kl -
+    entropy_coef * entropy); for a mean, weight is 1 / count.  dlogits may be
+    the logits themselves.  Returns (dlogits [T, V], logprob [T], stats [6],
+    dev_status); stats holds the sums of loss, gain, kl, entropy, clipped share
+    and weight."""
+    address, ld = _rows(logits, "logits")
+    T, V = (int(n) for n in logits.shape)
+    dev = logits.device
+    _per_row(T, actions=actions, old_logprob=old_logprob, advantage=advantage, ref_logprob=ref_logprob, weight=weight,
+             legal=legal)
+    dlogits = _room(dlogits, (T, V), logits.dtype, dev, "dlogits")
+    grad, ld_grad = _rows(dlogits, "dlogits")
+    logprob_out = _room(logprob_out, (T,), torch.float32, dev, "logprob_out")
+    stats_out = _room(stats_out, (6,), torch.float32, dev, "stats_out")
+    workspace = new_policy_workspace(T, V, dev) if workspace is None else workspace
+    dev_status = new_status(dev) if dev_status is None else dev_status
+    _one_device(logits, actions, old_logprob, advantage, ref_logprob, weight, legal, dlogits, logprob_out, stats_out,
+                workspace, dev_status)
+    _call("dora_policy_loss", stream, address, ld, actions, legal, old_logprob, ref_logprob, advantage, weight, T, V,
+          _dtype_code(logits), float(clip_low), float(clip_high), float(kl_coef), float(entropy_coef), grad, ld_grad,
+          logprob_out, stats_out, workspace, _bytes(workspace), dev_status)
+    return dlogits, logprob_out, stats_out, dev_status
+
+
+def dora_pl_policy_workspace_size(B: int) -> int:
+    return int(load_library().dora_pl_policy_workspace_size(int(B)))
+
+
+def new_pl_policy_workspace(B: int, device=None) -> torch.Tensor:
+    """A workspace for dora_pl_policy_loss (no required contents)."""
+    return _new_bytes("dora_pl_policy_workspace_size", dora_pl_policy_workspace_size(B), device)
+
+
+def dora_pl_policy_loss(scores: torch.Tensor, order: torch.Tensor, cu_order: torch.Tensor, old_logprob: torch.Tensor,
+                        advantage: torch.Tensor, ref_logprob: Optional[torch.Tensor] = None,
+                        weight: Optional[torch.Tensor] = None, cu_in: Optional[torch.Tensor] = None,
+                        N: Optional[int] = None, clip_low: float = 0.2, clip_high: float = 0.2, kl_coef: float = 0.0,
+                        dscores: Optional[torch.Tensor] = None, logprob_out: Optional[torch.Tensor] = None,
+                        stats_out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                        dev_status: Optional[torch.Tensor] = None, stream=None):
+    """The clipped policy loss of ordered Plackett-Luce draws and its gradient
+    with respect to the removal scores: scores, order, cu_order, cu_in and N as
+    for dora_pl_logprob, the rest as for dora_policy_loss, one entry per image.
+    Returns (dscores in the scores' layout, logprob [B], stats [6],
+    dev_status)."""
+    B = int(cu_order.shape[0]) - 1
+    N, total_in = _pl_geometry(scores, B, cu_in, N)
+    dev = scores.device
+    _per_row(B, old_logprob=old_logprob, advantage=advantage, ref_logprob=ref_logprob, weight=weight)
+    dscores = _room(dscores, scores.shape, torch.float32, dev, "dscores")
+    logprob_out = _room(logprob_out, (B,), torch.float32, dev, "logprob_out")
+    stats_out = _room(stats_out, (6,), torch.float32, dev, "stats_out")
+    workspace = new_pl_policy_workspace(B, dev) if workspace is None else workspace
+    dev_status = new_status(dev) if dev_status is None else dev_status
+    _one_device(scores, order, cu_order, cu_in, old_logprob, advantage, ref_logprob, weight, dscores, logprob_out,
+                stats_out, workspace, dev_status)
+    _call("dora_pl_policy_loss", stream, scores, order, cu_order, cu_in, total_in, old_logprob, ref_logprob, advantage,
+          weight, B, N, float(clip_low), float(clip_high), float(kl_coef), dscores, logprob_out, stats_out, workspace,
+          _bytes(workspace), dev_status)
+    return dscores, logprob_out, stats_out, dev_status
+
+
+def dora_grad_clip_workspace_size(n: int) -> int:
+    return int(load_library().dora_grad_clip_workspace_size(int(n)))
+
+
+def new_grad_clip_workspace(n: int, device=None) -> torch.Tensor:
+    """A workspace for dora_grad_clip over n tensors (no required contents)."""
+    return _new_bytes("dora_grad_clip_workspace_size", dora_grad_clip_workspace_size(n), device)
+
+
+def _spans(tensors, name: str):
+    """The tensors' spans and the device that holds them."""
+    tensors = list(tensors)
+    spans = (Span * len(tensors))()
+    if not tensors:
+        raise ValueError(f"{name} is empty")
+    load_library()
+    device = _native_spans(tensors, ctypes.addressof(spans))
+    if device is NotImplemented:
+        for i, t in enumerate(tensors):
+            spans[i] = Span(_dev(t, f"{name}[{i}]"), t.numel(), _dtype_code(t), 0)
+        _one_device(*tensors)
+        device = tensors[0].get_device()
+    return spans, device
+
+
+def dora_grad_clip(grads, max_norm: float, out=None, eps: float = 1e-6, norm_out: Optional[torch.Tensor] = None,
+                   workspace: Optional[torch.Tensor] = None, stream=None):
+    """Scale gradient tensors so that their global norm is at most max_norm.
+
+    grads: contiguous bf16 or fp32 tensors, types may be mixed; out: tensors of
+    the same sizes and types, or None: in place.  Every tensor is multiplied by
+    min(1, max_norm / (norm + eps)); with max_norm = infinity only the norm is
+    formed and nothing is written.  Returns (out, norm [1] fp32)."""
+    grads = list(grads)
+    spans, device = _spans(grads, "grads")
+    out_spans = None
+    if out is not None:
+        out = list(out)
+        if len(out) != len(grads):
+            raise ValueError("out must have a tensor for each of grads")
+        out_spans, out_device = _spans(out, "out")
+        if out_device != device:
+            raise ValueError(f"tensors on devices {device} and {out_device}")
+    dev = grads[0].device
+    norm_out = _room(norm_out, (1,), torch.float32, dev, "norm_out")
+    workspace = new_grad_clip_workspace(len(grads), dev) if workspace is None else workspace
+    _one_device(grads[0], norm_out, workspace)
+    _call("dora_grad_clip", stream, ctypes.addressof(spans), 0 if out_spans is None else ctypes.addressof(out_spans),
+          len(grads), float(max_norm), float(eps), norm_out, workspace, _bytes(workspace))
+    return grads if out is None else out, norm_out

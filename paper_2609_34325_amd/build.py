@@ -7,7 +7,9 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import tempfile
 import warnings
+from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -18,11 +20,16 @@ LIB = os.path.join(PKG, "libdora.so")
 CALIB_LIB = os.path.join(PKG, "libdora_calibrate.so")
 CALIB_SOURCES = ["calibrate.hip"]
 SOURCES = ["select_pack.hip", "varlen_attn.hip", "actor_decode.hip", "pl_sample.hip", "lc1_readout.hip", "flops.hip"]
+POLICY_SOURCES = ["policy_loss.hip", "pl_policy.hip", "grad_clip.hip"]
 # Native marshalling of the Python binding (host code only).
 HOST_LIB = os.path.join(PKG, "_host_call.so")
 ARCH = "gfx950"
 
-HIPCC_FLAGS = [
+# Flags of the policy kernels: the compiler's default scheduling.  They stream
+# rows through memory and live by the waves in flight; the scheduling below,
+# which the other kernels are built with, takes their registers to 160 and
+# more (and ends the compiler on one of them).
+POLICY_FLAGS = [
     f"--offload-arch={ARCH}",
     "-O3",
     "-std=c++17",
@@ -35,12 +42,15 @@ HIPCC_FLAGS = [
     # Queue tickets are taken by one lane; keep the atomic as written so its
     # result is not broadcast to scalar registers (and waited on) at issue.
     "-mllvm", "-amdgpu-atomic-optimizer-strategy=None",
+    "-I", INCLUDE,
+]
+HIPCC_FLAGS = POLICY_FLAGS[:-2] + [
     # The machine scheduler's iterative ILP strategy interleaves the softmax
     # VALU work with the matrix and LDS instructions better than the default
     # occupancy-driven one (DeiT-B attention 51.8 -> 49.1 us, select/pack
     # about 0.6 us faster; no VGPR spills).
     "-mllvm", "-amdgpu-sched-strategy=iterative-ilp",
-    "-I", INCLUDE,
+    *POLICY_FLAGS[-2:],
 ]
 
 
@@ -51,8 +61,8 @@ def hipcc() -> str:
 
 
 def build(verbose: bool = False) -> str:
-    _build_one(SOURCES, LIB, verbose)
-    _build_one(CALIB_SOURCES, CALIB_LIB, verbose)
+    _build_lib([(s, HIPCC_FLAGS) for s in SOURCES] + [(s, POLICY_FLAGS) for s in POLICY_SOURCES], LIB, verbose)
+    _build_lib([(s, HIPCC_FLAGS) for s in CALIB_SOURCES], CALIB_LIB, verbose)
     _build_host(verbose)
     return LIB
 
@@ -88,10 +98,8 @@ def _build_host(verbose: bool) -> None:
     warnings.warn("the native marshalling was not built, calls will go through ctypes:\n" + failed)
 
 
-def _build_one(sources, lib: str, verbose: bool) -> None:
-    srcs = [os.path.join(CSRC, s) for s in sources]
-    tmp = lib + ".tmp%d" % os.getpid()
-    cmd = [hipcc(), *HIPCC_FLAGS, *srcs, "-o", tmp]
+def _hipcc(args, verbose: bool) -> None:
+    cmd = [hipcc(), *args]
     if verbose:
         print(" ".join(cmd), flush=True)
     res = subprocess.run(cmd, capture_output=True, text=True)
@@ -102,6 +110,21 @@ def _build_one(sources, lib: str, verbose: bool) -> None:
         raise RuntimeError("hipcc failed:\n" + "\n".join(msgs))
     if verbose and msgs:
         print("\n".join(msgs))
+
+
+def _build_lib(sources, lib: str, verbose: bool) -> None:
+    """Compile each (source, flags), a few at a time, and link them."""
+    tmp = lib + ".tmp%d" % os.getpid()
+    with tempfile.TemporaryDirectory(dir=PKG, prefix="_build") as objs:
+        def compile_one(item):
+            name, flags = item
+            obj = os.path.join(objs, name + ".o")
+            _hipcc([*(f for f in flags if f != "-shared"), "-c", os.path.join(CSRC, name), "-o", obj], verbose)
+            return obj
+
+        with ThreadPoolExecutor(min(8, os.cpu_count() or 1)) as pool:
+            done = list(pool.map(compile_one, sources))
+        _hipcc([f"--offload-arch={ARCH}", "-fPIC", "-shared", *done, "-o", tmp], verbose)
     os.replace(tmp, lib)
 
 

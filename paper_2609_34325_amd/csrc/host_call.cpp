@@ -115,8 +115,34 @@ const Entry kEntries[] = {
                                a[8].n, a[9].f, type_of(a[10]), a[11].p, a[12].p, static_cast<size_t>(a[13].n),
                                ptr<int32_t>(a[14]), a[15].p);
      }},
+    {"snIifnnnFfanIs",
+     [](void* fn, const Arg* a) {
+       return at_address(dora_action_logprob, fn)(a[0].p, a[1].n, ptr<int32_t>(a[2]), ptr<int32_t>(a[3]), ptr<float>(a[4]),
+                                  i32(a[5]), i32(a[6]), type_of(a[7]), ptr<float>(a[8]), ptr<float>(a[9]), a[10].p,
+                                  static_cast<size_t>(a[11].n), ptr<int32_t>(a[12]), a[13].p);
+     }},
+    {"snIiFfFfnnneeeesnFFAnIs",
+     [](void* fn, const Arg* a) {
+       return at_address(dora_policy_loss, fn)(a[0].p, a[1].n, ptr<int32_t>(a[2]), ptr<int32_t>(a[3]), ptr<float>(a[4]),
+                               ptr<float>(a[5]), ptr<float>(a[6]), ptr<float>(a[7]), i32(a[8]), i32(a[9]),
+                               type_of(a[10]), a[11].f, a[12].f, a[13].f, a[14].f, a[15].p, a[16].n, ptr<float>(a[17]),
+                               ptr<float>(a[18]), a[19].p, static_cast<size_t>(a[20].n), ptr<int32_t>(a[21]), a[22].p);
+     }},
+    {"FIIinFfFfnneeeFFFAnIs",
+     [](void* fn, const Arg* a) {
+       return at_address(dora_pl_policy_loss, fn)(ptr<float>(a[0]), ptr<int32_t>(a[1]), ptr<int32_t>(a[2]), ptr<int32_t>(a[3]),
+                                  a[4].n, ptr<float>(a[5]), ptr<float>(a[6]), ptr<float>(a[7]), ptr<float>(a[8]),
+                                  i32(a[9]), i32(a[10]), a[11].f, a[12].f, a[13].f, ptr<float>(a[14]),
+                                  ptr<float>(a[15]), ptr<float>(a[16]), a[17].p, static_cast<size_t>(a[18].n),
+                                  ptr<int32_t>(a[19]), a[20].p);
+     }},
+    {"ssneeFAns",
+     [](void* fn, const Arg* a) {
+       return at_address(dora_grad_clip, fn)(ptr<dora_span>(a[0]), ptr<dora_span>(a[1]), i32(a[2]), a[3].f, a[4].f,
+                             ptr<float>(a[5]), a[6].p, static_cast<size_t>(a[7].n), a[8].p);
+     }},
 };
-constexpr int kMaxArgs = 20;
+constexpr int kMaxArgs = 24;
 
 bool tensor_arg(PyObject* o, char kind, Arg* out) {
   if (o == Py_None) {
@@ -181,7 +207,37 @@ PyObject* call(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   return PyLong_FromLong(rc);
 }
 
+// spans(tensors, address): writes a dora_span per tensor of the list at the
+// address (the caller's room for them) and returns the device that holds them
+// all, or NotImplemented where the checks in Python should see the list.
+PyObject* spans(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  if (nargs != 2 || !PyList_CheckExact(args[0]) || at::impl::torch_function_mode_enabled()) Py_RETURN_NOTIMPLEMENTED;
+  dora_span* out = static_cast<dora_span*>(PyLong_AsVoidPtr(args[1]));
+  if (out == nullptr) {
+    if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "no room for the spans");
+    return nullptr;
+  }
+  long device = -1;
+  try {
+    for (Py_ssize_t i = 0; i < PyList_GET_SIZE(args[0]); ++i) {
+      PyObject* o = PyList_GET_ITEM(args[0], i);
+      if (!THPVariable_CheckExact(o)) Py_RETURN_NOTIMPLEMENTED;
+      const at::Tensor& t = THPVariable_Unpack(o);
+      const at::ScalarType type = t.scalar_type();
+      if (!t.is_cuda() || !t.is_contiguous() || (type != at::kFloat && type != at::kBFloat16)) Py_RETURN_NOTIMPLEMENTED;
+      if (i > 0 && t.get_device() != device) Py_RETURN_NOTIMPLEMENTED;
+      device = t.get_device();
+      out[i] = dora_span{t.data_ptr(), t.numel(), type == at::kFloat ? DORA_F32 : DORA_BF16, 0};
+    }
+  } catch (...) {
+    Py_RETURN_NOTIMPLEMENTED;
+  }
+  return PyLong_FromLong(device);
+}
+
 PyMethodDef kMethods[] = {
+    {"spans", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(spans)), METH_FASTCALL,
+     "spans(tensors, address): the device, or NotImplemented"},
     {"call", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(call)), METH_FASTCALL,
      "call(index, address, *args): the status, or NotImplemented"},
     {nullptr, nullptr, 0, nullptr}};

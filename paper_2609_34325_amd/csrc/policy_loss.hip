@@ -1,0 +1,414 @@
+// Log-probabilities of chosen actions and the clipped policy loss with its
+// gradient, from logits.  DORA (arXiv 2609.34325): Sec. 3.2 "Sampling and
+// deployment" and App. A.3 (the gate and the budget are categorical choices,
+// the budget masked to the legal ones, a prefix of the grid); App. D (clipped
+// policy updates).  The same loss trains any head that chooses one of V
+// actions per row, up to the vocabulary of a language model.
+//
+// Row t with logits x_j, 0 <= j < n (n legal actions), action a:
+//   m = max x, s = sum exp(x_j - m), logp = x_a - m - log s
+//   H = log s - sum exp(x_j - m)(x_j - m) / s
+//   d loss / d x_j = slope ([j = a] - p_j) + entropy_coef w p_j (log p_j + H)
+// with slope = d loss / d logp (policy_terms.h).
+//
+// One pass over a row keeps a running (m, sum, entropy sum) per lane: a piece
+// of 16 bytes raises m at most once, and the older sums are rescaled then.
+// The lanes' triples are merged the same way.  Sums are fp32, the row's own
+// figures 64 bits.
+#include <algorithm>
+
+#include "dora_internal.h"
+#include "policy_terms.h"
+
+namespace dora {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kMaxGroups = 16384;  // workgroups, each with one set of sums in the workspace
+constexpr float kLog2E = 1.4426950408889634f;
+constexpr double kLn2 = 0.6931471805599453;
+constexpr float kFarDown = -30000.0f;  // exp2 of it is 0, and 0 times it is 0
+
+struct RowParams {
+  const char* logits;
+  int64_t ld;  // elements between rows
+  const int32_t* actions;
+  const int32_t* legal;
+  const float* old;
+  const float* ref;
+  const float* adv;
+  const float* weight;
+  int32_t T, V;
+  PolicyCoef coef;
+  char* grad;
+  int64_t ld_grad;
+  float* logp_out;
+  float* entropy_out;
+  double* parts;  // [workgroups][kPolicyTerms]
+  float* stats;
+  int32_t* status;
+};
+
+// 16 bytes of a row.  Rows start wherever their leading dimension puts them,
+// so pieces are loaded and stored at the element's alignment; the hardware
+// takes unaligned 16-byte accesses and splits those that cross a cache line.
+template <bool BF16>
+struct Elem;
+template <>
+struct Elem<true> {
+  static constexpr int kPer = 8;
+  static constexpr int kBytes = 2;
+  typedef u32x4 __attribute__((aligned(2))) Vec;
+  __device__ static float get(const char* p) {
+    return __uint_as_float(static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(p)) << 16);
+  }
+  __device__ static void put(char* p, float v) { *reinterpret_cast<__bf16*>(p) = static_cast<__bf16>(v); }
+  __device__ static void unpack(u32x4 v, float (&f)[kPer]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f[2 * i] = __uint_as_float(v[i] << 16);
+      f[2 * i + 1] = __uint_as_float(v[i] & 0xFFFF0000u);
+    }
+  }
+  __device__ static u32x4 pack(const float (&f)[kPer]) {
+    bf16x8 b;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) b[i] = static_cast<__bf16>(f[i]);
+    return __builtin_bit_cast(u32x4, b);
+  }
+};
+template <>
+struct Elem<false> {
+  static constexpr int kPer = 4;
+  static constexpr int kBytes = 4;
+  typedef u32x4 __attribute__((aligned(4))) Vec;
+  __device__ static float get(const char* p) { return *reinterpret_cast<const float*>(p); }
+  __device__ static void put(char* p, float v) { *reinterpret_cast<float*>(p) = v; }
+  __device__ static void unpack(u32x4 v, float (&f)[kPer]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = __uint_as_float(v[i]);
+  }
+  __device__ static u32x4 pack(const float (&f)[kPer]) {
+    u32x4 v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = __float_as_uint(f[i]);
+    return v;
+  }
+};
+
+template <bool BF16>
+__device__ __forceinline__ u32x4 load_piece(const char* p) {
+  return *reinterpret_cast<const typename Elem<BF16>::Vec*>(p);
+}
+template <bool BF16>
+__device__ __forceinline__ void store_piece(char* p, u32x4 v) {
+  *reinterpret_cast<typename Elem<BF16>::Vec*>(p) = v;
+}
+
+// A row's exponentials are 2^d with d = x c1 - e, c1 = log2(e) rounded and e
+// the whole number next to m c1: one fused step whose only error is its own
+// rounding, and raising m scales the older sums by a power of two, exactly.
+// The shift in natural units is then e / c1 (in 64 bits): terms near the
+// largest, which make up the sums, all carry c1's rounding alike.
+// Past 5e8 two different floats lie at least 32 apart, so any factor tells
+// them from each other, and m c1 would leave a large rest or overflow: there
+// d = x - m (a row whose open logits all hold the type's lowest value is
+// uniform).
+constexpr float kVast = 5.0e8f;
+struct Shift {
+  float c1, e;
+  __device__ explicit Shift(float m) {
+    const bool vast = fabsf(m) > kVast;
+    c1 = vast ? 1.0f : kLog2E;
+    e = vast ? (m == -__builtin_inff() ? 0.0f : m) : rintf(m * kLog2E);
+  }
+  __device__ float operator()(float x) const { return fmaf(x, c1, -e); }
+  __device__ double natural() const { return static_cast<double>(e) / static_cast<double>(c1); }
+};
+
+// Running softmax statistics: m = max x, s = sum 2^d, h = sum 2^d d.
+// fmaxf passes over NaN, so m never is one; a NaN logit reaches s and h.
+struct Stat {
+  float m, s, h;
+  __device__ void raise(float to) {
+    const bool vast = fabsf(m) > kVast || fabsf(to) > kVast;
+    const float step = vast ? m - to : rintf(m * kLog2E) - rintf(to * kLog2E);
+    const float delta = fmaxf(step, kFarDown);  // also where both are -inf
+    const float f = __builtin_amdgcn_exp2f(delta);
+    h = f * fmaf(s, delta, h);
+    s *= f;
+    m = to;
+  }
+  __device__ void merge(Stat o) {
+    const float to = fmaxf(m, o.m);
+    raise(to);
+    o.raise(to);
+    s += o.s;
+    h += o.h;
+  }
+  template <int N>
+  __device__ void take(const float (&x)[N]) {
+    float top = x[0];
+#pragma unroll
+    for (int i = 1; i < N; ++i) top = fmaxf(top, x[i]);
+    raise(fmaxf(m, top));
+    const Shift sh(m);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float d = sh(x[i]), e = __builtin_amdgcn_exp2f(d);
+      s += e;
+      h = fmaf(e, fmaxf(d, kFarDown), h);
+    }
+  }
+};
+
+// Merged over the L threads of a row; every thread gets the same triple.
+// L <= 64: a group of lanes.  L == kThreads: the workgroup.
+template <int L>
+__device__ __forceinline__ Stat merge_row(Stat a, Stat* s_red) {
+#pragma unroll
+  for (int off = 1; off < (L < 64 ? L : 64); off <<= 1) {
+    const Stat o{__shfl_xor(a.m, off), __shfl_xor(a.s, off), __shfl_xor(a.h, off)};
+    a.merge(o);
+  }
+  if constexpr (L > 64) {
+    const int wave = threadIdx.x >> 6;
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) s_red[wave] = a;
+    __syncthreads();
+    a = s_red[0];
+#pragma unroll
+    for (int w = 1; w < L / 64; ++w) a.merge(s_red[w]);
+  }
+  return a;
+}
+
+// Coefficients of a row's gradient: e (q + k0 + k1 d), and slope more at the action.
+struct RowSlope {
+  float q, k0, k1, slope;
+};
+
+// L threads a row, kThreads / L rows at a time; rows are read once for the
+// statistics and again for the gradient.
+template <bool BF16, int L, bool GRAD>
+__global__ __launch_bounds__(kThreads) void policy_rows_kernel(RowParams p) {
+  using X = Elem<BF16>;
+  constexpr int E = X::kPer, kRows = kThreads / L;
+  __shared__ Stat s_red[kThreads / 64];
+  __shared__ PolicyTerms s_terms[kRows];
+  const int lane = threadIdx.x % L, group = threadIdx.x / L;
+  PolicyTerms sum{};
+  for (int64_t t = static_cast<int64_t>(blockIdx.x) * kRows + group; t < p.T;
+       t += static_cast<int64_t>(gridDim.x) * kRows) {
+    const char* row = p.logits + t * p.ld * X::kBytes;
+    char* out = GRAD ? p.grad + t * p.ld_grad * X::kBytes : nullptr;
+    const float w = p.weight ? p.weight[t] : 1.0f;
+    int n = 0, a = 0;
+    bool good = false;
+    if (w != 0.0f) {
+      n = p.legal ? p.legal[t] : p.V;
+      a = p.actions[t];
+      good = n >= 1 && n <= p.V && a >= 0 && a < n;
+      n = good ? n : 0;
+    }
+    const int whole = n / E;
+    Stat st{-__builtin_inff(), 0.0f, 0.0f};
+    for (int i = lane; i < whole; i += L) {
+      float x[E];
+      X::unpack(load_piece<BF16>(row + static_cast<int64_t>(i) * 16), x);
+      st.take(x);
+    }
+    if (whole * E + lane < n) {
+      const float x[1] = {X::get(row + static_cast<int64_t>(whole * E + lane) * X::kBytes)};
+      st.take(x);
+    }
+    const float xa = good ? X::get(row + static_cast<int64_t>(a) * X::kBytes) : 0.0f;
+    st = merge_row<L>(st, s_red);
+    if (good && st.m == -__builtin_inff() && st.s == 0.0f) good = false;  // nothing open (s is NaN where a logit is)
+    double logp = 0.0, entropy = 0.0;
+    RowSlope rs{0.0f, 0.0f, 0.0f, 0.0f};
+    if (good) {
+      const double logs = log(static_cast<double>(st.s));
+      logp = static_cast<double>(xa) - Shift(st.m).natural() - logs;
+      entropy = logs - static_cast<double>(st.h) / static_cast<double>(st.s) * kLn2;
+      if constexpr (GRAD) {
+        PolicyTerms one{};
+        const double slope = policy_decision(logp, entropy, p.old[t], p.adv[t], w, p.ref, t, p.coef, one);
+        if (lane == 0)
+#pragma unroll
+          for (int i = 0; i < kPolicyTerms; ++i) sum.v[i] += one.v[i];
+        rs.slope = static_cast<float>(slope);
+        rs.q = static_cast<float>(-slope / static_cast<double>(st.s));
+        if (p.coef.entropy != 0.0f) {
+          const double c = static_cast<double>(p.coef.entropy) * w / static_cast<double>(st.s);
+          rs.k0 = static_cast<float>(c * (entropy - logs));
+          rs.k1 = static_cast<float>(c * kLn2);
+        }
+      }
+    } else if (w != 0.0f) {
+      logp = entropy = __builtin_nan("");
+      if (lane == 0) atomicOr(p.status, DORA_DEV_ACTION);
+    }
+    if (lane == 0) {
+      if (p.logp_out) p.logp_out[t] = static_cast<float>(logp);
+      if (p.entropy_out) p.entropy_out[t] = static_cast<float>(entropy);
+    }
+    if constexpr (GRAD) {
+      if (!good) n = 0;
+      const int full = good ? whole : 0;
+      const Shift sh(st.m);
+      const float base = rs.q + rs.k0;
+      auto slope_of = [&](float x) {
+        const float d = sh(x);
+        return __builtin_amdgcn_exp2f(d) * fmaf(rs.k1, fmaxf(d, kFarDown), base);
+      };
+      for (int i = lane; i < full; i += L) {
+        float x[E];
+        X::unpack(load_piece<BF16>(row + static_cast<int64_t>(i) * 16), x);
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] = slope_of(x[e]) + (i * E + e == a ? rs.slope : 0.0f);
+        store_piece<BF16>(out + static_cast<int64_t>(i) * 16, X::pack(x));
+      }
+      for (int j = full * E + lane; j < p.V; j += L) {
+        float g = 0.0f;
+        if (j < n) g = slope_of(X::get(row + static_cast<int64_t>(j) * X::kBytes)) + (j == a ? rs.slope : 0.0f);
+        X::put(out + static_cast<int64_t>(j) * X::kBytes, g);
+      }
+    }
+  }
+  if constexpr (GRAD) {
+    if (lane == 0) s_terms[group] = sum;
+    __syncthreads();
+    if (threadIdx.x < kPolicyTerms) {
+      double v = 0.0;
+      for (int r = 0; r < kRows; ++r) v += s_terms[r].v[threadIdx.x];
+      p.parts[static_cast<int64_t>(blockIdx.x) * kPolicyTerms + threadIdx.x] = v;
+    }
+  }
+}
+
+__global__ __launch_bounds__(kThreads) void policy_finish_kernel(const double* parts, int32_t n, float* stats) {
+  __shared__ double s_sum[kPolicyTerms][kThreads / 64];
+  double v[kPolicyTerms] = {};
+  for (int i = threadIdx.x; i < n; i += kThreads)
+#pragma unroll
+    for (int k = 0; k < kPolicyTerms; ++k) v[k] += parts[static_cast<int64_t>(i) * kPolicyTerms + k];
+#pragma unroll
+  for (int k = 0; k < kPolicyTerms; ++k) {
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) v[k] += __shfl_xor(v[k], off);
+    if ((threadIdx.x & 63) == 0) s_sum[k][threadIdx.x >> 6] = v[k];
+  }
+  __syncthreads();
+  if (threadIdx.x < kPolicyTerms) {
+    double t = 0.0;
+    for (int w = 0; w < kThreads / 64; ++w) t += s_sum[threadIdx.x][w];
+    stats[threadIdx.x] = static_cast<float>(t);
+  }
+}
+
+template <bool BF16, bool GRAD>
+void launch_rows(const RowParams& p, hipStream_t st) {
+  const bool narrow = p.V <= 64 * Elem<BF16>::kPer;
+  const int rows = narrow ? kThreads / 16 : 1;
+  const int groups = static_cast<int>(std::min<int64_t>((static_cast<int64_t>(p.T) + rows - 1) / rows, kMaxGroups));
+  if (narrow) hipLaunchKernelGGL((policy_rows_kernel<BF16, 16, GRAD>), dim3(groups), dim3(kThreads), 0, st, p);
+  else hipLaunchKernelGGL((policy_rows_kernel<BF16, kThreads, GRAD>), dim3(groups), dim3(kThreads), 0, st, p);
+  if constexpr (GRAD) launch_policy_finish(p.parts, groups, p.stats, st);
+}
+
+int check_rows(const void* logits, int64_t ld, const int32_t* actions, int32_t T, int32_t V, dora_dtype dtype,
+               const int32_t* dev_status) {
+  if (!logits || !actions || !dev_status) return DORA_ERR_NULL;
+  if (dtype != DORA_BF16 && dtype != DORA_F32) return DORA_ERR_DTYPE;
+  if (T < 1 || T > DORA_MAX_DECISIONS || V < 1 || V > DORA_MAX_ACTIONS || ld < V || ld > (int64_t{1} << 32))
+    return DORA_ERR_SHAPE;
+  if (reinterpret_cast<uintptr_t>(logits) % (dtype == DORA_BF16 ? 2 : 4)) return DORA_ERR_ALIGN;
+  return DORA_OK;
+}
+
+// Rows of V elements every ld at base against rows every ld_o at other: apart,
+// the same rows, or rows in the gaps of the others.
+bool rows_clash(uintptr_t base, int64_t ld, uintptr_t other, int64_t ld_o, int32_t T, int32_t V, int elt) {
+  const uintptr_t len = (static_cast<uintptr_t>(T - 1) * ld + V) * elt;
+  const uintptr_t len_o = (static_cast<uintptr_t>(T - 1) * ld_o + V) * elt;
+  if (base + len <= other || other + len_o <= base) return false;
+  if (ld != ld_o) return true;
+  if (base == other) return false;
+  const uintptr_t off = (other > base ? other - base : base - other) % (static_cast<uintptr_t>(ld) * elt);
+  const uintptr_t row = static_cast<uintptr_t>(V) * elt;
+  return off < row || off + row > static_cast<uintptr_t>(ld) * elt;
+}
+
+}  // namespace
+
+void launch_policy_finish(const double* parts, int32_t n, float* stats, hipStream_t stream) {
+  hipLaunchKernelGGL(policy_finish_kernel, dim3(1), dim3(kThreads), 0, stream, parts, n, stats);
+}
+
+}  // namespace dora
+
+extern "C" size_t dora_policy_workspace_size(int32_t T, int32_t V) {
+  using namespace dora;
+  if (T < 1 || T > DORA_MAX_DECISIONS || V < 1 || V > DORA_MAX_ACTIONS) return 0;
+  const size_t groups = T < kMaxGroups ? T : kMaxGroups;
+  return (groups * sizeof(PolicyTerms) + 255) & ~size_t(255);
+}
+
+extern "C" int dora_action_logprob(const void* logits, int64_t ld, const int32_t* actions, const int32_t* legal,
+                                   const float* weight, int32_t T, int32_t V, dora_dtype dtype, float* logprob_out,
+                                   float* entropy_out, void* workspace, size_t workspace_bytes, int32_t* dev_status,
+                                   void* stream) {
+  using namespace dora;
+  const int rc = check_rows(logits, ld, actions, T, V, dtype, dev_status);
+  if (rc != DORA_OK) return rc;
+  if (!logprob_out) return DORA_ERR_NULL;
+  if (workspace &&
+      (reinterpret_cast<uintptr_t>(workspace) & 255u || workspace_bytes < dora_policy_workspace_size(T, V)))
+    return DORA_ERR_WORKSPACE;
+  RowParams p{};
+  p.logits = static_cast<const char*>(logits);
+  p.ld = ld;
+  p.actions = actions;
+  p.legal = legal;
+  p.weight = weight;
+  p.T = T;
+  p.V = V;
+  p.logp_out = logprob_out;
+  p.entropy_out = entropy_out;
+  p.status = dev_status;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (dtype == DORA_BF16) launch_rows<true, false>(p, st);
+  else launch_rows<false, false>(p, st);
+  return hipGetLastError() == hipSuccess ? DORA_OK : DORA_ERR_HIP;
+}
+
+extern "C" int dora_policy_loss(const void* logits, int64_t ld, const int32_t* actions, const int32_t* legal,
+                                const float* old_logprob, const float* ref_logprob, const float* advantage,
+                                const float* weight, int32_t T, int32_t V, dora_dtype dtype, float clip_low,
+                                float clip_high, float kl_coef, float entropy_coef, void* dlogits, int64_t ld_grad,
+                                float* logprob_out, float* stats_out, void* workspace, size_t workspace_bytes,
+                                int32_t* dev_status, void* stream) {
+  using namespace dora;
+  const int rc = check_rows(logits, ld, actions, T, V, dtype, dev_status);
+  if (rc != DORA_OK) return rc;
+  if (!old_logprob || !advantage || !dlogits || !logprob_out || !stats_out) return DORA_ERR_NULL;
+  if (ld_grad < V || ld_grad > (int64_t{1} << 32)) return DORA_ERR_SHAPE;
+  if (!(clip_low >= 0.0f && clip_low <= 1.0f && clip_high >= 0.0f)) return DORA_ERR_SHAPE;
+  if (!(kl_coef - kl_coef == 0.0f && entropy_coef - entropy_coef == 0.0f)) return DORA_ERR_SHAPE;
+  if (kl_coef != 0.0f && !ref_logprob) return DORA_ERR_NULL;
+  const int elt = dtype == DORA_BF16 ? 2 : 4;
+  if (reinterpret_cast<uintptr_t>(dlogits) % elt) return DORA_ERR_ALIGN;
+  if (rows_clash(reinterpret_cast<uintptr_t>(logits), ld, reinterpret_cast<uintptr_t>(dlogits), ld_grad, T, V, elt))
+    return DORA_ERR_OVERLAP;
+  if (!workspace || reinterpret_cast<uintptr_t>(workspace) & 255u ||
+      workspace_bytes < dora_policy_workspace_size(T, V))
+    return DORA_ERR_WORKSPACE;
+  RowParams p{static_cast<const char*>(logits), ld, actions, legal, old_logprob, ref_logprob, advantage, weight, T, V,
+              PolicyCoef{clip_low, clip_high, kl_coef, entropy_coef}, static_cast<char*>(dlogits), ld_grad,
+              logprob_out, nullptr, static_cast<double*>(workspace), stats_out, dev_status};
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (dtype == DORA_BF16) launch_rows<true, true>(p, st);
+  else launch_rows<false, true>(p, st);
+  return hipGetLastError() == hipSuccess ? DORA_OK : DORA_ERR_HIP;
+}

@@ -1,0 +1,58 @@
+// The clipped policy loss of one decision, shared by the losses on logits and
+// on ordered Plackett-Luce draws, and the sum of the decisions' terms.
+//
+//   r = exp(logp - old),  gain = min(r A, clip(r, 1 - low, 1 + high) A)
+//   kl = exp(ref - logp) - (ref - logp) - 1     (0 without a reference)
+//   loss = w (-gain + kl_coef kl - entropy_coef H)
+//   slope = w (-r A where the clip does not bind + kl_coef (1 - exp(ref - logp)))
+//
+// slope is d loss / d logp without the entropy's share.  One decision is a few
+// dozen operations beside the thousands of its row, so they are done in 64
+// bits: kl is the small difference of numbers near one, and a ratio's side of
+// the clip's border does not hang on an fp32 rounding.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include "dora.h"
+
+namespace dora {
+
+struct PolicyCoef {
+  float clip_low, clip_high, kl, entropy;
+};
+
+// Sums over decisions, in the order of stats_out.
+constexpr int kPolicyTerms = 6;
+struct PolicyTerms {
+  double v[kPolicyTerms];  // loss, gain, kl, entropy, clipped, weight: each times w
+};
+
+__device__ __forceinline__ double policy_decision(double logp, double entropy, float old, float adv, float w,
+                                                  const float* ref, int64_t row, const PolicyCoef& c,
+                                                  PolicyTerms& sum) {
+  const double r = exp(logp - static_cast<double>(old)), a = adv, wd = w;
+  const double lo = 1.0 - static_cast<double>(c.clip_low), hi = 1.0 + static_cast<double>(c.clip_high);
+  const double held = (r < lo ? lo : (r > hi ? hi : r)) * a, open = r * a;
+  const bool clipped = held < open;
+  const double gain = clipped ? held : open;
+  double slope = clipped ? 0.0 : -open, kl = 0.0;
+  if (ref) {
+    const double d = static_cast<double>(ref[row]) - logp, up = expm1(d);
+    kl = up - d;
+    if (c.kl != 0.0f) slope -= c.kl * up;  // an infinite distance counts for nothing at coefficient 0
+  }
+  sum.v[0] += wd * ((c.kl != 0.0f ? c.kl * kl : 0.0) - gain - (c.entropy != 0.0f ? c.entropy * entropy : 0.0));
+  sum.v[1] += wd * gain;
+  sum.v[2] += wd * kl;
+  sum.v[3] += wd * entropy;
+  sum.v[4] += clipped ? wd : 0.0;
+  sum.v[5] += wd;
+  return wd * slope;
+}
+
+// stats_out from the workgroups' sums, added in a fixed order (one workgroup,
+// launched after the one that wrote them).
+void launch_policy_finish(const double* parts, int32_t n, float* stats, hipStream_t stream);
+
+}  // namespace dora

@@ -1545,6 +1545,7 @@ extern "C" const char* dora_status_string(int status) {
     case DORA_ERR_HIP: return "DORA_ERR_HIP: HIP runtime error at launch";
     case DORA_ERR_WORKSPACE: return "DORA_ERR_WORKSPACE: workspace missing, misaligned or too small";
     case DORA_ERR_STATIC_LIMIT: return "DORA_ERR_STATIC_LIMIT: sizes need more than the library's static workspace";
+    case DORA_ERR_OVERLAP: return "DORA_ERR_OVERLAP: an output overlaps another tensor of the call";
     default: return "unknown dora status";
   }
 }
