@@ -212,7 +212,7 @@ __global__ __launch_bounds__(kThreads) void pl_policy_kernel(PLPolicyParams p) {
 extern "C" size_t dora_pl_policy_workspace_size(int32_t B) {
   using namespace dora;
   if (B < 1 || B > kPlanMaxB) return 0;
-  return (static_cast<size_t>(B) * sizeof(PolicyTerms) + 255) & ~size_t(255);
+  return policy_parts_bytes(B);
 }
 
 extern "C" int dora_pl_policy_loss(const float* scores, const int32_t* order, const int32_t* cu_order,

@@ -24,7 +24,6 @@ namespace dora {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kMaxGroups = 16384;  // workgroups, each with one set of sums in the workspace
 constexpr float kLog2E = 1.4426950408889634f;
 constexpr double kLn2 = 0.6931471805599453;
 constexpr float kFarDown = -30000.0f;  // exp2 of it is 0, and 0 times it is 0
@@ -162,58 +161,107 @@ struct Stat {
   }
 };
 
-// Merged over the L threads of a row; every thread gets the same triple.
-// L <= 64: a group of lanes.  L == kThreads: the workgroup.
-template <int L>
-__device__ __forceinline__ Stat merge_row(Stat a, Stat* s_red) {
+// Merged over groups of G lanes; every lane gets the same triple.
+template <int G>
+__device__ __forceinline__ Stat merge_lanes(Stat a) {
 #pragma unroll
-  for (int off = 1; off < (L < 64 ? L : 64); off <<= 1) {
+  for (int off = 1; off < G; off <<= 1) {
     const Stat o{__shfl_xor(a.m, off), __shfl_xor(a.s, off), __shfl_xor(a.h, off)};
     a.merge(o);
-  }
-  if constexpr (L > 64) {
-    const int wave = threadIdx.x >> 6;
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) s_red[wave] = a;
-    __syncthreads();
-    a = s_red[0];
-#pragma unroll
-    for (int w = 1; w < L / 64; ++w) a.merge(s_red[w]);
   }
   return a;
 }
 
-// Coefficients of a row's gradient: e (q + k0 + k1 d), and slope more at the action.
+// What a row's gradient needs: element j gets 2^d (base + k1 d), d from the
+// shift of m, and slope more at the action; n open elements (0: none).
 struct RowSlope {
-  float q, k0, k1, slope;
+  float m, base, k1, slope;
+  int n, action;
 };
 
-// L threads a row, kThreads / L rows at a time; rows are read once for the
-// statistics and again for the gradient.
-template <bool BF16, int L, bool GRAD>
-__global__ __launch_bounds__(kThreads) void policy_rows_kernel(RowParams p) {
+// The row's own figures, by every lane that calls it; `first` is the lane that
+// writes them and adds the row's terms to sum.
+template <bool GRAD>
+__device__ __forceinline__ RowSlope close_row(const RowParams& p, int64_t t, float w, int n, int a, float xa, Stat st,
+                                              bool first, PolicyTerms* sum) {
+  bool good = n > 0;
+  if (good && st.m == -__builtin_inff() && st.s == 0.0f) good = false;  // nothing open (s is NaN where a logit is)
+  double logp = 0.0, entropy = 0.0;
+  RowSlope rs{st.m, 0.0f, 0.0f, 0.0f, 0, a};
+  if (good) {
+    const double s = st.s, logs = log(s);
+    logp = static_cast<double>(xa) - Shift(st.m).natural() - logs;
+    entropy = logs - static_cast<double>(st.h) / s * kLn2;
+    if constexpr (GRAD) {
+      PolicyTerms one{};
+      const double slope = policy_decision(logp, entropy, p.old[t], p.adv[t], w, p.ref, t, p.coef, one);
+      if (first)
+#pragma unroll
+        for (int i = 0; i < kPolicyTerms; ++i) sum->v[i] += one.v[i];
+      const double c = static_cast<double>(p.coef.entropy) * w;
+      rs.n = n;
+      rs.slope = static_cast<float>(slope);
+      rs.base = static_cast<float>(((p.coef.entropy != 0.0f ? c * (entropy - logs) : 0.0) - slope) / s);
+      rs.k1 = p.coef.entropy != 0.0f ? static_cast<float>(c * kLn2 / s) : 0.0f;
+    }
+  } else if (w != 0.0f) {
+    logp = entropy = __builtin_nan("");
+    if (first) atomicOr(p.status, DORA_DEV_ACTION);
+  }
+  if (first) {
+    if (p.logp_out) p.logp_out[t] = static_cast<float>(logp);
+    if (p.entropy_out) p.entropy_out[t] = static_cast<float>(entropy);
+  }
+  return rs;
+}
+
+// L threads a row.  Each holds its first NV pieces (thread i: pieces i, i + L,
+// ...) in registers from the statistics to the gradient, so that a row of up
+// to L NV pieces is read once; what is past them is read again.  A
+// workgroup holds max(1, 256 / L) rows.
+template <bool BF16, int L, int NV, bool GRAD>
+__global__ __launch_bounds__((L > kThreads ? L : kThreads), 4) void policy_rows_kernel(RowParams p) {
   using X = Elem<BF16>;
-  constexpr int E = X::kPer, kRows = kThreads / L;
-  __shared__ Stat s_red[kThreads / 64];
+  constexpr int E = X::kPer, kWG = L > kThreads ? L : kThreads, kRows = kWG / L, kWaves = L / 64;
   __shared__ PolicyTerms s_terms[kRows];
+  __shared__ Stat s_red[L > 64 ? kWaves : 1];
+  __shared__ RowSlope s_slope;
   const int lane = threadIdx.x % L, group = threadIdx.x / L;
-  PolicyTerms sum{};
-  for (int64_t t = static_cast<int64_t>(blockIdx.x) * kRows + group; t < p.T;
-       t += static_cast<int64_t>(gridDim.x) * kRows) {
+  if (GRAD && lane == 0) s_terms[group] = PolicyTerms{};
+  // A workgroup ends with its rows.  (In a loop over rows the compiler keeps
+  // the constants of the 64-bit functions in registers, which the rows need:
+  // up to 256 of them, and the longest spill.)
+  const int64_t t = static_cast<int64_t>(blockIdx.x) * kRows + group;
+  if (t < p.T) {
     const char* row = p.logits + t * p.ld * X::kBytes;
-    char* out = GRAD ? p.grad + t * p.ld_grad * X::kBytes : nullptr;
     const float w = p.weight ? p.weight[t] : 1.0f;
     int n = 0, a = 0;
-    bool good = false;
     if (w != 0.0f) {
       n = p.legal ? p.legal[t] : p.V;
       a = p.actions[t];
-      good = n >= 1 && n <= p.V && a >= 0 && a < n;
-      n = good ? n : 0;
+      if (!(n >= 1 && n <= p.V && a >= 0 && a < n)) n = 0;
     }
     const int whole = n / E;
     Stat st{-__builtin_inff(), 0.0f, 0.0f};
-    for (int i = lane; i < whole; i += L) {
+    u32x4 held[NV];
+    if (whole > 0) {  // the same for all threads of a row
+      // Loads are unconditional (a piece past the last one is the last one
+      // again), so that they are counted and waited for one by one.
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+        held[i] = load_piece<BF16>(row + static_cast<int64_t>(min(lane + i * L, whole - 1)) * 16);
+      asm volatile("" ::: "memory");
+    }
+    const float xa = n > 0 ? X::get(row + static_cast<int64_t>(a) * X::kBytes) : 0.0f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      if (lane + i * L < whole) {
+        float x[E];
+        X::unpack(held[i], x);
+        st.take(x);
+      }
+    }
+    for (int i = lane + NV * L; i < whole; i += L) {
       float x[E];
       X::unpack(load_piece<BF16>(row + static_cast<int64_t>(i) * 16), x);
       st.take(x);
@@ -222,62 +270,55 @@ __global__ __launch_bounds__(kThreads) void policy_rows_kernel(RowParams p) {
       const float x[1] = {X::get(row + static_cast<int64_t>(whole * E + lane) * X::kBytes)};
       st.take(x);
     }
-    const float xa = good ? X::get(row + static_cast<int64_t>(a) * X::kBytes) : 0.0f;
-    st = merge_row<L>(st, s_red);
-    if (good && st.m == -__builtin_inff() && st.s == 0.0f) good = false;  // nothing open (s is NaN where a logit is)
-    double logp = 0.0, entropy = 0.0;
-    RowSlope rs{0.0f, 0.0f, 0.0f, 0.0f};
-    if (good) {
-      const double logs = log(static_cast<double>(st.s));
-      logp = static_cast<double>(xa) - Shift(st.m).natural() - logs;
-      entropy = logs - static_cast<double>(st.h) / static_cast<double>(st.s) * kLn2;
-      if constexpr (GRAD) {
-        PolicyTerms one{};
-        const double slope = policy_decision(logp, entropy, p.old[t], p.adv[t], w, p.ref, t, p.coef, one);
-        if (lane == 0)
-#pragma unroll
-          for (int i = 0; i < kPolicyTerms; ++i) sum.v[i] += one.v[i];
-        rs.slope = static_cast<float>(slope);
-        rs.q = static_cast<float>(-slope / static_cast<double>(st.s));
-        if (p.coef.entropy != 0.0f) {
-          const double c = static_cast<double>(p.coef.entropy) * w / static_cast<double>(st.s);
-          rs.k0 = static_cast<float>(c * (entropy - logs));
-          rs.k1 = static_cast<float>(c * kLn2);
-        }
+    RowSlope rs;
+    if constexpr (L <= 64) {
+      rs = close_row<GRAD>(p, t, w, n, a, xa, merge_lanes<L>(st), lane == 0, &s_terms[group]);
+    } else {
+      // One wave closes the row: 64-bit exp and log by all of them would cost
+      // as much as the row's own exponentials.
+      st = merge_lanes<64>(st);
+      if ((threadIdx.x & 63) == 0) s_red[threadIdx.x >> 6] = st;
+      __syncthreads();
+      if (threadIdx.x < 64) {
+        st = merge_lanes<kWaves>(s_red[threadIdx.x % kWaves]);
+        rs = close_row<GRAD>(p, t, w, n, a, xa, st, threadIdx.x == 0, &s_terms[0]);
+        if (GRAD && threadIdx.x == 0) s_slope = rs;
       }
-    } else if (w != 0.0f) {
-      logp = entropy = __builtin_nan("");
-      if (lane == 0) atomicOr(p.status, DORA_DEV_ACTION);
-    }
-    if (lane == 0) {
-      if (p.logp_out) p.logp_out[t] = static_cast<float>(logp);
-      if (p.entropy_out) p.entropy_out[t] = static_cast<float>(entropy);
+      __syncthreads();
+      if constexpr (GRAD) rs = s_slope;
     }
     if constexpr (GRAD) {
-      if (!good) n = 0;
-      const int full = good ? whole : 0;
-      const Shift sh(st.m);
-      const float base = rs.q + rs.k0;
+      char* out = p.grad + t * p.ld_grad * X::kBytes;
+      const Shift sh(rs.m);
       auto slope_of = [&](float x) {
         const float d = sh(x);
-        return __builtin_amdgcn_exp2f(d) * fmaf(rs.k1, fmaxf(d, kFarDown), base);
+        return __builtin_amdgcn_exp2f(d) * fmaf(rs.k1, fmaxf(d, kFarDown), rs.base);
       };
-      for (int i = lane; i < full; i += L) {
+      auto put = [&](u32x4 v, int i) {
         float x[E];
-        X::unpack(load_piece<BF16>(row + static_cast<int64_t>(i) * 16), x);
+        X::unpack(v, x);
 #pragma unroll
-        for (int e = 0; e < E; ++e) x[e] = slope_of(x[e]) + (i * E + e == a ? rs.slope : 0.0f);
+        for (int e = 0; e < E; ++e) x[e] = slope_of(x[e]) + (i * E + e == rs.action ? rs.slope : 0.0f);
         store_piece<BF16>(out + static_cast<int64_t>(i) * 16, X::pack(x));
-      }
+      };
+      // Opaque to the compiler, which would otherwise keep the pieces unpacked
+      // (twice the registers) from the statistics on.
+#pragma unroll
+      for (int i = 0; i < NV; ++i) asm volatile("" : "+v"(held[i]));
+      const int full = rs.n / E;
+      for (int i = lane + NV * L; i < full; i += L) put(load_piece<BF16>(row + static_cast<int64_t>(i) * 16), i);
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+        if (lane + i * L < full) put(held[i], lane + i * L);
       for (int j = full * E + lane; j < p.V; j += L) {
         float g = 0.0f;
-        if (j < n) g = slope_of(X::get(row + static_cast<int64_t>(j) * X::kBytes)) + (j == a ? rs.slope : 0.0f);
+        if (j < rs.n)
+          g = slope_of(X::get(row + static_cast<int64_t>(j) * X::kBytes)) + (j == rs.action ? rs.slope : 0.0f);
         X::put(out + static_cast<int64_t>(j) * X::kBytes, g);
       }
     }
   }
   if constexpr (GRAD) {
-    if (lane == 0) s_terms[group] = sum;
     __syncthreads();
     if (threadIdx.x < kPolicyTerms) {
       double v = 0.0;
@@ -287,12 +328,16 @@ __global__ __launch_bounds__(kThreads) void policy_rows_kernel(RowParams p) {
   }
 }
 
-__global__ __launch_bounds__(kThreads) void policy_finish_kernel(const double* parts, int32_t n, float* stats) {
+// Sums of the terms of workgroups [blockIdx per_group, + per_group) of n, to
+// out[blockIdx] or, rounded, to stats.
+__global__ __launch_bounds__(kThreads) void policy_finish_kernel(const double* parts, int32_t n, int32_t per_group,
+                                                                 double* out, float* stats) {
   __shared__ double s_sum[kPolicyTerms][kThreads / 64];
   double v[kPolicyTerms] = {};
-  for (int i = threadIdx.x; i < n; i += kThreads)
+  const int64_t lo = static_cast<int64_t>(blockIdx.x) * per_group, hi = min(static_cast<int64_t>(n), lo + per_group);
+  for (int64_t i = lo + threadIdx.x; i < hi; i += kThreads)
 #pragma unroll
-    for (int k = 0; k < kPolicyTerms; ++k) v[k] += parts[static_cast<int64_t>(i) * kPolicyTerms + k];
+    for (int k = 0; k < kPolicyTerms; ++k) v[k] += parts[i * kPolicyTerms + k];
 #pragma unroll
   for (int k = 0; k < kPolicyTerms; ++k) {
 #pragma unroll
@@ -303,18 +348,44 @@ __global__ __launch_bounds__(kThreads) void policy_finish_kernel(const double* p
   if (threadIdx.x < kPolicyTerms) {
     double t = 0.0;
     for (int w = 0; w < kThreads / 64; ++w) t += s_sum[threadIdx.x][w];
-    stats[threadIdx.x] = static_cast<float>(t);
+    if (stats) stats[threadIdx.x] = static_cast<float>(t);
+    else out[static_cast<int64_t>(blockIdx.x) * kPolicyTerms + threadIdx.x] = t;
   }
 }
 
+template <bool BF16, bool GRAD, int L, int NV>
+void launch_shape(const RowParams& p, hipStream_t st) {
+  constexpr int kWG = L > kThreads ? L : kThreads, kRows = kWG / L;
+  const int groups = (p.T + kRows - 1) / kRows;
+  hipLaunchKernelGGL((policy_rows_kernel<BF16, L, NV, GRAD>), dim3(groups), dim3(kWG), 0, st, p);
+  if constexpr (GRAD) launch_policy_finish(p.parts, groups, p.stats, st);
+}
+
+// The fewest threads a row that hold it in 16 pieces each: short rows share a
+// wave, and the threads left over take other rows.
 template <bool BF16, bool GRAD>
 void launch_rows(const RowParams& p, hipStream_t st) {
-  const bool narrow = p.V <= 64 * Elem<BF16>::kPer;
-  const int rows = narrow ? kThreads / 16 : 1;
-  const int groups = static_cast<int>(std::min<int64_t>((static_cast<int64_t>(p.T) + rows - 1) / rows, kMaxGroups));
-  if (narrow) hipLaunchKernelGGL((policy_rows_kernel<BF16, 16, GRAD>), dim3(groups), dim3(kThreads), 0, st, p);
-  else hipLaunchKernelGGL((policy_rows_kernel<BF16, kThreads, GRAD>), dim3(groups), dim3(kThreads), 0, st, p);
-  if constexpr (GRAD) launch_policy_finish(p.parts, groups, p.stats, st);
+  const int pieces = (p.V + Elem<BF16>::kPer - 1) / Elem<BF16>::kPer;
+  if (pieces <= 16) launch_shape<BF16, GRAD, 16, 1>(p, st);
+  else if (pieces <= 32) launch_shape<BF16, GRAD, 16, 2>(p, st);
+  else if (pieces <= 64) launch_shape<BF16, GRAD, 16, 4>(p, st);
+  else if (pieces <= 256) launch_shape<BF16, GRAD, 64, 4>(p, st);
+  else if (pieces <= 512) launch_shape<BF16, GRAD, 64, 8>(p, st);
+  else if (pieces <= 1024) launch_shape<BF16, GRAD, 256, 4>(p, st);
+  else if (pieces <= 2048) launch_shape<BF16, GRAD, 256, 8>(p, st);
+  else if (pieces <= 4096) launch_shape<BF16, GRAD, 256, 16>(p, st);
+  else if (pieces <= 6144) launch_shape<BF16, GRAD, 512, 12>(p, st);
+  else if (pieces <= 8192) launch_shape<BF16, GRAD, 512, 16>(p, st);
+  else if (pieces <= 12288) launch_shape<BF16, GRAD, 1024, 12>(p, st);
+  else launch_shape<BF16, GRAD, 1024, 16>(p, st);
+}
+
+// Sets of sums that the workgroups of T rows of V elements write (of the
+// element type that has fewer rows a workgroup).
+int32_t row_groups(int32_t T, int32_t V) {
+  const int pieces = (V + 3) / 4;
+  const int rows = pieces <= 64 ? kThreads / 16 : (pieces <= 512 ? kThreads / 64 : 1);
+  return (T + rows - 1) / rows;
 }
 
 int check_rows(const void* logits, int64_t ld, const int32_t* actions, int32_t T, int32_t V, dora_dtype dtype,
@@ -342,8 +413,15 @@ bool rows_clash(uintptr_t base, int64_t ld, uintptr_t other, int64_t ld_o, int32
 
 }  // namespace
 
-void launch_policy_finish(const double* parts, int32_t n, float* stats, hipStream_t stream) {
-  hipLaunchKernelGGL(policy_finish_kernel, dim3(1), dim3(kThreads), 0, stream, parts, n, stats);
+void launch_policy_finish(double* parts, int32_t n, float* stats, hipStream_t stream) {
+  if (n > kFinishDirect) {
+    const int32_t each = (n + kFinishGroups - 1) / kFinishGroups, groups = (n + each - 1) / each;
+    double* mid = parts + static_cast<int64_t>(n) * kPolicyTerms;
+    hipLaunchKernelGGL(policy_finish_kernel, dim3(groups), dim3(kThreads), 0, stream, parts, n, each, mid, nullptr);
+    parts = mid;
+    n = groups;
+  }
+  hipLaunchKernelGGL(policy_finish_kernel, dim3(1), dim3(kThreads), 0, stream, parts, n, n, nullptr, stats);
 }
 
 }  // namespace dora
@@ -351,8 +429,7 @@ void launch_policy_finish(const double* parts, int32_t n, float* stats, hipStrea
 extern "C" size_t dora_policy_workspace_size(int32_t T, int32_t V) {
   using namespace dora;
   if (T < 1 || T > DORA_MAX_DECISIONS || V < 1 || V > DORA_MAX_ACTIONS) return 0;
-  const size_t groups = T < kMaxGroups ? T : kMaxGroups;
-  return (groups * sizeof(PolicyTerms) + 255) & ~size_t(255);
+  return policy_parts_bytes(row_groups(T, V));
 }
 
 extern "C" int dora_action_logprob(const void* logits, int64_t ld, const int32_t* actions, const int32_t* legal,
