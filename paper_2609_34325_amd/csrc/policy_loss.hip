@@ -24,6 +24,7 @@ namespace dora {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kMaxSplit = 64;  // workgroups a row
 constexpr float kLog2E = 1.4426950408889634f;
 constexpr double kLn2 = 0.6931471805599453;
 constexpr float kFarDown = -30000.0f;  // exp2 of it is 0, and 0 times it is 0
@@ -44,6 +45,8 @@ struct RowParams {
   float* logp_out;
   float* entropy_out;
   double* parts;  // [workgroups][kPolicyTerms]
+  float4* split_stats;  // split rows: [T][split] of (m, s, h)
+  int32_t split;        // workgroups a row
   float* stats;
   int32_t* status;
 };
@@ -125,6 +128,16 @@ struct Shift {
   __device__ double natural() const { return static_cast<double>(e) / static_cast<double>(c1); }
 };
 
+// Open elements of row t (0: padding or a bad row), its weight and action.
+__device__ __forceinline__ int open_row(const RowParams& p, int64_t t, float& w, int& a) {
+  w = p.weight ? p.weight[t] : 1.0f;
+  a = 0;
+  if (w == 0.0f) return 0;
+  const int n = p.legal ? p.legal[t] : p.V;
+  a = p.actions[t];
+  return n >= 1 && n <= p.V && a >= 0 && a < n ? n : 0;
+}
+
 // Running softmax statistics: m = max x, s = sum 2^d, h = sum 2^d d.
 // fmaxf passes over NaN, so m never is one; a NaN logit reaches s and h.
 struct Stat {
@@ -177,6 +190,27 @@ __device__ __forceinline__ Stat merge_lanes(Stat a) {
 struct RowSlope {
   float m, base, k1, slope;
   int n, action;
+};
+
+// The gradient's elements from the logits'.
+struct Slope {
+  Shift sh;
+  RowSlope rs;
+  __device__ explicit Slope(const RowSlope& r) : sh(r.m), rs(r) {}
+  __device__ float open(float x, int j) const {
+    const float d = sh(x);
+    return __builtin_amdgcn_exp2f(d) * fmaf(rs.k1, fmaxf(d, kFarDown), rs.base) + (j == rs.action ? rs.slope : 0.0f);
+  }
+  __device__ float at(float x, int j) const { return j < rs.n ? open(x, j) : 0.0f; }
+  template <bool BF16>
+  __device__ u32x4 piece(u32x4 v, int i) const {
+    constexpr int E = Elem<BF16>::kPer;
+    float x[E];
+    Elem<BF16>::unpack(v, x);
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[e] = open(x[e], i * E + e);
+    return Elem<BF16>::pack(x);
+  }
 };
 
 // The row's own figures, by every lane that calls it; `first` is the lane that
@@ -234,13 +268,9 @@ __global__ __launch_bounds__((L > kThreads ? L : kThreads), 4) void policy_rows_
   const int64_t t = static_cast<int64_t>(blockIdx.x) * kRows + group;
   if (t < p.T) {
     const char* row = p.logits + t * p.ld * X::kBytes;
-    const float w = p.weight ? p.weight[t] : 1.0f;
-    int n = 0, a = 0;
-    if (w != 0.0f) {
-      n = p.legal ? p.legal[t] : p.V;
-      a = p.actions[t];
-      if (!(n >= 1 && n <= p.V && a >= 0 && a < n)) n = 0;
-    }
+    float w;
+    int a;
+    const int n = open_row(p, t, w, a);
     const int whole = n / E;
     Stat st{-__builtin_inff(), 0.0f, 0.0f};
     u32x4 held[NV];
@@ -289,17 +319,9 @@ __global__ __launch_bounds__((L > kThreads ? L : kThreads), 4) void policy_rows_
     }
     if constexpr (GRAD) {
       char* out = p.grad + t * p.ld_grad * X::kBytes;
-      const Shift sh(rs.m);
-      auto slope_of = [&](float x) {
-        const float d = sh(x);
-        return __builtin_amdgcn_exp2f(d) * fmaf(rs.k1, fmaxf(d, kFarDown), rs.base);
-      };
+      const Slope slope(rs);
       auto put = [&](u32x4 v, int i) {
-        float x[E];
-        X::unpack(v, x);
-#pragma unroll
-        for (int e = 0; e < E; ++e) x[e] = slope_of(x[e]) + (i * E + e == rs.action ? rs.slope : 0.0f);
-        store_piece<BF16>(out + static_cast<int64_t>(i) * 16, X::pack(x));
+        store_piece<BF16>(out + static_cast<int64_t>(i) * 16, slope.template piece<BF16>(v, i));
       };
       // Opaque to the compiler, which would otherwise keep the pieces unpacked
       // (twice the registers) from the statistics on.
@@ -311,10 +333,8 @@ __global__ __launch_bounds__((L > kThreads ? L : kThreads), 4) void policy_rows_
       for (int i = 0; i < NV; ++i)
         if (lane + i * L < full) put(held[i], lane + i * L);
       for (int j = full * E + lane; j < p.V; j += L) {
-        float g = 0.0f;
-        if (j < rs.n)
-          g = slope_of(X::get(row + static_cast<int64_t>(j) * X::kBytes)) + (j == rs.action ? rs.slope : 0.0f);
-        X::put(out + static_cast<int64_t>(j) * X::kBytes, g);
+        const float x = j < rs.n ? X::get(row + static_cast<int64_t>(j) * X::kBytes) : 0.0f;
+        X::put(out + static_cast<int64_t>(j) * X::kBytes, slope.at(x, j));
       }
     }
   }
@@ -325,6 +345,138 @@ __global__ __launch_bounds__((L > kThreads ? L : kThreads), 4) void policy_rows_
       for (int r = 0; r < kRows; ++r) v += s_terms[r].v[threadIdx.x];
       p.parts[static_cast<int64_t>(blockIdx.x) * kPolicyTerms + threadIdx.x] = v;
     }
+  }
+}
+
+// Statistics of the pieces [lo, hi) of a row and, if `end`, of the elements
+// behind its last piece.  Four pieces in flight a thread.
+template <bool BF16>
+__device__ __forceinline__ Stat range_stats(const char* row, int lo, int hi, bool end, int n) {
+  using X = Elem<BF16>;
+  constexpr int kFlight = 4;
+  Stat st{-__builtin_inff(), 0.0f, 0.0f};
+  for (int i = lo + threadIdx.x; i < hi; i += kFlight * kThreads) {
+    u32x4 v[kFlight];
+#pragma unroll
+    for (int k = 0; k < kFlight; ++k)
+      v[k] = load_piece<BF16>(row + static_cast<int64_t>(min(i + k * kThreads, hi - 1)) * 16);
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int k = 0; k < kFlight; ++k) {
+      if (i + k * kThreads < hi) {
+        float x[X::kPer];
+        X::unpack(v[k], x);
+        st.take(x);
+      }
+    }
+  }
+  const int j = n / X::kPer * X::kPer + threadIdx.x;
+  if (end && j < n) {
+    const float x[1] = {X::get(row + static_cast<int64_t>(j) * X::kBytes)};
+    st.take(x);
+  }
+  return st;
+}
+
+// This workgroup's share of the pieces of a row of V elements (of n open ones).
+template <bool BF16>
+__device__ __forceinline__ int2 chunk_of(const RowParams& p, int chunk, int n) {
+  constexpr int E = Elem<BF16>::kPer;
+  const int each = (p.V / E + p.split - 1) / p.split, whole = n / E;
+  return make_int2(min(whole, chunk * each), min(whole, (chunk + 1) * each));
+}
+
+// Statistics of long rows, p.split workgroups a row.  One a row: it closes the
+// row (log-probability only).  Several: each leaves its triple for the next launch.
+template <bool BF16>
+__global__ __launch_bounds__(kThreads) void policy_stats_kernel(RowParams p) {
+  __shared__ Stat s_red[kThreads / 64];
+  const int64_t t = blockIdx.x / p.split;
+  const int chunk = blockIdx.x % p.split;
+  float w;
+  int a;
+  const int n = open_row(p, t, w, a);
+  const char* row = p.logits + t * p.ld * Elem<BF16>::kBytes;
+  const int2 c = chunk_of<BF16>(p, chunk, n);
+  Stat st = merge_lanes<64>(range_stats<BF16>(row, c.x, c.y, chunk == p.split - 1, n));
+  if ((threadIdx.x & 63) == 0) s_red[threadIdx.x >> 6] = st;
+  __syncthreads();
+  if (threadIdx.x >= 64) return;
+  st = merge_lanes<kThreads / 64>(s_red[threadIdx.x % (kThreads / 64)]);
+  const float xa = n > 0 ? Elem<BF16>::get(row + static_cast<int64_t>(a) * Elem<BF16>::kBytes) : 0.0f;
+  if (p.split > 1) {
+    if (threadIdx.x == 0) p.split_stats[blockIdx.x] = make_float4(st.m, st.s, st.h, xa);
+    return;
+  }
+  close_row<false>(p, t, w, n, a, xa, st, threadIdx.x == 0, nullptr);
+}
+
+// Row t closed from its workgroups' triples by a group of G lanes.
+template <bool GRAD, int G>
+__device__ __forceinline__ RowSlope close_split_row(const RowParams& p, int64_t t, bool writes, PolicyTerms* sum) {
+  constexpr int kEach = kMaxSplit / G;
+  const int lane = threadIdx.x % G;
+  const float4* from = p.split_stats + t * p.split;
+  float4 v[kEach];
+#pragma unroll
+  for (int k = 0; k < kEach; ++k) v[k] = from[min(lane + k * G, p.split - 1)];
+  float w;
+  int a;
+  const int n = open_row(p, t, w, a);
+  Stat st{-__builtin_inff(), 0.0f, 0.0f};
+#pragma unroll
+  for (int k = 0; k < kEach; ++k)
+    if (lane + k * G < p.split) st.merge(Stat{v[k].x, v[k].y, v[k].z});
+  return close_row<GRAD>(p, t, w, n, a, v[0].w, merge_lanes<G>(st), writes && lane == 0, sum);
+}
+
+// Log-probabilities of split rows.
+__global__ __launch_bounds__(kThreads) void policy_close_kernel(RowParams p) {
+  const int64_t t = static_cast<int64_t>(blockIdx.x) * (kThreads / 8) + threadIdx.x / 8;
+  if (t < p.T) close_split_row<false, 8>(p, t, true, nullptr);
+}
+
+// Gradient of split rows: each workgroup closes its row for itself and writes
+// its chunk.  One workgroup more, the last, closes all rows for the outputs
+// and sums.
+template <bool BF16>
+__global__ __launch_bounds__(kThreads, 4) void policy_split_grad_kernel(RowParams p) {
+  using X = Elem<BF16>;
+  constexpr int E = X::kPer;
+  __shared__ RowSlope s_slope;
+  __shared__ PolicyTerms s_terms[kThreads / 8];
+  const int64_t t = blockIdx.x / p.split;
+  if (t == p.T) {
+    PolicyTerms sum{};
+    for (int64_t r = threadIdx.x / 8; r < p.T; r += kThreads / 8) close_split_row<true, 8>(p, r, true, &sum);
+    if (threadIdx.x % 8 == 0) s_terms[threadIdx.x / 8] = sum;
+    __syncthreads();
+    if (threadIdx.x < kPolicyTerms) {
+      double v = 0.0;
+      for (int i = 0; i < kThreads / 8; ++i) v += s_terms[i].v[threadIdx.x];
+      p.stats[threadIdx.x] = static_cast<float>(v);
+    }
+    return;
+  }
+  if (threadIdx.x < 64) {
+    PolicyTerms unused{};
+    const RowSlope rs = close_split_row<true, 64>(p, t, false, &unused);
+    if (threadIdx.x == 0) s_slope = rs;
+  }
+  __syncthreads();
+  const RowSlope rs = s_slope;
+  const char* row = p.logits + t * p.ld * X::kBytes;
+  char* out = p.grad + t * p.ld_grad * X::kBytes;
+  const int chunk = blockIdx.x % p.split;
+  const int2 open = chunk_of<BF16>(p, chunk, rs.n), all = chunk_of<BF16>(p, chunk, p.V);
+  const Slope slope(rs);
+  for (int i = open.x + threadIdx.x; i < open.y; i += kThreads)
+    store_piece<BF16>(out + static_cast<int64_t>(i) * 16,
+                      slope.template piece<BF16>(load_piece<BF16>(row + static_cast<int64_t>(i) * 16), i));
+  const int end = chunk == p.split - 1 ? p.V : all.y * E;
+  for (int j = max(open.y, all.x) * E + threadIdx.x; j < end; j += kThreads) {
+    const float x = j < rs.n ? X::get(row + static_cast<int64_t>(j) * X::kBytes) : 0.0f;
+    X::put(out + static_cast<int64_t>(j) * X::kBytes, slope.at(x, j));
   }
 }
 
@@ -361,23 +513,42 @@ void launch_shape(const RowParams& p, hipStream_t st) {
   if constexpr (GRAD) launch_policy_finish(p.parts, groups, p.stats, st);
 }
 
+// Workgroups a row, for long rows that are few: as many as bring about
+// kSplitGroups of them, each with at least two pieces a thread.
+constexpr int kSplitGroups = 512, kSplitRows = 128;
+int split_of(int32_t T, int pieces) {
+  if (T > kSplitRows) return 1;
+  return std::max(1, std::min({kSplitGroups / T, pieces / (2 * kThreads), kMaxSplit}));
+}
+
 // The fewest threads a row that hold it in 16 pieces each: short rows share a
 // wave, and the threads left over take other rows.
 template <bool BF16, bool GRAD>
-void launch_rows(const RowParams& p, hipStream_t st) {
+void launch_rows(RowParams p, hipStream_t st) {
   const int pieces = (p.V + Elem<BF16>::kPer - 1) / Elem<BF16>::kPer;
-  if (pieces <= 16) launch_shape<BF16, GRAD, 16, 1>(p, st);
-  else if (pieces <= 32) launch_shape<BF16, GRAD, 16, 2>(p, st);
-  else if (pieces <= 64) launch_shape<BF16, GRAD, 16, 4>(p, st);
-  else if (pieces <= 256) launch_shape<BF16, GRAD, 64, 4>(p, st);
-  else if (pieces <= 512) launch_shape<BF16, GRAD, 64, 8>(p, st);
-  else if (pieces <= 1024) launch_shape<BF16, GRAD, 256, 4>(p, st);
-  else if (pieces <= 2048) launch_shape<BF16, GRAD, 256, 8>(p, st);
-  else if (pieces <= 4096) launch_shape<BF16, GRAD, 256, 16>(p, st);
-  else if (pieces <= 6144) launch_shape<BF16, GRAD, 512, 12>(p, st);
-  else if (pieces <= 8192) launch_shape<BF16, GRAD, 512, 16>(p, st);
-  else if (pieces <= 12288) launch_shape<BF16, GRAD, 1024, 12>(p, st);
-  else launch_shape<BF16, GRAD, 1024, 16>(p, st);
+  if (pieces <= 16) return launch_shape<BF16, GRAD, 16, 1>(p, st);
+  if (pieces <= 32) return launch_shape<BF16, GRAD, 16, 2>(p, st);
+  if (pieces <= 64) return launch_shape<BF16, GRAD, 16, 4>(p, st);
+  if (pieces <= 256) return launch_shape<BF16, GRAD, 64, 4>(p, st);
+  if (pieces <= 512) return launch_shape<BF16, GRAD, 64, 8>(p, st);
+  p.split = p.split_stats ? split_of(p.T, pieces) : 1;
+  if (p.split > 1 || !GRAD) {
+    hipLaunchKernelGGL(policy_stats_kernel<BF16>, dim3(static_cast<uint32_t>(p.T) * p.split), dim3(kThreads), 0, st, p);
+    if constexpr (GRAD)
+      hipLaunchKernelGGL(policy_split_grad_kernel<BF16>, dim3(p.T * p.split + 1), dim3(kThreads), 0, st, p);
+    else if (p.split > 1)
+      hipLaunchKernelGGL(policy_close_kernel, dim3((p.T * 8 + kThreads - 1) / kThreads), dim3(kThreads), 0, st, p);
+    return;
+  }
+  if constexpr (GRAD) {
+    if (pieces <= 1024) launch_shape<BF16, GRAD, 256, 4>(p, st);
+    else if (pieces <= 2048) launch_shape<BF16, GRAD, 256, 8>(p, st);
+    else if (pieces <= 4096) launch_shape<BF16, GRAD, 256, 16>(p, st);
+    else if (pieces <= 6144) launch_shape<BF16, GRAD, 512, 12>(p, st);
+    else if (pieces <= 8192) launch_shape<BF16, GRAD, 512, 16>(p, st);
+    else if (pieces <= 12288) launch_shape<BF16, GRAD, 1024, 12>(p, st);
+    else launch_shape<BF16, GRAD, 1024, 16>(p, st);
+  }
 }
 
 // Sets of sums that the workgroups of T rows of V elements write (of the
@@ -429,7 +600,9 @@ void launch_policy_finish(double* parts, int32_t n, float* stats, hipStream_t st
 extern "C" size_t dora_policy_workspace_size(int32_t T, int32_t V) {
   using namespace dora;
   if (T < 1 || T > DORA_MAX_DECISIONS || V < 1 || V > DORA_MAX_ACTIONS) return 0;
-  return policy_parts_bytes(row_groups(T, V));
+  // Either the sums' sets or the split rows' triples; the type with more pieces a row splits further.
+  const size_t split = static_cast<size_t>(T) * split_of(T, (V + 3) / 4) * sizeof(float4);
+  return std::max(policy_parts_bytes(row_groups(T, V)), (split + 255) & ~size_t(255));
 }
 
 extern "C" int dora_action_logprob(const void* logits, int64_t ld, const int32_t* actions, const int32_t* legal,
@@ -453,6 +626,8 @@ extern "C" int dora_action_logprob(const void* logits, int64_t ld, const int32_t
   p.V = V;
   p.logp_out = logprob_out;
   p.entropy_out = entropy_out;
+  p.split_stats = static_cast<float4*>(workspace);
+  p.split = 1;
   p.status = dev_status;
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (dtype == DORA_BF16) launch_rows<true, false>(p, st);
@@ -483,7 +658,8 @@ extern "C" int dora_policy_loss(const void* logits, int64_t ld, const int32_t* a
     return DORA_ERR_WORKSPACE;
   RowParams p{static_cast<const char*>(logits), ld, actions, legal, old_logprob, ref_logprob, advantage, weight, T, V,
               PolicyCoef{clip_low, clip_high, kl_coef, entropy_coef}, static_cast<char*>(dlogits), ld_grad,
-              logprob_out, nullptr, static_cast<double*>(workspace), stats_out, dev_status};
+              logprob_out, nullptr, static_cast<double*>(workspace), static_cast<float4*>(workspace), 1, stats_out,
+              dev_status};
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (dtype == DORA_BF16) launch_rows<true, true>(p, st);
   else launch_rows<false, true>(p, st);
