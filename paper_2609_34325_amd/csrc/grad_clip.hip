@@ -4,14 +4,14 @@
 //   norm = sqrt(sum over tensors and elements of g^2)
 //   c = min(1, max_norm / (norm + eps)),  out = c g
 //
-// HBM bound: one read for the norm, one read and write to scale (what the
-// caches still hold of the first read is not read again).  The tensors'
-// addresses go in by kernel argument, kSpans at a launch; a chunk of
-// kChunk elements belongs to one tensor, and a workgroup takes every
-// gridDim-th chunk.  Squares are added in 64 bits: no fp32 gradient overflows
-// them, and the sum does not hang on the split.  Workgroups write their sums
-// to the workspace; every workgroup of the scaling launch adds them all in
-// the same order.
+// HBM bound: one read for the norm, one read and one write to scale.  The
+// tensors' addresses go in by kernel argument, as many as 4 KB hold; tensors
+// are cut into chunks, and a workgroup takes every gridDim-th chunk, four
+// 16-byte pieces in flight a thread.  The scaling launches take the chunks
+// from the back, so that what the caches still hold of the norm's pass is read
+// from there.  Squares are added in 64 bits: no fp32 gradient overflows them,
+// and the sum does not hang on the split.  Workgroups write their sums to the
+// workspace; every workgroup of a scaling launch adds them all in the same order.
 #include <algorithm>
 #include <cstdlib>
 
@@ -21,36 +21,106 @@ namespace dora {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kSpans = 96;         // tensors per launch: the argument block stays under 4 KB
-constexpr int kChunk = 16384;      // elements
-constexpr int kMaxGroups = 1024;   // workgroups of a launch
+constexpr int kFlight = 4;                      // pieces in flight a thread
+constexpr int kMinChunk = 2048;                 // elements; chunks are multiples of it
+constexpr int kMaxChunk = 32768;
+constexpr int kManyChunks = 4096;               // smaller chunks while there are fewer
+constexpr int kMaxGroups = 2048;                // workgroups of a pass, the share of each launch rounded up
 constexpr int kMaxSpans = 1 << 16;
+constexpr int64_t kPart = int64_t{1} << 30;     // longer tensors go in as several
+constexpr int64_t kMaxTotal = int64_t{1} << 40;  // elements of a call
+constexpr uint32_t kBF16 = 1u << 31;
 
+// Tensors of one launch, in at most 4 KB of arguments.
+template <int N, bool OUT>
 struct SpanBlock {
-  const char* in[kSpans];
-  char* out[kSpans];
-  int64_t numel[kSpans];
-  int64_t first[kSpans];  // chunks before the tensor, in this launch
-  uint64_t bf16[(kSpans + 63) / 64];
-  int64_t chunks;
-  int32_t n;
+  static constexpr int kSpans = N;
+  const char* in[N];
+  char* out[OUT ? N : 1];
+  uint32_t numel[N];  // | kBF16
+  int32_t first[N];   // chunks before the tensor, in this launch
+  int32_t n, chunks, chunk;
 };
-static_assert(sizeof(SpanBlock) + 64 <= 4096, "kernel arguments");
+typedef SpanBlock<248, false> InBlock;   // read, or scaled in place
+typedef SpanBlock<160, true> PairBlock;
+static_assert(sizeof(InBlock) + 64 <= 4096 && sizeof(PairBlock) + 64 <= 4096, "kernel arguments");
 
-__device__ __forceinline__ int find_span(const SpanBlock& b, int64_t chunk) {
-  int lo = 0, hi = b.n - 1;  // the last tensor that starts at or before the chunk
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) / 2;
-    if (b.first[mid] <= chunk) lo = mid;
-    else hi = mid - 1;
+// A chunk's tensor and elements.
+struct Chunk {
+  int span;
+  int64_t lo, hi;
+  bool bf16;
+};
+// The tensor is the last that starts at or before the chunk: the lanes compare
+// with all of them at once (a search by halves would wait for memory eight times).
+template <class B>
+__device__ __forceinline__ Chunk find_chunk(const B& b, int chunk) {
+  const int lane = threadIdx.x & 63;
+  int before = 0;
+#pragma unroll
+  for (int i = 0; i < B::kSpans; i += 64) {
+    const int j = i + lane;
+    before += __popcll(__ballot(j < b.n && b.first[min(j, B::kSpans - 1)] <= chunk));
   }
-  return lo;
+  const int t = __builtin_amdgcn_readfirstlane(before - 1);
+  const uint32_t code = b.numel[t];
+  const int64_t lo = static_cast<int64_t>(chunk - b.first[t]) * b.chunk;
+  return {t, lo, min(static_cast<int64_t>(code & ~kBF16), lo + b.chunk), (code & kBF16) != 0};
 }
 
+// Pieces of 16 bytes at the element's alignment: the hardware takes unaligned
+// ones, so that views into a flat buffer run like tensors of their own.
 template <bool BF16>
-__device__ __forceinline__ float element(const char* p, int64_t i) {
-  if constexpr (BF16) return __uint_as_float(static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(p)[i]) << 16);
-  else return reinterpret_cast<const float*>(p)[i];
+struct Piece;
+template <>
+struct Piece<true> {
+  static constexpr int E = 8, kBytes = 2;
+  typedef u32x4 __attribute__((aligned(2))) Vec;
+  __device__ static float get(const char* p) {
+    return __uint_as_float(static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(p)) << 16);
+  }
+  __device__ static void put(char* p, float v) { *reinterpret_cast<__bf16*>(p) = static_cast<__bf16>(v); }
+  __device__ static float part(u32x4 v, int i) {
+    return __uint_as_float(i & 1 ? v[i / 2] & 0xFFFF0000u : v[i / 2] << 16);
+  }
+  __device__ static u32x4 pack(const float (&f)[E]) {
+    bf16x8 b;
+#pragma unroll
+    for (int i = 0; i < E; ++i) b[i] = static_cast<__bf16>(f[i]);
+    return __builtin_bit_cast(u32x4, b);
+  }
+};
+template <>
+struct Piece<false> {
+  static constexpr int E = 4, kBytes = 4;
+  typedef u32x4 __attribute__((aligned(4))) Vec;
+  __device__ static float get(const char* p) { return *reinterpret_cast<const float*>(p); }
+  __device__ static void put(char* p, float v) { *reinterpret_cast<float*>(p) = v; }
+  __device__ static float part(u32x4 v, int i) { return __uint_as_float(v[i]); }
+  __device__ static u32x4 pack(const float (&f)[E]) {
+    return u32x4{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])};
+  }
+};
+
+// each(piece, its index) for the pieces of n elements from p on, and
+// rest(element, its index) for the elements behind the last piece.
+template <bool BF16, class Each, class Rest>
+__device__ __forceinline__ void for_pieces(const char* p, int n, Each each, Rest rest) {
+  using P = Piece<BF16>;
+  const int whole = n / P::E, tid = threadIdx.x;
+  for (int i = tid; i < whole; i += kFlight * kThreads) {
+    u32x4 v[kFlight];
+    // Unconditional, from clamped places: counted loads, waited for one by one.
+#pragma unroll
+    for (int k = 0; k < kFlight; ++k)
+      v[k] = *reinterpret_cast<const typename P::Vec*>(p + static_cast<int64_t>(min(i + k * kThreads, whole - 1)) * 16);
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int k = 0; k < kFlight; ++k)
+      if (i + k * kThreads < whole) each(v[k], i + k * kThreads);
+  }
+  const int j = whole * P::E + tid;
+  if (j < n) rest(P::get(p + static_cast<int64_t>(j) * P::kBytes), j);
 }
 
 __device__ __forceinline__ double block_sum(double v) {
@@ -67,22 +137,29 @@ __device__ __forceinline__ double block_sum(double v) {
 }
 
 template <bool BF16>
-__device__ __forceinline__ double chunk_squares(const char* p, int64_t lo, int64_t hi) {
+__device__ __forceinline__ double chunk_squares(const char* p, int n) {
+  using P = Piece<BF16>;
   double s = 0.0;
-  for (int64_t i = lo + threadIdx.x; i < hi; i += kThreads) {
-    const double g = element<BF16>(p, i);
-    s += g * g;
-  }
+  for_pieces<BF16>(
+      p, n,
+      [&](u32x4 v, int) {
+#pragma unroll
+        for (int e = 0; e < P::E; ++e) {
+          const double g = P::part(v, e);
+          s = fma(g, g, s);
+        }
+      },
+      [&](float x, int) { s += static_cast<double>(x) * x; });
   return s;
 }
 
-__global__ __launch_bounds__(kThreads) void grad_squares_kernel(SpanBlock b, double* parts) {
+__global__ __launch_bounds__(kThreads) void grad_squares_kernel(InBlock b, double* parts) {
   double s = 0.0;
-  for (int64_t c = blockIdx.x; c < b.chunks; c += gridDim.x) {
-    const int t = find_span(b, c);
-    const int64_t lo = (c - b.first[t]) * kChunk, hi = min(b.numel[t], lo + kChunk);
-    s += (b.bf16[t / 64] >> (t % 64)) & 1 ? chunk_squares<true>(b.in[t], lo, hi)
-                                          : chunk_squares<false>(b.in[t], lo, hi);
+  for (int c = blockIdx.x; c < b.chunks; c += gridDim.x) {
+    const Chunk k = find_chunk(b, c);
+    const char* p = b.in[k.span] + k.lo * (k.bf16 ? 2 : 4);
+    const int n = static_cast<int>(k.hi - k.lo);
+    s += k.bf16 ? chunk_squares<true>(p, n) : chunk_squares<false>(p, n);
   }
   s = block_sum(s);
   if (threadIdx.x == 0) parts[blockIdx.x] = s;
@@ -112,26 +189,39 @@ struct Factor {
 };
 
 template <bool BF16>
-__device__ __forceinline__ void chunk_scale(const char* in, char* out, int64_t lo, int64_t hi, Factor f) {
-  for (int64_t i = lo + threadIdx.x; i < hi; i += kThreads) {
-    const float g = f * element<BF16>(in, i);
-    if constexpr (BF16) reinterpret_cast<__bf16*>(out)[i] = static_cast<__bf16>(g);
-    else reinterpret_cast<float*>(out)[i] = g;
-  }
+__device__ __forceinline__ void chunk_scale(const char* in, char* out, int n, Factor f) {
+  using P = Piece<BF16>;
+  for_pieces<BF16>(
+      in, n,
+      [&](u32x4 v, int i) {
+        float x[P::E];
+#pragma unroll
+        for (int e = 0; e < P::E; ++e) x[e] = f * P::part(v, e);
+        *reinterpret_cast<typename P::Vec*>(out + static_cast<int64_t>(i) * 16) = P::pack(x);
+      },
+      [&](float x, int j) { P::put(out + static_cast<int64_t>(j) * P::kBytes, f * x); });
 }
 
-__global__ __launch_bounds__(kThreads) void grad_scale_kernel(SpanBlock b, const double* parts, int32_t n,
-                                                              float max_norm, float eps, float* norm_out) {
+// PairBlock: out of place; InBlock: in place.
+template <class B>
+__global__ __launch_bounds__(kThreads) void grad_scale_kernel(B b, const double* parts, int32_t n, float max_norm,
+                                                              float eps, float* norm_out) {
+  constexpr bool kInPlace = sizeof(b.out) == sizeof(char*);
   const double norm = norm_of(parts, n);
   if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = static_cast<float>(norm);
   const double ratio = norm == 0.0 ? 1.0 : static_cast<double>(max_norm) / (norm + static_cast<double>(eps));
   const Factor f(ratio >= 1.0 ? 1.0 : ratio);  // NaN stays
-  for (int64_t i = blockIdx.x; i < b.chunks; i += gridDim.x) {
-    const int t = find_span(b, i);
-    if (f.pre * f.c == 1.0f && b.in[t] == b.out[t]) continue;  // in place and nothing to clip
-    const int64_t lo = (i - b.first[t]) * kChunk, hi = min(b.numel[t], lo + kChunk);
-    if ((b.bf16[t / 64] >> (t % 64)) & 1) chunk_scale<true>(b.in[t], b.out[t], lo, hi, f);
-    else chunk_scale<false>(b.in[t], b.out[t], lo, hi, f);
+  const bool same = f.pre * f.c == 1.0f;
+  if (kInPlace && same) return;  // nothing to clip
+  for (int i = blockIdx.x; i < b.chunks; i += gridDim.x) {
+    const Chunk k = find_chunk(b, b.chunks - 1 - i);
+    const int64_t at = k.lo * (k.bf16 ? 2 : 4);
+    const char* in = b.in[k.span] + at;
+    char* out = kInPlace ? const_cast<char*>(in) : b.out[k.span] + at;
+    const int len = static_cast<int>(k.hi - k.lo);
+    if (same && in == out) continue;
+    if (k.bf16) chunk_scale<true>(in, out, len, f);
+    else chunk_scale<false>(in, out, len, f);
   }
 }
 
@@ -173,24 +263,41 @@ int check_spans(const dora_span* s, int32_t n) {
   return DORA_OK;
 }
 
-// The next launch's tensors from span `at` on, empty ones left out; returns
-// the span after them.
-int32_t fill_block(const dora_span* grads, const dora_span* out, int32_t n, int32_t at, SpanBlock* b) {
-  *b = SpanBlock{};
-  for (; at < n && b->n < kSpans; ++at) {
-    if (grads[at].numel == 0) continue;
-    const int i = b->n++;
-    b->in[i] = static_cast<const char*>(grads[at].data);
-    b->out[i] = static_cast<char*>(out ? out[at].data : grads[at].data);
-    b->numel[i] = grads[at].numel;
-    b->first[i] = b->chunks;
-    if (grads[at].dtype == DORA_BF16) b->bf16[i / 64] |= uint64_t{1} << (i % 64);
-    b->chunks += (grads[at].numel + kChunk - 1) / kChunk;
+// Where in the list a launch begins: a tensor and an element of it.
+struct Place {
+  int32_t span;
+  int64_t element;
+};
+
+// The next launch's tensors from `at` on, empty ones left out; returns where
+// the one after it begins.
+template <class B>
+Place fill_block(const dora_span* grads, const dora_span* out, int32_t n, Place at, int chunk, B* b) {
+  b->n = b->chunks = 0;
+  b->chunk = chunk;
+  while (at.span < n && b->n < B::kSpans) {
+    const dora_span& g = grads[at.span];
+    const int64_t len = std::min(g.numel - at.element, kPart);
+    if (len > 0) {
+      const int i = b->n++;
+      const int64_t byte = at.element * (g.dtype == DORA_BF16 ? 2 : 4);
+      b->in[i] = static_cast<const char*>(g.data) + byte;
+      if (sizeof(b->out) > sizeof(char*)) b->out[i] = static_cast<char*>(out[at.span].data) + byte;
+      b->numel[i] = static_cast<uint32_t>(len) | (g.dtype == DORA_BF16 ? kBF16 : 0u);
+      b->first[i] = b->chunks;
+      b->chunks += static_cast<int32_t>((len + chunk - 1) / chunk);
+      at.element += len;
+    }
+    if (at.element >= g.numel) at = {at.span + 1, 0};
   }
   return at;
 }
 
-int block_groups(const SpanBlock& b) { return static_cast<int>(std::min<int64_t>(b.chunks, kMaxGroups)); }
+// A launch's share of the pass's workgroups.
+int launch_groups(int32_t chunks, int64_t all) {
+  const int64_t share = (static_cast<int64_t>(chunks) * kMaxGroups + all - 1) / all;
+  return static_cast<int>(std::min<int64_t>(chunks, share));
+}
 
 }  // namespace
 }  // namespace dora
@@ -198,7 +305,10 @@ int block_groups(const SpanBlock& b) { return static_cast<int>(std::min<int64_t>
 extern "C" size_t dora_grad_clip_workspace_size(int32_t n) {
   using namespace dora;
   if (n < 1 || n > kMaxSpans) return 0;
-  return static_cast<size_t>((n + kSpans - 1) / kSpans) * kMaxGroups * sizeof(double);
+  // One sum a workgroup: kMaxGroups, and at most one more a launch.  A launch holds 248 tensors, or parts of
+  // longer ones, of which kMaxTotal elements make 1024 more.
+  const size_t launches = (static_cast<size_t>(n) + kMaxTotal / kPart) / InBlock::kSpans + 1;
+  return ((kMaxGroups + launches) * sizeof(double) + 255) & ~size_t(255);
 }
 
 extern "C" int dora_grad_clip(const dora_span* grads, const dora_span* out, int32_t n, float max_norm, float eps,
@@ -226,24 +336,42 @@ extern "C" int dora_grad_clip(const dora_span* grads, const dora_span* out, int3
   }
   double* parts = static_cast<double*>(workspace);
   hipStream_t st = static_cast<hipStream_t>(stream);
+  int64_t total = 0, all = 0;
+  for (int32_t i = 0; i < n; ++i) total += grads[i].numel;
+  if (total > kMaxTotal) return DORA_ERR_SHAPE;
+  const int chunk = static_cast<int>(std::min<int64_t>(
+      kMaxChunk, std::max<int64_t>(1, (total + kManyChunks * kMinChunk - 1) / (kManyChunks * kMinChunk)) * kMinChunk));
+  for (int32_t i = 0; i < n; ++i) all += (grads[i].numel + chunk - 1) / chunk;
   int32_t used = 0;
-  SpanBlock b;
-  for (int32_t at = 0; at < n;) {
-    at = fill_block(grads, out, n, at, &b);
-    const int groups = block_groups(b);
-    if (groups == 0) continue;
+  InBlock b;
+  for (Place at{0, 0}; at.span < n;) {
+    at = fill_block(grads, nullptr, n, at, chunk, &b);
+    if (b.n == 0) continue;
+    const int groups = launch_groups(b.chunks, all);
     hipLaunchKernelGGL(grad_squares_kernel, dim3(groups), dim3(kThreads), 0, st, b, parts + used);
     used += groups;
   }
-  bool norm_written = false;
-  for (int32_t at = 0; scale && at < n;) {
-    at = fill_block(grads, out, n, at, &b);
-    const int groups = block_groups(b);
-    if (groups == 0) continue;
-    hipLaunchKernelGGL(grad_scale_kernel, dim3(groups), dim3(kThreads), 0, st, b, parts, used, max_norm, eps,
-                       norm_written ? nullptr : norm_out);
-    norm_written = true;
+  if (!scale || used == 0) {
+    hipLaunchKernelGGL(grad_norm_kernel, dim3(1), dim3(kThreads), 0, st, parts, used, norm_out);
+  } else if (!out) {
+    float* norm = norm_out;
+    for (Place at{0, 0}; at.span < n;) {
+      at = fill_block(grads, nullptr, n, at, chunk, &b);
+      if (b.n == 0) continue;
+      hipLaunchKernelGGL(grad_scale_kernel<InBlock>, dim3(launch_groups(b.chunks, all)), dim3(kThreads), 0, st, b,
+                         parts, used, max_norm, eps, norm);
+      norm = nullptr;
+    }
+  } else {
+    float* norm = norm_out;
+    PairBlock pair;
+    for (Place at{0, 0}; at.span < n;) {
+      at = fill_block(grads, out, n, at, chunk, &pair);
+      if (pair.n == 0) continue;
+      hipLaunchKernelGGL(grad_scale_kernel<PairBlock>, dim3(launch_groups(pair.chunks, all)), dim3(kThreads), 0, st,
+                         pair, parts, used, max_norm, eps, norm);
+      norm = nullptr;
+    }
   }
-  if (!norm_written) hipLaunchKernelGGL(grad_norm_kernel, dim3(1), dim3(kThreads), 0, st, parts, used, norm_out);
   return hipGetLastError() == hipSuccess ? DORA_OK : DORA_ERR_HIP;
 }

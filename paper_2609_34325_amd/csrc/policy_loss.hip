@@ -440,7 +440,7 @@ __global__ __launch_bounds__(kThreads) void policy_close_kernel(RowParams p) {
 // its chunk.  One workgroup more, the last, closes all rows for the outputs
 // and sums.
 template <bool BF16>
-__global__ __launch_bounds__(kThreads, 4) void policy_split_grad_kernel(RowParams p) {
+__global__ __launch_bounds__(kThreads, 3) void policy_split_grad_kernel(RowParams p) {
   using X = Elem<BF16>;
   constexpr int E = X::kPer;
   __shared__ RowSlope s_slope;

@@ -173,7 +173,7 @@ def test_refusals(gpu):
         gpu.dora_grad_clip([g], -1.0)
     assert e.value.code == gpu.DORA_ERR_SHAPE
     with pytest.raises(gpu.DoraError) as e:
-        gpu.dora_grad_clip([g] * 200, 1.0, workspace=gpu.new_grad_clip_workspace(1), out=[g.clone() for _ in range(200)])
+        gpu.dora_grad_clip([g] * 200, 1.0, workspace=gpu.new_grad_clip_workspace(200)[:-1], out=[g.clone() for _ in range(200)])
     assert e.value.code == gpu.DORA_ERR_WORKSPACE
     # by ctypes, as where the native marshalling is not built
     spans, device = gpu._spans((t for t in [g, g.bfloat16()]), "grads")
