@@ -630,7 +630,8 @@ typedef struct {
  *              overlap in time.
  *
  * Returns DORA_OK or a negative dora_status (DORA_ERR_OVERLAP for tensors that
- * overlap otherwise); enqueues two kernels per 96 tensors.
+ * overlap otherwise); enqueues a kernel for the norm per 248 tensors and one to
+ * scale per 160 (in place 248).
  */
 size_t dora_grad_clip_workspace_size(int32_t n); /* 0 when n is out of range */
 int dora_grad_clip(const dora_span* grads, const dora_span* out, int32_t n, float max_norm, float eps,

@@ -128,6 +128,8 @@ _OPTIONAL = ("cu_in", "budget_logits", "removal_scores", "scores_out", "workspac
 _lib = None
 _native_call = None
 _native_spans = None
+_native_rows = None
+_native_vectors = None
 
 
 class FlopsConfig(ctypes.Structure):
@@ -154,7 +156,7 @@ def _leave_to_ctypes(*args):
 
 def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     """Load libdora.so (built in-tree by ``paper_2609_34325_amd.build``)."""
-    global _lib, _native_call, _native_spans
+    global _lib, _native_call, _native_spans, _native_rows, _native_vectors
     if _lib is not None and path is None:
         return _lib
     p = path or LIB_PATH
@@ -220,11 +222,12 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.addresses = tuple(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name, _ in _ENTRIES)
     if _native_call is None:
         try:
-            from ._host_call import call as _native_call, spans as _native_spans
+            from ._host_call import (call as _native_call, rows as _native_rows, spans as _native_spans,
+                                     vectors as _native_vectors)
         except ImportError as e:  # not built, or for another Python or torch
             warnings.warn(f"calls are marshalled by ctypes, about 5 us slower each: {e}; build the native marshalling "
                           "with `python -m paper_2609_34325_amd.build`")
-            _native_call = _native_spans = _leave_to_ctypes
+            _native_call = _native_spans = _native_rows = _native_vectors = _leave_to_ctypes
     if path is None:
         _lib = lib
     return lib
@@ -636,18 +639,12 @@ def dora_varlen_attn_noalloc(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, 
     return out
 
 
-def _one_device(*tensors) -> None:
-    """The tensors of a call share a device, the current one (whose stream runs it)."""
-    first = tensors[0].device
-    for t in tensors:
-        if t is not None and t.device != first:
-            raise ValueError(f"tensors on {first} and {t.device}")
-    if first.type == "cuda" and first.index != torch._C._cuda_getDevice():
-        raise ValueError(f"tensors on {first}, which is not the current device")
-
-
 def _rows(t: torch.Tensor, name: str):
-    """Address and leading dimension of rows whose elements are adjacent."""
+    """Address, leading dimension, sizes, type and device of rows whose elements
+    are adjacent."""
+    got = (_native_rows or _leave_to_ctypes)(t)
+    if got is not NotImplemented:
+        return got
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch tensor")
     if t.dim() != 2:
@@ -660,21 +657,24 @@ def _rows(t: torch.Tensor, name: str):
         ld = V
     if (V > 1 and one != 1) or ld < V:
         raise ValueError(f"{name} must have adjacent elements in each row, and rows apart")
-    return t.data_ptr(), ld
+    return t.data_ptr(), ld, T, V, _dtype_code(t), t.get_device()
 
 
-def _per_row(n: int, **tensors) -> None:
-    for name, t in tensors.items():
-        if t is not None and tuple(t.shape) != (n,):
-            raise ValueError(f"{name} must be [{n}]")
-
-
-def _room(t: Optional[torch.Tensor], shape, dtype, device, name: str) -> torch.Tensor:
-    if t is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
-        raise ValueError(f"{name} must be {list(shape)} {dtype}")
-    return t
+def _vectors(names, device: int, *sized) -> None:
+    """The tensors of a call (n, tensor, n, tensor, ...) are vectors of n elements
+    (n < 0: any tensor) on the device, the current one, whose stream runs it."""
+    if (_native_vectors or _leave_to_ctypes)(device, *sized) is NotImplemented:
+        for name, n, t in zip(names, sized[::2], sized[1::2]):
+            if t is None:
+                continue
+            if not isinstance(t, torch.Tensor):
+                raise TypeError(f"{name} must be a torch tensor")
+            if n >= 0 and tuple(t.shape) != (n,):
+                raise ValueError(f"{name} must be [{n}]")
+            if t.get_device() != device:
+                raise ValueError(f"tensors on devices {device} and {t.get_device()} (-1: the host): {name}")
+    if device >= 0 and device != torch._C._cuda_getDevice():
+        raise ValueError(f"tensors on device {device}, which is not the current one")
 
 
 def _bytes(workspace: Optional[torch.Tensor]) -> int:
@@ -708,20 +708,19 @@ def dora_action_logprob(logits: torch.Tensor, actions: torch.Tensor, weight: Opt
     workspace (a new one when None) few long rows may be split over several
     workgroups; single=True passes none.  Returns (logprob [T], entropy [T],
     dev_status)."""
-    address, ld = _rows(logits, "logits")
-    T, V = (int(n) for n in logits.shape)
+    address, ld, T, V, code, device = _rows(logits, "logits")
     dev = logits.device
-    _per_row(T, actions=actions, weight=weight, legal=legal)
-    logprob_out = _room(logprob_out, (T,), torch.float32, dev, "logprob_out")
-    entropy_out = _room(entropy_out, (T,), torch.float32, dev, "entropy_out")
+    logprob_out = torch.empty(T, dtype=torch.float32, device=dev) if logprob_out is None else logprob_out
+    entropy_out = torch.empty(T, dtype=torch.float32, device=dev) if entropy_out is None else entropy_out
     if single:
         workspace = None
     elif workspace is None:
         workspace = new_policy_workspace(T, V, dev)
     dev_status = new_status(dev) if dev_status is None else dev_status
-    _one_device(logits, actions, weight, legal, logprob_out, entropy_out, workspace, dev_status)
-    _call("dora_action_logprob", stream, address, ld, actions, legal, weight, T, V, _dtype_code(logits), logprob_out,
-          entropy_out, workspace, _bytes(workspace), dev_status)
+    _vectors(("actions", "legal", "weight", "logprob_out", "entropy_out", "workspace", "dev_status"), device,
+             T, actions, T, legal, T, weight, T, logprob_out, T, entropy_out, -1, workspace, -1, dev_status)
+    _call("dora_action_logprob", stream, address, ld, actions, legal, weight, T, V, code, logprob_out, entropy_out,
+          workspace, _bytes(workspace), dev_status)
     return logprob_out, entropy_out, dev_status
 
 
@@ -740,22 +739,22 @@ def dora_policy_loss(logits: torch.Tensor, actions: torch.Tensor, old_logprob: t
     the logits themselves.  Returns (dlogits [T, V], logprob [T], stats [6],
     dev_status); stats holds the sums of loss, gain, kl, entropy, clipped share
     and weight."""
-    address, ld = _rows(logits, "logits")
-    T, V = (int(n) for n in logits.shape)
+    address, ld, T, V, code, device = _rows(logits, "logits")
     dev = logits.device
-    _per_row(T, actions=actions, old_logprob=old_logprob, advantage=advantage, ref_logprob=ref_logprob, weight=weight,
-             legal=legal)
-    dlogits = _room(dlogits, (T, V), logits.dtype, dev, "dlogits")
-    grad, ld_grad = _rows(dlogits, "dlogits")
-    logprob_out = _room(logprob_out, (T,), torch.float32, dev, "logprob_out")
-    stats_out = _room(stats_out, (6,), torch.float32, dev, "stats_out")
+    dlogits = torch.empty((T, V), dtype=logits.dtype, device=dev) if dlogits is None else dlogits
+    grad, ld_grad, *like = _rows(dlogits, "dlogits")
+    if like != [T, V, code, device]:
+        raise ValueError("dlogits must have the logits' shape, type and device")
+    logprob_out = torch.empty(T, dtype=torch.float32, device=dev) if logprob_out is None else logprob_out
+    stats_out = torch.empty(6, dtype=torch.float32, device=dev) if stats_out is None else stats_out
     workspace = new_policy_workspace(T, V, dev) if workspace is None else workspace
     dev_status = new_status(dev) if dev_status is None else dev_status
-    _one_device(logits, actions, old_logprob, advantage, ref_logprob, weight, legal, dlogits, logprob_out, stats_out,
-                workspace, dev_status)
+    _vectors(("actions", "legal", "old_logprob", "ref_logprob", "advantage", "weight", "logprob_out", "stats_out",
+              "workspace", "dev_status"), device, T, actions, T, legal, T, old_logprob, T, ref_logprob, T, advantage,
+             T, weight, T, logprob_out, 6, stats_out, -1, workspace, -1, dev_status)
     _call("dora_policy_loss", stream, address, ld, actions, legal, old_logprob, ref_logprob, advantage, weight, T, V,
-          _dtype_code(logits), float(clip_low), float(clip_high), float(kl_coef), float(entropy_coef), grad, ld_grad,
-          logprob_out, stats_out, workspace, _bytes(workspace), dev_status)
+          code, float(clip_low), float(clip_high), float(kl_coef), float(entropy_coef), grad, ld_grad, logprob_out,
+          stats_out, workspace, _bytes(workspace), dev_status)
     return dlogits, logprob_out, stats_out, dev_status
 
 
@@ -783,14 +782,17 @@ def dora_pl_policy_loss(scores: torch.Tensor, order: torch.Tensor, cu_order: tor
     B = int(cu_order.shape[0]) - 1
     N, total_in = _pl_geometry(scores, B, cu_in, N)
     dev = scores.device
-    _per_row(B, old_logprob=old_logprob, advantage=advantage, ref_logprob=ref_logprob, weight=weight)
-    dscores = _room(dscores, scores.shape, torch.float32, dev, "dscores")
-    logprob_out = _room(logprob_out, (B,), torch.float32, dev, "logprob_out")
-    stats_out = _room(stats_out, (6,), torch.float32, dev, "stats_out")
+    dscores = torch.empty_like(scores) if dscores is None else dscores
+    if dscores.shape != scores.shape:
+        raise ValueError("dscores must be of the scores' shape")
+    logprob_out = torch.empty(B, dtype=torch.float32, device=dev) if logprob_out is None else logprob_out
+    stats_out = torch.empty(6, dtype=torch.float32, device=dev) if stats_out is None else stats_out
     workspace = new_pl_policy_workspace(B, dev) if workspace is None else workspace
     dev_status = new_status(dev) if dev_status is None else dev_status
-    _one_device(scores, order, cu_order, cu_in, old_logprob, advantage, ref_logprob, weight, dscores, logprob_out,
-                stats_out, workspace, dev_status)
+    _vectors(("old_logprob", "ref_logprob", "advantage", "weight", "logprob_out", "stats_out", "order", "cu_order",
+              "cu_in", "dscores", "workspace", "dev_status"), scores.get_device(), B, old_logprob, B, ref_logprob,
+             B, advantage, B, weight, B, logprob_out, 6, stats_out, -1, order, B + 1, cu_order, B + 1, cu_in,
+             -1, dscores, -1, workspace, -1, dev_status)
     _call("dora_pl_policy_loss", stream, scores, order, cu_order, cu_in, total_in, old_logprob, ref_logprob, advantage,
           weight, B, N, float(clip_low), float(clip_high), float(kl_coef), dscores, logprob_out, stats_out, workspace,
           _bytes(workspace), dev_status)
@@ -817,8 +819,8 @@ def _spans(tensors, name: str):
     if device is NotImplemented:
         for i, t in enumerate(tensors):
             spans[i] = Span(_dev(t, f"{name}[{i}]"), t.numel(), _dtype_code(t), 0)
-        _one_device(*tensors)
         device = tensors[0].get_device()
+        _vectors([f"{name}[{i}]" for i in range(len(tensors))], device, *(x for t in tensors for x in (-1, t)))
     return spans, device
 
 
@@ -841,9 +843,9 @@ def dora_grad_clip(grads, max_norm: float, out=None, eps: float = 1e-6, norm_out
         if out_device != device:
             raise ValueError(f"tensors on devices {device} and {out_device}")
     dev = grads[0].device
-    norm_out = _room(norm_out, (1,), torch.float32, dev, "norm_out")
+    norm_out = torch.empty(1, dtype=torch.float32, device=dev) if norm_out is None else norm_out
     workspace = new_grad_clip_workspace(len(grads), dev) if workspace is None else workspace
-    _one_device(grads[0], norm_out, workspace)
+    _vectors(("norm_out", "workspace"), device, 1, norm_out, -1, workspace)
     _call("dora_grad_clip", stream, ctypes.addressof(spans), 0 if out_spans is None else ctypes.addressof(out_spans),
           len(grads), float(max_norm), float(eps), norm_out, workspace, _bytes(workspace))
     return grads if out is None else out, norm_out

@@ -7,9 +7,8 @@
 // HBM bound: one read for the norm, one read and one write to scale.  The
 // tensors' addresses go in by kernel argument, as many as 4 KB hold; tensors
 // are cut into chunks, and a workgroup takes every gridDim-th chunk, four
-// 16-byte pieces in flight a thread.  The scaling launches take the chunks
-// from the back, so that what the caches still hold of the norm's pass is read
-// from there.  Squares are added in 64 bits: no fp32 gradient overflows them,
+// 16-byte pieces in flight a thread.  The norm's pass takes the list from its
+// end, so that the scaling begins with what the caches still hold.  Squares are added in 64 bits: no fp32 gradient overflows them,
 // and the sum does not hang on the split.  Workgroups write their sums to the
 // workspace; every workgroup of a scaling launch adds them all in the same order.
 #include <algorithm>
@@ -21,13 +20,13 @@ namespace dora {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kFlight = 4;                      // pieces in flight a thread
-constexpr int kMinChunk = 2048;                 // elements; chunks are multiples of it
-constexpr int kMaxChunk = 32768;
-constexpr int kManyChunks = 4096;               // smaller chunks while there are fewer
-constexpr int kMaxGroups = 2048;                // workgroups of a pass, the share of each launch rounded up
+constexpr int kFlight = 4;                       // pieces in flight a thread
+// Elements of a chunk: what makes about 2048 of them, one a workgroup, within
+// these bounds.  (22M bf16 elements: 2048 chunks 27.5 us, 4096 29.9.)
+constexpr int kMinChunk = 2048, kMaxChunk = 32768, kManyChunks = 2048;
+constexpr int kMaxGroups = 2048;                 // workgroups of a pass, the share of each launch rounded up
 constexpr int kMaxSpans = 1 << 16;
-constexpr int64_t kPart = int64_t{1} << 30;     // longer tensors go in as several
+constexpr int64_t kPart = int64_t{1} << 30;      // longer tensors go in as several
 constexpr int64_t kMaxTotal = int64_t{1} << 40;  // elements of a call
 constexpr uint32_t kBF16 = 1u << 31;
 
@@ -45,7 +44,7 @@ typedef SpanBlock<248, false> InBlock;   // read, or scaled in place
 typedef SpanBlock<160, true> PairBlock;
 static_assert(sizeof(InBlock) + 64 <= 4096 && sizeof(PairBlock) + 64 <= 4096, "kernel arguments");
 
-// A chunk's tensor and elements.
+// A chunk's tensor and elements.  BACK: the tensor's chunks from its end.
 struct Chunk {
   int span;
   int64_t lo, hi;
@@ -53,7 +52,7 @@ struct Chunk {
 };
 // The tensor is the last that starts at or before the chunk: the lanes compare
 // with all of them at once (a search by halves would wait for memory eight times).
-template <class B>
+template <bool BACK, class B>
 __device__ __forceinline__ Chunk find_chunk(const B& b, int chunk) {
   const int lane = threadIdx.x & 63;
   int before = 0;
@@ -64,8 +63,9 @@ __device__ __forceinline__ Chunk find_chunk(const B& b, int chunk) {
   }
   const int t = __builtin_amdgcn_readfirstlane(before - 1);
   const uint32_t code = b.numel[t];
-  const int64_t lo = static_cast<int64_t>(chunk - b.first[t]) * b.chunk;
-  return {t, lo, min(static_cast<int64_t>(code & ~kBF16), lo + b.chunk), (code & kBF16) != 0};
+  const int numel = static_cast<int>(code & ~kBF16), place = chunk - b.first[t];
+  const int64_t lo = static_cast<int64_t>(BACK ? (numel - 1) / b.chunk - place : place) * b.chunk;
+  return {t, lo, min(static_cast<int64_t>(numel), lo + b.chunk), (code & kBF16) != 0};
 }
 
 // Pieces of 16 bytes at the element's alignment: the hardware takes unaligned
@@ -75,7 +75,6 @@ struct Piece;
 template <>
 struct Piece<true> {
   static constexpr int E = 8, kBytes = 2;
-  typedef u32x4 __attribute__((aligned(2))) Vec;
   __device__ static float get(const char* p) {
     return __uint_as_float(static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(p)) << 16);
   }
@@ -93,7 +92,6 @@ struct Piece<true> {
 template <>
 struct Piece<false> {
   static constexpr int E = 4, kBytes = 4;
-  typedef u32x4 __attribute__((aligned(4))) Vec;
   __device__ static float get(const char* p) { return *reinterpret_cast<const float*>(p); }
   __device__ static void put(char* p, float v) { *reinterpret_cast<float*>(p) = v; }
   __device__ static float part(u32x4 v, int i) { return __uint_as_float(v[i]); }
@@ -102,26 +100,24 @@ struct Piece<false> {
   }
 };
 
-// each(piece, its index) for the pieces of n elements from p on, and
-// rest(element, its index) for the elements behind the last piece.
-template <bool BF16, class Each, class Rest>
-__device__ __forceinline__ void for_pieces(const char* p, int n, Each each, Rest rest) {
-  using P = Piece<BF16>;
-  const int whole = n / P::E, tid = threadIdx.x;
-  for (int i = tid; i < whole; i += kFlight * kThreads) {
-    u32x4 v[kFlight];
-    // Unconditional, from clamped places: counted loads, waited for one by one.
+// kFlight pieces of a thread, from piece `first` on.  Loaded unconditionally,
+// from clamped places: counted loads, waited for one by one.  whole > 0.
+struct Batch {
+  typedef u32x4 __attribute__((aligned(2))) Vec;
+  u32x4 v[kFlight];
+  __device__ void load(const char* p, int first, int whole) {
 #pragma unroll
     for (int k = 0; k < kFlight; ++k)
-      v[k] = *reinterpret_cast<const typename P::Vec*>(p + static_cast<int64_t>(min(i + k * kThreads, whole - 1)) * 16);
+      v[k] = *reinterpret_cast<const Vec*>(p + static_cast<int64_t>(min(first + k * kThreads, whole - 1)) * 16);
     asm volatile("" ::: "memory");
+  }
+  template <class Each>
+  __device__ void each(int first, int whole, Each f) const {
 #pragma unroll
     for (int k = 0; k < kFlight; ++k)
-      if (i + k * kThreads < whole) each(v[k], i + k * kThreads);
+      if (first + k * kThreads < whole) f(v[k], first + k * kThreads);
   }
-  const int j = whole * P::E + tid;
-  if (j < n) rest(P::get(p + static_cast<int64_t>(j) * P::kBytes), j);
-}
+};
 
 __device__ __forceinline__ double block_sum(double v) {
   __shared__ double s_red[kThreads / 64];
@@ -139,24 +135,31 @@ __device__ __forceinline__ double block_sum(double v) {
 template <bool BF16>
 __device__ __forceinline__ double chunk_squares(const char* p, int n) {
   using P = Piece<BF16>;
+  const int whole = n / P::E;
   double s = 0.0;
-  for_pieces<BF16>(
-      p, n,
-      [&](u32x4 v, int) {
+  for (int i = threadIdx.x; i < whole; i += kFlight * kThreads) {
+    Batch b;
+    b.load(p, i, whole);
+    b.each(i, whole, [&](u32x4 v, int) {
 #pragma unroll
-        for (int e = 0; e < P::E; ++e) {
-          const double g = P::part(v, e);
-          s = fma(g, g, s);
-        }
-      },
-      [&](float x, int) { s += static_cast<double>(x) * x; });
+      for (int e = 0; e < P::E; ++e) {
+        const double g = P::part(v, e);
+        s = fma(g, g, s);
+      }
+    });
+  }
+  const int j = whole * P::E + threadIdx.x;
+  if (j < n) {
+    const double g = P::get(p + static_cast<int64_t>(j) * P::kBytes);
+    s = fma(g, g, s);
+  }
   return s;
 }
 
 __global__ __launch_bounds__(kThreads) void grad_squares_kernel(InBlock b, double* parts) {
   double s = 0.0;
   for (int c = blockIdx.x; c < b.chunks; c += gridDim.x) {
-    const Chunk k = find_chunk(b, c);
+    const Chunk k = find_chunk<true>(b, c);
     const char* p = b.in[k.span] + k.lo * (k.bf16 ? 2 : 4);
     const int n = static_cast<int>(k.hi - k.lo);
     s += k.bf16 ? chunk_squares<true>(p, n) : chunk_squares<false>(p, n);
@@ -165,9 +168,18 @@ __global__ __launch_bounds__(kThreads) void grad_squares_kernel(InBlock b, doubl
   if (threadIdx.x == 0) parts[blockIdx.x] = s;
 }
 
+// Every workgroup that asks gets the same value.
 __device__ __forceinline__ double norm_of(const double* parts, int32_t n) {
+  constexpr int kAtOnce = kMaxGroups / kThreads;
   double s = 0.0;
-  for (int i = threadIdx.x; i < n; i += kThreads) s += parts[i];
+  for (int i = threadIdx.x; i < n; i += kAtOnce * kThreads) {
+    double v[kAtOnce];
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) v[k] = parts[min(i + k * kThreads, n - 1)];
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) s += i + k * kThreads < n ? v[k] : 0.0;
+  }
   return sqrt(block_sum(s));
 }
 
@@ -186,42 +198,52 @@ struct Factor {
     c = static_cast<float>(tiny ? f * 0x1p64 : f);
   }
   __device__ float operator*(float g) const { return g * pre * c; }
+  __device__ bool keeps() const { return pre == 1.0f && c == 1.0f; }
 };
 
+// The chunk's n elements scaled, the thread's first pieces being there.
 template <bool BF16>
-__device__ __forceinline__ void chunk_scale(const char* in, char* out, int n, Factor f) {
+__device__ __forceinline__ void chunk_scale(const char* in, char* out, int n, Batch b, Factor f) {
   using P = Piece<BF16>;
-  for_pieces<BF16>(
-      in, n,
-      [&](u32x4 v, int i) {
-        float x[P::E];
+  const int whole = n / P::E;
+  for (int i = threadIdx.x; i < whole;) {
+    b.each(i, whole, [&](u32x4 v, int at) {
+      float x[P::E];
 #pragma unroll
-        for (int e = 0; e < P::E; ++e) x[e] = f * P::part(v, e);
-        *reinterpret_cast<typename P::Vec*>(out + static_cast<int64_t>(i) * 16) = P::pack(x);
-      },
-      [&](float x, int j) { P::put(out + static_cast<int64_t>(j) * P::kBytes, f * x); });
+      for (int e = 0; e < P::E; ++e) x[e] = f * P::part(v, e);
+      *reinterpret_cast<Batch::Vec*>(out + static_cast<int64_t>(at) * 16) = P::pack(x);
+    });
+    i += kFlight * kThreads;
+    if (i < whole) b.load(in, i, whole);
+  }
+  const int j = whole * P::E + threadIdx.x;
+  if (j < n) P::put(out + static_cast<int64_t>(j) * P::kBytes, f * P::get(in + static_cast<int64_t>(j) * P::kBytes));
 }
 
-// PairBlock: out of place; InBlock: in place.
+// PairBlock: out of place; InBlock: in place.  Every workgroup has a chunk;
+// its first pieces are on their way while the norm is added up.
 template <class B>
-__global__ __launch_bounds__(kThreads) void grad_scale_kernel(B b, const double* parts, int32_t n, float max_norm,
+__global__ __launch_bounds__(kThreads, 6) void grad_scale_kernel(B b, const double* parts, int32_t n, float max_norm,
                                                               float eps, float* norm_out) {
   constexpr bool kInPlace = sizeof(b.out) == sizeof(char*);
-  const double norm = norm_of(parts, n);
-  if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = static_cast<float>(norm);
-  const double ratio = norm == 0.0 ? 1.0 : static_cast<double>(max_norm) / (norm + static_cast<double>(eps));
-  const Factor f(ratio >= 1.0 ? 1.0 : ratio);  // NaN stays
-  const bool same = f.pre * f.c == 1.0f;
-  if (kInPlace && same) return;  // nothing to clip
+  Factor f(1.0);
   for (int i = blockIdx.x; i < b.chunks; i += gridDim.x) {
-    const Chunk k = find_chunk(b, b.chunks - 1 - i);
-    const int64_t at = k.lo * (k.bf16 ? 2 : 4);
-    const char* in = b.in[k.span] + at;
-    char* out = kInPlace ? const_cast<char*>(in) : b.out[k.span] + at;
-    const int len = static_cast<int>(k.hi - k.lo);
-    if (same && in == out) continue;
-    if (k.bf16) chunk_scale<true>(in, out, len, f);
-    else chunk_scale<false>(in, out, len, f);
+    const Chunk k = find_chunk<false>(b, i);
+    const int len = static_cast<int>(k.hi - k.lo), size = k.bf16 ? 2 : 4;
+    const char* in = b.in[k.span] + k.lo * size;
+    char* out = kInPlace ? const_cast<char*>(in) : b.out[k.span] + k.lo * size;
+    Batch first;
+    if (len * size >= 16) first.load(in, threadIdx.x, len * size / 16);
+    if (i == blockIdx.x) {
+      const double norm = norm_of(parts, n);
+      if (norm_out && i == 0 && threadIdx.x == 0) *norm_out = static_cast<float>(norm);
+      const double ratio = norm == 0.0 ? 1.0 : static_cast<double>(max_norm) / (norm + static_cast<double>(eps));
+      f = Factor(ratio >= 1.0 ? 1.0 : ratio);  // NaN stays
+      if (kInPlace && f.keeps()) return;
+    }
+    if (f.keeps() && in == out) continue;
+    if (k.bf16) chunk_scale<true>(in, out, len, first, f);
+    else chunk_scale<false>(in, out, len, first, f);
   }
 }
 
@@ -263,34 +285,33 @@ int check_spans(const dora_span* s, int32_t n) {
   return DORA_OK;
 }
 
-// Where in the list a launch begins: a tensor and an element of it.
+// How far a pass over the list has come: tensors, and elements of the next one.
 struct Place {
-  int32_t span;
-  int64_t element;
+  int32_t spans;
+  int64_t elements;
 };
 
-// The next launch's tensors from `at` on, empty ones left out; returns where
-// the one after it begins.
-template <class B>
-Place fill_block(const dora_span* grads, const dora_span* out, int32_t n, Place at, int chunk, B* b) {
+// The next launch's tensors, empty ones left out; BACK: from the list's end.
+template <bool BACK, class B>
+void fill_block(const dora_span* grads, const dora_span* out, int32_t n, Place& at, int chunk, B* b) {
   b->n = b->chunks = 0;
   b->chunk = chunk;
-  while (at.span < n && b->n < B::kSpans) {
-    const dora_span& g = grads[at.span];
-    const int64_t len = std::min(g.numel - at.element, kPart);
+  while (at.spans < n && b->n < B::kSpans) {
+    const int32_t s = BACK ? n - 1 - at.spans : at.spans;
+    const dora_span& g = grads[s];
+    const int64_t len = std::min(g.numel - at.elements, kPart);
     if (len > 0) {
       const int i = b->n++;
-      const int64_t byte = at.element * (g.dtype == DORA_BF16 ? 2 : 4);
+      const int64_t byte = (BACK ? g.numel - at.elements - len : at.elements) * (g.dtype == DORA_BF16 ? 2 : 4);
       b->in[i] = static_cast<const char*>(g.data) + byte;
-      if (sizeof(b->out) > sizeof(char*)) b->out[i] = static_cast<char*>(out[at.span].data) + byte;
+      if (sizeof(b->out) > sizeof(char*)) b->out[i] = static_cast<char*>(out[s].data) + byte;
       b->numel[i] = static_cast<uint32_t>(len) | (g.dtype == DORA_BF16 ? kBF16 : 0u);
       b->first[i] = b->chunks;
       b->chunks += static_cast<int32_t>((len + chunk - 1) / chunk);
-      at.element += len;
+      at.elements += len;
     }
-    if (at.element >= g.numel) at = {at.span + 1, 0};
+    if (at.elements >= g.numel) at = {at.spans + 1, 0};
   }
-  return at;
 }
 
 // A launch's share of the pass's workgroups.
@@ -344,8 +365,8 @@ extern "C" int dora_grad_clip(const dora_span* grads, const dora_span* out, int3
   for (int32_t i = 0; i < n; ++i) all += (grads[i].numel + chunk - 1) / chunk;
   int32_t used = 0;
   InBlock b;
-  for (Place at{0, 0}; at.span < n;) {
-    at = fill_block(grads, nullptr, n, at, chunk, &b);
+  for (Place at{0, 0}; at.spans < n;) {
+    fill_block<true>(grads, nullptr, n, at, chunk, &b);
     if (b.n == 0) continue;
     const int groups = launch_groups(b.chunks, all);
     hipLaunchKernelGGL(grad_squares_kernel, dim3(groups), dim3(kThreads), 0, st, b, parts + used);
@@ -353,23 +374,21 @@ extern "C" int dora_grad_clip(const dora_span* grads, const dora_span* out, int3
   }
   if (!scale || used == 0) {
     hipLaunchKernelGGL(grad_norm_kernel, dim3(1), dim3(kThreads), 0, st, parts, used, norm_out);
-  } else if (!out) {
-    float* norm = norm_out;
-    for (Place at{0, 0}; at.span < n;) {
-      at = fill_block(grads, nullptr, n, at, chunk, &b);
-      if (b.n == 0) continue;
-      hipLaunchKernelGGL(grad_scale_kernel<InBlock>, dim3(launch_groups(b.chunks, all)), dim3(kThreads), 0, st, b,
-                         parts, used, max_norm, eps, norm);
-      norm = nullptr;
-    }
   } else {
-    float* norm = norm_out;
+    float* norm = norm_out;  // written by the first launch
     PairBlock pair;
-    for (Place at{0, 0}; at.span < n;) {
-      at = fill_block(grads, out, n, at, chunk, &pair);
-      if (pair.n == 0) continue;
-      hipLaunchKernelGGL(grad_scale_kernel<PairBlock>, dim3(launch_groups(pair.chunks, all)), dim3(kThreads), 0, st,
-                         pair, parts, used, max_norm, eps, norm);
+    for (Place at{0, 0}; at.spans < n;) {
+      if (out) {
+        fill_block<false>(grads, out, n, at, chunk, &pair);
+        if (pair.n == 0) continue;
+        hipLaunchKernelGGL(grad_scale_kernel<PairBlock>, dim3(launch_groups(pair.chunks, all)), dim3(kThreads), 0, st,
+                           pair, parts, used, max_norm, eps, norm);
+      } else {
+        fill_block<false>(grads, out, n, at, chunk, &b);
+        if (b.n == 0) continue;
+        hipLaunchKernelGGL(grad_scale_kernel<InBlock>, dim3(launch_groups(b.chunks, all)), dim3(kThreads), 0, st, b,
+                           parts, used, max_norm, eps, norm);
+      }
       norm = nullptr;
     }
   }
