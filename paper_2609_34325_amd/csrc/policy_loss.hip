@@ -16,6 +16,7 @@
 // The lanes' triples are merged the same way.  Sums are fp32, the row's own
 // figures 64 bits.
 #include <algorithm>
+#include <cfloat>
 
 #include "dora_internal.h"
 #include "policy_terms.h"
@@ -108,10 +109,10 @@ __device__ __forceinline__ void store_piece(char* p, u32x4 v) {
 }
 
 // A row's exponentials are 2^d with d = x c1 - e, c1 = log2(e) rounded and e
-// the whole number next to m c1: one fused step whose only error is its own
-// rounding, and raising m scales the older sums by a power of two, exactly.
-// The shift in natural units is then e / c1 (in 64 bits): terms near the
-// largest, which make up the sums, all carry c1's rounding alike.
+// the whole number next to m c1 for a reference m: one fused step whose only
+// error is its own rounding, and another m scales the older sums by a power of
+// two, exactly.  The shift in natural units is then e / c1 (in 64 bits): terms
+// near the largest, which make up the sums, all carry c1's rounding alike.
 // Past 5e8 two different floats lie at least 32 apart, so any factor tells
 // them from each other, and m c1 would leave a large rest or overflow: there
 // d = x - m (a row whose open logits all hold the type's lowest value is
@@ -122,30 +123,22 @@ struct Shift {
   __device__ explicit Shift(float m) {
     const bool vast = fabsf(m) > kVast;
     c1 = vast ? 1.0f : kLog2E;
-    e = vast ? (m == -__builtin_inff() ? 0.0f : m) : rintf(m * kLog2E);
+    e = vast ? m : rintf(m * kLog2E);
   }
   __device__ float operator()(float x) const { return fmaf(x, c1, -e); }
   __device__ double natural() const { return static_cast<double>(e) / static_cast<double>(c1); }
 };
 
-// Open elements of row t (0: padding or a bad row), its weight and action.
-__device__ __forceinline__ int open_row(const RowParams& p, int64_t t, float& w, int& a) {
-  w = p.weight ? p.weight[t] : 1.0f;
-  a = 0;
-  if (w == 0.0f) return 0;
-  const int n = p.legal ? p.legal[t] : p.V;
-  a = p.actions[t];
-  return n >= 1 && n <= p.V && a >= 0 && a < n ? n : 0;
-}
-
-// Running softmax statistics: m = max x, s = sum 2^d, h = sum 2^d d.
-// fmaxf passes over NaN, so m never is one; a NaN logit reaches s and h.
+// Running softmax statistics: s = sum 2^d, h = sum 2^d d at reference m.  m is
+// an element that was seen, or the lowest float; s = 0 where nothing but -inf
+// was.  fmaxf passes over NaN, so m never is one; a NaN logit reaches s and h.
 struct Stat {
   float m, s, h;
+  __device__ static Stat none() { return {-FLT_MAX, 0.0f, 0.0f}; }
   __device__ void raise(float to) {
     const bool vast = fabsf(m) > kVast || fabsf(to) > kVast;
     const float step = vast ? m - to : rintf(m * kLog2E) - rintf(to * kLog2E);
-    const float delta = fmaxf(step, kFarDown);  // also where both are -inf
+    const float delta = fmaxf(step, kFarDown);
     const float f = __builtin_amdgcn_exp2f(delta);
     h = f * fmaf(s, delta, h);
     s *= f;
@@ -158,21 +151,42 @@ struct Stat {
     s += o.s;
     h += o.h;
   }
+};
+
+// The statistics while a thread takes its pieces.  The reference is raised
+// only past 2^24 of it: hardly ever after the first piece.
+struct Taker {
+  Stat st = Stat::none();
+  Shift sh{-FLT_MAX};
   template <int N>
   __device__ void take(const float (&x)[N]) {
     float top = x[0];
 #pragma unroll
     for (int i = 1; i < N; ++i) top = fmaxf(top, x[i]);
-    raise(fmaxf(m, top));
-    const Shift sh(m);
+    if (sh(top) > 24.0f) {
+      st.raise(top);
+      sh = Shift(top);
+    }
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const float d = sh(x[i]), e = __builtin_amdgcn_exp2f(d);
-      s += e;
-      h = fmaf(e, fmaxf(d, kFarDown), h);
+      st.s += e;
+      st.h = fmaf(e, fmaxf(d, kFarDown), st.h);
     }
   }
 };
+
+// Open elements of row t (0: padding or a bad row), its weight and action (0
+// for such a row).
+__device__ __forceinline__ int open_row(const RowParams& p, int64_t t, float& w, int& a) {
+  w = p.weight ? p.weight[t] : 1.0f;
+  a = 0;
+  if (w == 0.0f) return 0;
+  const int n = p.legal ? p.legal[t] : p.V, act = p.actions[t];
+  if (!(n >= 1 && n <= p.V && act >= 0 && act < n)) return 0;
+  a = act;
+  return n;
+}
 
 // Merged over groups of G lanes; every lane gets the same triple.
 template <int G>
@@ -192,24 +206,29 @@ struct RowSlope {
   int n, action;
 };
 
-// The gradient's elements from the logits'.
+// The gradient's elements from the logits'.  ENT: with an entropy term.
+template <bool BF16, bool ENT>
 struct Slope {
+  using X = Elem<BF16>;
   Shift sh;
   RowSlope rs;
   __device__ explicit Slope(const RowSlope& r) : sh(r.m), rs(r) {}
-  __device__ float open(float x, int j) const {
-    const float d = sh(x);
-    return __builtin_amdgcn_exp2f(d) * fmaf(rs.k1, fmaxf(d, kFarDown), rs.base) + (j == rs.action ? rs.slope : 0.0f);
+  __device__ float open(float x) const {
+    const float d = sh(x), e = __builtin_amdgcn_exp2f(d);
+    return ENT ? e * fmaf(rs.k1, fmaxf(d, kFarDown), rs.base) : e * rs.base;
   }
-  __device__ float at(float x, int j) const { return j < rs.n ? open(x, j) : 0.0f; }
-  template <bool BF16>
+  __device__ float at(float x, int j) const {
+    return j < rs.n ? open(x) + (j == rs.action ? rs.slope : 0.0f) : 0.0f;
+  }
   __device__ u32x4 piece(u32x4 v, int i) const {
-    constexpr int E = Elem<BF16>::kPer;
-    float x[E];
-    Elem<BF16>::unpack(v, x);
+    float x[X::kPer];
+    X::unpack(v, x);
 #pragma unroll
-    for (int e = 0; e < E; ++e) x[e] = open(x[e], i * E + e);
-    return Elem<BF16>::pack(x);
+    for (int e = 0; e < X::kPer; ++e) x[e] = open(x[e]);
+    if (i == rs.action / X::kPer)
+#pragma unroll
+      for (int e = 0; e < X::kPer; ++e) x[e] += e == rs.action % X::kPer ? rs.slope : 0.0f;
+    return X::pack(x);
   }
 };
 
@@ -219,7 +238,7 @@ template <bool GRAD>
 __device__ __forceinline__ RowSlope close_row(const RowParams& p, int64_t t, float w, int n, int a, float xa, Stat st,
                                               bool first, PolicyTerms* sum) {
   bool good = n > 0;
-  if (good && st.m == -__builtin_inff() && st.s == 0.0f) good = false;  // nothing open (s is NaN where a logit is)
+  if (good && st.s == 0.0f) good = false;  // nothing open
   double logp = 0.0, entropy = 0.0;
   RowSlope rs{st.m, 0.0f, 0.0f, 0.0f, 0, a};
   if (good) {
@@ -253,7 +272,7 @@ __device__ __forceinline__ RowSlope close_row(const RowParams& p, int64_t t, flo
 // ...) in registers from the statistics to the gradient, so that a row of up
 // to L NV pieces is read once; what is past them is read again.  A
 // workgroup holds max(1, 256 / L) rows.
-template <bool BF16, int L, int NV, bool GRAD>
+template <bool BF16, int L, int NV, bool GRAD, bool ENT>
 __global__ __launch_bounds__((L > kThreads ? L : kThreads), 4) void policy_rows_kernel(RowParams p) {
   using X = Elem<BF16>;
   constexpr int E = X::kPer, kWG = L > kThreads ? L : kThreads, kRows = kWG / L, kWaves = L / 64;
@@ -272,7 +291,9 @@ __global__ __launch_bounds__((L > kThreads ? L : kThreads), 4) void policy_rows_
     int a;
     const int n = open_row(p, t, w, a);
     const int whole = n / E;
-    Stat st{-__builtin_inff(), 0.0f, 0.0f};
+    // The action's logit, ahead of the pieces: waiting for it is not waiting for them.
+    const float xa = X::get(row + static_cast<int64_t>(a) * X::kBytes);
+    Taker tk;
     u32x4 held[NV];
     if (whole > 0) {  // the same for all threads of a row
       // Loads are unconditional (a piece past the last one is the last one
@@ -282,31 +303,30 @@ __global__ __launch_bounds__((L > kThreads ? L : kThreads), 4) void policy_rows_
         held[i] = load_piece<BF16>(row + static_cast<int64_t>(min(lane + i * L, whole - 1)) * 16);
       asm volatile("" ::: "memory");
     }
-    const float xa = n > 0 ? X::get(row + static_cast<int64_t>(a) * X::kBytes) : 0.0f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       if (lane + i * L < whole) {
         float x[E];
         X::unpack(held[i], x);
-        st.take(x);
+        tk.take(x);
       }
     }
     for (int i = lane + NV * L; i < whole; i += L) {
       float x[E];
       X::unpack(load_piece<BF16>(row + static_cast<int64_t>(i) * 16), x);
-      st.take(x);
+      tk.take(x);
     }
     if (whole * E + lane < n) {
       const float x[1] = {X::get(row + static_cast<int64_t>(whole * E + lane) * X::kBytes)};
-      st.take(x);
+      tk.take(x);
     }
     RowSlope rs;
     if constexpr (L <= 64) {
-      rs = close_row<GRAD>(p, t, w, n, a, xa, merge_lanes<L>(st), lane == 0, &s_terms[group]);
+      rs = close_row<GRAD>(p, t, w, n, a, xa, merge_lanes<L>(tk.st), lane == 0, &s_terms[group]);
     } else {
       // One wave closes the row: 64-bit exp and log by all of them would cost
       // as much as the row's own exponentials.
-      st = merge_lanes<64>(st);
+      Stat st = merge_lanes<64>(tk.st);
       if ((threadIdx.x & 63) == 0) s_red[threadIdx.x >> 6] = st;
       __syncthreads();
       if (threadIdx.x < 64) {
@@ -319,10 +339,8 @@ __global__ __launch_bounds__((L > kThreads ? L : kThreads), 4) void policy_rows_
     }
     if constexpr (GRAD) {
       char* out = p.grad + t * p.ld_grad * X::kBytes;
-      const Slope slope(rs);
-      auto put = [&](u32x4 v, int i) {
-        store_piece<BF16>(out + static_cast<int64_t>(i) * 16, slope.template piece<BF16>(v, i));
-      };
+      const Slope<BF16, ENT> slope(rs);
+      auto put = [&](u32x4 v, int i) { store_piece<BF16>(out + static_cast<int64_t>(i) * 16, slope.piece(v, i)); };
       // Opaque to the compiler, which would otherwise keep the pieces unpacked
       // (twice the registers) from the statistics on.
 #pragma unroll
@@ -354,7 +372,7 @@ template <bool BF16>
 __device__ __forceinline__ Stat range_stats(const char* row, int lo, int hi, bool end, int n) {
   using X = Elem<BF16>;
   constexpr int kFlight = 4;
-  Stat st{-__builtin_inff(), 0.0f, 0.0f};
+  Taker tk;
   for (int i = lo + threadIdx.x; i < hi; i += kFlight * kThreads) {
     u32x4 v[kFlight];
 #pragma unroll
@@ -366,16 +384,16 @@ __device__ __forceinline__ Stat range_stats(const char* row, int lo, int hi, boo
       if (i + k * kThreads < hi) {
         float x[X::kPer];
         X::unpack(v[k], x);
-        st.take(x);
+        tk.take(x);
       }
     }
   }
   const int j = n / X::kPer * X::kPer + threadIdx.x;
   if (end && j < n) {
     const float x[1] = {X::get(row + static_cast<int64_t>(j) * X::kBytes)};
-    st.take(x);
+    tk.take(x);
   }
-  return st;
+  return tk.st;
 }
 
 // This workgroup's share of the pieces of a row of V elements (of n open ones).
@@ -423,7 +441,7 @@ __device__ __forceinline__ RowSlope close_split_row(const RowParams& p, int64_t 
   float w;
   int a;
   const int n = open_row(p, t, w, a);
-  Stat st{-__builtin_inff(), 0.0f, 0.0f};
+  Stat st = Stat::none();
 #pragma unroll
   for (int k = 0; k < kEach; ++k)
     if (lane + k * G < p.split) st.merge(Stat{v[k].x, v[k].y, v[k].z});
@@ -439,7 +457,7 @@ __global__ __launch_bounds__(kThreads) void policy_close_kernel(RowParams p) {
 // Gradient of split rows: each workgroup closes its row for itself and writes
 // its chunk.  One workgroup more, the last, closes all rows for the outputs
 // and sums.
-template <bool BF16>
+template <bool BF16, bool ENT>
 __global__ __launch_bounds__(kThreads, 3) void policy_split_grad_kernel(RowParams p) {
   using X = Elem<BF16>;
   constexpr int E = X::kPer;
@@ -469,10 +487,10 @@ __global__ __launch_bounds__(kThreads, 3) void policy_split_grad_kernel(RowParam
   char* out = p.grad + t * p.ld_grad * X::kBytes;
   const int chunk = blockIdx.x % p.split;
   const int2 open = chunk_of<BF16>(p, chunk, rs.n), all = chunk_of<BF16>(p, chunk, p.V);
-  const Slope slope(rs);
+  const Slope<BF16, ENT> slope(rs);
   for (int i = open.x + threadIdx.x; i < open.y; i += kThreads)
     store_piece<BF16>(out + static_cast<int64_t>(i) * 16,
-                      slope.template piece<BF16>(load_piece<BF16>(row + static_cast<int64_t>(i) * 16), i));
+                      slope.piece(load_piece<BF16>(row + static_cast<int64_t>(i) * 16), i));
   const int end = chunk == p.split - 1 ? p.V : all.y * E;
   for (int j = max(open.y, all.x) * E + threadIdx.x; j < end; j += kThreads) {
     const float x = j < rs.n ? X::get(row + static_cast<int64_t>(j) * X::kBytes) : 0.0f;
@@ -505,11 +523,11 @@ __global__ __launch_bounds__(kThreads) void policy_finish_kernel(const double* p
   }
 }
 
-template <bool BF16, bool GRAD, int L, int NV>
+template <bool BF16, bool GRAD, bool ENT, int L, int NV>
 void launch_shape(const RowParams& p, hipStream_t st) {
   constexpr int kWG = L > kThreads ? L : kThreads, kRows = kWG / L;
   const int groups = (p.T + kRows - 1) / kRows;
-  hipLaunchKernelGGL((policy_rows_kernel<BF16, L, NV, GRAD>), dim3(groups), dim3(kWG), 0, st, p);
+  hipLaunchKernelGGL((policy_rows_kernel<BF16, L, NV, GRAD, ENT>), dim3(groups), dim3(kWG), 0, st, p);
   if constexpr (GRAD) launch_policy_finish(p.parts, groups, p.stats, st);
 }
 
@@ -523,31 +541,31 @@ int split_of(int32_t T, int pieces) {
 
 // The fewest threads a row that hold it in 16 pieces each: short rows share a
 // wave, and the threads left over take other rows.
-template <bool BF16, bool GRAD>
+template <bool BF16, bool GRAD, bool ENT>
 void launch_rows(RowParams p, hipStream_t st) {
   const int pieces = (p.V + Elem<BF16>::kPer - 1) / Elem<BF16>::kPer;
-  if (pieces <= 16) return launch_shape<BF16, GRAD, 16, 1>(p, st);
-  if (pieces <= 32) return launch_shape<BF16, GRAD, 16, 2>(p, st);
-  if (pieces <= 64) return launch_shape<BF16, GRAD, 16, 4>(p, st);
-  if (pieces <= 256) return launch_shape<BF16, GRAD, 64, 4>(p, st);
-  if (pieces <= 512) return launch_shape<BF16, GRAD, 64, 8>(p, st);
+  if (pieces <= 16) return launch_shape<BF16, GRAD, ENT, 16, 1>(p, st);
+  if (pieces <= 32) return launch_shape<BF16, GRAD, ENT, 16, 2>(p, st);
+  if (pieces <= 64) return launch_shape<BF16, GRAD, ENT, 16, 4>(p, st);
+  if (pieces <= 256) return launch_shape<BF16, GRAD, ENT, 64, 4>(p, st);
+  if (pieces <= 512) return launch_shape<BF16, GRAD, ENT, 64, 8>(p, st);
   p.split = p.split_stats ? split_of(p.T, pieces) : 1;
   if (p.split > 1 || !GRAD) {
     hipLaunchKernelGGL(policy_stats_kernel<BF16>, dim3(static_cast<uint32_t>(p.T) * p.split), dim3(kThreads), 0, st, p);
     if constexpr (GRAD)
-      hipLaunchKernelGGL(policy_split_grad_kernel<BF16>, dim3(p.T * p.split + 1), dim3(kThreads), 0, st, p);
+      hipLaunchKernelGGL((policy_split_grad_kernel<BF16, ENT>), dim3(p.T * p.split + 1), dim3(kThreads), 0, st, p);
     else if (p.split > 1)
       hipLaunchKernelGGL(policy_close_kernel, dim3((p.T * 8 + kThreads - 1) / kThreads), dim3(kThreads), 0, st, p);
     return;
   }
   if constexpr (GRAD) {
-    if (pieces <= 1024) launch_shape<BF16, GRAD, 256, 4>(p, st);
-    else if (pieces <= 2048) launch_shape<BF16, GRAD, 256, 8>(p, st);
-    else if (pieces <= 4096) launch_shape<BF16, GRAD, 256, 16>(p, st);
-    else if (pieces <= 6144) launch_shape<BF16, GRAD, 512, 12>(p, st);
-    else if (pieces <= 8192) launch_shape<BF16, GRAD, 512, 16>(p, st);
-    else if (pieces <= 12288) launch_shape<BF16, GRAD, 1024, 12>(p, st);
-    else launch_shape<BF16, GRAD, 1024, 16>(p, st);
+    if (pieces <= 1024) launch_shape<BF16, GRAD, ENT, 256, 4>(p, st);
+    else if (pieces <= 2048) launch_shape<BF16, GRAD, ENT, 256, 8>(p, st);
+    else if (pieces <= 4096) launch_shape<BF16, GRAD, ENT, 256, 16>(p, st);
+    else if (pieces <= 6144) launch_shape<BF16, GRAD, ENT, 512, 12>(p, st);
+    else if (pieces <= 8192) launch_shape<BF16, GRAD, ENT, 512, 16>(p, st);
+    else if (pieces <= 12288) launch_shape<BF16, GRAD, ENT, 1024, 12>(p, st);
+    else launch_shape<BF16, GRAD, ENT, 1024, 16>(p, st);
   }
 }
 
@@ -630,8 +648,8 @@ extern "C" int dora_action_logprob(const void* logits, int64_t ld, const int32_t
   p.split = 1;
   p.status = dev_status;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  if (dtype == DORA_BF16) launch_rows<true, false>(p, st);
-  else launch_rows<false, false>(p, st);
+  if (dtype == DORA_BF16) launch_rows<true, false, false>(p, st);
+  else launch_rows<false, false, false>(p, st);
   return hipGetLastError() == hipSuccess ? DORA_OK : DORA_ERR_HIP;
 }
 
@@ -661,7 +679,8 @@ extern "C" int dora_policy_loss(const void* logits, int64_t ld, const int32_t* a
               logprob_out, nullptr, static_cast<double*>(workspace), static_cast<float4*>(workspace), 1, stats_out,
               dev_status};
   hipStream_t st = static_cast<hipStream_t>(stream);
-  if (dtype == DORA_BF16) launch_rows<true, true>(p, st);
-  else launch_rows<false, true>(p, st);
+  const bool ent = entropy_coef != 0.0f;
+  if (dtype == DORA_BF16) ent ? launch_rows<true, true, true>(p, st) : launch_rows<true, true, false>(p, st);
+  else ent ? launch_rows<false, true, true>(p, st) : launch_rows<false, true, false>(p, st);
   return hipGetLastError() == hipSuccess ? DORA_OK : DORA_ERR_HIP;
 }
