@@ -25,6 +25,7 @@ namespace dora {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kFinishThreads = 1024;
 constexpr int kMaxSplit = 64;  // workgroups a row
 constexpr float kLog2E = 1.4426950408889634f;
 constexpr double kLn2 = 0.6931471805599453;
@@ -176,6 +177,12 @@ struct Taker {
   }
 };
 
+template <bool BF16>
+__device__ __forceinline__ void take_one(Taker& tk, const char* row, int j) {
+  const float x[1] = {Elem<BF16>::get(row + static_cast<int64_t>(j) * Elem<BF16>::kBytes)};
+  tk.take(x);
+}
+
 // Open elements of row t (0: padding or a bad row), its weight and action (0
 // for such a row).
 __device__ __forceinline__ int open_row(const RowParams& p, int64_t t, float& w, int& a) {
@@ -206,178 +213,225 @@ struct RowSlope {
   int n, action;
 };
 
+// A row cut at the 16-byte boundaries of memory (of the gradient's, where
+// there is one): `head` elements, `all` pieces, fewer elements than a piece.
+// The first `open` pieces are all open, the next may be in part.
+template <bool BF16>
+struct RowCut {
+  static constexpr int E = Elem<BF16>::kPer, kBytes = Elem<BF16>::kBytes;
+  int head, open, all, n, V;
+  __device__ RowCut(const char* at, int n_, int V_) : n(n_), V(V_) {
+    head = min(V, static_cast<int>((16 - (reinterpret_cast<uintptr_t>(at) & 15)) & 15) / kBytes);
+    all = (V - head) / E;
+    open = max(n - head, 0) / E;
+  }
+  __device__ int64_t byte(int piece) const { return static_cast<int64_t>(piece) * 16 + head * kBytes; }
+  // The element outside the pieces that is the lane's, V or more: none.
+  __device__ int edge(int lane) const {
+    return lane < 8 ? (lane < head ? lane : V) : (lane < 16 ? head + all * E + lane - 8 : V);
+  }
+  // Its element of the piece that is open in part; n or more: none.
+  __device__ int part(int lane) const { return lane < E && open < all ? head + open * E + lane : n; }
+  __device__ int closed() const { return open + (part(0) < n ? 1 : 0); }  // the first piece with nothing open
+};
+
 // The gradient's elements from the logits'.  ENT: with an entropy term.
 template <bool BF16, bool ENT>
 struct Slope {
   using X = Elem<BF16>;
   Shift sh;
   RowSlope rs;
-  __device__ explicit Slope(const RowSlope& r) : sh(r.m), rs(r) {}
+  int at_piece, at_element;
+  __device__ Slope(const RowSlope& r, int head) : sh(r.m), rs(r) {
+    at_piece = (r.action - head) >> (BF16 ? 3 : 2);
+    at_element = (r.action - head) & (X::kPer - 1);
+  }
   __device__ float open(float x) const {
     const float d = sh(x), e = __builtin_amdgcn_exp2f(d);
     return ENT ? e * fmaf(rs.k1, fmaxf(d, kFarDown), rs.base) : e * rs.base;
-  }
-  __device__ float at(float x, int j) const {
-    return j < rs.n ? open(x) + (j == rs.action ? rs.slope : 0.0f) : 0.0f;
   }
   __device__ u32x4 piece(u32x4 v, int i) const {
     float x[X::kPer];
     X::unpack(v, x);
 #pragma unroll
     for (int e = 0; e < X::kPer; ++e) x[e] = open(x[e]);
-    if (i == rs.action / X::kPer)
+    if (i == at_piece)
 #pragma unroll
-      for (int e = 0; e < X::kPer; ++e) x[e] += e == rs.action % X::kPer ? rs.slope : 0.0f;
+      for (int e = 0; e < X::kPer; ++e) x[e] += e == at_element ? rs.slope : 0.0f;
     return X::pack(x);
+  }
+  // Element j < V of the row.
+  __device__ void one(const char* row, char* out, int j) const {
+    float g = 0.0f;
+    if (j < rs.n) g = open(X::get(row + static_cast<int64_t>(j) * X::kBytes)) + (j == rs.action ? rs.slope : 0.0f);
+    X::put(out + static_cast<int64_t>(j) * X::kBytes, g);
   }
 };
 
-// The row's own figures, by every lane that calls it; `first` is the lane that
-// writes them and adds the row's terms to sum.
-template <bool GRAD>
-__device__ __forceinline__ RowSlope close_row(const RowParams& p, int64_t t, float w, int n, int a, float xa, Stat st,
-                                              bool first, PolicyTerms* sum) {
-  bool good = n > 0;
-  if (good && st.s == 0.0f) good = false;  // nothing open
+// What closing a row takes, beside its statistics.
+struct RowIn {
+  float w, xa;
+  int n, a;
+};
+
+// The row's own figures; WRITES: to the outputs, and its terms are added to sum.
+template <bool GRAD, bool WRITES>
+__device__ __forceinline__ RowSlope close_row(const RowParams& p, int64_t t, RowIn in, Stat st, PolicyTerms* sum) {
   double logp = 0.0, entropy = 0.0;
-  RowSlope rs{st.m, 0.0f, 0.0f, 0.0f, 0, a};
-  if (good) {
+  RowSlope rs{st.m, 0.0f, 0.0f, 0.0f, 0, in.a};
+  if (in.n > 0 && st.s != 0.0f) {  // 0: nothing open
     const double s = st.s, logs = log(s);
-    logp = static_cast<double>(xa) - Shift(st.m).natural() - logs;
+    logp = static_cast<double>(in.xa) - Shift(st.m).natural() - logs;
     entropy = logs - static_cast<double>(st.h) / s * kLn2;
     if constexpr (GRAD) {
-      PolicyTerms one{};
-      const double slope = policy_decision(logp, entropy, p.old[t], p.adv[t], w, p.ref, t, p.coef, one);
-      if (first)
-#pragma unroll
-        for (int i = 0; i < kPolicyTerms; ++i) sum->v[i] += one.v[i];
-      const double c = static_cast<double>(p.coef.entropy) * w;
-      rs.n = n;
+      PolicyTerms unused{};
+      const double slope =
+          policy_decision(logp, entropy, p.old[t], p.adv[t], in.w, p.ref, t, p.coef, WRITES ? *sum : unused);
+      const double c = static_cast<double>(p.coef.entropy) * in.w;
+      rs.n = in.n;
       rs.slope = static_cast<float>(slope);
       rs.base = static_cast<float>(((p.coef.entropy != 0.0f ? c * (entropy - logs) : 0.0) - slope) / s);
       rs.k1 = p.coef.entropy != 0.0f ? static_cast<float>(c * kLn2 / s) : 0.0f;
     }
-  } else if (w != 0.0f) {
+  } else if (in.w != 0.0f) {
     logp = entropy = __builtin_nan("");
-    if (first) atomicOr(p.status, DORA_DEV_ACTION);
+    if (WRITES) atomicOr(p.status, DORA_DEV_ACTION);
   }
-  if (first) {
-    if (p.logp_out) p.logp_out[t] = static_cast<float>(logp);
+  if (WRITES) {
+    p.logp_out[t] = static_cast<float>(logp);
     if (p.entropy_out) p.entropy_out[t] = static_cast<float>(entropy);
   }
   return rs;
 }
 
+// Threads of a workgroup for rows of L threads.
+constexpr int group_threads(int L) { return L >= 256 ? L : (L == 64 ? 512 : 256); }
+
 // L threads a row.  Each holds its first NV pieces (thread i: pieces i, i + L,
 // ...) in registers from the statistics to the gradient, so that a row of up
-// to L NV pieces is read once; what is past them is read again.  A
-// workgroup holds max(1, 256 / L) rows.
+// to L NV pieces is read once; what is past them is read again.
 template <bool BF16, int L, int NV, bool GRAD, bool ENT>
-__global__ __launch_bounds__((L > kThreads ? L : kThreads), 4) void policy_rows_kernel(RowParams p) {
+__global__ __launch_bounds__(group_threads(L), 4) void policy_rows_kernel(RowParams p) {
   using X = Elem<BF16>;
-  constexpr int E = X::kPer, kWG = L > kThreads ? L : kThreads, kRows = kWG / L, kWaves = L / 64;
-  __shared__ PolicyTerms s_terms[kRows];
-  __shared__ Stat s_red[L > 64 ? kWaves : 1];
-  __shared__ RowSlope s_slope;
+  constexpr int kRows = group_threads(L) / L, kWaves = L / 64;
+  constexpr bool kPark = GRAD && NV > 4;
+  __shared__ Stat s_stat[L > 64 ? kWaves : kRows];
+  __shared__ RowIn s_in[kRows];
+  __shared__ RowSlope s_slope[kRows];
+  __shared__ u32x4 s_held[kPark ? NV * 64 : 1];
   const int lane = threadIdx.x % L, group = threadIdx.x / L;
-  if (GRAD && lane == 0) s_terms[group] = PolicyTerms{};
-  // A workgroup ends with its rows.  (In a loop over rows the compiler keeps
-  // the constants of the 64-bit functions in registers, which the rows need:
-  // up to 256 of them, and the longest spill.)
-  const int64_t t = static_cast<int64_t>(blockIdx.x) * kRows + group;
-  if (t < p.T) {
-    const char* row = p.logits + t * p.ld * X::kBytes;
-    float w;
-    int a;
-    const int n = open_row(p, t, w, a);
-    const int whole = n / E;
-    // The action's logit, ahead of the pieces: waiting for it is not waiting for them.
-    const float xa = X::get(row + static_cast<int64_t>(a) * X::kBytes);
-    Taker tk;
-    u32x4 held[NV];
-    if (whole > 0) {  // the same for all threads of a row
-      // Loads are unconditional (a piece past the last one is the last one
-      // again), so that they are counted and waited for one by one.
+  const int64_t t0 = static_cast<int64_t>(blockIdx.x) * kRows, t = min(t0 + group, static_cast<int64_t>(p.T) - 1);
+  const bool mine = t0 + group < p.T;  // a group past the last row goes along with it, and writes nothing
+  const char* row = p.logits + t * p.ld * X::kBytes;
+  char* out = GRAD ? p.grad + t * p.ld_grad * X::kBytes : nullptr;
+  RowIn in;
+  in.n = open_row(p, t, in.w, in.a);
+  const RowCut<BF16> cut(GRAD ? out : row, in.n, p.V);
+  // The action's logit, ahead of the pieces: waiting for it is not waiting for them.
+  in.xa = X::get(row + static_cast<int64_t>(in.a) * X::kBytes);
+  Taker tk;
+  u32x4 held[NV];
+  if (cut.open > 0) {  // the same for all threads of a row
+    // Loads are unconditional (a piece past the last one is the last one
+    // again), so that they are counted and waited for one by one.
 #pragma unroll
-      for (int i = 0; i < NV; ++i)
-        held[i] = load_piece<BF16>(row + static_cast<int64_t>(min(lane + i * L, whole - 1)) * 16);
+    for (int i = 0; i < NV; ++i) held[i] = load_piece<BF16>(row + cut.byte(min(lane + i * L, cut.open - 1)));
+    asm volatile("" ::: "memory");
+  }
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    if (lane + i * L < cut.open) {
+      float x[X::kPer];
+      X::unpack(held[i], x);
+      tk.take(x);
+    }
+  }
+  for (int i = lane + NV * L; i < cut.open; i += L) {
+    float x[X::kPer];
+    X::unpack(load_piece<BF16>(row + cut.byte(i)), x);
+    tk.take(x);
+  }
+  if (cut.edge(lane) < in.n) take_one<BF16>(tk, row, cut.edge(lane));
+  if (cut.part(lane) < in.n) take_one<BF16>(tk, row, cut.part(lane));
+
+  // The first wave closes the workgroup's rows, a lane a row (all its lanes the
+  // one row of a wide group): 64-bit exp and log by all waves would cost as
+  // much as the rows' own exponentials.
+  const Stat st = merge_lanes<(L < 64 ? L : 64)>(tk.st);
+  if (lane == 0) s_in[group] = in;
+  if constexpr (L > 64) {
+    if ((threadIdx.x & 63) == 0) s_stat[threadIdx.x >> 6] = st;
+  } else {
+    if (lane == 0) s_stat[group] = st;
+  }
+  __syncthreads();
+  if (threadIdx.x < 64) {
+    // Its pieces wait in shared memory meanwhile: the registers of the 64-bit
+    // functions would come on top of them, for every wave.
+    if constexpr (kPark) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) s_held[i * 64 + threadIdx.x] = held[i];
       asm volatile("" ::: "memory");
     }
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      if (lane + i * L < whole) {
-        float x[E];
-        X::unpack(held[i], x);
-        tk.take(x);
-      }
-    }
-    for (int i = lane + NV * L; i < whole; i += L) {
-      float x[E];
-      X::unpack(load_piece<BF16>(row + static_cast<int64_t>(i) * 16), x);
-      tk.take(x);
-    }
-    if (whole * E + lane < n) {
-      const float x[1] = {X::get(row + static_cast<int64_t>(whole * E + lane) * X::kBytes)};
-      tk.take(x);
-    }
-    RowSlope rs;
-    if constexpr (L <= 64) {
-      rs = close_row<GRAD>(p, t, w, n, a, xa, merge_lanes<L>(tk.st), lane == 0, &s_terms[group]);
+    PolicyTerms sum{};
+    if constexpr (L > 64) {
+      const Stat all = merge_lanes<kWaves>(s_stat[threadIdx.x % kWaves]);
+      if (threadIdx.x == 0) s_slope[0] = close_row<GRAD, true>(p, t0, s_in[0], all, &sum);
     } else {
-      // One wave closes the row: 64-bit exp and log by all of them would cost
-      // as much as the row's own exponentials.
-      Stat st = merge_lanes<64>(tk.st);
-      if ((threadIdx.x & 63) == 0) s_red[threadIdx.x >> 6] = st;
-      __syncthreads();
-      if (threadIdx.x < 64) {
-        st = merge_lanes<kWaves>(s_red[threadIdx.x % kWaves]);
-        rs = close_row<GRAD>(p, t, w, n, a, xa, st, threadIdx.x == 0, &s_terms[0]);
-        if (GRAD && threadIdx.x == 0) s_slope = rs;
-      }
-      __syncthreads();
-      if constexpr (GRAD) rs = s_slope;
+      const int r = threadIdx.x;
+      if (r < kRows && t0 + r < p.T) s_slope[r] = close_row<GRAD, true>(p, t0 + r, s_in[r], s_stat[r], &sum);
+#pragma unroll
+      for (int k = 0; GRAD && k < kPolicyTerms; ++k)
+#pragma unroll
+        for (int off = kRows / 2; off > 0; off >>= 1) sum.v[k] += __shfl_xor(sum.v[k], off);
     }
     if constexpr (GRAD) {
-      char* out = p.grad + t * p.ld_grad * X::kBytes;
-      const Slope<BF16, ENT> slope(rs);
-      auto put = [&](u32x4 v, int i) { store_piece<BF16>(out + static_cast<int64_t>(i) * 16, slope.piece(v, i)); };
-      // Opaque to the compiler, which would otherwise keep the pieces unpacked
-      // (twice the registers) from the statistics on.
+      if (threadIdx.x == 0)
 #pragma unroll
-      for (int i = 0; i < NV; ++i) asm volatile("" : "+v"(held[i]));
-      const int full = rs.n / E;
-      for (int i = lane + NV * L; i < full; i += L) put(load_piece<BF16>(row + static_cast<int64_t>(i) * 16), i);
+        for (int k = 0; k < kPolicyTerms; ++k)
+          p.parts[static_cast<int64_t>(blockIdx.x) * kPolicyTerms + k] = sum.v[k];
+    }
+    if constexpr (kPark) {
+      asm volatile("" ::: "memory");
 #pragma unroll
-      for (int i = 0; i < NV; ++i)
-        if (lane + i * L < full) put(held[i], lane + i * L);
-      for (int j = full * E + lane; j < p.V; j += L) {
-        const float x = j < rs.n ? X::get(row + static_cast<int64_t>(j) * X::kBytes) : 0.0f;
-        X::put(out + static_cast<int64_t>(j) * X::kBytes, slope.at(x, j));
-      }
+      for (int i = 0; i < NV; ++i) held[i] = s_held[i * 64 + threadIdx.x];
     }
   }
   if constexpr (GRAD) {
     __syncthreads();
-    if (threadIdx.x < kPolicyTerms) {
-      double v = 0.0;
-      for (int r = 0; r < kRows; ++r) v += s_terms[r].v[threadIdx.x];
-      p.parts[static_cast<int64_t>(blockIdx.x) * kPolicyTerms + threadIdx.x] = v;
-    }
+    if (!mine) return;
+    const RowSlope rs = s_slope[group];
+    // A row that was found bad after all has nothing open.
+    const RowCut<BF16> cut(out, rs.n, p.V);
+    const Slope<BF16, ENT> slope(rs, cut.head);
+    // Opaque to the compiler, which would otherwise keep the pieces unpacked
+    // (twice the registers) from the statistics on.
+#pragma unroll
+    for (int i = 0; i < NV; ++i) asm volatile("" : "+v"(held[i]));
+    auto put = [&](u32x4 v, int i) { store_piece<BF16>(out + cut.byte(i), slope.piece(v, i)); };
+    for (int i = lane + NV * L; i < cut.open; i += L) put(load_piece<BF16>(row + cut.byte(i)), i);
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      if (lane + i * L < cut.open) put(held[i], lane + i * L);
+    for (int i = cut.closed() + lane; i < cut.all; i += L) store_piece<BF16>(out + cut.byte(i), u32x4{});
+    if (lane < X::kPer && cut.part(0) < rs.n)
+      slope.one(row, out, cut.head + cut.open * X::kPer + lane);
+    if (cut.edge(lane) < p.V) slope.one(row, out, cut.edge(lane));
   }
 }
 
-// Statistics of the pieces [lo, hi) of a row and, if `end`, of the elements
-// behind its last piece.  Four pieces in flight a thread.
+// Statistics of the open pieces [lo, hi) of a row and, if `ends`, of the open
+// elements outside the pieces that are open.  Four pieces in flight a thread.
 template <bool BF16>
-__device__ __forceinline__ Stat range_stats(const char* row, int lo, int hi, bool end, int n) {
+__device__ __forceinline__ Stat range_stats(const char* row, const RowCut<BF16>& cut, int lo, int hi, bool ends) {
   using X = Elem<BF16>;
   constexpr int kFlight = 4;
+  const int tid = threadIdx.x;
   Taker tk;
-  for (int i = lo + threadIdx.x; i < hi; i += kFlight * kThreads) {
+  for (int i = lo + tid; i < hi; i += kFlight * kThreads) {
     u32x4 v[kFlight];
 #pragma unroll
-    for (int k = 0; k < kFlight; ++k)
-      v[k] = load_piece<BF16>(row + static_cast<int64_t>(min(i + k * kThreads, hi - 1)) * 16);
+    for (int k = 0; k < kFlight; ++k) v[k] = load_piece<BF16>(row + cut.byte(min(i + k * kThreads, hi - 1)));
     asm volatile("" ::: "memory");
 #pragma unroll
     for (int k = 0; k < kFlight; ++k) {
@@ -388,124 +442,121 @@ __device__ __forceinline__ Stat range_stats(const char* row, int lo, int hi, boo
       }
     }
   }
-  const int j = n / X::kPer * X::kPer + threadIdx.x;
-  if (end && j < n) {
-    const float x[1] = {X::get(row + static_cast<int64_t>(j) * X::kBytes)};
-    tk.take(x);
-  }
+  if (ends && cut.edge(tid) < cut.n) take_one<BF16>(tk, row, cut.edge(tid));
+  if (ends && cut.part(tid) < cut.n) take_one<BF16>(tk, row, cut.part(tid));
   return tk.st;
 }
 
-// This workgroup's share of the pieces of a row of V elements (of n open ones).
-template <bool BF16>
-__device__ __forceinline__ int2 chunk_of(const RowParams& p, int chunk, int n) {
-  constexpr int E = Elem<BF16>::kPer;
-  const int each = (p.V / E + p.split - 1) / p.split, whole = n / E;
-  return make_int2(min(whole, chunk * each), min(whole, (chunk + 1) * each));
+// A workgroup's share of a row's pieces, split over p.split.
+__device__ __forceinline__ int2 share_of(const RowParams& p, int chunk, int all) {
+  const int each = (all + p.split - 1) / p.split;
+  return make_int2(min(all, chunk * each), min(all, (chunk + 1) * each));
 }
 
 // Statistics of long rows, p.split workgroups a row.  One a row: it closes the
-// row (log-probability only).  Several: each leaves its triple for the next launch.
+// row (log-probability only).  Several: each leaves its triple for the next
+// launch, with the action's logit (which a gradient over the logits would
+// overwrite).
 template <bool BF16>
 __global__ __launch_bounds__(kThreads) void policy_stats_kernel(RowParams p) {
+  using X = Elem<BF16>;
   __shared__ Stat s_red[kThreads / 64];
   const int64_t t = blockIdx.x / p.split;
   const int chunk = blockIdx.x % p.split;
-  float w;
-  int a;
-  const int n = open_row(p, t, w, a);
-  const char* row = p.logits + t * p.ld * Elem<BF16>::kBytes;
-  const int2 c = chunk_of<BF16>(p, chunk, n);
-  Stat st = merge_lanes<64>(range_stats<BF16>(row, c.x, c.y, chunk == p.split - 1, n));
+  RowIn in;
+  in.n = open_row(p, t, in.w, in.a);
+  const char* row = p.logits + t * p.ld * X::kBytes;
+  const RowCut<BF16> cut(p.grad ? p.grad + t * p.ld_grad * X::kBytes : row, in.n, p.V);
+  const int2 c = share_of(p, chunk, cut.all);
+  Stat st = merge_lanes<64>(range_stats<BF16>(row, cut, min(c.x, cut.open), min(c.y, cut.open), chunk == 0));
   if ((threadIdx.x & 63) == 0) s_red[threadIdx.x >> 6] = st;
   __syncthreads();
   if (threadIdx.x >= 64) return;
   st = merge_lanes<kThreads / 64>(s_red[threadIdx.x % (kThreads / 64)]);
-  const float xa = n > 0 ? Elem<BF16>::get(row + static_cast<int64_t>(a) * Elem<BF16>::kBytes) : 0.0f;
-  if (p.split > 1) {
-    if (threadIdx.x == 0) p.split_stats[blockIdx.x] = make_float4(st.m, st.s, st.h, xa);
-    return;
-  }
-  close_row<false>(p, t, w, n, a, xa, st, threadIdx.x == 0, nullptr);
+  in.xa = X::get(row + static_cast<int64_t>(in.a) * X::kBytes);
+  if (threadIdx.x > 0) return;
+  if (p.split > 1) p.split_stats[blockIdx.x] = make_float4(st.m, st.s, st.h, in.xa);
+  else close_row<false, true>(p, t, in, st, nullptr);
 }
 
 // Row t closed from its workgroups' triples by a group of G lanes.
-template <bool GRAD, int G>
-__device__ __forceinline__ RowSlope close_split_row(const RowParams& p, int64_t t, bool writes, PolicyTerms* sum) {
+template <bool GRAD, bool WRITES, int G>
+__device__ __forceinline__ RowSlope close_split_row(const RowParams& p, int64_t t, PolicyTerms* sum) {
   constexpr int kEach = kMaxSplit / G;
   const int lane = threadIdx.x % G;
   const float4* from = p.split_stats + t * p.split;
   float4 v[kEach];
 #pragma unroll
   for (int k = 0; k < kEach; ++k) v[k] = from[min(lane + k * G, p.split - 1)];
-  float w;
-  int a;
-  const int n = open_row(p, t, w, a);
+  RowIn in;
+  in.n = open_row(p, t, in.w, in.a);
+  in.xa = v[0].w;
   Stat st = Stat::none();
 #pragma unroll
   for (int k = 0; k < kEach; ++k)
     if (lane + k * G < p.split) st.merge(Stat{v[k].x, v[k].y, v[k].z});
-  return close_row<GRAD>(p, t, w, n, a, v[0].w, merge_lanes<G>(st), writes && lane == 0, sum);
+  st = merge_lanes<G>(st);
+  RowSlope rs{};
+  if (lane == 0) rs = close_row<GRAD, WRITES>(p, t, in, st, sum);
+  return rs;  // the first lane's
 }
 
 // Log-probabilities of split rows.
 __global__ __launch_bounds__(kThreads) void policy_close_kernel(RowParams p) {
   const int64_t t = static_cast<int64_t>(blockIdx.x) * (kThreads / 8) + threadIdx.x / 8;
-  if (t < p.T) close_split_row<false, 8>(p, t, true, nullptr);
+  if (t < p.T) close_split_row<false, true, 8>(p, t, nullptr);
 }
 
 // Gradient of split rows: each workgroup closes its row for itself and writes
-// its chunk.  One workgroup more, the last, closes all rows for the outputs
+// its share.  One workgroup more, the last, closes all rows for the outputs
 // and sums.
 template <bool BF16, bool ENT>
 __global__ __launch_bounds__(kThreads, 3) void policy_split_grad_kernel(RowParams p) {
   using X = Elem<BF16>;
-  constexpr int E = X::kPer;
   __shared__ RowSlope s_slope;
   __shared__ PolicyTerms s_terms[kThreads / 8];
   const int64_t t = blockIdx.x / p.split;
+  const int tid = threadIdx.x;
   if (t == p.T) {
     PolicyTerms sum{};
-    for (int64_t r = threadIdx.x / 8; r < p.T; r += kThreads / 8) close_split_row<true, 8>(p, r, true, &sum);
-    if (threadIdx.x % 8 == 0) s_terms[threadIdx.x / 8] = sum;
+    for (int64_t r = tid / 8; r < p.T; r += kThreads / 8) close_split_row<true, true, 8>(p, r, &sum);
+    if (tid % 8 == 0) s_terms[tid / 8] = sum;
     __syncthreads();
-    if (threadIdx.x < kPolicyTerms) {
+    if (tid < kPolicyTerms) {
       double v = 0.0;
-      for (int i = 0; i < kThreads / 8; ++i) v += s_terms[i].v[threadIdx.x];
-      p.stats[threadIdx.x] = static_cast<float>(v);
+      for (int i = 0; i < kThreads / 8; ++i) v += s_terms[i].v[tid];
+      p.stats[tid] = static_cast<float>(v);
     }
     return;
   }
-  if (threadIdx.x < 64) {
-    PolicyTerms unused{};
-    const RowSlope rs = close_split_row<true, 64>(p, t, false, &unused);
-    if (threadIdx.x == 0) s_slope = rs;
+  if (tid < 64) {
+    const RowSlope rs = close_split_row<true, false, 64>(p, t, nullptr);
+    if (tid == 0) s_slope = rs;
   }
   __syncthreads();
   const RowSlope rs = s_slope;
   const char* row = p.logits + t * p.ld * X::kBytes;
   char* out = p.grad + t * p.ld_grad * X::kBytes;
+  const RowCut<BF16> cut(out, rs.n, p.V);
+  const Slope<BF16, ENT> slope(rs, cut.head);
   const int chunk = blockIdx.x % p.split;
-  const int2 open = chunk_of<BF16>(p, chunk, rs.n), all = chunk_of<BF16>(p, chunk, p.V);
-  const Slope<BF16, ENT> slope(rs);
-  for (int i = open.x + threadIdx.x; i < open.y; i += kThreads)
-    store_piece<BF16>(out + static_cast<int64_t>(i) * 16,
-                      slope.piece(load_piece<BF16>(row + static_cast<int64_t>(i) * 16), i));
-  const int end = chunk == p.split - 1 ? p.V : all.y * E;
-  for (int j = max(open.y, all.x) * E + threadIdx.x; j < end; j += kThreads) {
-    const float x = j < rs.n ? X::get(row + static_cast<int64_t>(j) * X::kBytes) : 0.0f;
-    X::put(out + static_cast<int64_t>(j) * X::kBytes, slope.at(x, j));
-  }
+  const int2 c = share_of(p, chunk, cut.all);
+  for (int i = c.x + tid; i < min(c.y, cut.open); i += kThreads)
+    store_piece<BF16>(out + cut.byte(i), slope.piece(load_piece<BF16>(row + cut.byte(i)), i));
+  for (int i = max(c.x, cut.closed()) + tid; i < c.y; i += kThreads) store_piece<BF16>(out + cut.byte(i), u32x4{});
+  if (c.x <= cut.open && cut.open < c.y && cut.part(0) < rs.n && tid < X::kPer)
+    slope.one(row, out, cut.head + cut.open * X::kPer + tid);
+  if (chunk == 0 && cut.edge(tid) < p.V) slope.one(row, out, cut.edge(tid));
 }
 
 // Sums of the terms of workgroups [blockIdx per_group, + per_group) of n, to
 // out[blockIdx] or, rounded, to stats.
-__global__ __launch_bounds__(kThreads) void policy_finish_kernel(const double* parts, int32_t n, int32_t per_group,
+__global__ __launch_bounds__(kFinishThreads) void policy_finish_kernel(const double* parts, int32_t n, int32_t per_group,
                                                                  double* out, float* stats) {
-  __shared__ double s_sum[kPolicyTerms][kThreads / 64];
+  __shared__ double s_sum[kPolicyTerms][kFinishThreads / 64];
   double v[kPolicyTerms] = {};
   const int64_t lo = static_cast<int64_t>(blockIdx.x) * per_group, hi = min(static_cast<int64_t>(n), lo + per_group);
-  for (int64_t i = lo + threadIdx.x; i < hi; i += kThreads)
+  for (int64_t i = lo + threadIdx.x; i < hi; i += kFinishThreads)
 #pragma unroll
     for (int k = 0; k < kPolicyTerms; ++k) v[k] += parts[i * kPolicyTerms + k];
 #pragma unroll
@@ -517,7 +568,7 @@ __global__ __launch_bounds__(kThreads) void policy_finish_kernel(const double* p
   __syncthreads();
   if (threadIdx.x < kPolicyTerms) {
     double t = 0.0;
-    for (int w = 0; w < kThreads / 64; ++w) t += s_sum[threadIdx.x][w];
+    for (int w = 0; w < kFinishThreads / 64; ++w) t += s_sum[threadIdx.x][w];
     if (stats) stats[threadIdx.x] = static_cast<float>(t);
     else out[static_cast<int64_t>(blockIdx.x) * kPolicyTerms + threadIdx.x] = t;
   }
@@ -525,9 +576,9 @@ __global__ __launch_bounds__(kThreads) void policy_finish_kernel(const double* p
 
 template <bool BF16, bool GRAD, bool ENT, int L, int NV>
 void launch_shape(const RowParams& p, hipStream_t st) {
-  constexpr int kWG = L > kThreads ? L : kThreads, kRows = kWG / L;
+  constexpr int kRows = group_threads(L) / L;
   const int groups = (p.T + kRows - 1) / kRows;
-  hipLaunchKernelGGL((policy_rows_kernel<BF16, L, NV, GRAD, ENT>), dim3(groups), dim3(kWG), 0, st, p);
+  hipLaunchKernelGGL((policy_rows_kernel<BF16, L, NV, GRAD, ENT>), dim3(groups), dim3(group_threads(L)), 0, st, p);
   if constexpr (GRAD) launch_policy_finish(p.parts, groups, p.stats, st);
 }
 
@@ -563,6 +614,7 @@ void launch_rows(RowParams p, hipStream_t st) {
     else if (pieces <= 2048) launch_shape<BF16, GRAD, ENT, 256, 8>(p, st);
     else if (pieces <= 4096) launch_shape<BF16, GRAD, ENT, 256, 16>(p, st);
     else if (pieces <= 6144) launch_shape<BF16, GRAD, ENT, 512, 12>(p, st);
+    else if (pieces <= 6656) launch_shape<BF16, GRAD, ENT, 512, 13>(p, st);
     else if (pieces <= 8192) launch_shape<BF16, GRAD, ENT, 512, 16>(p, st);
     else if (pieces <= 12288) launch_shape<BF16, GRAD, ENT, 1024, 12>(p, st);
     else launch_shape<BF16, GRAD, ENT, 1024, 16>(p, st);
@@ -573,7 +625,7 @@ void launch_rows(RowParams p, hipStream_t st) {
 // element type that has fewer rows a workgroup).
 int32_t row_groups(int32_t T, int32_t V) {
   const int pieces = (V + 3) / 4;
-  const int rows = pieces <= 64 ? kThreads / 16 : (pieces <= 512 ? kThreads / 64 : 1);
+  const int rows = pieces <= 64 ? group_threads(16) / 16 : (pieces <= 512 ? group_threads(64) / 64 : 1);
   return (T + rows - 1) / rows;
 }
 
@@ -606,11 +658,11 @@ void launch_policy_finish(double* parts, int32_t n, float* stats, hipStream_t st
   if (n > kFinishDirect) {
     const int32_t each = (n + kFinishGroups - 1) / kFinishGroups, groups = (n + each - 1) / each;
     double* mid = parts + static_cast<int64_t>(n) * kPolicyTerms;
-    hipLaunchKernelGGL(policy_finish_kernel, dim3(groups), dim3(kThreads), 0, stream, parts, n, each, mid, nullptr);
+    hipLaunchKernelGGL(policy_finish_kernel, dim3(groups), dim3(kFinishThreads), 0, stream, parts, n, each, mid, nullptr);
     parts = mid;
     n = groups;
   }
-  hipLaunchKernelGGL(policy_finish_kernel, dim3(1), dim3(kThreads), 0, stream, parts, n, n, nullptr, stats);
+  hipLaunchKernelGGL(policy_finish_kernel, dim3(1), dim3(kFinishThreads), 0, stream, parts, n, n, nullptr, stats);
 }
 
 }  // namespace dora
