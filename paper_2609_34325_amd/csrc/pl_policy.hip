@@ -188,7 +188,8 @@ __global__ __launch_bounds__(kThreads) void pl_policy_kernel(PLPolicyParams p) {
   for (int i = 0; i < kWaves; ++i) lp += s_sum[i];
 
   PolicyTerms terms{};
-  const double slope = policy_decision(lp, 0.0, p.old[b], p.adv[b], w, p.ref, b, p.coef, terms);
+  const double slope = policy_decision(lp, 0.0, p.old[b], p.adv[b], w, p.ref != nullptr,
+                                       p.ref ? p.ref[b] : 0.0f, p.coef, terms);
   if (tid == 0) {
     p.logp[b] = static_cast<float>(lp);
 #pragma unroll

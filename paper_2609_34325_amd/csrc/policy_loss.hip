@@ -17,6 +17,7 @@
 // figures 64 bits.
 #include <algorithm>
 #include <cfloat>
+#include <type_traits>
 
 #include "dora_internal.h"
 #include "policy_terms.h"
@@ -25,7 +26,6 @@ namespace dora {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kFinishThreads = 1024;
 constexpr int kMaxSplit = 64;  // workgroups a row
 constexpr float kLog2E = 1.4426950408889634f;
 constexpr double kLn2 = 0.6931471805599453;
@@ -184,25 +184,44 @@ __device__ __forceinline__ void take_one(Taker& tk, const char* row, int j) {
 }
 
 // Open elements of row t (0: padding or a bad row), its weight and action (0
-// for such a row).
+// for such a row).  The three are loaded side by side.
 __device__ __forceinline__ int open_row(const RowParams& p, int64_t t, float& w, int& a) {
   w = p.weight ? p.weight[t] : 1.0f;
-  a = 0;
-  if (w == 0.0f) return 0;
   const int n = p.legal ? p.legal[t] : p.V, act = p.actions[t];
-  if (!(n >= 1 && n <= p.V && act >= 0 && act < n)) return 0;
-  a = act;
-  return n;
+  const bool good = w != 0.0f && n >= 1 && n <= p.V && act >= 0 && act < n;
+  a = good ? act : 0;
+  return good ? n : 0;
+}
+
+// A value of the lanes of a group of G (all active) folded by op, to every
+// lane: inside 16 lanes by DPP, then by row swaps; no trip through shared memory.
+template <int G, class Op>
+__device__ __forceinline__ float fold_lanes(float v, Op op) {
+  auto dpp = [](float x, auto ctrl) {
+    return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), decltype(ctrl)::value, 0xF, 0xF, false));
+  };
+  if constexpr (G >= 2) v = op(v, dpp(v, std::integral_constant<int, 0xB1>()));    // quad_perm 1,0,3,2
+  if constexpr (G >= 4) v = op(v, dpp(v, std::integral_constant<int, 0x4E>()));    // quad_perm 2,3,0,1
+  if constexpr (G >= 8) v = op(v, dpp(v, std::integral_constant<int, 0x141>()));   // row_half_mirror
+  if constexpr (G >= 16) v = op(v, dpp(v, std::integral_constant<int, 0x140>()));  // row_mirror
+  if constexpr (G >= 32) {
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = op(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  }
+  if constexpr (G >= 64) {
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = op(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  }
+  return v;
 }
 
 // Merged over groups of G lanes; every lane gets the same triple.
 template <int G>
 __device__ __forceinline__ Stat merge_lanes(Stat a) {
-#pragma unroll
-  for (int off = 1; off < G; off <<= 1) {
-    const Stat o{__shfl_xor(a.m, off), __shfl_xor(a.s, off), __shfl_xor(a.h, off)};
-    a.merge(o);
-  }
+  a.raise(fold_lanes<G>(a.m, [](float x, float y) { return fmaxf(x, y); }));
+  const auto add = [](float x, float y) { return x + y; };
+  a.s = fold_lanes<G>(a.s, add);
+  a.h = fold_lanes<G>(a.h, add);
   return a;
 }
 
@@ -273,10 +292,20 @@ struct RowIn {
   float w, xa;
   int n, a;
 };
+// Its constants of the loss.
+struct RowLoss {
+  float old, adv, ref;
+};
+template <bool GRAD>
+__device__ __forceinline__ RowLoss row_loss(const RowParams& p, int64_t t) {
+  if constexpr (GRAD) return {p.old[t], p.adv[t], p.ref ? p.ref[t] : 0.0f};
+  return {};
+}
 
 // The row's own figures; WRITES: to the outputs, and its terms are added to sum.
 template <bool GRAD, bool WRITES>
-__device__ __forceinline__ RowSlope close_row(const RowParams& p, int64_t t, RowIn in, Stat st, PolicyTerms* sum) {
+__device__ __forceinline__ RowSlope close_row(const RowParams& p, int64_t t, RowIn in, RowLoss lc, Stat st,
+                                              PolicyTerms* sum) {
   double logp = 0.0, entropy = 0.0;
   RowSlope rs{st.m, 0.0f, 0.0f, 0.0f, 0, in.a};
   if (in.n > 0 && st.s != 0.0f) {  // 0: nothing open
@@ -286,7 +315,7 @@ __device__ __forceinline__ RowSlope close_row(const RowParams& p, int64_t t, Row
     if constexpr (GRAD) {
       PolicyTerms unused{};
       const double slope =
-          policy_decision(logp, entropy, p.old[t], p.adv[t], in.w, p.ref, t, p.coef, WRITES ? *sum : unused);
+          policy_decision(logp, entropy, lc.old, lc.adv, in.w, p.ref != nullptr, lc.ref, p.coef, WRITES ? *sum : unused);
       const double c = static_cast<double>(p.coef.entropy) * in.w;
       rs.n = in.n;
       rs.slope = static_cast<float>(slope);
@@ -324,20 +353,29 @@ __global__ __launch_bounds__(group_threads(L), 4) void policy_rows_kernel(RowPar
   const bool mine = t0 + group < p.T;  // a group past the last row goes along with it, and writes nothing
   const char* row = p.logits + t * p.ld * X::kBytes;
   char* out = GRAD ? p.grad + t * p.ld_grad * X::kBytes : nullptr;
-  RowIn in;
-  in.n = open_row(p, t, in.w, in.a);
-  const RowCut<BF16> cut(GRAD ? out : row, in.n, p.V);
-  // The action's logit, ahead of the pieces: waiting for it is not waiting for them.
-  in.xa = X::get(row + static_cast<int64_t>(in.a) * X::kBytes);
+  // For the row that this thread may close.
+  const RowLoss lc = row_loss<GRAD>(p, min(t0 + static_cast<int>(threadIdx.x) % kRows, static_cast<int64_t>(p.T) - 1));
   Taker tk;
   u32x4 held[NV];
-  if (cut.open > 0) {  // the same for all threads of a row
-    // Loads are unconditional (a piece past the last one is the last one
-    // again), so that they are counted and waited for one by one.
+  // Loads are unconditional (a piece past the last one is the last one again),
+  // so that they are counted and waited for one by one.
+  auto load = [&](const RowCut<BF16>& cut, int last) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) held[i] = load_piece<BF16>(row + cut.byte(min(lane + i * L, cut.open - 1)));
+    for (int i = 0; i < NV; ++i) held[i] = load_piece<BF16>(row + cut.byte(min(lane + i * L, last)));
     asm volatile("" ::: "memory");
+  };
+  RowIn in;
+  if constexpr (L <= 64) {
+    // Short rows are loaded beside what says whether they count, long ones
+    // after it.
+    const RowCut<BF16> whole(GRAD ? out : row, p.V, p.V);
+    if (whole.all > 0) load(whole, whole.all - 1);
   }
+  in.n = open_row(p, t, in.w, in.a);
+  const RowCut<BF16> cut(GRAD ? out : row, in.n, p.V);
+  // The action's logit, ahead of a long row's pieces: waiting for it is not waiting for them.
+  in.xa = X::get(row + static_cast<int64_t>(in.a) * X::kBytes);
+  if (L > 64 && cut.open > 0) load(cut, cut.open - 1);  // the same for all threads of a row
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     if (lane + i * L < cut.open) {
@@ -376,10 +414,10 @@ __global__ __launch_bounds__(group_threads(L), 4) void policy_rows_kernel(RowPar
     PolicyTerms sum{};
     if constexpr (L > 64) {
       const Stat all = merge_lanes<kWaves>(s_stat[threadIdx.x % kWaves]);
-      if (threadIdx.x == 0) s_slope[0] = close_row<GRAD, true>(p, t0, s_in[0], all, &sum);
+      if (threadIdx.x == 0) s_slope[0] = close_row<GRAD, true>(p, t0, s_in[0], lc, all, &sum);
     } else {
       const int r = threadIdx.x;
-      if (r < kRows && t0 + r < p.T) s_slope[r] = close_row<GRAD, true>(p, t0 + r, s_in[r], s_stat[r], &sum);
+      if (r < kRows && t0 + r < p.T) s_slope[r] = close_row<GRAD, true>(p, t0 + r, s_in[r], lc, s_stat[r], &sum);
 #pragma unroll
       for (int k = 0; GRAD && k < kPolicyTerms; ++k)
 #pragma unroll
@@ -476,7 +514,7 @@ __global__ __launch_bounds__(kThreads) void policy_stats_kernel(RowParams p) {
   in.xa = X::get(row + static_cast<int64_t>(in.a) * X::kBytes);
   if (threadIdx.x > 0) return;
   if (p.split > 1) p.split_stats[blockIdx.x] = make_float4(st.m, st.s, st.h, in.xa);
-  else close_row<false, true>(p, t, in, st, nullptr);
+  else close_row<false, true>(p, t, in, RowLoss{}, st, nullptr);
 }
 
 // Row t closed from its workgroups' triples by a group of G lanes.
@@ -490,6 +528,7 @@ __device__ __forceinline__ RowSlope close_split_row(const RowParams& p, int64_t 
   for (int k = 0; k < kEach; ++k) v[k] = from[min(lane + k * G, p.split - 1)];
   RowIn in;
   in.n = open_row(p, t, in.w, in.a);
+  const RowLoss lc = row_loss<GRAD>(p, t);
   in.xa = v[0].w;
   Stat st = Stat::none();
 #pragma unroll
@@ -497,7 +536,7 @@ __device__ __forceinline__ RowSlope close_split_row(const RowParams& p, int64_t 
     if (lane + k * G < p.split) st.merge(Stat{v[k].x, v[k].y, v[k].z});
   st = merge_lanes<G>(st);
   RowSlope rs{};
-  if (lane == 0) rs = close_row<GRAD, WRITES>(p, t, in, st, sum);
+  if (lane == 0) rs = close_row<GRAD, WRITES>(p, t, in, lc, st, sum);
   return rs;  // the first lane's
 }
 
@@ -551,12 +590,13 @@ __global__ __launch_bounds__(kThreads, 3) void policy_split_grad_kernel(RowParam
 
 // Sums of the terms of workgroups [blockIdx per_group, + per_group) of n, to
 // out[blockIdx] or, rounded, to stats.
-__global__ __launch_bounds__(kFinishThreads) void policy_finish_kernel(const double* parts, int32_t n, int32_t per_group,
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void policy_finish_kernel(const double* parts, int32_t n, int32_t per_group,
                                                                  double* out, float* stats) {
-  __shared__ double s_sum[kPolicyTerms][kFinishThreads / 64];
+  __shared__ double s_sum[kPolicyTerms][THREADS / 64];
   double v[kPolicyTerms] = {};
   const int64_t lo = static_cast<int64_t>(blockIdx.x) * per_group, hi = min(static_cast<int64_t>(n), lo + per_group);
-  for (int64_t i = lo + threadIdx.x; i < hi; i += kFinishThreads)
+  for (int64_t i = lo + threadIdx.x; i < hi; i += THREADS)
 #pragma unroll
     for (int k = 0; k < kPolicyTerms; ++k) v[k] += parts[i * kPolicyTerms + k];
 #pragma unroll
@@ -568,7 +608,7 @@ __global__ __launch_bounds__(kFinishThreads) void policy_finish_kernel(const dou
   __syncthreads();
   if (threadIdx.x < kPolicyTerms) {
     double t = 0.0;
-    for (int w = 0; w < kFinishThreads / 64; ++w) t += s_sum[threadIdx.x][w];
+    for (int w = 0; w < THREADS / 64; ++w) t += s_sum[threadIdx.x][w];
     if (stats) stats[threadIdx.x] = static_cast<float>(t);
     else out[static_cast<int64_t>(blockIdx.x) * kPolicyTerms + threadIdx.x] = t;
   }
@@ -658,11 +698,13 @@ void launch_policy_finish(double* parts, int32_t n, float* stats, hipStream_t st
   if (n > kFinishDirect) {
     const int32_t each = (n + kFinishGroups - 1) / kFinishGroups, groups = (n + each - 1) / each;
     double* mid = parts + static_cast<int64_t>(n) * kPolicyTerms;
-    hipLaunchKernelGGL(policy_finish_kernel, dim3(groups), dim3(kFinishThreads), 0, stream, parts, n, each, mid, nullptr);
+    hipLaunchKernelGGL(policy_finish_kernel<256>, dim3(groups), dim3(256), 0, stream, parts, n, each, mid, nullptr);
     parts = mid;
     n = groups;
   }
-  hipLaunchKernelGGL(policy_finish_kernel, dim3(1), dim3(kFinishThreads), 0, stream, parts, n, n, nullptr, stats);
+  // 64 sets: 2.5 us by 256 threads, 4.4 by 1024.
+  if (n <= 512) hipLaunchKernelGGL(policy_finish_kernel<256>, dim3(1), dim3(256), 0, stream, parts, n, n, nullptr, stats);
+  else hipLaunchKernelGGL(policy_finish_kernel<1024>, dim3(1), dim3(1024), 0, stream, parts, n, n, nullptr, stats);
 }
 
 }  // namespace dora

@@ -29,16 +29,15 @@ struct PolicyTerms {
 };
 
 __device__ __forceinline__ double policy_decision(double logp, double entropy, float old, float adv, float w,
-                                                  const float* ref, int64_t row, const PolicyCoef& c,
-                                                  PolicyTerms& sum) {
+                                                  bool with_ref, float ref, const PolicyCoef& c, PolicyTerms& sum) {
   const double r = exp(logp - static_cast<double>(old)), a = adv, wd = w;
   const double lo = 1.0 - static_cast<double>(c.clip_low), hi = 1.0 + static_cast<double>(c.clip_high);
   const double held = (r < lo ? lo : (r > hi ? hi : r)) * a, open = r * a;
   const bool clipped = held < open;
   const double gain = clipped ? held : open;
   double slope = clipped ? 0.0 : -open, kl = 0.0;
-  if (ref) {
-    const double d = static_cast<double>(ref[row]) - logp, up = expm1(d);
+  if (with_ref) {
+    const double d = static_cast<double>(ref) - logp, up = expm1(d);
     kl = up - d;
     if (c.kl != 0.0f) slope -= c.kl * up;  // an infinite distance counts for nothing at coefficient 0
   }
