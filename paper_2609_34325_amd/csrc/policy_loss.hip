@@ -589,28 +589,41 @@ __global__ __launch_bounds__(kThreads, 3) void policy_split_grad_kernel(RowParam
 }
 
 // Sums of the terms of workgroups [blockIdx per_group, + per_group) of n, to
-// out[blockIdx] or, rounded, to stats.
-template <int THREADS>
-__global__ __launch_bounds__(THREADS) void policy_finish_kernel(const double* parts, int32_t n, int32_t per_group,
-                                                                 double* out, float* stats) {
-  __shared__ double s_sum[kPolicyTerms][THREADS / 64];
-  double v[kPolicyTerms] = {};
+// out[blockIdx] or, rounded, to stats.  Thread i adds term i % 6 of every 64th
+// set, eight sets in flight; then 8 x 8 sums a term meet in order.
+constexpr int kFinishSets = 64, kFinishThreads = kFinishSets * kPolicyTerms;
+__global__ __launch_bounds__(kFinishThreads) void policy_finish_kernel(const double* parts, int32_t n, int32_t per_group,
+                                                                       double* out, float* stats) {
+  constexpr int kFlight = 8;
+  __shared__ double s_sum[kFinishThreads];
+  const int tid = threadIdx.x;
   const int64_t lo = static_cast<int64_t>(blockIdx.x) * per_group, hi = min(static_cast<int64_t>(n), lo + per_group);
-  for (int64_t i = lo + threadIdx.x; i < hi; i += THREADS)
+  double sum = 0.0;
+  for (int64_t i = lo + tid / kPolicyTerms; i < hi; i += kFlight * kFinishSets) {
+    double v[kFlight];
 #pragma unroll
-    for (int k = 0; k < kPolicyTerms; ++k) v[k] += parts[i * kPolicyTerms + k];
+    for (int k = 0; k < kFlight; ++k)
+      v[k] = parts[min(i + k * kFinishSets, hi - 1) * kPolicyTerms + tid % kPolicyTerms];
+    asm volatile("" ::: "memory");
 #pragma unroll
-  for (int k = 0; k < kPolicyTerms; ++k) {
+    for (int k = 0; k < kFlight; ++k) sum += i + k * kFinishSets < hi ? v[k] : 0.0;
+  }
+  s_sum[tid] = sum;
+  __syncthreads();
+  if (tid < 8 * kPolicyTerms) {
+    sum = 0.0;
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) v[k] += __shfl_xor(v[k], off);
-    if ((threadIdx.x & 63) == 0) s_sum[k][threadIdx.x >> 6] = v[k];
+    for (int k = 0; k < 8; ++k) sum += s_sum[tid + k * 8 * kPolicyTerms];
   }
   __syncthreads();
-  if (threadIdx.x < kPolicyTerms) {
-    double t = 0.0;
-    for (int w = 0; w < THREADS / 64; ++w) t += s_sum[threadIdx.x][w];
-    if (stats) stats[threadIdx.x] = static_cast<float>(t);
-    else out[static_cast<int64_t>(blockIdx.x) * kPolicyTerms + threadIdx.x] = t;
+  if (tid < 8 * kPolicyTerms) s_sum[tid] = sum;
+  __syncthreads();
+  if (tid < kPolicyTerms) {
+    sum = 0.0;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum += s_sum[tid + k * kPolicyTerms];
+    if (stats) stats[tid] = static_cast<float>(sum);
+    else out[static_cast<int64_t>(blockIdx.x) * kPolicyTerms + tid] = sum;
   }
 }
 
@@ -698,13 +711,11 @@ void launch_policy_finish(double* parts, int32_t n, float* stats, hipStream_t st
   if (n > kFinishDirect) {
     const int32_t each = (n + kFinishGroups - 1) / kFinishGroups, groups = (n + each - 1) / each;
     double* mid = parts + static_cast<int64_t>(n) * kPolicyTerms;
-    hipLaunchKernelGGL(policy_finish_kernel<256>, dim3(groups), dim3(256), 0, stream, parts, n, each, mid, nullptr);
+    hipLaunchKernelGGL(policy_finish_kernel, dim3(groups), dim3(kFinishThreads), 0, stream, parts, n, each, mid, nullptr);
     parts = mid;
     n = groups;
   }
-  // 64 sets: 2.5 us by 256 threads, 4.4 by 1024.
-  if (n <= 512) hipLaunchKernelGGL(policy_finish_kernel<256>, dim3(1), dim3(256), 0, stream, parts, n, n, nullptr, stats);
-  else hipLaunchKernelGGL(policy_finish_kernel<1024>, dim3(1), dim3(1024), 0, stream, parts, n, n, nullptr, stats);
+  hipLaunchKernelGGL(policy_finish_kernel, dim3(1), dim3(kFinishThreads), 0, stream, parts, n, n, nullptr, stats);
 }
 
 }  // namespace dora
