@@ -9,16 +9,17 @@
 //   d logp / d s_j = [j drawn] - exp(s_j) sum_{t <= tau_j} 1 / S_t
 // with tau_j the draw that takes j, or k - 1 for a token never drawn.  Both
 // sums are scans along the drawing order: the S_t from the back (the tokens
-// left at the end are one term), the sums of 1 / S_t from the front.  Terms
-// and sums are pairs v 2^e with 64-bit v, joined at the larger e by shifting
-// exponents: a score far below the largest, drawn late, neither vanishes nor
-// divides zero by zero, and no exp is taken inside the scans.  64 bits because
-// logp sums up to 2047 logarithms of running sums and the loss takes exp of
-// its difference to the old one.
+// left at the end are one term), the sums of 1 / S_t from the front.  64 bits,
+// because logp sums up to 2047 logarithms of running sums and the loss takes
+// exp of its difference to the old one.  Terms are relative to the image's
+// largest score while all are within 2^900 of it, else pairs v 2^e, joined at
+// the larger e by shifting exponents: a score however far below, drawn late,
+// neither vanishes nor divides zero by zero.
 //
-// One workgroup per image; launch and barrier latency bound (an image is a few
-// KB).  Loss terms per image go to the workspace and are added by a second
-// launch in a fixed order.
+// One workgroup per image; launch, memory and barrier latency bound (an image
+// is a few KB).  Shared memory is sized by N, so that several images share a
+// compute unit.  Loss terms per image go to the workspace and are added by a
+// second launch in a fixed order.
 #include "dora_internal.h"
 #include "policy_terms.h"
 
@@ -27,8 +28,6 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
-constexpr int kSlots = DORA_MAX_ROW_TOKENS;
-constexpr double kNever = -1e300;  // exponent of no term
 constexpr double kLog2E = 1.4426950408889634, kLn2 = 0.6931471805599453;
 
 struct PLPolicyParams {
@@ -49,89 +48,191 @@ struct PLPolicyParams {
   int32_t* status;
 };
 
+// exp(x) 2^-ref, where every score is within 2^900 of the largest, 2^ref.
+struct Plain {
+  double v;
+  __device__ static Plain zero() { return {0.0}; }
+  __device__ static Plain exp_of(float x, double ref) { return {exp2(x * kLog2E - ref)}; }
+  __device__ Plain operator+(Plain o) const { return {v + o.v}; }
+  __device__ Plain inverse() const { return {1.0 / v}; }
+  __device__ double log_of(double ref) const { return log(v) + ref * kLn2; }
+  __device__ double times(Plain o) const { return v * o.v; }
+  __device__ Plain down(int d) const { return {__shfl_down(v, d)}; }
+  __device__ Plain up(int d) const { return {__shfl_up(v, d)}; }
+};
+
 // v 2^e, e a whole number (64 bits hold one for every fp32 score).
 struct Scaled {
   double v, e;
+  __device__ static Scaled zero() { return {0.0, -1e300}; }
+  __device__ static Scaled exp_of(float x, double) {
+    const double y = x * kLog2E, e = floor(y);
+    return {exp2(y - e), e};
+  }
+  __device__ double at(double to) const { return ldexp(v, static_cast<int>(fmax(e - to, -4000.0))); }
+  __device__ Scaled operator+(Scaled o) const {
+    const double to = fmax(e, o.e);
+    return {at(to) + o.at(to), to};
+  }
+  __device__ Scaled inverse() const { return {1.0 / v, -e}; }
+  __device__ double log_of(double) const { return log(v) + e * kLn2; }
+  __device__ double times(Scaled o) const { return Scaled{v * o.v, e + o.e}.at(0.0); }
+  __device__ Scaled down(int d) const { return {__shfl_down(v, d), __shfl_down(e, d)}; }
+  __device__ Scaled up(int d) const { return {__shfl_up(v, d), __shfl_up(e, d)}; }
 };
-__device__ __forceinline__ double shifted(Scaled x, double e) {
-  return ldexp(x.v, static_cast<int>(fmax(x.e - e, -4000.0)));
-}
-__device__ __forceinline__ Scaled operator+(Scaled x, Scaled y) {
-  const double e = fmax(x.e, y.e);
-  return {shifted(x, e) + shifted(y, e), e};
-}
-__device__ __forceinline__ Scaled exp_of(float x) {
-  const double y = x * kLog2E, e = floor(y);
-  return {exp2(y - e), e};
-}
-__device__ __forceinline__ Scaled shfl_down(Scaled x, int d) { return {__shfl_down(x.v, d), __shfl_down(x.e, d)}; }
-__device__ __forceinline__ Scaled shfl_up(Scaled x, int d) { return {__shfl_up(x.v, d), __shfl_up(x.e, d)}; }
 
-// Sum of the values of the threads after (before, if FRONT) this one.
-template <bool FRONT>
-__device__ Scaled scan_others(Scaled own, Scaled* s_red) {
+// Shared memory: what depends on N, 24 bytes a token.
+struct Tokens {
+  float* x;       // visual scores by position - 1
+  int* rank;      // draw that takes the position, -1: none
+  char* scan;     // 16 bytes a token: Scaled sums of 1 / S by draw; or Plain, exp by position before them
+};
+constexpr int kTokenBytes = 24;
+
+// Sum of the values of the threads after (before, if FRONT) this one; s_red is
+// this scan's own.
+template <bool FRONT, class T>
+__device__ __forceinline__ T scan_others(T own, T* s_red) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  Scaled incl = own;
+  T incl = own;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
-    const Scaled y = FRONT ? shfl_up(incl, d) : shfl_down(incl, d);
+    const T y = FRONT ? incl.up(d) : incl.down(d);
     if (FRONT ? lane >= d : lane + d < 64) incl = incl + y;
   }
-  Scaled excl = FRONT ? shfl_up(incl, 1) : shfl_down(incl, 1);
-  if (lane == (FRONT ? 0 : 63)) excl = {0.0, kNever};
-  __syncthreads();
   if (lane == (FRONT ? 63 : 0)) s_red[wave] = incl;
+  T excl = FRONT ? incl.up(1) : incl.down(1);
+  if (lane == (FRONT ? 0 : 63)) excl = T::zero();
   __syncthreads();
-  for (int w = 0; w < kWaves; ++w)
+#pragma unroll
+  for (int i = 0; i < kWaves - 1; ++i) {
+    const int w = FRONT ? i : i + 1;
     if (FRONT ? w < wave : w > wave) excl = excl + s_red[w];
+  }
   return excl;
 }
 
-__global__ __launch_bounds__(kThreads) void pl_policy_kernel(PLPolicyParams p) {
-  __shared__ float s_x[kSlots];       // visual scores by position - 1
-  __shared__ int s_rank[kSlots];      // draw that takes the position, -1: none
-  __shared__ Scaled s_exp[kSlots];    // exp of the scores
-  __shared__ Scaled s_front[kSlots];  // sum over the draws up to and with t of 1 / S
-  __shared__ Scaled s_red[kWaves];
+// The image's log-probability; its sums of 1 / S by draw are left in `front`.
+// Called by the whole workgroup, the tokens and ranks being there.
+template <class T>
+__device__ __forceinline__ double scan_draws(const Tokens& s, const int32_t* order, int nv, int k, double ref, T* front) {
+  constexpr bool kStored = sizeof(T) == sizeof(Plain);  // exp is looked up, not formed again
+  __shared__ T s_left[kWaves], s_back[kWaves], s_front[kWaves];
   __shared__ double s_sum[kWaves];
+  const int tid = threadIdx.x;
+  T* const exps = front + nv;  // Plain only
+  T left = T::zero();
+  for (int j = tid; j < nv; j += kThreads) {
+    const T e = T::exp_of(s.x[j], ref);
+    if constexpr (kStored) exps[j] = e;
+    if (s.rank[j] < 0) left = left + e;
+  }
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) left = left + left.down(d);  // lane 0 has all
+  if ((tid & 63) == 0) s_left[tid >> 6] = left;
+  __syncthreads();
+  auto exp_at = [&](int pos) {
+    if constexpr (kStored) return exps[pos];
+    else return T::exp_of(s.x[pos], ref);
+  };
+  // S from the back.  Thread i scans the draws [i c, (i + 1) c); the last one adds what is left.
+  const int c = (k + kThreads - 1) / kThreads, first = min(k, tid * c), last = min(k, first + c);
+  T own = T::zero();
+  if (tid == kThreads - 1) {
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) own = own + s_left[w];
+  }
+  left = own;
+  for (int t = last - 1; t >= first; --t) own = own + exp_at(order[t] - 1);
+  T run = scan_others<false>(own, s_back);
+  if (tid == kThreads - 1) run = left;
+  double lp = 0.0;
+  own = T::zero();
+  for (int t = last - 1; t >= first; --t) {
+    const int pos = order[t] - 1;
+    run = run + exp_at(pos);
+    lp += s.x[pos] - run.log_of(ref);
+    front[t] = run.inverse();
+    own = own + front[t];
+  }
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) lp += __shfl_xor(lp, d);
+  if ((tid & 63) == 0) s_sum[tid >> 6] = lp;
+  run = scan_others<true>(own, s_front);  // its barrier is s_sum's too
+  for (int t = first; t < last; ++t) {
+    run = run + front[t];
+    front[t] = run;
+  }
+  __syncthreads();
+  lp = 0.0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) lp += s_sum[w];
+  return lp;
+}
+
+// d loss / d s of the visual tokens.
+template <class T>
+__device__ __forceinline__ void put_gradient(const Tokens& s, const T* front, int nv, int k, double ref, double slope,
+                                             float* grad) {
+  for (int j = threadIdx.x; j < nv; j += kThreads) {
+    float g = 0.0f;
+    if (k > 0) {
+      const int r = s.rank[j];
+      T e;
+      if constexpr (sizeof(T) == sizeof(Plain)) e = front[nv + j];
+      else e = T::exp_of(s.x[j], ref);
+      g = static_cast<float>(slope * ((r < 0 ? 0.0 : 1.0) - e.times(front[r < 0 ? k - 1 : r])));
+    }
+    grad[j] = g;
+  }
+}
+
+__global__ __launch_bounds__(kThreads) void pl_policy_kernel(PLPolicyParams p) {
+  extern __shared__ double s_tokens[];
+  __shared__ float s_max[kWaves], s_min[kWaves];
   __shared__ int s_bad;
   const int b = blockIdx.x, tid = threadIdx.x;
-
-  int64_t off;
-  int n;
-  bool seg_ok = true;
-  if (p.cu_in) {
-    const int lo = p.cu_in[b], hi = p.cu_in[b + 1];
-    off = lo;
-    n = hi - lo;
-    seg_ok = lo >= 0 && hi > lo && n <= p.N && hi <= p.total_in && (b > 0 || lo == 0);
-  } else {
-    off = static_cast<int64_t>(b) * p.N;
-    n = p.N;
-  }
+  // Everything that says where the image lies is loaded side by side.
+  const int lo = p.cu_in ? p.cu_in[b] : 0, hi = p.cu_in ? p.cu_in[b + 1] : 0;
+  const int o0 = p.cu_order[b], o1 = p.cu_order[b + 1], oend = p.cu_order[p.B], ofirst = p.cu_order[0];
+  const float w = p.weight ? p.weight[b] : 1.0f, old = p.old[b], adv = p.adv[b], refp = p.ref ? p.ref[b] : 0.0f;
+  const int64_t off = p.cu_in ? lo : static_cast<int64_t>(b) * p.N;
+  const int n = p.cu_in ? hi - lo : p.N;
+  const bool seg_ok = !p.cu_in || (lo >= 0 && hi > lo && n <= p.N && hi <= p.total_in && (b > 0 || lo == 0));
   const int nv = seg_ok ? n - 1 : 0;
-  const float w = p.weight ? p.weight[b] : 1.0f;
-  const int o0 = p.cu_order[b], o1 = p.cu_order[b + 1], oend = p.cu_order[p.B];
-  const int k = (o0 >= 0 && o1 >= o0 && o1 <= oend && p.cu_order[0] == 0) ? o1 - o0 : -1;
-  const bool on = seg_ok && w != 0.0f;
-  bool ok = on && k >= 0 && k <= nv;
+  const int k = (o0 >= 0 && o1 >= o0 && o1 <= oend && ofirst == 0) ? o1 - o0 : -1;
+  bool ok = seg_ok && w != 0.0f && k >= 0 && k <= nv;
 
-  if (tid == 0) s_bad = 0;
-  for (int j = tid; j < nv; j += kThreads) {
-    const float x = p.s[off + j + 1];
-    s_x[j] = x;
-    s_exp[j] = exp_of(x);
-    s_rank[j] = -1;
-  }
-  __syncthreads();
+  char* const at = reinterpret_cast<char*>(s_tokens);
+  const Tokens s{reinterpret_cast<float*>(at + 16 * p.N), reinterpret_cast<int*>(at + 20 * p.N), at};
+  const int32_t* const order = p.order + o0;
   if (ok) {
-    for (int t = tid; t < k; t += kThreads) {
-      const int pos = p.order[o0 + t];
-      if (pos < 1 || pos > nv || atomicCAS(&s_rank[pos - 1], -1, t) != -1) s_bad = 1;
+    float top = -__builtin_inff(), low = __builtin_inff();
+    if (tid == 0) s_bad = 0;
+    for (int j = tid; j < nv; j += kThreads) {
+      const float x = p.s[off + j + 1];
+      s.x[j] = x;
+      s.rank[j] = -1;
+      top = fmaxf(top, x);
+      low = fminf(low, x);
     }
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) {
+      top = fmaxf(top, __shfl_xor(top, d));
+      low = fminf(low, __shfl_xor(low, d));
+    }
+    if ((tid & 63) == 0) {
+      s_max[tid >> 6] = top;
+      s_min[tid >> 6] = low;
+    }
+    __syncthreads();
+    for (int t = tid; t < k; t += kThreads) {
+      const int pos = order[t];
+      if (pos < 1 || pos > nv || atomicCAS(&s.rank[pos - 1], -1, t) != -1) s_bad = 1;
+    }
+    __syncthreads();
+    ok = s_bad == 0;
   }
-  __syncthreads();
-  ok = ok && s_bad == 0;
   if (!ok) {
     for (int j = tid; seg_ok && j < n; j += kThreads) p.grad[off + j] = 0.0f;
     if (tid < kPolicyTerms) p.parts[static_cast<int64_t>(b) * kPolicyTerms + tid] = 0.0;
@@ -142,69 +243,27 @@ __global__ __launch_bounds__(kThreads) void pl_policy_kernel(PLPolicyParams p) {
     }
     return;
   }
-
-  // The tokens left at the end: one term after the last draw.
-  Scaled left{0.0, kNever};
-  for (int j = tid; j < nv; j += kThreads)
-    if (s_rank[j] < 0) left = left + s_exp[j];
+  float top = s_max[0], low = s_min[0];
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) left = left + Scaled{__shfl_xor(left.v, d), __shfl_xor(left.e, d)};
-  if ((tid & 63) == 0) s_red[tid >> 6] = left;
-  __syncthreads();
-  left = s_red[0];
-#pragma unroll
-  for (int i = 1; i < kWaves; ++i) left = left + s_red[i];
-  __syncthreads();  // s_red is used again
-
-  // S from the back.  Thread i scans the draws [i c, (i + 1) c); the last one adds what is left.
-  const int c = (k + kThreads - 1) / kThreads, first = min(k, tid * c), last = min(k, first + c);
-  Scaled own = tid == kThreads - 1 ? left : Scaled{0.0, kNever};
-  for (int t = last - 1; t >= first; --t) own = own + s_exp[p.order[o0 + t] - 1];
-  Scaled run = scan_others<false>(own, s_red);
-  if (tid == kThreads - 1) run = left;
-  double lp = 0.0;
-  own = {0.0, kNever};
-  for (int t = last - 1; t >= first; --t) {
-    const int pos = p.order[o0 + t] - 1;
-    run = run + s_exp[pos];
-    lp += s_x[pos] - (log(run.v) + run.e * kLn2);
-    const Scaled inv{1.0 / run.v, -run.e};
-    s_front[t] = inv;
-    own = own + inv;
+  for (int i = 1; i < kWaves; ++i) {
+    top = fmaxf(top, s_max[i]);
+    low = fminf(low, s_min[i]);
   }
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) lp += __shfl_xor(lp, d);
-  if ((tid & 63) == 0) s_sum[tid >> 6] = lp;
-
-  // Sums of 1 / S from the front (the scan's barriers cover s_sum too).
-  run = scan_others<true>(own, s_red);
-  for (int t = first; t < last; ++t) {
-    run = run + s_front[t];
-    s_front[t] = run;
-  }
-  __syncthreads();
-  lp = 0.0;
-#pragma unroll
-  for (int i = 0; i < kWaves; ++i) lp += s_sum[i];
-
+  const double ref = nv > 0 ? top * kLog2E : 0.0;
+  const bool plain = (static_cast<double>(top) - low) * kLog2E < 900.0;  // also for no token: -inf
+  const double lp = plain ? scan_draws(s, order, nv, k, ref, reinterpret_cast<Plain*>(s.scan))
+                          : scan_draws(s, order, nv, k, ref, reinterpret_cast<Scaled*>(s.scan));
   PolicyTerms terms{};
-  const double slope = policy_decision(lp, 0.0, p.old[b], p.adv[b], w, p.ref != nullptr,
-                                       p.ref ? p.ref[b] : 0.0f, p.coef, terms);
+  const double slope = policy_decision(lp, 0.0, old, adv, w, p.ref != nullptr, refp, p.coef, terms);
   if (tid == 0) {
     p.logp[b] = static_cast<float>(lp);
 #pragma unroll
     for (int i = 0; i < kPolicyTerms; ++i) p.parts[static_cast<int64_t>(b) * kPolicyTerms + i] = terms.v[i];
     p.grad[off] = 0.0f;  // CLS is never drawn
   }
-  for (int j = tid; j < nv; j += kThreads) {
-    float g = 0.0f;
-    if (k > 0) {
-      const int r = s_rank[j];
-      const Scaled f = s_front[r < 0 ? k - 1 : r], e = s_exp[j];
-      g = static_cast<float>(slope * ((r < 0 ? 0.0 : 1.0) - shifted({e.v * f.v, e.e + f.e}, 0.0)));
-    }
-    p.grad[off + j + 1] = g;
-  }
+  float* const grad = p.grad + off + 1;
+  if (plain) put_gradient(s, reinterpret_cast<const Plain*>(s.scan), nv, k, ref, slope, grad);
+  else put_gradient(s, reinterpret_cast<const Scaled*>(s.scan), nv, k, ref, slope, grad);
 }
 
 }  // namespace
@@ -241,7 +300,7 @@ extern "C" int dora_pl_policy_loss(const float* scores, const int32_t* order, co
                    PolicyCoef{clip_low, clip_high, kl_coef, 0.0f}, dscores, logprob_out,
                    static_cast<double*>(workspace), dev_status};
   hipStream_t st = static_cast<hipStream_t>(stream);
-  hipLaunchKernelGGL(pl_policy_kernel, dim3(B), dim3(kThreads), 0, st, p);
+  hipLaunchKernelGGL(pl_policy_kernel, dim3(B), dim3(kThreads), static_cast<size_t>(N) * kTokenBytes, st, p);
   launch_policy_finish(p.parts, B, stats_out, st);
   return hipGetLastError() == hipSuccess ? DORA_OK : DORA_ERR_HIP;
 }

@@ -65,8 +65,12 @@ def check(dora, h, kl=0.05, **kw):
     got = ds.cpu().numpy().astype(np.float64).reshape(-1)
     for b, (o, n) in enumerate(h["segs"]):
         sl = slice(o, o + n)
-        top = np.abs(g[sl]).max()
-        assert np.all(np.abs(got[sl] - g[sl]) <= u * np.abs(g[sl]) + 1e-11 * (1 + size[b]) * (top + 1e-30) + 1e-38), b
+        # dscores is slope times a difference, 1 - exp(s_j) sum 1 / S: its two sides are up to the number of draws, each
+        # with a few 2^-53 of itself (1 - x (1 / x) is 2^-53, not 0), so the error scales with slope, not with what is left
+        w = 1.0 if h["weight"] is None else float(h["weight"][b])
+        pull = w * (abs(float(h["A"][b])) * np.exp(lp[b] - float(h["old"][b])) +
+                    (0.0 if h["ref"] is None else kl * (1 + np.exp(float(h["ref"][b]) - lp[b])))) if w else 0.0
+        assert np.all(np.abs(got[sl] - g[sl]) <= u * np.abs(g[sl]) + 1e-11 * (1 + size[b]) * pull + 1e-38), b
     got = st.cpu().numpy().astype(np.float64)
     assert np.all(np.abs(got - stats) <= u * np.abs(stats) + 1e-11 * (1 + size.max()) * scale + 1e-30), (got, stats)
     return ds, glp, st
