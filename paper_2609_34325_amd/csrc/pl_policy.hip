@@ -83,73 +83,73 @@ struct Scaled {
 
 // Shared memory: what depends on N, 24 bytes a token.
 struct Tokens {
+  char* scan;     // 16 bytes a token: Scaled sums of 1 / S by draw; or Plain, and exp by position behind them
   float* x;       // visual scores by position - 1
-  int* rank;      // draw that takes the position, -1: none
-  char* scan;     // 16 bytes a token: Scaled sums of 1 / S by draw; or Plain, exp by position before them
+  int16_t* rank;  // draw that takes the position, -1: none
+  int16_t* draw;  // position - 1 of each draw
 };
 constexpr int kTokenBytes = 24;
 
-// Sum of the values of the threads after (before, if FRONT) this one; s_red is
-// this scan's own.
+// Sum of the values of the wave's lanes after (before, if FRONT) this one; the
+// wave's whole sum goes to *total.
 template <bool FRONT, class T>
-__device__ __forceinline__ T scan_others(T own, T* s_red) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+__device__ __forceinline__ T scan_lanes(T own, T* total) {
+  const int lane = threadIdx.x & 63;
   T incl = own;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
     const T y = FRONT ? incl.up(d) : incl.down(d);
     if (FRONT ? lane >= d : lane + d < 64) incl = incl + y;
   }
-  if (lane == (FRONT ? 63 : 0)) s_red[wave] = incl;
-  T excl = FRONT ? incl.up(1) : incl.down(1);
-  if (lane == (FRONT ? 0 : 63)) excl = T::zero();
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < kWaves - 1; ++i) {
-    const int w = FRONT ? i : i + 1;
-    if (FRONT ? w < wave : w > wave) excl = excl + s_red[w];
-  }
-  return excl;
+  if (lane == (FRONT ? 63 : 0)) *total = incl;
+  const T excl = FRONT ? incl.up(1) : incl.down(1);
+  return lane == (FRONT ? 0 : 63) ? T::zero() : excl;
 }
 
 // The image's log-probability; its sums of 1 / S by draw are left in `front`.
-// Called by the whole workgroup, the tokens and ranks being there.
+// Called by the whole workgroup, scores and draws being there and the ranks
+// all -1; *bad is set where a position is drawn twice (what comes out then is
+// of no use, but all of it stays in bounds).
 template <class T>
-__device__ __forceinline__ double scan_draws(const Tokens& s, const int32_t* order, int nv, int k, double ref, T* front) {
+__device__ __forceinline__ double scan_draws(const Tokens& s, int nv, int k, double ref, T* front, int* bad) {
   constexpr bool kStored = sizeof(T) == sizeof(Plain);  // exp is looked up, not formed again
   __shared__ T s_left[kWaves], s_back[kWaves], s_front[kWaves];
   __shared__ double s_sum[kWaves];
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, wave = tid >> 6;
   T* const exps = front + nv;  // Plain only
-  T left = T::zero();
-  for (int j = tid; j < nv; j += kThreads) {
-    const T e = T::exp_of(s.x[j], ref);
-    if constexpr (kStored) exps[j] = e;
-    if (s.rank[j] < 0) left = left + e;
-  }
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) left = left + left.down(d);  // lane 0 has all
-  if ((tid & 63) == 0) s_left[tid >> 6] = left;
+  for (int t = tid; t < k; t += kThreads) s.rank[s.draw[t]] = static_cast<int16_t>(t);
+  if constexpr (kStored)
+    for (int j = tid; j < nv; j += kThreads) exps[j] = T::exp_of(s.x[j], ref);
   __syncthreads();
   auto exp_at = [&](int pos) {
     if constexpr (kStored) return exps[pos];
     else return T::exp_of(s.x[pos], ref);
   };
-  // S from the back.  Thread i scans the draws [i c, (i + 1) c); the last one adds what is left.
+  T left = T::zero();  // the tokens never drawn
+  for (int j = tid; j < nv; j += kThreads)
+    if (s.rank[j] < 0) left = left + exp_at(j);
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) left = left + left.down(d);  // lane 0 has all
+  if ((tid & 63) == 0) s_left[wave] = left;
+  // S from the back.  Thread i scans the draws [i c, (i + 1) c).
   const int c = (k + kThreads - 1) / kThreads, first = min(k, tid * c), last = min(k, first + c);
   T own = T::zero();
-  if (tid == kThreads - 1) {
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) own = own + s_left[w];
+  for (int t = last - 1; t >= first; --t) {
+    const int pos = s.draw[t];
+    if (s.rank[pos] != t) *bad = 1;
+    own = own + exp_at(pos);
   }
-  left = own;
-  for (int t = last - 1; t >= first; --t) own = own + exp_at(order[t] - 1);
-  T run = scan_others<false>(own, s_back);
-  if (tid == kThreads - 1) run = left;
+  T run = scan_lanes<false>(own, &s_back[wave]);
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    run = run + s_left[w];
+    if (w > wave) run = run + s_back[w];
+  }
   double lp = 0.0;
   own = T::zero();
   for (int t = last - 1; t >= first; --t) {
-    const int pos = order[t] - 1;
+    const int pos = s.draw[t];
     run = run + exp_at(pos);
     lp += s.x[pos] - run.log_of(ref);
     front[t] = run.inverse();
@@ -157,16 +157,20 @@ __device__ __forceinline__ double scan_draws(const Tokens& s, const int32_t* ord
   }
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) lp += __shfl_xor(lp, d);
-  if ((tid & 63) == 0) s_sum[tid >> 6] = lp;
-  run = scan_others<true>(own, s_front);  // its barrier is s_sum's too
+  if ((tid & 63) == 0) s_sum[wave] = lp;
+  run = scan_lanes<true>(own, &s_front[wave]);
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kWaves - 1; ++w)
+    if (w < wave) run = run + s_front[w];
   for (int t = first; t < last; ++t) {
     run = run + front[t];
     front[t] = run;
   }
-  __syncthreads();
   lp = 0.0;
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) lp += s_sum[w];
+  __syncthreads();
   return lp;
 }
 
@@ -204,15 +208,21 @@ __global__ __launch_bounds__(kThreads) void pl_policy_kernel(PLPolicyParams p) {
   bool ok = seg_ok && w != 0.0f && k >= 0 && k <= nv;
 
   char* const at = reinterpret_cast<char*>(s_tokens);
-  const Tokens s{reinterpret_cast<float*>(at + 16 * p.N), reinterpret_cast<int*>(at + 20 * p.N), at};
-  const int32_t* const order = p.order + o0;
+  const Tokens s{at, reinterpret_cast<float*>(at + 16 * p.N), reinterpret_cast<int16_t*>(at + 20 * p.N),
+                 reinterpret_cast<int16_t*>(at + 22 * p.N)};
+  double lp = 0.0, ref = 0.0;
+  bool plain = true;
   if (ok) {
     float top = -__builtin_inff(), low = __builtin_inff();
     if (tid == 0) s_bad = 0;
-    for (int j = tid; j < nv; j += kThreads) {
-      const float x = p.s[off + j + 1];
-      s.x[j] = x;
-      s.rank[j] = -1;
+    bool bad = false;
+    for (int t = tid; t < nv; t += kThreads) {  // scores and draws (no more of them) side by side
+      const float x = p.s[off + t + 1];
+      const int pos = t < k ? p.order[o0 + t] - 1 : 0;
+      s.x[t] = x;
+      s.rank[t] = -1;
+      s.draw[t] = static_cast<int16_t>(min(max(pos, 0), nv - 1));
+      bad = bad || pos < 0 || pos >= nv;
       top = fmaxf(top, x);
       low = fminf(low, x);
     }
@@ -226,11 +236,18 @@ __global__ __launch_bounds__(kThreads) void pl_policy_kernel(PLPolicyParams p) {
       s_min[tid >> 6] = low;
     }
     __syncthreads();
-    for (int t = tid; t < k; t += kThreads) {
-      const int pos = order[t];
-      if (pos < 1 || pos > nv || atomicCAS(&s.rank[pos - 1], -1, t) != -1) s_bad = 1;
+    if (bad) s_bad = 1;
+    top = s_max[0];
+    low = s_min[0];
+#pragma unroll
+    for (int i = 1; i < kWaves; ++i) {
+      top = fmaxf(top, s_max[i]);
+      low = fminf(low, s_min[i]);
     }
-    __syncthreads();
+    ref = nv > 0 ? top * kLog2E : 0.0;
+    plain = (static_cast<double>(top) - low) * kLog2E < 900.0;  // also for no token: -inf
+    lp = plain ? scan_draws(s, nv, k, ref, reinterpret_cast<Plain*>(s.scan), &s_bad)
+               : scan_draws(s, nv, k, ref, reinterpret_cast<Scaled*>(s.scan), &s_bad);
     ok = s_bad == 0;
   }
   if (!ok) {
@@ -243,16 +260,6 @@ __global__ __launch_bounds__(kThreads) void pl_policy_kernel(PLPolicyParams p) {
     }
     return;
   }
-  float top = s_max[0], low = s_min[0];
-#pragma unroll
-  for (int i = 1; i < kWaves; ++i) {
-    top = fmaxf(top, s_max[i]);
-    low = fminf(low, s_min[i]);
-  }
-  const double ref = nv > 0 ? top * kLog2E : 0.0;
-  const bool plain = (static_cast<double>(top) - low) * kLog2E < 900.0;  // also for no token: -inf
-  const double lp = plain ? scan_draws(s, order, nv, k, ref, reinterpret_cast<Plain*>(s.scan))
-                          : scan_draws(s, order, nv, k, ref, reinterpret_cast<Scaled*>(s.scan));
   PolicyTerms terms{};
   const double slope = policy_decision(lp, 0.0, old, adv, w, p.ref != nullptr, refp, p.coef, terms);
   if (tid == 0) {
