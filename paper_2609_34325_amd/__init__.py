@@ -639,6 +639,14 @@ def dora_varlen_attn_noalloc(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, 
     return out
 
 
+def _in_stream(stream):
+    """The context of a given stream: what a call allocates and clears belongs to
+    the stream that it runs on."""
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(stream)) if int(stream) else torch.cuda.default_stream()
+    return torch.cuda.stream(stream)
+
+
 def _rows(t: torch.Tensor, name: str):
     """Address, leading dimension, sizes, type and device of rows whose elements
     are adjacent."""
@@ -708,6 +716,10 @@ def dora_action_logprob(logits: torch.Tensor, actions: torch.Tensor, weight: Opt
     workspace (a new one when None) few long rows may be split over several
     workgroups; single=True passes none.  Returns (logprob [T], entropy [T],
     dev_status)."""
+    if stream is not None:
+        with _in_stream(stream):
+            return dora_action_logprob(logits, actions, weight, legal, logprob_out, entropy_out, workspace, single,
+                                       dev_status)
     address, ld, T, V, code, device = _rows(logits, "logits")
     dev = logits.device
     logprob_out = torch.empty(T, dtype=torch.float32, device=dev) if logprob_out is None else logprob_out
@@ -719,7 +731,7 @@ def dora_action_logprob(logits: torch.Tensor, actions: torch.Tensor, weight: Opt
     dev_status = new_status(dev) if dev_status is None else dev_status
     _vectors(("actions", "legal", "weight", "logprob_out", "entropy_out", "workspace", "dev_status"), device,
              T, actions, T, legal, T, weight, T, logprob_out, T, entropy_out, -1, workspace, -1, dev_status)
-    _call("dora_action_logprob", stream, address, ld, actions, legal, weight, T, V, code, logprob_out, entropy_out,
+    _call("dora_action_logprob", None, address, ld, actions, legal, weight, T, V, code, logprob_out, entropy_out,
           workspace, _bytes(workspace), dev_status)
     return logprob_out, entropy_out, dev_status
 
@@ -739,6 +751,11 @@ def dora_policy_loss(logits: torch.Tensor, actions: torch.Tensor, old_logprob: t
     the logits themselves.  Returns (dlogits [T, V], logprob [T], stats [6],
     dev_status); stats holds the sums of loss, gain, kl, entropy, clipped share
     and weight."""
+    if stream is not None:
+        with _in_stream(stream):
+            return dora_policy_loss(logits, actions, old_logprob, advantage, ref_logprob, weight, legal, clip_low,
+                                    clip_high, kl_coef, entropy_coef, dlogits, logprob_out, stats_out, workspace,
+                                    dev_status)
     address, ld, T, V, code, device = _rows(logits, "logits")
     dev = logits.device
     dlogits = torch.empty((T, V), dtype=logits.dtype, device=dev) if dlogits is None else dlogits
@@ -752,7 +769,7 @@ def dora_policy_loss(logits: torch.Tensor, actions: torch.Tensor, old_logprob: t
     _vectors(("actions", "legal", "old_logprob", "ref_logprob", "advantage", "weight", "logprob_out", "stats_out",
               "workspace", "dev_status"), device, T, actions, T, legal, T, old_logprob, T, ref_logprob, T, advantage,
              T, weight, T, logprob_out, 6, stats_out, -1, workspace, -1, dev_status)
-    _call("dora_policy_loss", stream, address, ld, actions, legal, old_logprob, ref_logprob, advantage, weight, T, V,
+    _call("dora_policy_loss", None, address, ld, actions, legal, old_logprob, ref_logprob, advantage, weight, T, V,
           code, float(clip_low), float(clip_high), float(kl_coef), float(entropy_coef), grad, ld_grad, logprob_out,
           stats_out, workspace, _bytes(workspace), dev_status)
     return dlogits, logprob_out, stats_out, dev_status
@@ -779,6 +796,11 @@ def dora_pl_policy_loss(scores: torch.Tensor, order: torch.Tensor, cu_order: tor
     for dora_pl_logprob, the rest as for dora_policy_loss, one entry per image.
     Returns (dscores in the scores' layout, logprob [B], stats [6],
     dev_status)."""
+    if stream is not None:
+        with _in_stream(stream):
+            return dora_pl_policy_loss(scores, order, cu_order, old_logprob, advantage, ref_logprob, weight, cu_in, N,
+                                       clip_low, clip_high, kl_coef, dscores, logprob_out, stats_out, workspace,
+                                       dev_status)
     B = int(cu_order.shape[0]) - 1
     N, total_in = _pl_geometry(scores, B, cu_in, N)
     dev = scores.device
@@ -793,7 +815,7 @@ def dora_pl_policy_loss(scores: torch.Tensor, order: torch.Tensor, cu_order: tor
               "cu_in", "dscores", "workspace", "dev_status"), scores.get_device(), B, old_logprob, B, ref_logprob,
              B, advantage, B, weight, B, logprob_out, 6, stats_out, -1, order, B + 1, cu_order, B + 1, cu_in,
              -1, dscores, -1, workspace, -1, dev_status)
-    _call("dora_pl_policy_loss", stream, scores, order, cu_order, cu_in, total_in, old_logprob, ref_logprob, advantage,
+    _call("dora_pl_policy_loss", None, scores, order, cu_order, cu_in, total_in, old_logprob, ref_logprob, advantage,
           weight, B, N, float(clip_low), float(clip_high), float(kl_coef), dscores, logprob_out, stats_out, workspace,
           _bytes(workspace), dev_status)
     return dscores, logprob_out, stats_out, dev_status
@@ -832,6 +854,9 @@ def dora_grad_clip(grads, max_norm: float, out=None, eps: float = 1e-6, norm_out
     the same sizes and types, or None: in place.  Every tensor is multiplied by
     min(1, max_norm / (norm + eps)); with max_norm = infinity only the norm is
     formed and nothing is written.  Returns (out, norm [1] fp32)."""
+    if stream is not None:
+        with _in_stream(stream):
+            return dora_grad_clip(grads, max_norm, out, eps, norm_out, workspace)
     grads = list(grads)
     spans, device = _spans(grads, "grads")
     out_spans = None
@@ -846,6 +871,6 @@ def dora_grad_clip(grads, max_norm: float, out=None, eps: float = 1e-6, norm_out
     norm_out = torch.empty(1, dtype=torch.float32, device=dev) if norm_out is None else norm_out
     workspace = new_grad_clip_workspace(len(grads), dev) if workspace is None else workspace
     _vectors(("norm_out", "workspace"), device, 1, norm_out, -1, workspace)
-    _call("dora_grad_clip", stream, ctypes.addressof(spans), 0 if out_spans is None else ctypes.addressof(out_spans),
+    _call("dora_grad_clip", None, ctypes.addressof(spans), 0 if out_spans is None else ctypes.addressof(out_spans),
           len(grads), float(max_norm), float(eps), norm_out, workspace, _bytes(workspace))
     return grads if out is None else out, norm_out

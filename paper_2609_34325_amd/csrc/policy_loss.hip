@@ -155,7 +155,9 @@ struct Stat {
 };
 
 // The statistics while a thread takes its pieces.  The reference is raised
-// only past 2^24 of it: hardly ever after the first piece.
+// only past 2^kRaise of it: seldom after the first piece.  (h grows with the
+// distance to the reference, and the entropy is a difference with it.)
+constexpr float kRaise = 10.0f;
 struct Taker {
   Stat st = Stat::none();
   Shift sh{-FLT_MAX};
@@ -164,7 +166,7 @@ struct Taker {
     float top = x[0];
 #pragma unroll
     for (int i = 1; i < N; ++i) top = fmaxf(top, x[i]);
-    if (sh(top) > 24.0f) {
+    if (sh(top) > kRaise) {
       st.raise(top);
       sh = Shift(top);
     }

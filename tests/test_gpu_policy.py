@@ -322,27 +322,34 @@ def test_repeats_to_the_last_bit(gpu, T, V):
         assert torch.equal(a, b)
 
 
-def test_on_a_stream(gpu):
-    """Enqueued on the given stream, after what that stream waits for."""
+@pytest.mark.parametrize("by_handle", [False, True])
+def test_on_a_stream(gpu, by_handle):
+    """Enqueued on the given stream, after what that stream waits for, with all
+    that the call makes for itself; the current stream need not wait."""
     logits, h = make(300, 5000, "bf16", seed=15)
     want = run(gpu, logits, h, kl=0.05)
     side = torch.cuda.Stream()
     late = torch.zeros_like(logits)
     args = {k: dev(h[k]) for k in ("actions", "old", "A", "ref")}
     torch.cuda.synchronize()
+    busy = torch.ones(1 << 28, device="cuda")
+    for _ in range(20):
+        busy.mul_(1.0)                                 # the current stream has work of its own
     with torch.cuda.stream(side):
         for _ in range(20):
             late.copy_(logits)
         late.neg_().neg_()
+    stream = side.cuda_stream if by_handle else side
     got = gpu.dora_policy_loss(late, args["actions"], args["old"], args["A"], ref_logprob=args["ref"], clip_low=0.2,
-                               clip_high=0.28, kl_coef=0.05, dlogits=torch.empty_like(logits),
-                               logprob_out=torch.empty(300, device="cuda"), stats_out=torch.empty(6, device="cuda"),
-                               workspace=gpu.new_policy_workspace(300, 5000),
-                               dev_status=torch.zeros(1, dtype=torch.int32, device="cuda"), stream=side)
+                               clip_high=0.28, kl_coef=0.05, stream=stream)
+    lp, H, st = gpu.dora_action_logprob(late, args["actions"], stream=stream)
+    out, norm = gpu.dora_grad_clip([got[0]], 1e9, out=[torch.empty_like(late)], stream=stream)
     side.synchronize()
-    torch.cuda.synchronize()
+    assert int(got[3].item()) == 0 and int(st.item()) == 0
     for a, b in zip(got[:3], want[:3]):
         assert torch.equal(a, b)
+    assert torch.equal(out[0], want[0])
+    assert torch.all((lp - want[1]).abs() <= 2 * (5000 / 16 + 68) * P.U32 + 2 * P.U32 * want[1].abs())
 
 
 def test_refusals(gpu):
