@@ -57,8 +57,6 @@ struct Plain {
   __device__ Plain inverse() const { return {1.0 / v}; }
   __device__ double log_of(double ref) const { return log(v) + ref * kLn2; }
   __device__ double times(Plain o) const { return v * o.v; }
-  __device__ Plain down(int d) const { return {__shfl_down(v, d)}; }
-  __device__ Plain up(int d) const { return {__shfl_up(v, d)}; }
 };
 
 // v 2^e, e a whole number (64 bits hold one for every fp32 score).
@@ -91,19 +89,52 @@ struct Tokens {
 constexpr int kTokenBytes = 24;
 
 // Sum of the values of the wave's lanes after (before, if FRONT) this one; the
-// wave's whole sum goes to *total.
-template <bool FRONT, class T>
-__device__ __forceinline__ T scan_lanes(T own, T* total) {
+// wave's whole sum goes to *total.  All lanes active.
+template <bool FRONT>
+__device__ __forceinline__ Scaled scan_lanes(Scaled own, Scaled* total) {
   const int lane = threadIdx.x & 63;
-  T incl = own;
+  Scaled incl = own;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
-    const T y = FRONT ? incl.up(d) : incl.down(d);
+    const Scaled y = FRONT ? incl.up(d) : incl.down(d);
     if (FRONT ? lane >= d : lane + d < 64) incl = incl + y;
   }
-  if (lane == (FRONT ? 63 : 0)) *total = incl;
-  const T excl = FRONT ? incl.up(1) : incl.down(1);
-  return lane == (FRONT ? 0 : 63) ? T::zero() : excl;
+  total->v = __shfl(incl.v, FRONT ? 63 : 0);
+  total->e = __shfl(incl.e, FRONT ? 63 : 0);
+  const Scaled excl = FRONT ? incl.up(1) : incl.down(1);
+  return lane == (FRONT ? 0 : 63) ? Scaled::zero() : excl;
+}
+
+// The value of the lane CTRL (a DPP shift inside a row of 16 lanes) points to, 0 past the row.
+template <int CTRL>
+__device__ __forceinline__ double row_shift(double v) {
+  const int lo = __builtin_amdgcn_update_dpp(0, __double2loint(v), CTRL, 0xF, 0xF, true);
+  const int hi = __builtin_amdgcn_update_dpp(0, __double2hiint(v), CTRL, 0xF, 0xF, true);
+  return __hiloint2double(hi, lo);
+}
+__device__ __forceinline__ double lane_value(double v, int lane) {
+  return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), lane),
+                          __builtin_amdgcn_readlane(__double2loint(v), lane));
+}
+// The same without shared memory: shifts inside rows of 16 lanes, and the rows'
+// sums as scalars.
+template <bool FRONT>
+__device__ __forceinline__ Plain scan_lanes(Plain own, Plain* total) {
+  constexpr int kShift = FRONT ? 0x110 : 0x100;  // row_shr, row_shl
+  double v = own.v;
+  v += row_shift<kShift + 1>(v);
+  v += row_shift<kShift + 2>(v);
+  v += row_shift<kShift + 4>(v);
+  v += row_shift<kShift + 8>(v);
+  constexpr int kEnd = FRONT ? 15 : 0;
+  const int row = (threadIdx.x & 63) >> 4;
+  const double r0 = lane_value(v, kEnd), r1 = lane_value(v, kEnd + 16), r2 = lane_value(v, kEnd + 32),
+               r3 = lane_value(v, kEnd + 48);
+  double others;
+  if (FRONT) others = row == 0 ? 0.0 : (row == 1 ? r0 : (row == 2 ? r0 + r1 : r0 + r1 + r2));
+  else others = row == 3 ? 0.0 : (row == 2 ? r3 : (row == 1 ? r3 + r2 : r3 + r2 + r1));
+  total->v = (r0 + r1) + (r2 + r3);
+  return {others + row_shift<kShift + 1>(v)};
 }
 
 // The image's log-probability; its sums of 1 / S by draw are left in `front`.
@@ -128,9 +159,9 @@ __device__ __forceinline__ double scan_draws(const Tokens& s, int nv, int k, dou
   T left = T::zero();  // the tokens never drawn
   for (int j = tid; j < nv; j += kThreads)
     if (s.rank[j] < 0) left = left + exp_at(j);
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) left = left + left.down(d);  // lane 0 has all
-  if ((tid & 63) == 0) s_left[wave] = left;
+  T sum;
+  scan_lanes<false>(left, &sum);
+  if ((tid & 63) == 0) s_left[wave] = sum;
   // S from the back.  Thread i scans the draws [i c, (i + 1) c).
   const int c = (k + kThreads - 1) / kThreads, first = min(k, tid * c), last = min(k, first + c);
   T own = T::zero();
@@ -139,7 +170,8 @@ __device__ __forceinline__ double scan_draws(const Tokens& s, int nv, int k, dou
     if (s.rank[pos] != t) *bad = 1;
     own = own + exp_at(pos);
   }
-  T run = scan_lanes<false>(own, &s_back[wave]);
+  T run = scan_lanes<false>(own, &sum);
+  if ((tid & 63) == 0) s_back[wave] = sum;
   __syncthreads();
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) {
@@ -155,10 +187,13 @@ __device__ __forceinline__ double scan_draws(const Tokens& s, int nv, int k, dou
     front[t] = run.inverse();
     own = own + front[t];
   }
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) lp += __shfl_xor(lp, d);
-  if ((tid & 63) == 0) s_sum[wave] = lp;
-  run = scan_lanes<true>(own, &s_front[wave]);
+  Plain part;
+  scan_lanes<false>(Plain{lp}, &part);
+  run = scan_lanes<true>(own, &sum);
+  if ((tid & 63) == 0) {
+    s_sum[wave] = part.v;
+    s_front[wave] = sum;
+  }
   __syncthreads();
 #pragma unroll
   for (int w = 0; w < kWaves - 1; ++w)
