@@ -26,8 +26,6 @@
 namespace dora {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kWaves = kThreads / 64;
 constexpr double kLog2E = 1.4426950408889634, kLn2 = 0.6931471805599453;
 
 struct PLPolicyParams {
@@ -141,8 +139,9 @@ __device__ __forceinline__ Plain scan_lanes(Plain own, Plain* total) {
 // Called by the whole workgroup, scores and draws being there and the ranks
 // all -1; *bad is set where a position is drawn twice (what comes out then is
 // of no use, but all of it stays in bounds).
-template <class T>
+template <int kThreads, class T>
 __device__ __forceinline__ double scan_draws(const Tokens& s, int nv, int k, double ref, T* front, int* bad) {
+  constexpr int kWaves = kThreads / 64;
   constexpr bool kStored = sizeof(T) == sizeof(Plain);  // exp is looked up, not formed again
   __shared__ T s_left[kWaves], s_back[kWaves], s_front[kWaves];
   __shared__ double s_sum[kWaves];
@@ -210,7 +209,7 @@ __device__ __forceinline__ double scan_draws(const Tokens& s, int nv, int k, dou
 }
 
 // d loss / d s of the visual tokens.
-template <class T>
+template <int kThreads, class T>
 __device__ __forceinline__ void put_gradient(const Tokens& s, const T* front, int nv, int k, double ref, double slope,
                                              float* grad) {
   for (int j = threadIdx.x; j < nv; j += kThreads) {
@@ -226,7 +225,9 @@ __device__ __forceinline__ void put_gradient(const Tokens& s, const T* front, in
   }
 }
 
+template <int kThreads>
 __global__ __launch_bounds__(kThreads) void pl_policy_kernel(PLPolicyParams p) {
+  constexpr int kWaves = kThreads / 64;
   extern __shared__ double s_tokens[];
   __shared__ float s_max[kWaves], s_min[kWaves];
   __shared__ int s_bad;
@@ -281,8 +282,8 @@ __global__ __launch_bounds__(kThreads) void pl_policy_kernel(PLPolicyParams p) {
     }
     ref = nv > 0 ? top * kLog2E : 0.0;
     plain = (static_cast<double>(top) - low) * kLog2E < 900.0;  // also for no token: -inf
-    lp = plain ? scan_draws(s, nv, k, ref, reinterpret_cast<Plain*>(s.scan), &s_bad)
-               : scan_draws(s, nv, k, ref, reinterpret_cast<Scaled*>(s.scan), &s_bad);
+    lp = plain ? scan_draws<kThreads>(s, nv, k, ref, reinterpret_cast<Plain*>(s.scan), &s_bad)
+               : scan_draws<kThreads>(s, nv, k, ref, reinterpret_cast<Scaled*>(s.scan), &s_bad);
     ok = s_bad == 0;
   }
   if (!ok) {
@@ -304,8 +305,8 @@ __global__ __launch_bounds__(kThreads) void pl_policy_kernel(PLPolicyParams p) {
     p.grad[off] = 0.0f;  // CLS is never drawn
   }
   float* const grad = p.grad + off + 1;
-  if (plain) put_gradient(s, reinterpret_cast<const Plain*>(s.scan), nv, k, ref, slope, grad);
-  else put_gradient(s, reinterpret_cast<const Scaled*>(s.scan), nv, k, ref, slope, grad);
+  if (plain) put_gradient<kThreads>(s, reinterpret_cast<const Plain*>(s.scan), nv, k, ref, slope, grad);
+  else put_gradient<kThreads>(s, reinterpret_cast<const Scaled*>(s.scan), nv, k, ref, slope, grad);
 }
 
 }  // namespace
@@ -342,7 +343,17 @@ extern "C" int dora_pl_policy_loss(const float* scores, const int32_t* order, co
                    PolicyCoef{clip_low, clip_high, kl_coef, 0.0f}, dscores, logprob_out,
                    static_cast<double*>(workspace), dev_status};
   hipStream_t st = static_cast<hipStream_t>(stream);
-  hipLaunchKernelGGL(pl_policy_kernel, dim3(B), dim3(kThreads), static_cast<size_t>(N) * kTokenBytes, st, p);
+  // Wide workgroups shorten a long row's way through the scans, narrow ones
+  // repeat less (every wave takes the loss's exp and log) where the images fill
+  // the GPU.  64 / 128 / 256 threads, us a pass: 8192 x 257 tokens 30 / 34 / 45,
+  // 512 x 257 9.6 / 9.4 / 9.2, 8192 x 577 52 / 46 / 55, 512 x 577 13.4 / 11.3 / 9.9,
+  // 2048 x 1200 47 / 34 / 27, 2048 x 65 9.6 / 10.8 / 14.4.
+  const bool many = B > 1024;
+  const int threads = N <= 128 || (N <= 320 && many) ? 64 : (N <= 320 || (N <= 800 && many) ? 128 : 256);
+  const size_t lds = static_cast<size_t>(N) * kTokenBytes;
+  if (threads == 64) hipLaunchKernelGGL(pl_policy_kernel<64>, dim3(B), dim3(64), lds, st, p);
+  else if (threads == 128) hipLaunchKernelGGL(pl_policy_kernel<128>, dim3(B), dim3(128), lds, st, p);
+  else hipLaunchKernelGGL(pl_policy_kernel<256>, dim3(B), dim3(256), lds, st, p);
   launch_policy_finish(p.parts, B, stats_out, st);
   return hipGetLastError() == hipSuccess ? DORA_OK : DORA_ERR_HIP;
 }

@@ -87,6 +87,14 @@ def test_sizes(gpu, B, N, packed):
     check(gpu, make(lens, packed=packed, seed=1))
 
 
+@pytest.mark.parametrize("B,N", [(1100, 130), (1030, 321), (1025, 800)])
+def test_many_images(gpu, B, N):
+    """Batches and lengths that take workgroups of other widths."""
+    lens = np.random.default_rng(B).integers(1, N + 1, B)
+    lens[7] = N
+    check(gpu, make(lens, packed=True, seed=12, frac=0.15))
+
+
 @pytest.mark.parametrize("N", [2, 5, 197, 258, 2048])
 def test_no_draw_one_and_all(gpu, N):
     h = make([N] * 3, ks=[0, 1, N - 1], seed=2)
