@@ -100,13 +100,17 @@ struct Elem<false> {
   }
 };
 
-template <bool BF16>
+// PASSING: data that is not to stay in the caches (read or written once).
+template <bool BF16, bool PASSING = false>
 __device__ __forceinline__ u32x4 load_piece(const char* p) {
-  return *reinterpret_cast<const typename Elem<BF16>::Vec*>(p);
+  const auto* from = reinterpret_cast<const typename Elem<BF16>::Vec*>(p);
+  return PASSING ? __builtin_nontemporal_load(from) : *from;
 }
-template <bool BF16>
+template <bool BF16, bool PASSING = false>
 __device__ __forceinline__ void store_piece(char* p, u32x4 v) {
-  *reinterpret_cast<typename Elem<BF16>::Vec*>(p) = v;
+  auto* to = reinterpret_cast<typename Elem<BF16>::Vec*>(p);
+  if (PASSING) __builtin_nontemporal_store(v, to);
+  else *to = v;
 }
 
 // A row's exponentials are 2^d with d = x c1 - e, c1 = log2(e) rounded and e
@@ -346,6 +350,12 @@ __global__ __launch_bounds__(group_threads(L), 4) void policy_rows_kernel(RowPar
   using X = Elem<BF16>;
   constexpr int kRows = group_threads(L) / L, kWaves = L / 64;
   constexpr bool kPark = GRAD && NV > 4;
+  // Past the caches, us a pass without and with: stores of 1024 x 32000 fp32
+  // 54.6, 48.8, of 8192 x 4096 bf16 36.7, 30.5; rows of 1024 threads are better
+  // off through them (8192 x 131072 bf16 800, 811).  Loads as well only for 256
+  // threads a row (8192 x 32768 bf16 227, 204; for 64 and 512 30.5, 33.2 and
+  // 48.8, 50.7).
+  constexpr bool kPassStores = L <= 512, kPassLoads = GRAD && L == 256;
   __shared__ Stat s_stat[L > 64 ? kWaves : kRows];
   __shared__ RowIn s_in[kRows];
   __shared__ RowSlope s_slope[kRows];
@@ -363,7 +373,7 @@ __global__ __launch_bounds__(group_threads(L), 4) void policy_rows_kernel(RowPar
   // so that they are counted and waited for one by one.
   auto load = [&](const RowCut<BF16>& cut, int last) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) held[i] = load_piece<BF16>(row + cut.byte(min(lane + i * L, last)));
+    for (int i = 0; i < NV; ++i) held[i] = load_piece<BF16, kPassLoads>(row + cut.byte(min(lane + i * L, last)));
     asm volatile("" ::: "memory");
   };
   RowIn in;
@@ -448,12 +458,12 @@ __global__ __launch_bounds__(group_threads(L), 4) void policy_rows_kernel(RowPar
     // (twice the registers) from the statistics on.
 #pragma unroll
     for (int i = 0; i < NV; ++i) asm volatile("" : "+v"(held[i]));
-    auto put = [&](u32x4 v, int i) { store_piece<BF16>(out + cut.byte(i), slope.piece(v, i)); };
+    auto put = [&](u32x4 v, int i) { store_piece<BF16, kPassStores>(out + cut.byte(i), slope.piece(v, i)); };
     for (int i = lane + NV * L; i < cut.open; i += L) put(load_piece<BF16>(row + cut.byte(i)), i);
 #pragma unroll
     for (int i = 0; i < NV; ++i)
       if (lane + i * L < cut.open) put(held[i], lane + i * L);
-    for (int i = cut.closed() + lane; i < cut.all; i += L) store_piece<BF16>(out + cut.byte(i), u32x4{});
+    for (int i = cut.closed() + lane; i < cut.all; i += L) store_piece<BF16, kPassStores>(out + cut.byte(i), u32x4{});
     if (lane < X::kPer && cut.part(0) < rs.n)
       slope.one(row, out, cut.head + cut.open * X::kPer + lane);
     if (cut.edge(lane) < p.V) slope.one(row, out, cut.edge(lane));
@@ -462,7 +472,7 @@ __global__ __launch_bounds__(group_threads(L), 4) void policy_rows_kernel(RowPar
 
 // Statistics of the open pieces [lo, hi) of a row and, if `ends`, of the open
 // elements outside the pieces that are open.  Four pieces in flight a thread.
-template <bool BF16>
+template <bool BF16, bool PASSING>
 __device__ __forceinline__ Stat range_stats(const char* row, const RowCut<BF16>& cut, int lo, int hi, bool ends) {
   using X = Elem<BF16>;
   constexpr int kFlight = 4;
@@ -471,7 +481,7 @@ __device__ __forceinline__ Stat range_stats(const char* row, const RowCut<BF16>&
   for (int i = lo + tid; i < hi; i += kFlight * kThreads) {
     u32x4 v[kFlight];
 #pragma unroll
-    for (int k = 0; k < kFlight; ++k) v[k] = load_piece<BF16>(row + cut.byte(min(i + k * kThreads, hi - 1)));
+    for (int k = 0; k < kFlight; ++k) v[k] = load_piece<BF16, PASSING>(row + cut.byte(min(i + k * kThreads, hi - 1)));
     asm volatile("" ::: "memory");
 #pragma unroll
     for (int k = 0; k < kFlight; ++k) {
@@ -494,10 +504,11 @@ __device__ __forceinline__ int2 share_of(const RowParams& p, int chunk, int all)
 }
 
 // Statistics of long rows, p.split workgroups a row.  One a row: it closes the
-// row (log-probability only).  Several: each leaves its triple for the next
+// row (log-probability only), and the logits pass the caches by (4096 x 50257
+// bf16 54 us; through them 62).  Several: each leaves its triple for the next
 // launch, with the action's logit (which a gradient over the logits would
 // overwrite).
-template <bool BF16>
+template <bool BF16, bool SPLIT>
 __global__ __launch_bounds__(kThreads) void policy_stats_kernel(RowParams p) {
   using X = Elem<BF16>;
   __shared__ Stat s_red[kThreads / 64];
@@ -508,14 +519,14 @@ __global__ __launch_bounds__(kThreads) void policy_stats_kernel(RowParams p) {
   const char* row = p.logits + t * p.ld * X::kBytes;
   const RowCut<BF16> cut(p.grad ? p.grad + t * p.ld_grad * X::kBytes : row, in.n, p.V);
   const int2 c = share_of(p, chunk, cut.all);
-  Stat st = merge_lanes<64>(range_stats<BF16>(row, cut, min(c.x, cut.open), min(c.y, cut.open), chunk == 0));
+  Stat st = merge_lanes<64>(range_stats<BF16, !SPLIT>(row, cut, min(c.x, cut.open), min(c.y, cut.open), chunk == 0));
   if ((threadIdx.x & 63) == 0) s_red[threadIdx.x >> 6] = st;
   __syncthreads();
   if (threadIdx.x >= 64) return;
   st = merge_lanes<kThreads / 64>(s_red[threadIdx.x % (kThreads / 64)]);
   in.xa = X::get(row + static_cast<int64_t>(in.a) * X::kBytes);
   if (threadIdx.x > 0) return;
-  if (p.split > 1) p.split_stats[blockIdx.x] = make_float4(st.m, st.s, st.h, in.xa);
+  if (SPLIT) p.split_stats[blockIdx.x] = make_float4(st.m, st.s, st.h, in.xa);
   else close_row<false, true>(p, t, in, RowLoss{}, st, nullptr);
 }
 
@@ -638,15 +649,22 @@ void launch_shape(const RowParams& p, hipStream_t st) {
 }
 
 // Workgroups a row, for long rows that are few: as many as bring about
-// kSplitGroups of them, each with at least two pieces a thread.
-constexpr int kSplitGroups = 512, kSplitRows = 128;
-int split_of(int32_t T, int pieces) {
-  if (T > kSplitRows) return 1;
+// kSplitGroups of them, each with at least two pieces a thread.  It pays where
+// a row is long against the batch; the loss closes all rows in one workgroup
+// besides.  us a pass split and not, bf16: loss of 8 x 131072 8.3, 20.2, 128 x
+// 131072 23.0, 24.9, 64 x 32768 9.9, 11.9, but 192 x 131072 34.9, 27.7, 128 x
+// 32768 14.3, 11.9, 64 x 10000 9.3, 8.8; log-probabilities of 8 x 131072 7.9, 20.4,
+// 256 x 131072 18.2, 22.4, but 8 x 32768 8.0, 7.1.
+constexpr int kSplitGroups = 512;
+int split_of(bool grad, int32_t T, int pieces) {
+  if (grad ? T > 128 || pieces / 64 < T : T > 256 || pieces <= 4096) return 1;
   return std::max(1, std::min({kSplitGroups / T, pieces / (2 * kThreads), kMaxSplit}));
 }
 
-// The fewest threads a row that hold it in 16 pieces each: short rows share a
-// wave, and the threads left over take other rows.
+// The fewest threads a row that hold it in 16 pieces each (8 where rows share
+// a workgroup), and the fewest pieces, of those there are kernels for: a piece
+// too many is registers that another row could use (2048 x 50257 bf16, 13 of
+// 16 pieces in use 114 us, of 13 106).
 template <bool BF16, bool GRAD, bool ENT>
 void launch_rows(RowParams p, hipStream_t st) {
   const int pieces = (p.V + Elem<BF16>::kPer - 1) / Elem<BF16>::kPer;
@@ -655,9 +673,11 @@ void launch_rows(RowParams p, hipStream_t st) {
   if (pieces <= 64) return launch_shape<BF16, GRAD, ENT, 16, 4>(p, st);
   if (pieces <= 256) return launch_shape<BF16, GRAD, ENT, 64, 4>(p, st);
   if (pieces <= 512) return launch_shape<BF16, GRAD, ENT, 64, 8>(p, st);
-  p.split = p.split_stats ? split_of(p.T, pieces) : 1;
+  p.split = p.split_stats ? split_of(GRAD, p.T, pieces) : 1;
   if (p.split > 1 || !GRAD) {
-    hipLaunchKernelGGL(policy_stats_kernel<BF16>, dim3(static_cast<uint32_t>(p.T) * p.split), dim3(kThreads), 0, st, p);
+    const dim3 groups(static_cast<uint32_t>(p.T) * p.split);
+    if (p.split > 1) hipLaunchKernelGGL((policy_stats_kernel<BF16, true>), groups, dim3(kThreads), 0, st, p);
+    else hipLaunchKernelGGL((policy_stats_kernel<BF16, false>), groups, dim3(kThreads), 0, st, p);
     if constexpr (GRAD)
       hipLaunchKernelGGL((policy_split_grad_kernel<BF16, ENT>), dim3(p.T * p.split + 1), dim3(kThreads), 0, st, p);
     else if (p.split > 1)
@@ -665,14 +685,23 @@ void launch_rows(RowParams p, hipStream_t st) {
     return;
   }
   if constexpr (GRAD) {
-    if (pieces <= 1024) launch_shape<BF16, GRAD, ENT, 256, 4>(p, st);
-    else if (pieces <= 2048) launch_shape<BF16, GRAD, ENT, 256, 8>(p, st);
-    else if (pieces <= 4096) launch_shape<BF16, GRAD, ENT, 256, 16>(p, st);
-    else if (pieces <= 6144) launch_shape<BF16, GRAD, ENT, 512, 12>(p, st);
-    else if (pieces <= 6656) launch_shape<BF16, GRAD, ENT, 512, 13>(p, st);
-    else if (pieces <= 8192) launch_shape<BF16, GRAD, ENT, 512, 16>(p, st);
-    else if (pieces <= 12288) launch_shape<BF16, GRAD, ENT, 1024, 12>(p, st);
-    else launch_shape<BF16, GRAD, ENT, 1024, 16>(p, st);
+    const int L = pieces <= 256 * 16 ? 256 : (pieces <= 512 * 16 ? 512 : 1024), each = (pieces + L - 1) / L;
+    if (L == 256) {
+      if (each <= 4) launch_shape<BF16, GRAD, ENT, 256, 4>(p, st);
+      else if (each <= 8) launch_shape<BF16, GRAD, ENT, 256, 8>(p, st);
+      else if (each <= 12) launch_shape<BF16, GRAD, ENT, 256, 12>(p, st);
+      else launch_shape<BF16, GRAD, ENT, 256, 16>(p, st);
+    } else if (L == 512) {
+      if (each <= 10) launch_shape<BF16, GRAD, ENT, 512, 10>(p, st);
+      else if (each <= 12) launch_shape<BF16, GRAD, ENT, 512, 12>(p, st);
+      else if (each <= 14) launch_shape<BF16, GRAD, ENT, 512, 14>(p, st);
+      else launch_shape<BF16, GRAD, ENT, 512, 16>(p, st);
+    } else {
+      if (each <= 10) launch_shape<BF16, GRAD, ENT, 1024, 10>(p, st);
+      else if (each <= 12) launch_shape<BF16, GRAD, ENT, 1024, 12>(p, st);
+      else if (each <= 14) launch_shape<BF16, GRAD, ENT, 1024, 14>(p, st);
+      else launch_shape<BF16, GRAD, ENT, 1024, 16>(p, st);
+    }
   }
 }
 
@@ -726,7 +755,8 @@ extern "C" size_t dora_policy_workspace_size(int32_t T, int32_t V) {
   using namespace dora;
   if (T < 1 || T > DORA_MAX_DECISIONS || V < 1 || V > DORA_MAX_ACTIONS) return 0;
   // Either the sums' sets or the split rows' triples; the type with more pieces a row splits further.
-  const size_t split = static_cast<size_t>(T) * split_of(T, (V + 3) / 4) * sizeof(float4);
+  const int most = std::max(split_of(true, T, (V + 3) / 4), split_of(false, T, (V + 3) / 4));
+  const size_t split = static_cast<size_t>(T) * most * sizeof(float4);
   return std::max(policy_parts_bytes(row_groups(T, V)), (split + 255) & ~size_t(255));
 }
 
