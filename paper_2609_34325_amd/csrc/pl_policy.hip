@@ -43,6 +43,7 @@ struct PLPolicyParams {
   float* grad;
   float* logp;
   double* parts;
+  float* stats;
   int32_t* status;
 };
 
@@ -288,7 +289,10 @@ __global__ __launch_bounds__(kThreads) void pl_policy_kernel(PLPolicyParams p) {
   }
   if (!ok) {
     for (int j = tid; seg_ok && j < n; j += kThreads) p.grad[off + j] = 0.0f;
-    if (tid < kPolicyTerms) p.parts[static_cast<int64_t>(b) * kPolicyTerms + tid] = 0.0;
+    if (tid < kPolicyTerms) {
+      if (gridDim.x == 1) p.stats[tid] = 0.0f;
+      else p.parts[static_cast<int64_t>(b) * kPolicyTerms + tid] = 0.0;
+    }
     if (tid == 0) {
       p.logp[b] = seg_ok && w == 0.0f ? 0.0f : __builtin_nanf("");
       if (!seg_ok) atomicOr(p.status, DORA_DEV_CU_IN);
@@ -301,7 +305,10 @@ __global__ __launch_bounds__(kThreads) void pl_policy_kernel(PLPolicyParams p) {
   if (tid == 0) {
     p.logp[b] = static_cast<float>(lp);
 #pragma unroll
-    for (int i = 0; i < kPolicyTerms; ++i) p.parts[static_cast<int64_t>(b) * kPolicyTerms + i] = terms.v[i];
+    for (int i = 0; i < kPolicyTerms; ++i) {
+      if (gridDim.x == 1) p.stats[i] = static_cast<float>(terms.v[i]);  // there is nothing to add to it
+      else p.parts[static_cast<int64_t>(b) * kPolicyTerms + i] = terms.v[i];
+    }
     p.grad[off] = 0.0f;  // CLS is never drawn
   }
   float* const grad = p.grad + off + 1;
@@ -341,7 +348,7 @@ extern "C" int dora_pl_policy_loss(const float* scores, const int32_t* order, co
     return DORA_ERR_WORKSPACE;
   PLPolicyParams p{scores, order, cu_order, cu_in, total_in, old_logprob, ref_logprob, advantage, weight, B, N,
                    PolicyCoef{clip_low, clip_high, kl_coef, 0.0f}, dscores, logprob_out,
-                   static_cast<double*>(workspace), dev_status};
+                   static_cast<double*>(workspace), stats_out, dev_status};
   hipStream_t st = static_cast<hipStream_t>(stream);
   // Wide workgroups shorten a long row's way through the scans, narrow ones
   // repeat less (every wave takes the loss's exp and log) where the images fill
@@ -354,6 +361,6 @@ extern "C" int dora_pl_policy_loss(const float* scores, const int32_t* order, co
   if (threads == 64) hipLaunchKernelGGL(pl_policy_kernel<64>, dim3(B), dim3(64), lds, st, p);
   else if (threads == 128) hipLaunchKernelGGL(pl_policy_kernel<128>, dim3(B), dim3(128), lds, st, p);
   else hipLaunchKernelGGL(pl_policy_kernel<256>, dim3(B), dim3(256), lds, st, p);
-  launch_policy_finish(p.parts, B, stats_out, st);
+  if (B > 1) launch_policy_finish(p.parts, B, stats_out, st);
   return hipGetLastError() == hipSuccess ? DORA_OK : DORA_ERR_HIP;
 }

@@ -436,10 +436,13 @@ __global__ __launch_bounds__(group_threads(L), 4) void policy_rows_kernel(RowPar
         for (int off = kRows / 2; off > 0; off >>= 1) sum.v[k] += __shfl_xor(sum.v[k], off);
     }
     if constexpr (GRAD) {
-      if (threadIdx.x == 0)
+      if (threadIdx.x == 0) {
 #pragma unroll
-        for (int k = 0; k < kPolicyTerms; ++k)
-          p.parts[static_cast<int64_t>(blockIdx.x) * kPolicyTerms + k] = sum.v[k];
+        for (int k = 0; k < kPolicyTerms; ++k) {
+          if (gridDim.x == 1) p.stats[k] = static_cast<float>(sum.v[k]);  // there is nothing to add to it
+          else p.parts[static_cast<int64_t>(blockIdx.x) * kPolicyTerms + k] = sum.v[k];
+        }
+      }
     }
     if constexpr (kPark) {
       asm volatile("" ::: "memory");
@@ -645,7 +648,7 @@ void launch_shape(const RowParams& p, hipStream_t st) {
   constexpr int kRows = group_threads(L) / L;
   const int groups = (p.T + kRows - 1) / kRows;
   hipLaunchKernelGGL((policy_rows_kernel<BF16, L, NV, GRAD, ENT>), dim3(groups), dim3(group_threads(L)), 0, st, p);
-  if constexpr (GRAD) launch_policy_finish(p.parts, groups, p.stats, st);
+  if (GRAD && groups > 1) launch_policy_finish(p.parts, groups, p.stats, st);
 }
 
 // Workgroups a row, for long rows that are few: as many as bring about
