@@ -118,11 +118,11 @@ __device__ __forceinline__ void store_piece(char* p, u32x4 v) {
 // error is its own rounding, and another m scales the older sums by a power of
 // two, exactly.  The shift in natural units is then e / c1 (in 64 bits): terms
 // near the largest, which make up the sums, all carry c1's rounding alike.
-// Past 5e8 two different floats lie at least 32 apart, so any factor tells
-// them from each other, and m c1 would leave a large rest or overflow: there
-// d = x - m (a row whose open logits all hold the type's lowest value is
-// uniform).
-constexpr float kVast = 5.0e8f;
+// Past 1e9 two different floats lie at least 64 apart, so any factor tells
+// them from each other (a million of 2^-64 are nothing beside 1), and m c1
+// would leave a large rest or overflow: there d = x - m (a row whose open
+// logits all hold the type's lowest value is uniform).
+constexpr float kVast = 1.0e9f;
 struct Shift {
   float c1, e;
   __device__ explicit Shift(float m) {

@@ -190,6 +190,27 @@ def test_masked_places(gpu, V, dtype):
     check(gpu, logits, h, dtype, ent=0.01)
 
 
+@pytest.mark.parametrize("base", [2e6, 5.3e8, 9e8, 1.2e9, -5.3e8, -1.2e9, 3.3e38, -3.3e38])
+@pytest.mark.parametrize("V", [300, 70000])
+def test_vast_logits(gpu, V, base):
+    """A few logits of one value, all others the next float below: as far apart
+    as the type allows there, so the few share the probability (at 2e6 they
+    differ by an eighth)."""
+    logits, h = make(2, V, "f32", seed=17)
+    top = np.float32(base)
+    logits[:] = float(np.nextafter(top, np.float32(-np.inf)))
+    logits[:, 5:8] = float(top)
+    h["actions"][:] = [6, V - 1]
+    h["x"] = logits.double().cpu().numpy()
+    lp = np.array([P.softmax_row(h["x"][t], h["actions"][t])[0] for t in range(2)])
+    h["old"] = P.off_border(lp, np.full(2, 0.05), h["low"], h["high"])
+    h["ref"] = (lp + 0.1).astype(np.float32)
+    if abs(base) > 1e8:      # the second row's action has no chance
+        h["actions"][1] = 7
+        h["old"][1], h["ref"][1] = h["old"][0], h["ref"][0]
+    check(gpu, logits, h, "f32", ent=0.01)
+
+
 @pytest.mark.parametrize("V", [40, 700, 9000, 70000])
 def test_rows_left_out(gpu, V):
     """Padding rows are not looked at; bad rows are reported, get NaN and a
