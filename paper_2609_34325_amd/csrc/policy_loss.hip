@@ -343,9 +343,12 @@ __device__ __forceinline__ RowSlope close_row(const RowParams& p, int64_t t, Row
 constexpr int group_threads(int L) { return L >= 256 ? L : (L == 64 ? 512 : 256); }
 
 // L threads a row.  Each holds its first NV pieces (thread i: pieces i, i + L,
-// ...) in registers from the statistics to the gradient, so that a row of up
-// to L NV pieces is read once; what is past them is read again.
-template <bool BF16, int L, int NV, bool GRAD, bool ENT>
+// ...) in registers from the statistics to the gradient and the next NS in
+// shared memory, so that a row of up to L (NV + NS) pieces is read once; what
+// is past them is read again.  Shared memory only extends the longest rows
+// (2048 x 131072 fp32 505 -> 456 us); taking registers off shorter ones for a
+// third workgroup a compute unit made them slower (2048 x 50257 bf16 83 -> 89).
+template <bool BF16, int L, int NV, int NS, bool GRAD, bool ENT>
 __global__ __launch_bounds__(group_threads(L), 4) void policy_rows_kernel(RowParams p) {
   using X = Elem<BF16>;
   constexpr int kRows = group_threads(L) / L, kWaves = L / 64;
@@ -360,6 +363,7 @@ __global__ __launch_bounds__(group_threads(L), 4) void policy_rows_kernel(RowPar
   __shared__ RowIn s_in[kRows];
   __shared__ RowSlope s_slope[kRows];
   __shared__ u32x4 s_held[kPark ? NV * 64 : 1];
+  __shared__ u32x4 s_stash[NS > 0 ? NS * L : 1];
   const int lane = threadIdx.x % L, group = threadIdx.x / L;
   const int64_t t0 = static_cast<int64_t>(blockIdx.x) * kRows, t = min(t0 + group, static_cast<int64_t>(p.T) - 1);
   const bool mine = t0 + group < p.T;  // a group past the last row goes along with it, and writes nothing
@@ -396,7 +400,29 @@ __global__ __launch_bounds__(group_threads(L), 4) void policy_rows_kernel(RowPar
       tk.take(x);
     }
   }
-  for (int i = lane + NV * L; i < cut.open; i += L) {
+  if constexpr (NS > 0) {
+    constexpr int kFlight = 2;
+#pragma unroll
+    for (int b = 0; b < NS; b += kFlight) {
+      u32x4 v[kFlight];
+      if (NV * L + b * L < cut.open) {
+#pragma unroll
+        for (int k = 0; k < kFlight; ++k)
+          v[k] = load_piece<BF16, kPassLoads>(row + cut.byte(min(lane + (NV + b + k) * L, cut.open - 1)));
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int k = 0; k < kFlight; ++k) {
+          if (b + k < NS && lane + (NV + b + k) * L < cut.open) {
+            s_stash[(b + k) * L + lane] = v[k];
+            float x[X::kPer];
+            X::unpack(v[k], x);
+            tk.take(x);
+          }
+        }
+      }
+    }
+  }
+  for (int i = lane + (NV + NS) * L; i < cut.open; i += L) {
     float x[X::kPer];
     X::unpack(load_piece<BF16>(row + cut.byte(i)), x);
     tk.take(x);
@@ -462,7 +488,11 @@ __global__ __launch_bounds__(group_threads(L), 4) void policy_rows_kernel(RowPar
 #pragma unroll
     for (int i = 0; i < NV; ++i) asm volatile("" : "+v"(held[i]));
     auto put = [&](u32x4 v, int i) { store_piece<BF16, kPassStores>(out + cut.byte(i), slope.piece(v, i)); };
-    for (int i = lane + NV * L; i < cut.open; i += L) put(load_piece<BF16>(row + cut.byte(i)), i);
+    for (int i = lane + (NV + NS) * L; i < cut.open; i += L) put(load_piece<BF16>(row + cut.byte(i)), i);
+    if constexpr (NS > 0)
+#pragma unroll
+      for (int k = 0; k < NS; ++k)
+        if (lane + (NV + k) * L < cut.open) put(s_stash[k * L + lane], lane + (NV + k) * L);
 #pragma unroll
     for (int i = 0; i < NV; ++i)
       if (lane + i * L < cut.open) put(held[i], lane + i * L);
@@ -643,11 +673,11 @@ __global__ __launch_bounds__(kFinishThreads) void policy_finish_kernel(const dou
   }
 }
 
-template <bool BF16, bool GRAD, bool ENT, int L, int NV>
+template <bool BF16, bool GRAD, bool ENT, int L, int NV, int NS = 0>
 void launch_shape(const RowParams& p, hipStream_t st) {
   constexpr int kRows = group_threads(L) / L;
   const int groups = (p.T + kRows - 1) / kRows;
-  hipLaunchKernelGGL((policy_rows_kernel<BF16, L, NV, GRAD, ENT>), dim3(groups), dim3(group_threads(L)), 0, st, p);
+  hipLaunchKernelGGL((policy_rows_kernel<BF16, L, NV, NS, GRAD, ENT>), dim3(groups), dim3(group_threads(L)), 0, st, p);
   if (GRAD && groups > 1) launch_policy_finish(p.parts, groups, p.stats, st);
 }
 
@@ -703,7 +733,8 @@ void launch_rows(RowParams p, hipStream_t st) {
       if (each <= 10) launch_shape<BF16, GRAD, ENT, 1024, 10>(p, st);
       else if (each <= 12) launch_shape<BF16, GRAD, ENT, 1024, 12>(p, st);
       else if (each <= 14) launch_shape<BF16, GRAD, ENT, 1024, 14>(p, st);
-      else launch_shape<BF16, GRAD, ENT, 1024, 16>(p, st);
+      else if (each <= 16) launch_shape<BF16, GRAD, ENT, 1024, 16>(p, st);
+      else launch_shape<BF16, GRAD, ENT, 1024, 16, 8>(p, st);
     }
   }
 }
