@@ -552,7 +552,9 @@ int dora_action_logprob(const void* logits, int64_t ld, const int32_t* actions, 
  *   dev_status  DORA_DEV_ACTION as for dora_action_logprob: log-probability
  *               NaN, gradient 0, no share in the sums.
  * Results do not depend on timing: the rows' terms are added in 64 bits in a
- * fixed order.
+ * fixed order.  A row's fp32 sums are grouped by the 16-byte boundaries that
+ * its gradient lies across and by the batch's size class, so its last bits can
+ * differ between places of another alignment and between small and large T.
  *
  * Returns DORA_OK or a negative dora_status (DORA_ERR_OVERLAP when dlogits
  * overlaps the logits otherwise than above); enqueues two kernels.

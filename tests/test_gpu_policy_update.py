@@ -146,3 +146,25 @@ def test_captured_and_replayed(gpu):
             assert int(b["flag"].item()) == 0
             for k in OUT:
                 assert torch.equal(b[k], eager[k]), (rep, k)
+
+
+def test_without_the_native_marshalling(gpu, monkeypatch):
+    """Through ctypes and the checks in Python, to the last bit the same."""
+    p = setup(gpu)
+    want, got = buffers(gpu), buffers(gpu)
+    update(gpu, p, want)
+    for name in ("_native_call", "_native_rows", "_native_spans", "_native_vectors"):
+        monkeypatch.setattr(gpu, name, gpu._leave_to_ctypes)
+    update(gpu, p, got)
+    lp, H, st = gpu.dora_action_logprob(p["keys"][:, 0] @ p["wb"], p["actions"], legal=p["legal"])
+    torch.cuda.synchronize()
+    assert int(got["flag"].item()) == 0 and int(st.item()) == 0
+    for k in OUT:
+        assert torch.equal(got[k], want[k]), k
+    assert torch.equal(lp[p["weight"] != 0], want["lp_b"][p["weight"] != 0])
+    with pytest.raises(ValueError, match="adjacent"):
+        gpu.dora_action_logprob(p["keys"][:, 0].t(), p["actions"])
+    with pytest.raises(ValueError, match=r"actions must be \[48\]"):
+        gpu.dora_action_logprob(p["keys"][:, 0], p["actions"][:3])
+    with pytest.raises(ValueError, match="tensors on devices"):
+        gpu.dora_grad_clip([got["gb"]], 1.0, norm_out=torch.zeros(1))

@@ -233,6 +233,27 @@ def test_binding_refusals():
         dora.dora_grad_clip([3], 1.0)
 
 
+def test_native_helpers_leave_the_rest_to_python():
+    """What the native checks do not take goes to those in Python."""
+    dora.load_library()
+    t = torch.zeros(4, 8)
+    room = (dora.Span * 2)()
+    for got in (dora._native_rows(t), dora._native_rows(3), dora._native_vectors(-1, 4, t[0]),
+                dora._native_vectors(0, 8, t[0]), dora._native_vectors(0, 8), dora._native_vectors("x", 8, t[0]),
+                dora._native_vectors(0, "x", t[0]), dora._native_spans([t], ctypes.addressof(room)),
+                dora._native_spans((t,), ctypes.addressof(room)), dora._native_spans([3], ctypes.addressof(room))):
+        assert got is NotImplemented
+    assert dora._native_vectors(0, 8, None, -1, None) is True
+    with pytest.raises(ValueError):
+        dora._native_spans([t], 0)
+    with pytest.raises(TypeError, match="b must be a torch tensor"):
+        dora._vectors(("a", "b"), -1, 8, None, 3, 5)
+    with pytest.raises(ValueError, match=r"a must be \[3\]"):
+        dora._vectors(("a",), -1, 3, t[0])
+    with pytest.raises(ValueError, match="tensors on devices 0 and -1"):
+        dora._vectors(("a",), 0, -1, t)
+
+
 @pytest.mark.parametrize("source", build.POLICY_SOURCES)
 def test_no_scratch(source):
     """No register of these kernels lives in scratch memory."""
