@@ -7,13 +7,11 @@
 // HBM bound: one read for the norm, one read and one write to scale.  The
 // tensors' addresses go in by kernel argument, as many as 4 KB hold; tensors
 // are cut into chunks, and a workgroup takes every gridDim-th chunk, four
-// 16-byte pieces in flight a thread.  The norm's pass takes the list from its
-// end, so that the scaling begins with what the caches still hold.  Squares
-// are added in 64 bits: no fp32 gradient overflows them, and the sum does not
-// hang on the split.  Workgroups write their sums to the workspace; every
-// workgroup of a scaling launch adds them all in the same order.  304M fp32
-// elements in 292 tensors, out of place: norm 237 us (5.1 TB/s), scaling 493
-// (4.9 TB/s); 22M bf16 in 150: 11 and 15.
+// 16-byte pieces in flight a thread.  Squares are added in 64 bits: no fp32
+// gradient overflows them, and the sum does not hang on the split.  Workgroups
+// write their sums to the workspace; every workgroup of a scaling launch adds
+// them all in the same order.  304M fp32 elements in 292 tensors, out of place:
+// norm 237 us (5.1 TB/s), scaling 493 (4.9 TB/s); 22M bf16 in 150: 11 and 15.
 #include <algorithm>
 #include <cstdlib>
 
@@ -29,6 +27,11 @@ constexpr int kFlight = 4;                       // pieces in flight a thread
 constexpr int kMinChunk = 2048, kMaxChunk = 32768, kManyChunks = 2048;
 constexpr int kMaxGroups = 2048;                 // workgroups of a pass, the share of each launch rounded up
 constexpr int kMaxSpans = 1 << 16;
+// Up to these bytes both passes give a chunk to the same workgroup, whose die
+// may still hold it; past them the norm's pass takes the list from its end, so
+// that the scaling begins with what the caches still hold.  us a pass the same
+// way and from the end: 21 MB 14.6, 15.5, 44 MB 27.1, 27.7, 1.2 GB 750.9, 747.8.
+constexpr int64_t kWhole = int64_t{64} << 20;
 constexpr int64_t kPart = int64_t{1} << 30;      // longer tensors go in as several
 constexpr int64_t kMaxTotal = int64_t{1} << 40;  // elements of a call
 constexpr uint32_t kBF16 = 1u << 31;
@@ -159,10 +162,11 @@ __device__ __forceinline__ double chunk_squares(const char* p, int n) {
   return s;
 }
 
+template <bool BACK>
 __global__ __launch_bounds__(kThreads) void grad_squares_kernel(InBlock b, double* parts) {
   double s = 0.0;
   for (int c = blockIdx.x; c < b.chunks; c += gridDim.x) {
-    const Chunk k = find_chunk<true>(b, c);
+    const Chunk k = find_chunk<BACK>(b, c);
     const char* p = b.in[k.span] + k.lo * (k.bf16 ? 2 : 4);
     const int n = static_cast<int>(k.hi - k.lo);
     s += k.bf16 ? chunk_squares<true>(p, n) : chunk_squares<false>(p, n);
@@ -360,8 +364,12 @@ extern "C" int dora_grad_clip(const dora_span* grads, const dora_span* out, int3
   }
   double* parts = static_cast<double*>(workspace);
   hipStream_t st = static_cast<hipStream_t>(stream);
-  int64_t total = 0, all = 0;
-  for (int32_t i = 0; i < n; ++i) total += grads[i].numel;
+  int64_t total = 0, bytes = 0, all = 0;
+  for (int32_t i = 0; i < n; ++i) {
+    total += grads[i].numel;
+    bytes += span_bytes(grads[i]);
+  }
+  const bool back = bytes > kWhole;
   if (total > kMaxTotal) return DORA_ERR_SHAPE;
   const int chunk = static_cast<int>(std::min<int64_t>(
       kMaxChunk, std::max<int64_t>(1, (total + kManyChunks * kMinChunk - 1) / (kManyChunks * kMinChunk)) * kMinChunk));
@@ -369,10 +377,12 @@ extern "C" int dora_grad_clip(const dora_span* grads, const dora_span* out, int3
   int32_t used = 0;
   InBlock b;
   for (Place at{0, 0}; at.spans < n;) {
-    fill_block<true>(grads, nullptr, n, at, chunk, &b);
+    if (back) fill_block<true>(grads, nullptr, n, at, chunk, &b);
+    else fill_block<false>(grads, nullptr, n, at, chunk, &b);
     if (b.n == 0) continue;
     const int groups = launch_groups(b.chunks, all);
-    hipLaunchKernelGGL(grad_squares_kernel, dim3(groups), dim3(kThreads), 0, st, b, parts + used);
+    if (back) hipLaunchKernelGGL(grad_squares_kernel<true>, dim3(groups), dim3(kThreads), 0, st, b, parts + used);
+    else hipLaunchKernelGGL(grad_squares_kernel<false>, dim3(groups), dim3(kThreads), 0, st, b, parts + used);
     used += groups;
   }
   if (!scale || used == 0) {
