@@ -557,7 +557,8 @@ int dora_action_logprob(const void* logits, int64_t ld, const int32_t* actions, 
  * differ between places of another alignment and between small and large T.
  *
  * Returns DORA_OK or a negative dora_status (DORA_ERR_OVERLAP when dlogits
- * overlaps the logits otherwise than above); enqueues two kernels.
+ * overlaps the logits otherwise than above); enqueues one kernel, two past one
+ * workgroup's rows, three past 8192 workgroups.
  */
 int dora_policy_loss(const void* logits, int64_t ld, const int32_t* actions, const int32_t* legal,
                      const float* old_logprob, const float* ref_logprob, const float* advantage, const float* weight,
@@ -593,7 +594,8 @@ int dora_policy_loss(const void* logits, int64_t ld, const int32_t* actions, con
  *               NaN, gradient 0 (not written for an invalid segment) and no
  *               share in the sums.
  *
- * Returns DORA_OK or a negative dora_status; enqueues two kernels.
+ * Returns DORA_OK or a negative dora_status; enqueues one kernel for one image,
+ * two for more.
  */
 size_t dora_pl_policy_workspace_size(int32_t B);  /* 0 when B is out of range */
 int dora_pl_policy_loss(const float* scores, const int32_t* order, const int32_t* cu_order, const int32_t* cu_in,
