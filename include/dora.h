@@ -577,7 +577,7 @@ int dora_policy_loss(const void* logits, int64_t ld, const int32_t* actions, con
  *   dscores_j = d loss / d logp ([j drawn] - exp(s_j) sum_{t <= tau_j} 1 / S_t)
  * tau_j the draw that takes j (the last one for a token never drawn), and 0
  * for CLS and where nothing is drawn.  Scores however far apart keep their
- * share of the gradient.
+ * share of the gradient; a score of -inf is a token of probability 0.
  *
  *   scores, order, cu_order, cu_in, total_in, B, N  as for dora_pl_logprob.
  *   old_logprob, ref_logprob, advantage, weight, clip_low, clip_high, kl_coef

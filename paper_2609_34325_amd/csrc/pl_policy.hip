@@ -14,12 +14,14 @@
 // exp of its difference to the old one.  Terms are relative to the image's
 // largest score while all are within 2^900 of it, else pairs v 2^e, joined at
 // the larger e by shifting exponents: a score however far below, drawn late,
-// neither vanishes nor divides zero by zero.
+// neither vanishes nor divides zero by zero.  A score of -inf is a token that
+// counts for nothing in either form.
 //
 // One workgroup per image; launch, memory and barrier latency bound (an image
-// is a few KB): 256 x 577 tokens 7.1 us, 48 x 2048 10.5, 8192 x 257 30 a pass.  Shared memory is sized by N, so that several images share a
-// compute unit.  Loss terms per image go to the workspace and are added by a
-// second launch in a fixed order.
+// is a few KB): 256 x 577 tokens 7.1 us, 48 x 2048 10.5, 8192 x 257 30 a pass.
+// Shared memory is sized by N, so that several images share a compute unit.
+// Loss terms per image go to the workspace and are added by a second launch in
+// a fixed order.
 #include "dora_internal.h"
 #include "policy_terms.h"
 
@@ -63,6 +65,7 @@ struct Scaled {
   double v, e;
   __device__ static Scaled zero() { return {0.0, -1e300}; }
   __device__ static Scaled exp_of(float x, double) {
+    if (x == -__builtin_inff()) return zero();
     const double y = x * kLog2E, e = floor(y);
     return {exp2(y - e), e};
   }
@@ -261,7 +264,7 @@ __global__ __launch_bounds__(kThreads) void pl_policy_kernel(PLPolicyParams p) {
       s.draw[t] = static_cast<int16_t>(min(max(pos, 0), nv - 1));
       bad = bad || pos < 0 || pos >= nv;
       top = fmaxf(top, x);
-      low = fminf(low, x);
+      low = fminf(low, x == -__builtin_inff() ? low : x);  // exp of it is 0 in either form
     }
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) {

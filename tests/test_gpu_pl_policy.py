@@ -121,6 +121,50 @@ def test_scores_far_apart(gpu, spread):
         check(gpu, h)
 
 
+@pytest.mark.parametrize("spread", [2.0, 3000.0])
+@pytest.mark.parametrize("n,masked", [(2, 1), (40, 7), (200, 400), (700, 1300)])
+def test_masked_scores(gpu, n, masked, spread):
+    """Scores of -inf that no draw takes are as if the tokens were not there."""
+    want = make([n] * 3, ks=[n - 1, n // 2, 0], seed=8, spread=spread, ref=False)
+    g, lp, _, _ = P.pl(want["s"].astype(np.float64), want["order"], want["cuo"], want["old"].astype(np.float64),
+                       want["A"].astype(np.float64), segments=want["segs"], low=float(np.float32(want["low"])),
+                       high=float(np.float32(want["high"])))
+    N = n + masked
+    h = dict(want, s=np.full(3 * N, -np.inf, np.float32), order=want["order"].copy(), N=N,
+             segs=[(b * N, N) for b in range(3)])
+    rng = np.random.default_rng(n)
+    at = [1 + np.sort(rng.permutation(N - 1)[:n - 1]) for _ in range(3)]    # where each image's open tokens stand
+    for b in range(3):
+        h["s"][b * N + at[b]] = want["s"][b * n + 1:(b + 1) * n]
+        sl = slice(want["cuo"][b], want["cuo"][b + 1])
+        h["order"][sl] = at[b][want["order"][sl] - 1]
+    ds, got, _, flag = run(gpu, h)
+    assert int(flag.item()) == 0
+    size = np.abs(want["s"]).max() * (n + 1)
+    assert np.all(np.abs(got.cpu().numpy() - lp) <= P.U32 * np.abs(lp) + 1e-12 * size)
+    ds = ds.cpu().numpy().astype(np.float64)
+    for b in range(3):
+        pull = abs(float(want["A"][b])) * np.exp(lp[b] - float(want["old"][b]))
+        w = g[b * n + 1:(b + 1) * n]
+        assert np.all(np.abs(ds[b, at[b]] - w) <= P.U32 * np.abs(w) + 1e-11 * (1 + size) * pull + 1e-38)
+        ds[b, at[b]] = 0.0
+    assert not ds.any()
+
+
+def test_masked_score_drawn(gpu):
+    """A draw of probability 0: log-probability -inf, ratio 0, gradient 0."""
+    h = make([30] * 3, ks=[6, 6, 6], seed=9, ref=False)
+    h["s"][h["order"][2]] = -np.inf                       # the first image's third draw
+    h["A"][:] = [1.0, -1.0, 0.5]
+    want = make([30] * 3, ks=[6, 6, 6], seed=9, ref=False)
+    want["A"][:] = h["A"]
+    clean = run(gpu, want)
+    ds, lp, st, flag = run(gpu, h)
+    assert int(flag.item()) == 0 and float(lp[0]) == -np.inf and not bool(ds[0].any())
+    assert torch.equal(ds[1:], clean[0][1:]) and torch.equal(lp[1:], clean[1][1:]) and bool(st.isfinite().all())
+    assert float(gpu.dora_pl_logprob(to_dev(h["s"]).view(3, 30), to_dev(h["order"]), to_dev(h["cuo"]))[0][0]) == -np.inf
+
+
 def test_agrees_with_logprob(gpu):
     h = make([197] * 32, seed=6)
     lp, st = gpu.dora_pl_logprob(to_dev(h["s"]).view(32, 197), to_dev(h["order"]), to_dev(h["cuo"]))
