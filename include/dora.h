@@ -77,7 +77,7 @@ typedef enum {
 #define DORA_MAX_ROW_TOKENS 2048     /* dora_select_pack: N (tokens per image, CLS included)  */
 #define DORA_MAX_SEQLEN 16384        /* dora_varlen_attn: max_seqlen                          */
 #define DORA_HEAD_DIM 64             /* dora_varlen_attn: D                                   */
-#define DORA_MAX_DECISIONS 16777216  /* dora_action_logprob, dora_policy_loss: T (rows)       */
+#define DORA_MAX_DECISIONS 16777215  /* dora_action_logprob, dora_policy_loss: T (rows)       */
 #define DORA_MAX_ACTIONS 1048576     /* dora_action_logprob, dora_policy_loss: V (choices)    */
 
 /*

@@ -52,7 +52,7 @@ DORA_DEV_ACTION = 0x40
 DORA_MAX_ROW_TOKENS = 2048
 DORA_MAX_SEQLEN = 16384
 DORA_HEAD_DIM = 64
-DORA_MAX_DECISIONS = 1 << 24
+DORA_MAX_DECISIONS = (1 << 24) - 1
 DORA_MAX_ACTIONS = 1 << 20
 DORA_NOALLOC_WORKSPACE_BYTES = 4 << 20
 

@@ -32,6 +32,9 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kMaxSplit = 64;  // workgroups a row
+// A launch has fewer than 2^32 threads; rows of more than kThreads are long, and
+// as many as this of them take more memory than there is.
+static_assert(int64_t{DORA_MAX_DECISIONS} * kThreads < int64_t{1} << 32, "threads of a launch");
 constexpr float kLog2E = 1.4426950408889634f;
 constexpr double kLn2 = 0.6931471805599453;
 constexpr float kFarDown = -30000.0f;  // exp2 of it is 0, and 0 times it is 0

@@ -150,6 +150,7 @@ def test_policy_sizes():
     assert dora.dora_policy_workspace_size(5, dora.DORA_MAX_ACTIONS + 1) == 0
     assert dora.dora_policy_workspace_size(dora.DORA_MAX_DECISIONS, dora.DORA_MAX_ACTIONS) > 0
     assert dora.dora_policy_workspace_size(5, 5) % 256 == 0
+    assert dora.DORA_MAX_DECISIONS * 256 < 1 << 32        # threads of a launch, for rows of 256 threads
     assert dora.dora_pl_policy_workspace_size(0) == 0 and dora.dora_pl_policy_workspace_size(8193) == 0
     assert dora.dora_grad_clip_workspace_size(0) == 0 and dora.dora_grad_clip_workspace_size(65537) == 0
     header = open(os.path.join(build.INCLUDE, "dora.h")).read()
