@@ -655,6 +655,8 @@ def _rows(t: torch.Tensor, name: str):
         return got
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch tensor")
+    if t.layout != torch.strided or t.is_nested:
+        raise ValueError(f"{name} must be a strided tensor, not a sparse or nested one")
     if t.dim() != 2:
         raise ValueError(f"{name} must be [T, V]")
     if not t.is_cuda:

@@ -240,19 +240,19 @@ PyObject* spans(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
 PyObject* rows(PyObject*, PyObject* o) {
   if (!THPVariable_CheckExact(o) || at::impl::torch_function_mode_enabled()) Py_RETURN_NOTIMPLEMENTED;
   const at::Tensor& t = THPVariable_Unpack(o);
-  const at::ScalarType type = t.scalar_type();
-  if (!t.is_cuda() || t.dim() != 2 || (type != at::kFloat && type != at::kBFloat16)) Py_RETURN_NOTIMPLEMENTED;
-  const int64_t n = t.size(0), v = t.size(1), ld = n > 1 ? t.stride(0) : v;
-  if (ld < v || (v > 1 && t.stride(1) != 1)) Py_RETURN_NOTIMPLEMENTED;
-  void* address = nullptr;
-  try {
-    address = t.data_ptr();
+  try {  // sizes, strides and addresses throw for layouts that have none
+    const at::ScalarType type = t.scalar_type();
+    if (t.layout() != at::kStrided || t.is_nested() || !t.is_cuda() || t.dim() != 2 ||
+        (type != at::kFloat && type != at::kBFloat16))
+      Py_RETURN_NOTIMPLEMENTED;
+    const int64_t n = t.size(0), v = t.size(1), ld = n > 1 ? t.stride(0) : v;
+    if (ld < v || (v > 1 && t.stride(1) != 1)) Py_RETURN_NOTIMPLEMENTED;
+    return Py_BuildValue("NLLLil", PyLong_FromVoidPtr(t.data_ptr()), static_cast<long long>(ld),
+                         static_cast<long long>(n), static_cast<long long>(v),
+                         type == at::kFloat ? DORA_F32 : DORA_BF16, static_cast<long>(t.get_device()));
   } catch (...) {
     Py_RETURN_NOTIMPLEMENTED;
   }
-  return Py_BuildValue("NLLLil", PyLong_FromVoidPtr(address), static_cast<long long>(ld), static_cast<long long>(n),
-                       static_cast<long long>(v), type == at::kFloat ? DORA_F32 : DORA_BF16,
-                       static_cast<long>(t.get_device()));
 }
 
 // vectors(device, n, t, n, t, ...): True where every t is None or a vector of
@@ -263,17 +263,21 @@ PyObject* vectors(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     if (PyErr_Occurred()) PyErr_Clear();
     Py_RETURN_NOTIMPLEMENTED;
   }
-  for (Py_ssize_t i = 1; i + 1 < nargs; i += 2) {
-    if (args[i + 1] == Py_None) continue;
-    const long n = PyLong_AsLong(args[i]);
-    if (n == -1 && PyErr_Occurred()) {
-      PyErr_Clear();
-      Py_RETURN_NOTIMPLEMENTED;
+  try {
+    for (Py_ssize_t i = 1; i + 1 < nargs; i += 2) {
+      if (args[i + 1] == Py_None) continue;
+      const long n = PyLong_AsLong(args[i]);
+      if (n == -1 && PyErr_Occurred()) {
+        PyErr_Clear();
+        Py_RETURN_NOTIMPLEMENTED;
+      }
+      if (!THPVariable_CheckExact(args[i + 1])) Py_RETURN_NOTIMPLEMENTED;
+      const at::Tensor& t = THPVariable_Unpack(args[i + 1]);
+      if (!t.is_cuda() || t.get_device() != device || (n >= 0 && (t.dim() != 1 || t.size(0) != n)))
+        Py_RETURN_NOTIMPLEMENTED;
     }
-    if (!THPVariable_CheckExact(args[i + 1])) Py_RETURN_NOTIMPLEMENTED;
-    const at::Tensor& t = THPVariable_Unpack(args[i + 1]);
-    if (!t.is_cuda() || t.get_device() != device || (n >= 0 && (t.dim() != 1 || t.size(0) != n)))
-      Py_RETURN_NOTIMPLEMENTED;
+  } catch (...) {
+    Py_RETURN_NOTIMPLEMENTED;
   }
   Py_RETURN_TRUE;
 }
