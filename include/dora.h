@@ -502,7 +502,10 @@ int dora_varlen_attn_noalloc(const void* q, const void* k, const void* v, const 
  *   weight      NULL or fp32 [T]: a row of weight 0 is padding.  Nothing else
  *               of it is looked at; its log-probability and entropy are 0.
  *   T           1 .. DORA_MAX_DECISIONS; V 1 .. DORA_MAX_ACTIONS.
- *   logprob_out fp32 [T]; entropy_out NULL or fp32 [T].
+ *   logprob_out fp32 [T]; entropy_out NULL or fp32 [T].  Either may take the
+ *               place of `weight` (same address); otherwise outputs, the
+ *               workspace and dev_status share no memory with each other or
+ *               with an input (DORA_ERR_OVERLAP).  They may lie between rows.
  *   workspace   NULL, or device memory of dora_policy_workspace_size(T, V)
  *               bytes, 256-byte aligned, no required contents: few long rows
  *               are then split over several workgroups.  Calls that share a
@@ -545,7 +548,10 @@ int dora_action_logprob(const void* logits, int64_t ld, const int32_t* actions, 
  *   dlogits     dtype, T rows of V elements ld_grad elements apart; may be
  *               the logits themselves (same address and ld).  Elements between
  *               rows are left as they were.
- *   logprob_out fp32 [T].
+ *   logprob_out fp32 [T].  It may take the place of old_logprob, ref_logprob,
+ *               advantage or weight (same address; few long rows are then not
+ *               split).  Otherwise outputs, the workspace and dev_status share
+ *               no memory with each other or with an input.
  *   stats_out   fp32 [6]: the sums over rows of loss, w gain, w kl, w H,
  *               w [the clip binds], w.
  *   workspace   as for dora_action_logprob, but not NULL.
@@ -556,8 +562,8 @@ int dora_action_logprob(const void* logits, int64_t ld, const int32_t* actions, 
  * its gradient lies across and by the batch's size class, so its last bits can
  * differ between places of another alignment and between small and large T.
  *
- * Returns DORA_OK or a negative dora_status (DORA_ERR_OVERLAP when dlogits
- * overlaps the logits otherwise than above); enqueues one kernel, two past one
+ * Returns DORA_OK or a negative dora_status (DORA_ERR_OVERLAP for tensors
+ * that share memory otherwise than above); enqueues one kernel, two past one
  * workgroup's rows, three past 8192 workgroups.
  */
 int dora_policy_loss(const void* logits, int64_t ld, const int32_t* actions, const int32_t* legal,

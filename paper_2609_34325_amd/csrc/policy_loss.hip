@@ -786,6 +786,20 @@ bool rows_clash(uintptr_t base, int64_t ld, uintptr_t other, int64_t ld_o, int32
   return off < row || off + row > static_cast<uintptr_t>(ld) * elt;
 }
 
+// Rows of V elements every ld at base against vectors, which may stand in the
+// gaps between the rows.
+bool rows_meet(const void* base, int64_t ld, int32_t T, int32_t V, int elt, std::initializer_list<Extent> vectors) {
+  const uintptr_t lo = reinterpret_cast<uintptr_t>(base), pitch = static_cast<uintptr_t>(ld) * elt;
+  const uintptr_t row = static_cast<uintptr_t>(V) * elt, end = lo + (T - 1) * pitch + row;
+  for (const Extent& v : vectors) {
+    if (!v.at || v.at >= end || v.at + v.bytes <= lo) continue;
+    // The last row that starts at or before the vector does, and the one after it.
+    const uintptr_t start = v.at > lo ? lo + (v.at - lo) / pitch * pitch : lo;
+    if (v.at < start + row || v.at + v.bytes > start + pitch) return true;
+  }
+  return false;
+}
+
 }  // namespace
 
 void launch_policy_finish(double* parts, int32_t n, float* stats, hipStream_t stream) {
@@ -821,6 +835,12 @@ extern "C" int dora_action_logprob(const void* logits, int64_t ld, const int32_t
   if (workspace &&
       (reinterpret_cast<uintptr_t>(workspace) & 255u || workspace_bytes < dora_policy_workspace_size(T, V)))
     return DORA_ERR_WORKSPACE;
+  const size_t vec = static_cast<size_t>(T) * 4;
+  const Extent lp_out(logprob_out, vec), ent_out(entropy_out, vec), ws(workspace, dora_policy_workspace_size(T, V)),
+      flag(dev_status, 4);
+  if (outputs_clash({lp_out, ent_out, ws, flag}, {Extent(actions, vec), Extent(legal, vec)}, {Extent(weight, vec)}) ||
+      rows_meet(logits, ld, T, V, dtype == DORA_BF16 ? 2 : 4, {lp_out, ent_out, ws, flag}))
+    return DORA_ERR_OVERLAP;
   RowParams p{};
   p.logits = static_cast<const char*>(logits);
   p.ld = ld;
@@ -861,10 +881,21 @@ extern "C" int dora_policy_loss(const void* logits, int64_t ld, const int32_t* a
   if (!workspace || reinterpret_cast<uintptr_t>(workspace) & 255u ||
       workspace_bytes < dora_policy_workspace_size(T, V))
     return DORA_ERR_WORKSPACE;
+  const size_t vec = static_cast<size_t>(T) * 4;
+  const Extent lp_out(logprob_out, vec), sums(stats_out, kPolicyTerms * 4), ws(workspace, dora_policy_workspace_size(T, V)),
+      flag(dev_status, 4), act(actions, vec), open(legal, vec), old(old_logprob, vec), ref(ref_logprob, vec),
+      adv(advantage, vec), w(weight, vec);
+  if (outputs_clash({sums, ws, flag}, {act, open, old, ref, adv, w, lp_out}, {}) ||
+      outputs_clash({lp_out}, {act, open}, {old, ref, adv, w}) ||
+      rows_meet(logits, ld, T, V, elt, {lp_out, sums, ws, flag}) ||
+      rows_meet(dlogits, ld_grad, T, V, elt, {lp_out, sums, ws, flag, act, open, old, ref, adv, w}))
+    return DORA_ERR_OVERLAP;
+  // Split rows are closed by several workgroups, of which one writes the log-probability: not in a constant's place.
+  const bool in_place = lp_out.meets(old) || lp_out.meets(ref) || lp_out.meets(adv) || lp_out.meets(w);
   RowParams p{static_cast<const char*>(logits), ld, actions, legal, old_logprob, ref_logprob, advantage, weight, T, V,
               PolicyCoef{clip_low, clip_high, kl_coef, entropy_coef}, static_cast<char*>(dlogits), ld_grad,
-              logprob_out, nullptr, static_cast<double*>(workspace), static_cast<float4*>(workspace), 1, stats_out,
-              dev_status};
+              logprob_out, nullptr, static_cast<double*>(workspace), in_place ? nullptr : static_cast<float4*>(workspace), 1,
+              stats_out, dev_status};
   hipStream_t st = static_cast<hipStream_t>(stream);
   const bool ent = entropy_coef != 0.0f;
   if (dtype == DORA_BF16) ent ? launch_rows<true, true, true>(p, st) : launch_rows<true, true, false>(p, st);

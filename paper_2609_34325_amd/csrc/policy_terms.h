@@ -14,6 +14,8 @@
 
 #include <hip/hip_runtime.h>
 
+#include <initializer_list>
+
 #include "dora.h"
 
 namespace dora {
@@ -60,5 +62,28 @@ inline size_t policy_parts_bytes(int32_t n) {
   return (sets * sizeof(PolicyTerms) + 255) & ~size_t(255);
 }
 void launch_policy_finish(double* parts, int32_t n, float* stats, hipStream_t stream);
+
+// Memory of a call's tensor (address 0: not given).
+struct Extent {
+  uintptr_t at;
+  size_t bytes;
+  Extent(const void* p, size_t n) : at(reinterpret_cast<uintptr_t>(p)), bytes(n) {}
+  bool meets(Extent o) const { return at && o.at && at < o.at + o.bytes && o.at < at + bytes; }
+};
+// Outputs that share memory with another output or with an input.  `own` are
+// inputs whose place an output may take as a whole: a row reads its entry of
+// them before it writes its own.
+inline bool outputs_clash(std::initializer_list<Extent> out, std::initializer_list<Extent> in,
+                          std::initializer_list<Extent> own) {
+  for (const Extent* o = out.begin(); o != out.end(); ++o) {
+    for (const Extent* q = out.begin(); q != o; ++q)
+      if (o->meets(*q)) return true;
+    for (const Extent& i : in)
+      if (o->meets(i)) return true;
+    for (const Extent& i : own)
+      if (o->meets(i) && (o->at != i.at || o->bytes != i.bytes)) return true;
+  }
+  return false;
+}
 
 }  // namespace dora
