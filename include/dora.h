@@ -328,10 +328,18 @@ int dora_pl_sample(const float* scores, const float* gumbel, const int32_t* k, c
  *              1 .. n_b - 1.
  * Other arguments as for dora_pl_sample.  Returns DORA_OK or a negative
  * dora_status; enqueues one kernel.
+ *
+ * dora_pl_logprob_cap: the same where order holds cap entries (0 .. ; NULL for
+ * 0), fewer than cu_order[B] after a dora_pl_sample with too small a capacity:
+ * no entry past them is read, an image whose draws reach there is one whose
+ * offsets break the above.
  */
 int dora_pl_logprob(const float* scores, const int32_t* order, const int32_t* cu_order, const int32_t* cu_in,
                     int64_t total_in, int32_t B, int32_t N, float* logprob_out, int32_t* dev_status,
                     void* stream);
+int dora_pl_logprob_cap(const float* scores, const int32_t* order, const int32_t* cu_order, int64_t cap,
+                        const int32_t* cu_in, int64_t total_in, int32_t B, int32_t N, float* logprob_out,
+                        int32_t* dev_status, void* stream);
 
 /*
  * dora_lc1_readout -- readout input of a DINOv2 linear classifier on the
@@ -602,6 +610,9 @@ int dora_policy_loss(const void* logits, int64_t ld, const int32_t* actions, con
  *
  * Returns DORA_OK or a negative dora_status; enqueues one kernel for one image,
  * two for more.
+ *
+ * dora_pl_policy_loss_cap: the same where order holds cap entries, as for
+ * dora_pl_logprob_cap.
  */
 size_t dora_pl_policy_workspace_size(int32_t B);  /* 0 when B is out of range */
 int dora_pl_policy_loss(const float* scores, const int32_t* order, const int32_t* cu_order, const int32_t* cu_in,
@@ -609,6 +620,11 @@ int dora_pl_policy_loss(const float* scores, const int32_t* order, const int32_t
                         const float* weight, int32_t B, int32_t N, float clip_low, float clip_high, float kl_coef,
                         float* dscores, float* logprob_out, float* stats_out, void* workspace, size_t workspace_bytes,
                         int32_t* dev_status, void* stream);
+int dora_pl_policy_loss_cap(const float* scores, const int32_t* order, const int32_t* cu_order, int64_t cap,
+                            const int32_t* cu_in, int64_t total_in, const float* old_logprob, const float* ref_logprob,
+                            const float* advantage, const float* weight, int32_t B, int32_t N, float clip_low,
+                            float clip_high, float kl_coef, float* dscores, float* logprob_out, float* stats_out,
+                            void* workspace, size_t workspace_bytes, int32_t* dev_status, void* stream);
 
 /* One tensor of a list: numel elements of dtype from data on (aligned to the element). */
 typedef struct {

@@ -64,6 +64,7 @@ EXPORTS = (
     "dora_actor_decode",
     "dora_pl_sample",
     "dora_pl_logprob",
+    "dora_pl_logprob_cap",
     "dora_lc1_readout_workspace_size",
     "dora_lc1_readout",
     "dora_trajectory_flops",
@@ -77,6 +78,7 @@ EXPORTS = (
     "dora_policy_loss",
     "dora_pl_policy_workspace_size",
     "dora_pl_policy_loss",
+    "dora_pl_policy_loss_cap",
     "dora_grad_clip_workspace_size",
     "dora_grad_clip",
     "dora_status_string",
@@ -105,7 +107,7 @@ _ENTRIES = (
                            None, ("on_rank", _I32), ("keep_out", _I32), ("scores_out", _F32)) + _STATUS),
     ("dora_pl_sample", (("scores", _F32), ("gumbel", _F32), ("k", _I32), ("cu_in", _I32), None, None, None,
                         ("order_out", _I32), ("cu_order_out", _I32), ("logprob_out", _F32), None) + _STATUS),
-    ("dora_pl_logprob", (("scores", _F32), ("order", _I32), ("cu_order", _I32), ("cu_in", _I32), None, None, None,
+    ("dora_pl_logprob_cap", (("scores", _F32), ("order", _I32), ("cu_order", _I32), None, ("cu_in", _I32), None, None, None,
                          ("logprob_out", _F32)) + _STATUS),
     ("dora_lc1_readout", (("x", _ANY), ("cu_seqlens", _I32), None, None, None, None, ("gamma", _F32), ("beta", _F32),
                           None, ("out", _F32), ("workspace", _ANY), None) + _STATUS),
@@ -116,7 +118,7 @@ _ENTRIES = (
     ("dora_action_logprob", _LOGITS + (("weight", _F32), None, None, None, ("logprob_out", _F32),
                                        ("entropy_out", _F32), ("workspace", _ANY), None) + _STATUS),
     ("dora_policy_loss", _LOGITS + _DECISIONS + (None,) * 9 + _LOSS_OUT),
-    ("dora_pl_policy_loss", (("scores", _F32), ("order", _I32), ("cu_order", _I32), ("cu_in", _I32), None) +
+    ("dora_pl_policy_loss_cap", (("scores", _F32), ("order", _I32), ("cu_order", _I32), None, ("cu_in", _I32), None) +
      _DECISIONS + (None,) * 5 + (("dscores", _F32),) + _LOSS_OUT),
     ("dora_grad_clip", (None,) * 5 + (("norm_out", _F32), ("workspace", _ANY), None, None)),
 )
@@ -182,6 +184,8 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.dora_pl_sample.argtypes = [vp, vp, vp, vp, i64, i32, i32, vp, vp, vp, i64, vp, vp]
     lib.dora_pl_logprob.restype = ctypes.c_int
     lib.dora_pl_logprob.argtypes = [vp, vp, vp, vp, i64, i32, i32, vp, vp, vp]
+    lib.dora_pl_logprob_cap.restype = ctypes.c_int
+    lib.dora_pl_logprob_cap.argtypes = [vp, vp, vp, i64, vp, i64, i32, i32, vp, vp, vp]
     lib.dora_lc1_readout.restype = ctypes.c_int
     lib.dora_lc1_readout.argtypes = [vp, vp, i64, i32, i32, ctypes.c_int, vp, vp, ctypes.c_float, vp, vp, sz, vp,
                                      vp]
@@ -213,6 +217,9 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.dora_pl_policy_loss.restype = ctypes.c_int
     lib.dora_pl_policy_loss.argtypes = [vp, vp, vp, vp, i64, vp, vp, vp, vp, i32, i32, f32, f32, f32, vp, vp, vp, vp,
                                         sz, vp, vp]
+    lib.dora_pl_policy_loss_cap.restype = ctypes.c_int
+    lib.dora_pl_policy_loss_cap.argtypes = lib.dora_pl_policy_loss.argtypes[:3] + [i64] + \
+        lib.dora_pl_policy_loss.argtypes[3:]
     lib.dora_grad_clip_workspace_size.restype = sz
     lib.dora_grad_clip_workspace_size.argtypes = [i32]
     lib.dora_grad_clip.restype = ctypes.c_int
@@ -451,6 +458,10 @@ def dora_actor_decode(budget_logits: torch.Tensor, on_rank: torch.Tensor, N: int
     return keep_out, scores_out, dev_status
 
 
+def _numel(t) -> int:
+    return t.numel() if isinstance(t, torch.Tensor) else 0  # anything else is refused with the other arguments
+
+
 def _pl_geometry(scores, B, cu_in, N):
     if cu_in is None:
         if scores.dim() != 2 or int(scores.shape[0]) != B:
@@ -493,13 +504,15 @@ def dora_pl_logprob(scores: torch.Tensor, order: torch.Tensor, cu_order: torch.T
                     logprob_out: Optional[torch.Tensor] = None, dev_status: Optional[torch.Tensor] = None,
                     stream=None):
     """Ordered log-probability of given draws (order, cu_order) under scores.
-    Returns (logprob [B], dev_status)."""
+    Images whose draws lie past the end of order are reported
+    (DORA_DEV_KEEP_RANGE).  Returns (logprob [B], dev_status)."""
     B = int(cu_order.shape[0]) - 1
     N, total_in = _pl_geometry(scores, B, cu_in, N)
     dev = scores.device
     logprob_out = torch.empty(B, dtype=torch.float32, device=dev) if logprob_out is None else logprob_out
     dev_status = new_status(dev) if dev_status is None else dev_status
-    _call("dora_pl_logprob", stream, scores, order, cu_order, cu_in, total_in, B, N, logprob_out, dev_status)
+    _call("dora_pl_logprob_cap", stream, scores, order, cu_order, _numel(order), cu_in, total_in, B, N, logprob_out,
+          dev_status)
     return logprob_out, dev_status
 
 
@@ -817,9 +830,9 @@ def dora_pl_policy_loss(scores: torch.Tensor, order: torch.Tensor, cu_order: tor
               "cu_in", "dscores", "workspace", "dev_status"), scores.get_device(), B, old_logprob, B, ref_logprob,
              B, advantage, B, weight, B, logprob_out, 6, stats_out, -1, order, B + 1, cu_order, B + 1, cu_in,
              -1, dscores, -1, workspace, -1, dev_status)
-    _call("dora_pl_policy_loss", None, scores, order, cu_order, cu_in, total_in, old_logprob, ref_logprob, advantage,
-          weight, B, N, float(clip_low), float(clip_high), float(kl_coef), dscores, logprob_out, stats_out, workspace,
-          _bytes(workspace), dev_status)
+    _call("dora_pl_policy_loss_cap", None, scores, order, cu_order, _numel(order), cu_in, total_in, old_logprob,
+          ref_logprob, advantage, weight, B, N, float(clip_low), float(clip_high), float(kl_coef), dscores, logprob_out,
+          stats_out, workspace, _bytes(workspace), dev_status)
     return dscores, logprob_out, stats_out, dev_status
 
 

@@ -82,10 +82,11 @@ const Entry kEntries[] = {
                              i32(a[5]), i32(a[6]), ptr<int32_t>(a[7]), ptr<int32_t>(a[8]), ptr<float>(a[9]), a[10].n,
                              ptr<int32_t>(a[11]), a[12].p);
      }},
-    {"FIIinnnFIs",
+    {"FIIninnnFIs",
      [](void* fn, const Arg* a) {
-       return at_address(dora_pl_logprob, fn)(ptr<float>(a[0]), ptr<int32_t>(a[1]), ptr<int32_t>(a[2]), ptr<int32_t>(a[3]), a[4].n,
-                              i32(a[5]), i32(a[6]), ptr<float>(a[7]), ptr<int32_t>(a[8]), a[9].p);
+       return at_address(dora_pl_logprob_cap, fn)(ptr<float>(a[0]), ptr<int32_t>(a[1]), ptr<int32_t>(a[2]), a[3].n,
+                                  ptr<int32_t>(a[4]), a[5].n, i32(a[6]), i32(a[7]), ptr<float>(a[8]),
+                                  ptr<int32_t>(a[9]), a[10].p);
      }},
     {"AInnnnFFeFanIs",
      [](void* fn, const Arg* a) {
@@ -128,13 +129,13 @@ const Entry kEntries[] = {
                                type_of(a[10]), a[11].f, a[12].f, a[13].f, a[14].f, a[15].p, a[16].n, ptr<float>(a[17]),
                                ptr<float>(a[18]), a[19].p, static_cast<size_t>(a[20].n), ptr<int32_t>(a[21]), a[22].p);
      }},
-    {"FIIinFfFfnneeeFFFAnIs",
+    {"FIIninFfFfnneeeFFFAnIs",
      [](void* fn, const Arg* a) {
-       return at_address(dora_pl_policy_loss, fn)(ptr<float>(a[0]), ptr<int32_t>(a[1]), ptr<int32_t>(a[2]), ptr<int32_t>(a[3]),
-                                  a[4].n, ptr<float>(a[5]), ptr<float>(a[6]), ptr<float>(a[7]), ptr<float>(a[8]),
-                                  i32(a[9]), i32(a[10]), a[11].f, a[12].f, a[13].f, ptr<float>(a[14]),
-                                  ptr<float>(a[15]), ptr<float>(a[16]), a[17].p, static_cast<size_t>(a[18].n),
-                                  ptr<int32_t>(a[19]), a[20].p);
+       return at_address(dora_pl_policy_loss_cap, fn)(ptr<float>(a[0]), ptr<int32_t>(a[1]), ptr<int32_t>(a[2]), a[3].n,
+                                  ptr<int32_t>(a[4]), a[5].n, ptr<float>(a[6]), ptr<float>(a[7]), ptr<float>(a[8]),
+                                  ptr<float>(a[9]), i32(a[10]), i32(a[11]), a[12].f, a[13].f, a[14].f, ptr<float>(a[15]),
+                                  ptr<float>(a[16]), ptr<float>(a[17]), a[18].p, static_cast<size_t>(a[19].n),
+                                  ptr<int32_t>(a[20]), a[21].p);
      }},
     {"ssneeFAns",
      [](void* fn, const Arg* a) {

@@ -34,6 +34,7 @@ struct PLPolicyParams {
   const float* s;
   const int32_t* order;
   const int32_t* cu_order;
+  int64_t cap;  // entries of the order
   const int32_t* cu_in;
   int64_t total_in;
   const float* old;
@@ -244,7 +245,7 @@ __global__ __launch_bounds__(kThreads) void pl_policy_kernel(PLPolicyParams p) {
   const int n = p.cu_in ? hi - lo : p.N;
   const bool seg_ok = !p.cu_in || (lo >= 0 && hi > lo && n <= p.N && hi <= p.total_in && (b > 0 || lo == 0));
   const int nv = seg_ok ? n - 1 : 0;
-  const int k = (o0 >= 0 && o1 >= o0 && o1 <= oend && ofirst == 0) ? o1 - o0 : -1;
+  const int k = (o0 >= 0 && o1 >= o0 && o1 <= oend && o1 <= p.cap && ofirst == 0) ? o1 - o0 : -1;
   bool ok = seg_ok && w != 0.0f && k >= 0 && k <= nv;
 
   char* const at = reinterpret_cast<char*>(s_tokens);
@@ -334,12 +335,24 @@ extern "C" int dora_pl_policy_loss(const float* scores, const int32_t* order, co
                                    int32_t N, float clip_low, float clip_high, float kl_coef, float* dscores,
                                    float* logprob_out, float* stats_out, void* workspace, size_t workspace_bytes,
                                    int32_t* dev_status, void* stream) {
+  return dora_pl_policy_loss_cap(scores, order, cu_order, 0x7FFFFFFF, cu_in, total_in, old_logprob, ref_logprob,
+                                 advantage, weight, B, N, clip_low, clip_high, kl_coef, dscores, logprob_out, stats_out,
+                                 workspace, workspace_bytes, dev_status, stream);
+}
+
+extern "C" int dora_pl_policy_loss_cap(const float* scores, const int32_t* order, const int32_t* cu_order, int64_t cap,
+                                       const int32_t* cu_in, int64_t total_in, const float* old_logprob,
+                                       const float* ref_logprob, const float* advantage, const float* weight, int32_t B,
+                                       int32_t N, float clip_low, float clip_high, float kl_coef, float* dscores,
+                                       float* logprob_out, float* stats_out, void* workspace, size_t workspace_bytes,
+                                       int32_t* dev_status, void* stream) {
   using namespace dora;
-  if (!scores || !order || !cu_order || !old_logprob || !advantage || !dscores || !logprob_out || !stats_out ||
+  if (!scores || (!order && cap != 0) || !cu_order || !old_logprob || !advantage || !dscores || !logprob_out || !stats_out ||
       !dev_status)
     return DORA_ERR_NULL;
   if (B < 1 || B > kPlanMaxB || N < 1 || N > DORA_MAX_ROW_TOKENS) return DORA_ERR_SHAPE;
   if (cu_in && (total_in < 0 || total_in > 0x7FFFFFFF)) return DORA_ERR_SHAPE;
+  if (cap < 0) return DORA_ERR_CAPACITY;
   if (!(clip_low >= 0.0f && clip_low <= 1.0f && clip_high >= 0.0f) || !(kl_coef - kl_coef == 0.0f))
     return DORA_ERR_SHAPE;
   if (kl_coef != 0.0f && !ref_logprob) return DORA_ERR_NULL;
@@ -349,7 +362,7 @@ extern "C" int dora_pl_policy_loss(const float* scores, const int32_t* order, co
   if (!workspace || reinterpret_cast<uintptr_t>(workspace) & 255u ||
       workspace_bytes < dora_pl_policy_workspace_size(B))
     return DORA_ERR_WORKSPACE;
-  PLPolicyParams p{scores, order, cu_order, cu_in, total_in, old_logprob, ref_logprob, advantage, weight, B, N,
+  PLPolicyParams p{scores, order, cu_order, cap, cu_in, total_in, old_logprob, ref_logprob, advantage, weight, B, N,
                    PolicyCoef{clip_low, clip_high, kl_coef, 0.0f}, dscores, logprob_out,
                    static_cast<double*>(workspace), stats_out, dev_status};
   hipStream_t st = static_cast<hipStream_t>(stream);

@@ -37,7 +37,7 @@ struct PLParams {
   int32_t* order_out;
   int32_t* cu_order_out;
   float* logprob;
-  int64_t cap;
+  int64_t cap;  // entries of the order
   int32_t* status;
 };
 
@@ -270,11 +270,11 @@ __global__ __launch_bounds__(kPLThreads) void pl_kernel(PLParams p) {
     }
   } else {
     // The list of image b is [cu_order[b], cu_order[b+1]) inside the caller's
-    // cu_order[B] entries; offsets outside that range are rejected before any
-    // entry is read.
+    // cu_order[B] entries, of which cap are there; offsets outside that range
+    // are rejected before any entry is read.
     const int o0 = p.cu_order_in[b], o1 = p.cu_order_in[b + 1], oend = p.cu_order_in[p.B];
     out0 = o0;
-    kb = (o0 >= 0 && o1 >= o0 && o1 <= oend && p.cu_order_in[0] == 0) ? o1 - o0 : -1;
+    kb = (o0 >= 0 && o1 >= o0 && o1 <= oend && o1 <= p.cap && p.cu_order_in[0] == 0) ? o1 - o0 : -1;
   }
   bool ok = seg_ok && kb >= 0 && kb <= nv;
   if (!seg_ok && tid == 0) atomicOr(p.status, DORA_DEV_CU_IN);
@@ -389,12 +389,19 @@ extern "C" int dora_pl_sample(const float* scores, const float* gumbel, const in
 extern "C" int dora_pl_logprob(const float* scores, const int32_t* order, const int32_t* cu_order,
                                const int32_t* cu_in, int64_t total_in, int32_t B, int32_t N, float* logprob_out,
                                int32_t* dev_status, void* stream) {
+  return dora_pl_logprob_cap(scores, order, cu_order, 0x7FFFFFFF, cu_in, total_in, B, N, logprob_out, dev_status, stream);
+}
+
+extern "C" int dora_pl_logprob_cap(const float* scores, const int32_t* order, const int32_t* cu_order, int64_t cap,
+                                   const int32_t* cu_in, int64_t total_in, int32_t B, int32_t N, float* logprob_out,
+                                   int32_t* dev_status, void* stream) {
   using namespace dora;
   const int rc = check_pl(scores, cu_in, total_in, B, N);
   if (rc != DORA_OK) return rc;
-  if (!order || !cu_order || !logprob_out || !dev_status) return DORA_ERR_NULL;
+  if ((!order && cap != 0) || !cu_order || !logprob_out || !dev_status) return DORA_ERR_NULL;
+  if (cap < 0) return DORA_ERR_CAPACITY;
   PLParams p{scores, nullptr, nullptr, order, cu_order, cu_in, total_in, B, N, nullptr, nullptr,
-             logprob_out, 0, dev_status};
+             logprob_out, cap, dev_status};
   hipLaunchKernelGGL(pl_kernel<false>, dim3(B), dim3(kPLThreads), 0, static_cast<hipStream_t>(stream), p);
   return hipGetLastError() == hipSuccess ? DORA_OK : DORA_ERR_HIP;
 }
