@@ -601,6 +601,10 @@ int dora_policy_loss(const void* logits, int64_t ld, const int32_t* actions, con
  *   dscores     fp32 in the scores' layout, which it may share; rows outside
  *               every segment are left as they were.
  *   logprob_out fp32 [B]; stats_out fp32 [6] as for dora_policy_loss.
+ *               logprob_out may take the place of old_logprob, ref_logprob,
+ *               advantage or weight; otherwise outputs, the workspace and
+ *               dev_status share no memory with each other or with an input
+ *               (DORA_ERR_OVERLAP).
  *   workspace   device, 256-byte aligned, dora_pl_policy_workspace_size(B)
  *               bytes, no required contents; calls that share it must not
  *               overlap in time.

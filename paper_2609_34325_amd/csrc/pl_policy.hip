@@ -362,6 +362,15 @@ extern "C" int dora_pl_policy_loss_cap(const float* scores, const int32_t* order
   if (!workspace || reinterpret_cast<uintptr_t>(workspace) & 255u ||
       workspace_bytes < dora_pl_policy_workspace_size(B))
     return DORA_ERR_WORKSPACE;
+  // A list of no stated length counts as its first entry.
+  const size_t vec = static_cast<size_t>(B) * 4, ends = vec + 4, list = cap < 0x7FFFFFFF ? cap * sizeof(int32_t) : 4;
+  const Extent lp_out(logprob_out, vec), sums(stats_out, kPolicyTerms * 4), ws(workspace, dora_pl_policy_workspace_size(B)),
+      flag(dev_status, 4), grad(dscores, len), s_in(scores, len), draws(order, list), cuo(cu_order, ends), cu(cu_in, ends),
+      old(old_logprob, vec), ref(ref_logprob, vec), adv(advantage, vec), w(weight, vec);
+  if (outputs_clash({sums, ws, flag, grad}, {draws, cuo, cu, old, ref, adv, w, lp_out}, {}) ||
+      outputs_clash({sums, ws, flag}, {s_in}, {}) ||
+      outputs_clash({lp_out}, {s_in, draws, cuo, cu}, {old, ref, adv, w}))
+    return DORA_ERR_OVERLAP;
   PLPolicyParams p{scores, order, cu_order, cap, cu_in, total_in, old_logprob, ref_logprob, advantage, weight, B, N,
                    PolicyCoef{clip_low, clip_high, kl_coef, 0.0f}, dscores, logprob_out,
                    static_cast<double*>(workspace), stats_out, dev_status};

@@ -73,6 +73,38 @@ def test_loss_outputs_apart():
     assert loss(stats=a["x"] - 20) == dora.DORA_ERR_OVERLAP
 
 
+def draws(packed=True, cap=50, entry="dora_pl_policy_loss_cap", **kw):
+    a = Room(("s", "order", "cuo", "cu", "old", "ref", "A", "w", "g", "lp", "stats", "ws", "st")).at
+    a.update(kw)
+    B, N = 7, 40
+    return getattr(dora.load_library(), entry)(
+        a["s"], a["order"], a["cuo"], *([cap] if entry.endswith("cap") else []), a["cu"] if packed else None,
+        200 if packed else 0, a["old"], a["ref"], a["A"], a["w"], B, N, 0.2, 0.2, 0.1, a["g"], a["lp"], a["stats"], a["ws"],
+        dora.dora_pl_policy_workspace_size(B), a["st"], None)
+
+
+def test_draws_outputs_apart():
+    a = Room(("s", "order", "cuo", "cu", "old", "ref", "A", "w", "g", "lp", "stats", "ws", "st")).at
+    for out in ("g", "lp", "stats", "ws", "st"):
+        for other in ("order", "cuo", "cu", "g", "lp", "stats", "ws", "st"):
+            if out != other:
+                assert draws(**{out: a[other]}) == dora.DORA_ERR_OVERLAP, (out, other)
+        for other in ("old", "ref", "A", "w"):
+            if out != "lp":
+                assert draws(**{out: a[other]}) == dora.DORA_ERR_OVERLAP
+        if out != "g":
+            assert draws(**{out: a["s"]}) == dora.DORA_ERR_OVERLAP
+            # the last score, packed (200 of them) and dense (7 of 40)
+            assert out == "ws" or draws(**{out: a["s"] + 199 * 4}) == dora.DORA_ERR_OVERLAP
+            assert out == "ws" or draws(packed=False, **{out: a["s"] + 279 * 4}) == dora.DORA_ERR_OVERLAP
+        assert draws(entry="dora_pl_policy_loss", **{out: a["order"]}) == dora.DORA_ERR_OVERLAP
+    for other in ("old", "ref", "A", "w"):
+        assert draws(lp=a[other] + 4) == dora.DORA_ERR_OVERLAP
+        assert draws(lp=a[other] - 24) == dora.DORA_ERR_OVERLAP
+    assert draws(lp=a["cuo"] + 7 * 4) == dora.DORA_ERR_OVERLAP       # the last offset
+    assert draws(lp=a["order"] + 49 * 4) == dora.DORA_ERR_OVERLAP    # the last draw
+
+
 def scored(dora, rows, V, dtype):
     """A batch, the actions' log-probabilities in 64 bits, and old ones off the clip's border."""
     g = torch.Generator("cuda").manual_seed(rows + V)
@@ -145,3 +177,25 @@ def test_outputs_in_the_gaps(gpu):
     with pytest.raises(gpu.DoraError) as e:
         gpu.dora_policy_loss(x, act, old, adv, dev_status=act[:1])
     assert e.value.code == gpu.DORA_ERR_OVERLAP
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", ["old_logprob", "ref_logprob", "advantage", "weight"])
+@pytest.mark.parametrize("B,N", [(1, 30), (48, 197), (1100, 577)])
+def test_draws_in_an_inputs_place(gpu, B, N, name):
+    g = torch.Generator("cuda").manual_seed(B)
+    s = torch.randn((B, N), generator=g, device="cuda")
+    gumbel = -torch.log(-torch.log(torch.rand((B, N), generator=g, device="cuda").clamp(1e-6, 1 - 1e-6)))
+    k = torch.randint(0, N, (B,), generator=g, device="cuda", dtype=torch.int32)
+    order, cu, old, _ = gpu.dora_pl_sample(s, gumbel, k)
+    if B > 2:
+        order[int(cu[1])] = -1                                # a bad image, and one that is padding
+    w = torch.full((B,), 0.5, device="cuda")
+    w[B // 2] = 0.0 if B > 1 else 0.5
+    c = dict(old_logprob=old - 0.1, ref_logprob=old + 0.1, advantage=torch.randn(B, generator=g, device="cuda"), weight=w)
+    want = gpu.dora_pl_policy_loss(s, order, cu, **{k: v.clone() for k, v in c.items()}, kl_coef=0.1)
+    for _ in range(3):
+        own = {k: v.clone() for k, v in c.items()}
+        got = gpu.dora_pl_policy_loss(s, order, cu, **own, kl_coef=0.1, logprob_out=own[name])
+        for a, b in zip(got, want):
+            assert torch.equal(a.nan_to_num(7.0), b.nan_to_num(7.0))
