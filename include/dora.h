@@ -654,10 +654,10 @@ typedef struct {
  *   n          1 .. 65536.
  *   max_norm   >= 0; infinity: only the norm is formed, out is ignored.
  *   eps        >= 0.
- *   norm_out   device fp32 [1].
+ *   norm_out   device fp32 [1], apart from the tensors and the workspace.
  *   workspace  device, 256-byte aligned, dora_grad_clip_workspace_size(n)
- *              bytes, no required contents; calls that share it must not
- *              overlap in time.
+ *              bytes, apart from the tensors, no required contents; calls
+ *              that share it must not overlap in time.
  *
  * Returns DORA_OK or a negative dora_status (DORA_ERR_OVERLAP for tensors that
  * overlap otherwise); enqueues a kernel for the norm per 248 tensors and one to

@@ -16,6 +16,7 @@
 #include <cstdlib>
 
 #include "dora_internal.h"
+#include "policy_terms.h"
 
 namespace dora {
 namespace {
@@ -355,6 +356,14 @@ extern "C" int dora_grad_clip(const dora_span* grads, const dora_span* out, int3
   }
   if (!workspace || reinterpret_cast<uintptr_t>(workspace) & 255u || workspace_bytes < dora_grad_clip_workspace_size(n))
     return DORA_ERR_WORKSPACE;
+  const Extent norm_at(norm_out, sizeof(float)), ws(workspace, dora_grad_clip_workspace_size(n));
+  bool shared = norm_at.meets(ws);
+  for (const dora_span* s : {grads, scale ? out : nullptr})
+    for (int32_t i = 0; s && i < n; ++i) {
+      const Extent t(s[i].data, span_bytes(s[i]));
+      shared = shared || t.meets(norm_at) || t.meets(ws);
+    }
+  if (shared) return DORA_ERR_OVERLAP;
   if (scale) {
     Range* r = static_cast<Range*>(std::malloc(sizeof(Range) * 2 * static_cast<size_t>(n)));
     if (!r) return DORA_ERR_CAPACITY;

@@ -63,12 +63,14 @@ inline size_t policy_parts_bytes(int32_t n) {
 }
 void launch_policy_finish(double* parts, int32_t n, float* stats, hipStream_t stream);
 
-// Memory of a call's tensor (address 0: not given).
+// Memory of a call's tensor (none at address 0 or without elements).
 struct Extent {
   uintptr_t at;
   size_t bytes;
   Extent(const void* p, size_t n) : at(reinterpret_cast<uintptr_t>(p)), bytes(n) {}
-  bool meets(Extent o) const { return at && o.at && at < o.at + o.bytes && o.at < at + bytes; }
+  bool meets(Extent o) const {
+    return at && o.at && bytes && o.bytes && at < o.at + o.bytes && o.at < at + bytes;
+  }
 };
 // Outputs that share memory with another output or with an input.  `own` are
 // inputs whose place an output may take as a whole: a row reads its entry of

@@ -1,6 +1,8 @@
 """Outputs of the policy operators against the call's other tensors: refused
 where they share memory, but that a row's (image's) log-probability may take the
 place of one of its own inputs."""
+import ctypes
+
 import pytest
 import torch
 
@@ -105,6 +107,28 @@ def test_draws_outputs_apart():
     assert draws(lp=a["order"] + 49 * 4) == dora.DORA_ERR_OVERLAP    # the last draw
 
 
+def clip(grads, out=None, max_norm=1.0, norm=A, ws=A + (1 << 24)):
+    spans = lambda items: (dora.Span * len(items))(*(dora.Span(*i) for i in items))
+    g, o = spans(grads), None if out is None else spans(out)
+    return dora.load_library().dora_grad_clip(ctypes.addressof(g), None if o is None else ctypes.addressof(o), len(grads),
+                                              max_norm, 1e-6, norm, ws, dora.dora_grad_clip_workspace_size(len(grads)), None)
+
+
+@pytest.mark.parametrize("max_norm", [1.0, float("inf")])
+def test_clip_outputs_apart(max_norm):
+    """The norm and the workspace apart from every tensor, read or written."""
+    a, b = (A + (2 << 24), 100, 0, 0), (A + (3 << 24), 33, 1, 0)
+    for tensors in ([a, b], [b, a]):
+        for at in (a[0], a[0] + 396, b[0], b[0] + 64):
+            assert clip(tensors, max_norm=max_norm, norm=at) == dora.DORA_ERR_OVERLAP
+        for at in (a[0], b[0], a[0] - 256):
+            assert clip(tensors, max_norm=max_norm, ws=at) == dora.DORA_ERR_OVERLAP
+    assert clip([a], max_norm=max_norm, norm=A + (1 << 24) + 8) == dora.DORA_ERR_OVERLAP     # inside the workspace
+    if max_norm == 1.0:
+        assert clip([a], out=[(A + (4 << 24), 100, 0, 0)], norm=A + (4 << 24) + 8) == dora.DORA_ERR_OVERLAP
+        assert clip([a], out=[(A + (4 << 24), 100, 0, 0)], ws=A + (4 << 24)) == dora.DORA_ERR_OVERLAP
+
+
 def scored(dora, rows, V, dtype):
     """A batch, the actions' log-probabilities in 64 bits, and old ones off the clip's border."""
     g = torch.Generator("cuda").manual_seed(rows + V)
@@ -199,3 +223,20 @@ def test_draws_in_an_inputs_place(gpu, B, N, name):
         got = gpu.dora_pl_policy_loss(s, order, cu, **own, kl_coef=0.1, logprob_out=own[name])
         for a, b in zip(got, want):
             assert torch.equal(a.nan_to_num(7.0), b.nan_to_num(7.0))
+
+
+@pytest.mark.gpu
+def test_clip_beside_the_norm(gpu):
+    """Gradients, the norm and empty tensors as views of one buffer."""
+    flat = torch.randn(400, device="cuda")
+    ws = gpu.new_grad_clip_workspace(3)
+    want, norm = gpu.dora_grad_clip([flat[:100].clone(), flat[101:].clone()], 0.5)
+    empty = ws[64:64].view(torch.float32)
+    gpu.dora_grad_clip([flat[:100], flat[100:100], flat[101:], empty], 0.5, norm_out=flat[100:101],
+                       workspace=torch.cat([ws, ws]))
+    assert torch.equal(flat[:100], want[0]) and torch.equal(flat[101:], want[1]) and torch.equal(flat[100:101], norm)
+    out, norm2 = gpu.dora_grad_clip([want[0], empty], 1e9, out=[torch.empty_like(want[0]), empty], workspace=ws)
+    assert torch.equal(out[0], want[0])
+    with pytest.raises(gpu.DoraError) as e:
+        gpu.dora_grad_clip([flat[:101]], 0.5, norm_out=flat[100:101])
+    assert e.value.code == gpu.DORA_ERR_OVERLAP
