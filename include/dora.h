@@ -642,7 +642,7 @@ typedef struct {
  * dora_grad_clip -- global norm of many gradient tensors, and clipping by it
  * (App. D: the actor's gradients are clipped at a global norm).
  *   norm = sqrt(sum over tensors and elements of g^2)
- *   c    = min(1, max_norm / (norm + eps)), 1 for norm 0
+ *   c    = min(1, max_norm / (norm + eps)), 1 for norm 0 or max_norm infinity
  *   out  = c g, rounded once to the tensor's dtype
  * The squares are added in 64 bits in a fixed order.  NaN or infinite
  * gradients give a norm that is, and outputs as the formula gives them.
@@ -652,7 +652,7 @@ typedef struct {
  *              NULL: in place.  An output may be its own input and overlaps
  *              no other tensor (in place, no tensor may be given twice).
  *   n          1 .. 65536.
- *   max_norm   >= 0; infinity: only the norm is formed, out is ignored.
+ *   max_norm   >= 0; infinity: no limit (in place only the norm is formed).
  *   eps        >= 0.
  *   norm_out   device fp32 [1], apart from the tensors and the workspace.
  *   workspace  device, 256-byte aligned, dora_grad_clip_workspace_size(n)

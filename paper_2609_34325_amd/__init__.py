@@ -867,8 +867,8 @@ def dora_grad_clip(grads, max_norm: float, out=None, eps: float = 1e-6, norm_out
 
     grads: contiguous bf16 or fp32 tensors, types may be mixed; out: tensors of
     the same sizes and types, or None: in place.  Every tensor is multiplied by
-    min(1, max_norm / (norm + eps)); with max_norm = infinity only the norm is
-    formed and nothing is written.  Returns (out, norm [1] fp32)."""
+    min(1, max_norm / (norm + eps)), or 1 with max_norm = infinity, where in
+    place only the norm is formed.  Returns (out, norm [1] fp32)."""
     if stream is not None:
         with _in_stream(stream):
             return dora_grad_clip(grads, max_norm, out, eps, norm_out, workspace)

@@ -245,7 +245,9 @@ __global__ __launch_bounds__(kThreads, 6) void grad_scale_kernel(B b, const doub
     if (i == blockIdx.x) {
       const double norm = norm_of(parts, n);
       if (norm_out && i == 0 && threadIdx.x == 0) *norm_out = static_cast<float>(norm);
-      const double ratio = norm == 0.0 ? 1.0 : static_cast<double>(max_norm) / (norm + static_cast<double>(eps));
+      const double ratio = norm == 0.0 || max_norm == __builtin_inff()
+                               ? 1.0
+                               : static_cast<double>(max_norm) / (norm + static_cast<double>(eps));
       f = Factor(ratio >= 1.0 ? 1.0 : ratio);  // NaN stays
       if (kInPlace && f.keeps()) return;
     }
@@ -347,8 +349,8 @@ extern "C" int dora_grad_clip(const dora_span* grads, const dora_span* out, int3
   if (n < 1 || n > kMaxSpans || !(max_norm >= 0.0f) || !(eps >= 0.0f)) return DORA_ERR_SHAPE;
   int rc = check_spans(grads, n);
   if (rc != DORA_OK) return rc;
-  const bool scale = max_norm != __builtin_inff();
-  if (out && scale) {
+  const bool scale = out || max_norm != __builtin_inff();  // in place, no limit leaves nothing to write
+  if (out) {
     rc = check_spans(out, n);
     if (rc != DORA_OK) return rc;
     for (int32_t i = 0; i < n; ++i)
@@ -358,7 +360,7 @@ extern "C" int dora_grad_clip(const dora_span* grads, const dora_span* out, int3
     return DORA_ERR_WORKSPACE;
   const Extent norm_at(norm_out, sizeof(float)), ws(workspace, dora_grad_clip_workspace_size(n));
   bool shared = norm_at.meets(ws);
-  for (const dora_span* s : {grads, scale ? out : nullptr})
+  for (const dora_span* s : {grads, out})
     for (int32_t i = 0; s && i < n; ++i) {
       const Extent t(s[i].data, span_bytes(s[i]));
       shared = shared || t.meets(norm_at) || t.meets(ws);
