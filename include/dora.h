@@ -643,7 +643,8 @@ typedef struct {
  * (App. D: the actor's gradients are clipped at a global norm).
  *   norm = sqrt(sum over tensors and elements of g^2)
  *   c    = min(1, max_norm / (norm + eps)), 1 for norm 0 or max_norm infinity
- *   out  = c g, rounded once to the tensor's dtype
+ *   out  = c g: c in fp32, the product in fp32, then rounded to the tensor's
+ *          dtype
  * The squares are added in 64 bits in a fixed order.  NaN or infinite
  * gradients give a norm that is, and outputs as the formula gives them.
  *

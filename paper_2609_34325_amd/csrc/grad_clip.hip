@@ -196,14 +196,14 @@ __global__ __launch_bounds__(kThreads) void grad_norm_kernel(const double* parts
   if (threadIdx.x == 0) *norm = static_cast<float>(v);
 }
 
-// The factor as a product: a factor below 2^-64 (gradients near fp32's limit)
-// would itself be subnormal in fp32 and short of bits.
+// The factor as a product: a small one (gradients near fp32's limit) would
+// itself be subnormal in fp32 and short of bits, or 0.  Results that are not
+// subnormal have a factor of at least 2^-254, so c is not subnormal there.
 struct Factor {
   float pre, c;
   __device__ explicit Factor(double f) {
-    const bool tiny = f < 0x1p-64;
-    pre = tiny ? 0x1p-64f : 1.0f;
-    c = static_cast<float>(tiny ? f * 0x1p64 : f);
+    pre = f >= 0x1p-64 ? 1.0f : (f >= 0x1p-128 ? 0x1p-64f : 0x1p-128f);
+    c = static_cast<float>(f / pre);
   }
   __device__ float operator*(float g) const { return g * pre * c; }
   __device__ bool keeps() const { return pre == 1.0f && c == 1.0f; }

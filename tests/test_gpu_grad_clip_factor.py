@@ -41,3 +41,24 @@ def test_no_limit_refuses_like_a_limit(gpu):
         gpu.dora_grad_clip([g[:5], g[5:]], INF, out=[g[1:6], torch.empty_like(g[5:])])
     assert e.value.code == gpu.DORA_ERR_OVERLAP
     gpu.dora_grad_clip([g, g], INF)                            # only read
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("max_norm", [1e-10, 1e-19, 1e-22, 1e-30, 1e-38, 1e-40, 1e-44, 0.0])
+def test_small_factors(gpu, dtype, max_norm, in_place):
+    """Gradients near fp32's limit under a small limit: a factor down to 2^-277.
+    A subnormal result is a whole number of 2^-149 (bf16: 2^-133), off by half a
+    step of that for each of its up to three roundings."""
+    t = {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
+    g = torch.Generator("cuda").manual_seed(2)
+    grads = [(3e38 * (2 * torch.rand(n, generator=g, device="cuda") - 1)).to(t) for n in (7, 3000, 20001)]
+    ref = [widen(x) for x in grads]
+    limit = float(np.float32(max_norm))
+    norm = np.sqrt(sum((x ** 2).sum() for x in ref))
+    c = limit / (norm + float(np.float32(1e-6)))
+    got, _ = gpu.dora_grad_clip(grads, max_norm, out=None if in_place else [torch.empty_like(x) for x in grads])
+    step = 2.0 ** (-149 if dtype == "f32" else -133)
+    for x, w in zip(got, ref):
+        w = w * c
+        assert np.all(np.abs(widen(x) - w) <= (2.01 * U32 + HALF[dtype]) * np.abs(w) + 1.5 * step)
