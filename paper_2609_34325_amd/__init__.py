@@ -17,6 +17,7 @@ There is no fallback: if the library is missing, every call raises.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 import warnings
 from typing import Optional, Tuple
@@ -132,6 +133,7 @@ _native_call = None
 _native_spans = None
 _native_rows = None
 _native_vectors = None
+_native_written = None
 
 
 class FlopsConfig(ctypes.Structure):
@@ -158,7 +160,7 @@ def _leave_to_ctypes(*args):
 
 def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     """Load libdora.so (built in-tree by ``paper_2609_34325_amd.build``)."""
-    global _lib, _native_call, _native_spans, _native_rows, _native_vectors
+    global _lib, _native_call, _native_spans, _native_rows, _native_vectors, _native_written
     if _lib is not None and path is None:
         return _lib
     p = path or LIB_PATH
@@ -230,11 +232,11 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     if _native_call is None:
         try:
             from ._host_call import (call as _native_call, rows as _native_rows, spans as _native_spans,
-                                     vectors as _native_vectors)
+                                     vectors as _native_vectors, written as _native_written)
         except ImportError as e:  # not built, or for another Python or torch
             warnings.warn(f"calls are marshalled by ctypes, about 5 us slower each: {e}; build the native marshalling "
                           "with `python -m paper_2609_34325_amd.build`")
-            _native_call = _native_spans = _native_rows = _native_vectors = _leave_to_ctypes
+            _native_call = _native_spans = _native_rows = _native_vectors = _native_written = _leave_to_ctypes
     if path is None:
         _lib = lib
     return lib
@@ -700,6 +702,15 @@ def _vectors(names, device: int, *sized) -> None:
         raise ValueError(f"tensors on device {device}, which is not the current one")
 
 
+def _written(*outputs) -> None:
+    """Tensors (or lists of them) that a call wrote by their addresses: autograd
+    refuses a backward pass that saved one of them, as after torch's own
+    in-place operators."""
+    if (_native_written or _leave_to_ctypes)(*outputs) is NotImplemented:
+        for t in outputs:
+            torch.autograd.graph.increment_version(t)
+
+
 def _bytes(workspace: Optional[torch.Tensor]) -> int:
     return 0 if workspace is None else workspace.numel() * workspace.element_size()
 
@@ -748,6 +759,7 @@ def dora_action_logprob(logits: torch.Tensor, actions: torch.Tensor, weight: Opt
              T, actions, T, legal, T, weight, T, logprob_out, T, entropy_out, -1, workspace, -1, dev_status)
     _call("dora_action_logprob", None, address, ld, actions, legal, weight, T, V, code, logprob_out, entropy_out,
           workspace, _bytes(workspace), dev_status)
+    _written(logprob_out, entropy_out)
     return logprob_out, entropy_out, dev_status
 
 
@@ -763,9 +775,9 @@ def dora_policy_loss(logits: torch.Tensor, actions: torch.Tensor, old_logprob: t
     advantage and ref_logprob (needed for kl_coef != 0): fp32 [T].  The loss is
     the sum over rows of weight * (-min(r A, clip(r) A) + kl_coef * kl -
     entropy_coef * entropy); for a mean, weight is 1 / count.  dlogits may be
-    the logits themselves.  Returns (dlogits [T, V], logprob [T], stats [6],
-    dev_status); stats holds the sums of loss, gain, kl, entropy, clipped share
-    and weight."""
+    the logits themselves; logits.backward(dlogits) carries it on.  Returns
+    (dlogits [T, V], logprob [T], stats [6], dev_status); stats holds the sums
+    of loss, gain, kl, entropy, clipped share and weight."""
     if stream is not None:
         with _in_stream(stream):
             return dora_policy_loss(logits, actions, old_logprob, advantage, ref_logprob, weight, legal, clip_low,
@@ -787,6 +799,7 @@ def dora_policy_loss(logits: torch.Tensor, actions: torch.Tensor, old_logprob: t
     _call("dora_policy_loss", None, address, ld, actions, legal, old_logprob, ref_logprob, advantage, weight, T, V,
           code, float(clip_low), float(clip_high), float(kl_coef), float(entropy_coef), grad, ld_grad, logprob_out,
           stats_out, workspace, _bytes(workspace), dev_status)
+    _written(dlogits, logprob_out, stats_out)
     return dlogits, logprob_out, stats_out, dev_status
 
 
@@ -833,6 +846,7 @@ def dora_pl_policy_loss(scores: torch.Tensor, order: torch.Tensor, cu_order: tor
     _call("dora_pl_policy_loss_cap", None, scores, order, cu_order, _numel(order), cu_in, total_in, old_logprob,
           ref_logprob, advantage, weight, B, N, float(clip_low), float(clip_high), float(kl_coef), dscores, logprob_out,
           stats_out, workspace, _bytes(workspace), dev_status)
+    _written(dscores, logprob_out, stats_out)
     return dscores, logprob_out, stats_out, dev_status
 
 
@@ -888,4 +902,6 @@ def dora_grad_clip(grads, max_norm: float, out=None, eps: float = 1e-6, norm_out
     _vectors(("norm_out", "workspace"), device, 1, norm_out, -1, workspace)
     _call("dora_grad_clip", None, ctypes.addressof(spans), 0 if out_spans is None else ctypes.addressof(out_spans),
           len(grads), float(max_norm), float(eps), norm_out, workspace, _bytes(workspace))
-    return grads if out is None else out, norm_out
+    scaled = grads if out is None else out
+    _written([] if out is None and max_norm == math.inf else scaled, norm_out)
+    return scaled, norm_out

@@ -283,7 +283,33 @@ PyObject* vectors(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   Py_RETURN_TRUE;
 }
 
+// written(t, ...): autograd learns that the tensors (or the lists' tensors) were
+// written in place, as it does from torch's own operators.
+bool mark_written(PyObject* o) {
+  if (!THPVariable_Check(o)) return false;
+  const at::Tensor& t = THPVariable_Unpack(o);
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();  // inference tensors have no version
+  return true;
+}
+PyObject* written(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  try {
+    for (Py_ssize_t i = 0; i < nargs; ++i) {
+      if (!PyList_CheckExact(args[i])) {
+        if (!mark_written(args[i])) Py_RETURN_NOTIMPLEMENTED;
+        continue;
+      }
+      for (Py_ssize_t j = 0; j < PyList_GET_SIZE(args[i]); ++j)
+        if (!mark_written(PyList_GET_ITEM(args[i], j))) Py_RETURN_NOTIMPLEMENTED;
+    }
+  } catch (...) {
+    Py_RETURN_NOTIMPLEMENTED;
+  }
+  Py_RETURN_TRUE;
+}
+
 PyMethodDef kMethods[] = {
+    {"written", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(written)), METH_FASTCALL,
+     "written(tensor or list, ...): True, or NotImplemented"},
     {"rows", rows, METH_O, "rows(tensor): address, leading dimension, sizes, type and device, or NotImplemented"},
     {"vectors", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(vectors)), METH_FASTCALL,
      "vectors(device, n, tensor, ...): True, or NotImplemented"},
