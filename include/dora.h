@@ -494,7 +494,8 @@ int dora_varlen_attn_noalloc(const void* q, const void* k, const void* v, const 
  * deployment": the gate and the budget are categorical choices, the budget
  * masked to the legal ones).  What scores a rollout under the old and the
  * reference policy; any head with up to DORA_MAX_ACTIONS choices, a language
- * model's vocabulary among them.
+ * model's vocabulary among them.  A gate with one logit x is the row (0, x):
+ * action 1 is the gate on, d loss / d x the gradient's second column.
  *
  * Row t, with n = legal[t] open choices (V without `legal`), the first n of
  * its logits x, and p = softmax over them:
