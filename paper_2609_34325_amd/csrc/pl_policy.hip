@@ -50,14 +50,15 @@ struct PLPolicyParams {
   int32_t* status;
 };
 
-// exp(x) 2^-ref, where every score is within 2^900 of the largest, 2^ref.
+// exp(x - top), where every score is within 2^900 of the largest, top.
 struct Plain {
   double v;
   __device__ static Plain zero() { return {0.0}; }
-  __device__ static Plain exp_of(float x, double ref) { return {exp2(x * kLog2E - ref)}; }
+  __device__ static Plain exp_of(float x, double top) { return {exp2((x - top) * kLog2E)}; }
   __device__ Plain operator+(Plain o) const { return {v + o.v}; }
   __device__ Plain inverse() const { return {1.0 / v}; }
-  __device__ double log_of(double ref) const { return log(v) + ref * kLn2; }
+  // log of exp(x) over this sum.
+  __device__ double share_of(float x, double top) const { return (x - top) - log(v); }
   __device__ double times(Plain o) const { return v * o.v; }
 };
 
@@ -65,9 +66,16 @@ struct Plain {
 struct Scaled {
   double v, e;
   __device__ static Scaled zero() { return {0.0, -1e300}; }
+  // Rounded before anything is taken from it: the rest that a fused step would
+  // keep is 1e22 for the lowest score (a mask), and differs between 0 and that
+  // for what is equal.
+  __device__ static double log2_of(float x) {
+#pragma clang fp contract(off)
+    return x * kLog2E;
+  }
   __device__ static Scaled exp_of(float x, double) {
     if (x == -__builtin_inff()) return zero();
-    const double y = x * kLog2E, e = floor(y);
+    const double y = log2_of(x), e = floor(y);
     return {exp2(y - e), e};
   }
   __device__ double at(double to) const { return ldexp(v, static_cast<int>(fmax(e - to, -4000.0))); }
@@ -76,7 +84,7 @@ struct Scaled {
     return {at(to) + o.at(to), to};
   }
   __device__ Scaled inverse() const { return {1.0 / v, -e}; }
-  __device__ double log_of(double) const { return log(v) + e * kLn2; }
+  __device__ double share_of(float x, double) const { return (log2_of(x) - e) * kLn2 - log(v); }
   __device__ double times(Scaled o) const { return Scaled{v * o.v, e + o.e}.at(0.0); }
   __device__ Scaled down(int d) const { return {__shfl_down(v, d), __shfl_down(e, d)}; }
   __device__ Scaled up(int d) const { return {__shfl_up(v, d), __shfl_up(e, d)}; }
@@ -145,7 +153,7 @@ __device__ __forceinline__ Plain scan_lanes(Plain own, Plain* total) {
 // all -1; *bad is set where a position is drawn twice (what comes out then is
 // of no use, but all of it stays in bounds).
 template <int kThreads, class T>
-__device__ __forceinline__ double scan_draws(const Tokens& s, int nv, int k, double ref, T* front, int* bad) {
+__device__ __forceinline__ double scan_draws(const Tokens& s, int nv, int k, double top, T* front, int* bad) {
   constexpr int kWaves = kThreads / 64;
   constexpr bool kStored = sizeof(T) == sizeof(Plain);  // exp is looked up, not formed again
   __shared__ T s_left[kWaves], s_back[kWaves], s_front[kWaves];
@@ -154,11 +162,11 @@ __device__ __forceinline__ double scan_draws(const Tokens& s, int nv, int k, dou
   T* const exps = front + nv;  // Plain only
   for (int t = tid; t < k; t += kThreads) s.rank[s.draw[t]] = static_cast<int16_t>(t);
   if constexpr (kStored)
-    for (int j = tid; j < nv; j += kThreads) exps[j] = T::exp_of(s.x[j], ref);
+    for (int j = tid; j < nv; j += kThreads) exps[j] = T::exp_of(s.x[j], top);
   __syncthreads();
   auto exp_at = [&](int pos) {
     if constexpr (kStored) return exps[pos];
-    else return T::exp_of(s.x[pos], ref);
+    else return T::exp_of(s.x[pos], top);
   };
   T left = T::zero();  // the tokens never drawn
   for (int j = tid; j < nv; j += kThreads)
@@ -187,7 +195,7 @@ __device__ __forceinline__ double scan_draws(const Tokens& s, int nv, int k, dou
   for (int t = last - 1; t >= first; --t) {
     const int pos = s.draw[t];
     run = run + exp_at(pos);
-    lp += s.x[pos] - run.log_of(ref);
+    lp += run.share_of(s.x[pos], top);
     front[t] = run.inverse();
     own = own + front[t];
   }
@@ -215,7 +223,7 @@ __device__ __forceinline__ double scan_draws(const Tokens& s, int nv, int k, dou
 
 // d loss / d s of the visual tokens.
 template <int kThreads, class T>
-__device__ __forceinline__ void put_gradient(const Tokens& s, const T* front, int nv, int k, double ref, double slope,
+__device__ __forceinline__ void put_gradient(const Tokens& s, const T* front, int nv, int k, double top, double slope,
                                              float* grad) {
   for (int j = threadIdx.x; j < nv; j += kThreads) {
     float g = 0.0f;
@@ -223,7 +231,7 @@ __device__ __forceinline__ void put_gradient(const Tokens& s, const T* front, in
       const int r = s.rank[j];
       T e;
       if constexpr (sizeof(T) == sizeof(Plain)) e = front[nv + j];
-      else e = T::exp_of(s.x[j], ref);
+      else e = T::exp_of(s.x[j], top);
       g = static_cast<float>(slope * ((r < 0 ? 0.0 : 1.0) - e.times(front[r < 0 ? k - 1 : r])));
     }
     grad[j] = g;
@@ -251,7 +259,7 @@ __global__ __launch_bounds__(kThreads) void pl_policy_kernel(PLPolicyParams p) {
   char* const at = reinterpret_cast<char*>(s_tokens);
   const Tokens s{at, reinterpret_cast<float*>(at + 16 * p.N), reinterpret_cast<int16_t*>(at + 20 * p.N),
                  reinterpret_cast<int16_t*>(at + 22 * p.N)};
-  double lp = 0.0, ref = 0.0;
+  double lp = 0.0, ref = 0.0;  // ref: the largest score
   bool plain = true;
   if (ok) {
     float top = -__builtin_inff(), low = __builtin_inff();
@@ -285,7 +293,7 @@ __global__ __launch_bounds__(kThreads) void pl_policy_kernel(PLPolicyParams p) {
       top = fmaxf(top, s_max[i]);
       low = fminf(low, s_min[i]);
     }
-    ref = nv > 0 ? top * kLog2E : 0.0;
+    ref = nv > 0 ? top : 0.0;
     plain = (static_cast<double>(top) - low) * kLog2E < 900.0;  // also for no token: -inf
     lp = plain ? scan_draws<kThreads>(s, nv, k, ref, reinterpret_cast<Plain*>(s.scan), &s_bad)
                : scan_draws<kThreads>(s, nv, k, ref, reinterpret_cast<Scaled*>(s.scan), &s_bad);
