@@ -572,8 +572,8 @@ int dora_action_logprob(const void* logits, int64_t ld, const int32_t* actions, 
  * differ between places of another alignment and between small and large T.
  *
  * Returns DORA_OK or a negative dora_status (DORA_ERR_OVERLAP for tensors
- * that share memory otherwise than above); enqueues one kernel, two past one
- * workgroup's rows, three past 8192 workgroups.
+ * that share memory otherwise than above); enqueues one kernel, two where the
+ * rows take several workgroups or a row is split, three past 8192 workgroups.
  */
 int dora_policy_loss(const void* logits, int64_t ld, const int32_t* actions, const int32_t* legal,
                      const float* old_logprob, const float* ref_logprob, const float* advantage, const float* weight,

@@ -18,7 +18,7 @@
 // counts for nothing in either form.
 //
 // One workgroup per image; launch, memory and barrier latency bound (an image
-// is a few KB): 256 x 577 tokens 7.6 us, 48 x 2048 11.7, 8192 x 257 30.
+// is a few KB): 256 x 577 tokens 7.4 us, 48 x 2048 11.8, 8192 x 257 29.
 // Shared memory is sized by N, so that several images share a compute unit.
 // Loss terms per image go to the workspace and are added by a second launch in
 // a fixed order.

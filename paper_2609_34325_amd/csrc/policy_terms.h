@@ -54,8 +54,8 @@ __device__ __forceinline__ double policy_decision(double logp, double entropy, f
 
 // stats_out from n sets of sums, added in a fixed order: by one workgroup, or
 // past kFinishDirect sets first by up to kFinishGroups workgroups into the room
-// behind them (one workgroup: 32 sets 1.8 us, 1024 4.7, 8192 14; more threads or
-// loads in flight make no difference beside the rows).
+// behind them (one workgroup: 32 sets 1.8 us, 1024 4.1 to 4.7, 8192 14; more threads
+// or loads in flight made no difference to a pass over long rows).
 constexpr int kFinishDirect = 8192, kFinishGroups = 256;
 inline size_t policy_parts_bytes(int32_t n) {
   const size_t sets = static_cast<size_t>(n) + (n > kFinishDirect ? kFinishGroups : 0);
