@@ -10,8 +10,8 @@
 // 16-byte pieces in flight a thread.  Squares are added in 64 bits: no fp32
 // gradient overflows them, and the sum does not hang on the split.  Workgroups
 // write their sums to the workspace; every workgroup of a scaling launch adds
-// them all in the same order.  304M fp32 elements in 292 tensors, out of place:
-// norm 237 us (5.1 TB/s), scaling 493 (4.9 TB/s); 22M bf16 in 150: 11 and 15.
+// them all in the same order.  304M fp32 elements in 296 tensors, out of place:
+// norm 237 us (5.1 TB/s), scaling 493 (4.9 TB/s); 22M bf16 in 152: 11 and 15.
 #include <algorithm>
 #include <cstdlib>
 
