@@ -329,8 +329,8 @@ int dora_pl_sample(const float* scores, const float* gumbel, const int32_t* k, c
  * Other arguments as for dora_pl_sample.  Returns DORA_OK or a negative
  * dora_status; enqueues one kernel.
  *
- * dora_pl_logprob_cap: the same where order holds cap entries (0 .. ; NULL for
- * 0), fewer than cu_order[B] after a dora_pl_sample with too small a capacity:
+ * dora_pl_logprob_cap: the same where order holds cap entries (0 or more, else
+ * DORA_ERR_CAPACITY; may be NULL for 0), fewer than cu_order[B] after a dora_pl_sample with too small a capacity:
  * no entry past them is read, an image whose draws reach there is one whose
  * offsets break the above.
  */
