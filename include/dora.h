@@ -669,6 +669,164 @@ size_t dora_grad_clip_workspace_size(int32_t n); /* 0 when n is out of range */
 int dora_grad_clip(const dora_span* grads, const dora_span* out, int32_t n, float max_norm, float eps,
                    float* norm_out, void* workspace, size_t workspace_bytes, void* stream);
 
+/* Packed rows: element (r, h, d) is data[r row_stride + h head_stride + d], strides in elements, so that
+ * slices of a wider product and transposed layouts are described as they lie.  A matrix has one head. */
+typedef struct {
+  void* data;
+  int64_t rows;
+  int32_t heads, dim;
+  int64_t row_stride, head_stride; /* 0 or more; 0 reads one row (head) again and again, for inputs alone */
+  int32_t dtype;                   /* dora_dtype */
+  int32_t reserved;
+} dora_rows;
+
+/*
+ * dora_rope -- rotary positions: turns pairs of each head's elements by the
+ * angle of the row's position.  The positions are given, so the kept tokens of
+ * dora_select_pack (idx_out) and patches by row and column keep theirs.
+ *
+ * Pair i of R / 2, t = positions[row][i / (R / 2 / axes)] * freq[i], elements
+ * u, v at (i, i + R / 2) or, interleaved, at (2 i, 2 i + 1):
+ *   u' = scale (u cos t - v sin t),  v' = scale (u sin t + v cos t)
+ * inverse: -t in place of t, which is the gradient (and, at scale 1, the way
+ * back).  Elements from R on are copied.  The angle is formed and reduced in 64
+ * bits, so far positions keep their place; the turn is fp32, rounded once.
+ *
+ *   q, k       HOST descriptions, read during the call; k may be NULL, or has
+ *              q's rows, dim and dtype and its own heads (grouped heads).
+ *   positions  int32 [rows, axes], any values; 1 <= axes <= 4.
+ *   freq       float64 [R / 2], radians per position.
+ *   R          even, a multiple of 2 axes, 2 .. dim; dim at most 1024; at most
+ *              65535 heads of q and k together.
+ *   scale      multiplies the turned elements (longer contexts use one above 1).
+ *   q_out, k_out  descriptions of q's and k's sizes and type, in their places
+ *              (same address and strides) or apart from every other tensor.
+ * Addresses and strides are those of the elements' type; where they, R and dim
+ * allow pieces of 16 bytes, they are moved so.
+ *
+ * Returns DORA_OK or a negative dora_status; enqueues one kernel (none for 0
+ * rows).
+ */
+int dora_rope(const dora_rows* q, const dora_rows* k, const int32_t* positions, int32_t axes, const double* freq,
+              int32_t R, int32_t interleaved, int32_t inverse, float scale, const dora_rows* q_out,
+              const dora_rows* k_out, void* stream);
+
+/*
+ * dora_grouped_attn -- softmax attention inside packed sequences with grouped
+ * heads and a causal mask: dora_varlen_attn for language models and for
+ * training.  Sequence b has queries [cu_q[b], cu_q[b+1]) and keys [cu_k[b],
+ * cu_k[b+1]), nq and nk of them; head h of q reads head h / (H / Hk) of k and v.
+ * Query i sees keys j < nk, causal: j <= i + nk - nq (the last query sees all).
+ *   S = softmax_scale q k^T,  out = softmax(S) v,  lse = log sum exp S (natural)
+ * A query that sees no key, or only scores of -inf, has output 0 and lse -inf.
+ * Values that a query does not see count for nothing, infinities and NaN
+ * included.
+ *
+ *   q          [total_q, H, D]; k, v [total_k, Hk, D], H a multiple of Hk; HOST
+ *              descriptions, read during the call, 16-byte aligned throughout.
+ *              D 32, 64 or 128; H at most 256; one dtype.
+ *   cu_q, cu_k int32 [B+1], monotone from 0 or more to at most the rows; equal
+ *              pointers are allowed.  1 <= B <= DORA_MAX_SEQUENCES.
+ *   max_q      no sequence has more queries; total_q H / Hk at most 2^31 - 1.
+ *   softmax_scale  <= 0 selects 1/sqrt(D).
+ *   dtype      bf16: fp32 products and softmax, P rounded to bf16 for its
+ *              product; fp32: fp32 throughout.  Output rounded once.
+ *   out        q's sizes; rows outside every sequence are left as they were.
+ *   lse_out    NULL or fp32 [total_q, H], for the backward pass.
+ *   workspace  device, 256-byte aligned, dora_grouped_attn_workspace_size
+ *              bytes, no required contents: where there are few queries against
+ *              the GPU, the keys are split over workgroups and their parts
+ *              joined in a fixed order.  Calls that share it must not overlap
+ *              in time.
+ *   dev_status DORA_DEV_CU_SEQLENS for invalid offsets or a sequence of more
+ *              than max_q queries; such sequences are skipped.
+ * Outputs, workspace and dev_status share no memory with each other or with an
+ * input (DORA_ERR_OVERLAP).  Results do not depend on timing.
+ *
+ * Returns DORA_OK or a negative dora_status; enqueues one kernel, two where the
+ * keys are split (none for 0 queries).
+ *
+ * dora_grouped_attn_backward -- gradients of q, k and v from the output's, with
+ * out and lse as the forward pass gave them.  dk and dv are sums over the heads
+ * that read them.
+ *   P = exp(S - lse),  dS = P (dout v^T - rowsum(dout out))
+ *   dq = softmax_scale dS k,  dk = softmax_scale dS^T q,  dv = P^T dout
+ * bf16: P and dS rounded to bf16 for their products, sums in fp32, gradients
+ * rounded once.  Infinities and NaN stay inside their sequence.
+ *   dout, out  q's sizes; dq, dk, dv those of q, k, v, any strides (slices of
+ *              one tensor are allowed).  Rows outside every sequence are left
+ *              as they were; keys that no query sees get 0.
+ *   workspace  dora_grouped_attn_backward_workspace_size bytes.
+ * Enqueues two kernels, three where the queries of a key are split.
+ */
+#define DORA_MAX_SEQUENCES 65536 /* dora_grouped_attn: B */
+size_t dora_grouped_attn_workspace_size(int32_t B, int32_t H, int32_t Hk, int32_t D, int32_t max_q, int64_t total_q,
+                                        int64_t total_k); /* 0 for sizes out of range */
+size_t dora_grouped_attn_backward_workspace_size(int32_t B, int32_t H, int32_t Hk, int32_t D, int32_t max_q,
+                                                 int64_t total_q, int64_t total_k);
+int dora_grouped_attn(const dora_rows* q, const dora_rows* k, const dora_rows* v, const int32_t* cu_q,
+                      const int32_t* cu_k, int32_t B, int32_t max_q, int32_t causal, float softmax_scale,
+                      const dora_rows* out, float* lse_out, void* workspace, size_t workspace_bytes,
+                      int32_t* dev_status, void* stream);
+int dora_grouped_attn_backward(const dora_rows* dout, const dora_rows* q, const dora_rows* k, const dora_rows* v,
+                               const dora_rows* out, const float* lse, const int32_t* cu_q, const int32_t* cu_k,
+                               int32_t B, int32_t max_q, int32_t causal, float softmax_scale, const dora_rows* dq,
+                               const dora_rows* dk, const dora_rows* dv, void* workspace, size_t workspace_bytes,
+                               int32_t* dev_status, void* stream);
+
+/*
+ * dora_residual_norm -- what stands between two branches of a block, in one
+ * pass: the branch's output into the residual stream, and the norm that the
+ * next branch reads.  Row r, channel c:
+ *   u = a, or norm(a) with post_gamma and post_beta
+ *   h = x + gate[r] scale[c] u         (layer scale; a dropped branch's row has gate 0)
+ *   y = norm(h) with gamma and beta
+ *   norm(z) = (z - mean) / sqrt(var + eps) gamma + beta     (DORA_NORM_LAYER, biased variance)
+ *           = z / sqrt(mean of z^2 + eps) gamma + beta      (DORA_NORM_RMS)
+ * h is normed before it is rounded; everything fp32, h and y rounded once.  A
+ * gate of 0 leaves h = x whatever the branch holds.
+ *
+ *   x, a       HOST descriptions of matrices [T, C] (heads 1), read during the
+ *              call; a NULL: h = x (then scale, gate, post_gamma and post_beta
+ *              are NULL, and h_out may be).  16-byte aligned throughout, rows of
+ *              16 .. 32768 bytes, a multiple of 16.
+ *   gamma, beta, scale, post_gamma, post_beta  fp32 [C]; gate fp32 [T]; each
+ *              but gamma may be NULL (post_beta only without post_gamma too).
+ *   eps        >= 0.
+ *   h_out      NULL: not written.  h_out and y_out may be x or a as a whole;
+ *              otherwise they share no memory with each other or with an input.
+ * Returns DORA_OK or a negative dora_status; enqueues one kernel (none for 0
+ * rows).
+ *
+ * dora_residual_norm_backward -- the gradients, from those of y and of h, for
+ * the h that the forward pass wrote.  With g = dh + (d y / d h)^T dy:
+ *   dx = g,  du = g gate scale,  da = du or (d norm / d a)^T du
+ *   dgamma = sum_r dy (h normed),  dbeta = sum_r dy,  dscale = sum_r g gate u,
+ *   dgate = sum_c g scale u,  dpost_gamma, dpost_beta as dgamma, dbeta from du
+ * Sums over rows are fp32 in a workgroup and 64 bits across them, in a fixed
+ * order.
+ *   dy, dh     one may be NULL (no such gradient).  a is NULL where the forward
+ *              pass had none.
+ *   dx, da     may be dy, dh, h or a as a whole.  da NULL: not formed.
+ *   dgamma ... dpost_beta fp32 [C], dgate fp32 [T], each NULL or, where the
+ *              forward pass had the parameter (dbeta: or not), written whole.
+ *   workspace  device, 256-byte aligned, dora_residual_norm_workspace_size(T, C)
+ *              bytes, no required contents; calls that share it must not
+ *              overlap in time.
+ * Enqueues one kernel, two with a parameter's gradient.
+ */
+typedef enum { DORA_NORM_LAYER = 0, DORA_NORM_RMS = 1 } dora_norm;
+int dora_residual_norm(const dora_rows* x, const dora_rows* a, const float* gamma, const float* beta,
+                       const float* scale, const float* gate, const float* post_gamma, const float* post_beta,
+                       int32_t kind, float eps, const dora_rows* h_out, const dora_rows* y_out, void* stream);
+size_t dora_residual_norm_workspace_size(int64_t T, int32_t C); /* 0 when T or C is out of range */
+int dora_residual_norm_backward(const dora_rows* dy, const dora_rows* dh, const dora_rows* h, const dora_rows* a,
+                                const float* gamma, const float* scale, const float* gate, const float* post_gamma,
+                                const float* post_beta, int32_t kind, float eps, const dora_rows* dx,
+                                const dora_rows* da, float* dgamma, float* dbeta, float* dscale, float* dgate,
+                                float* dpost_gamma, float* dpost_beta, void* workspace, size_t workspace_bytes,
+                                void* stream);
+
 /* Human-readable name of a dora_status value (static string). */
 const char* dora_status_string(int status);
 

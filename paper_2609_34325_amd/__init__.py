@@ -20,7 +20,7 @@ import ctypes
 import math
 import os
 import warnings
-from typing import Optional, Tuple
+from typing import NamedTuple, Optional, Tuple
 
 import torch
 
@@ -56,6 +56,9 @@ DORA_HEAD_DIM = 64
 DORA_MAX_DECISIONS = (1 << 24) - 1
 DORA_MAX_ACTIONS = 1 << 20
 DORA_NOALLOC_WORKSPACE_BYTES = 4 << 20
+DORA_MAX_SEQUENCES = 65536
+DORA_NORM_LAYER = 0
+DORA_NORM_RMS = 1
 
 EXPORTS = (
     "dora_select_pack",
@@ -82,6 +85,14 @@ EXPORTS = (
     "dora_pl_policy_loss_cap",
     "dora_grad_clip_workspace_size",
     "dora_grad_clip",
+    "dora_rope",
+    "dora_grouped_attn_workspace_size",
+    "dora_grouped_attn_backward_workspace_size",
+    "dora_grouped_attn",
+    "dora_grouped_attn_backward",
+    "dora_residual_norm",
+    "dora_residual_norm_workspace_size",
+    "dora_residual_norm_backward",
     "dora_status_string",
 )
 
@@ -97,6 +108,8 @@ _ATTN = (("q", _ANY), ("k", _ANY), ("v", _ANY), ("cu_seqlens", _I32)) + (None,) 
 _LOGITS = (None, None, ("actions", _I32), ("legal", _I32))
 _DECISIONS = (("old_logprob", _F32), ("ref_logprob", _F32), ("advantage", _F32), ("weight", _F32))
 _LOSS_OUT = (("logprob_out", _F32), ("stats_out", _F32), ("workspace", _ANY), None) + _STATUS
+_NORM = ("gamma", "beta", "scale", "gate", "post_gamma", "post_beta")
+_NORM_GRADS = tuple("d" + n for n in ("gamma", "beta", "scale", "gate", "post_gamma", "post_beta"))
 _ENTRIES = (
     ("dora_select_pack", _PACK + (("cu_in", _I32),) + (None,) * 5 + _PACK_OUT + _STATUS),
     ("dora_select_pack_plan", _PACK + (("cu_in", _I32),) + (None,) * 5 + _PACK_OUT + (None,) * 3 +
@@ -122,11 +135,20 @@ _ENTRIES = (
     ("dora_pl_policy_loss_cap", (("scores", _F32), ("order", _I32), ("cu_order", _I32), None, ("cu_in", _I32), None) +
      _DECISIONS + (None,) * 5 + (("dscores", _F32),) + _LOSS_OUT),
     ("dora_grad_clip", (None,) * 5 + (("norm_out", _F32), ("workspace", _ANY), None, None)),
+    # Rows go by the address of their description (strided views are allowed).
+    ("dora_rope", (None, None, ("positions", _I32), None, ("freq", torch.float64)) + (None,) * 7),
+    ("dora_grouped_attn", (None,) * 3 + (("cu_q", _I32), ("cu_k", _I32)) + (None,) * 5 +
+     (("lse_out", _F32), ("workspace", _ANY), None) + _STATUS),
+    ("dora_grouped_attn_backward", (None,) * 5 + (("lse", _F32), ("cu_q", _I32), ("cu_k", _I32)) + (None,) * 7 +
+     (("workspace", _ANY), None) + _STATUS),
+    ("dora_residual_norm", (None, None) + tuple((n, _F32) for n in _NORM) + (None,) * 5),
+    ("dora_residual_norm_backward", (None,) * 4 + tuple((n, _F32) for n in _NORM if n != "beta") + (None,) * 4 +
+     tuple((n, _F32) for n in _NORM_GRADS) + (("workspace", _ANY), None, None)),
 )
 _INDEX = {name: i for i, (name, _) in enumerate(_ENTRIES)}
 
 _OPTIONAL = ("cu_in", "budget_logits", "removal_scores", "scores_out", "workspace", "legal", "weight", "ref_logprob",
-             "entropy_out")
+             "entropy_out", "lse_out") + _NORM[1:] + _NORM_GRADS
 
 _lib = None
 _native_call = None
@@ -134,6 +156,7 @@ _native_spans = None
 _native_rows = None
 _native_vectors = None
 _native_written = None
+_native_describe = None
 
 
 class FlopsConfig(ctypes.Structure):
@@ -145,6 +168,13 @@ class FlopsConfig(ctypes.Structure):
 class Span(ctypes.Structure):
     """dora_span of include/dora.h."""
     _fields_ = [("data", ctypes.c_void_p), ("numel", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
+
+
+class Rows(ctypes.Structure):
+    """dora_rows of include/dora.h."""
+    _fields_ = [("data", ctypes.c_void_p), ("rows", ctypes.c_int64), ("heads", ctypes.c_int32), ("dim", ctypes.c_int32),
+                ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("dtype", ctypes.c_int32),
                 ("reserved", ctypes.c_int32)]
 
 
@@ -160,7 +190,7 @@ def _leave_to_ctypes(*args):
 
 def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     """Load libdora.so (built in-tree by ``paper_2609_34325_amd.build``)."""
-    global _lib, _native_call, _native_spans, _native_rows, _native_vectors, _native_written
+    global _lib, _native_call, _native_spans, _native_rows, _native_vectors, _native_written, _native_describe
     if _lib is not None and path is None:
         return _lib
     p = path or LIB_PATH
@@ -226,17 +256,33 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.dora_grad_clip_workspace_size.argtypes = [i32]
     lib.dora_grad_clip.restype = ctypes.c_int
     lib.dora_grad_clip.argtypes = [vp, vp, i32, f32, f32, vp, vp, sz, vp]
+    lib.dora_rope.restype = ctypes.c_int
+    lib.dora_rope.argtypes = [vp, vp, vp, i32, vp, i32, i32, i32, f32, vp, vp, vp]
+    for name in ("dora_grouped_attn_workspace_size", "dora_grouped_attn_backward_workspace_size"):
+        getattr(lib, name).restype = sz
+        getattr(lib, name).argtypes = [i32, i32, i32, i32, i32, i64, i64]
+    lib.dora_grouped_attn.restype = ctypes.c_int
+    lib.dora_grouped_attn.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, f32, vp, vp, vp, sz, vp, vp]
+    lib.dora_grouped_attn_backward.restype = ctypes.c_int
+    lib.dora_grouped_attn_backward.argtypes = [vp] * 8 + [i32, i32, i32, f32, vp, vp, vp, vp, sz, vp, vp]
+    lib.dora_residual_norm.restype = ctypes.c_int
+    lib.dora_residual_norm.argtypes = [vp] * 8 + [i32, f32, vp, vp, vp]
+    lib.dora_residual_norm_workspace_size.restype = sz
+    lib.dora_residual_norm_workspace_size.argtypes = [i64, i32]
+    lib.dora_residual_norm_backward.restype = ctypes.c_int
+    lib.dora_residual_norm_backward.argtypes = [vp] * 9 + [i32, f32] + [vp] * 9 + [sz, vp]
     lib.dora_status_string.restype = ctypes.c_char_p
     lib.dora_status_string.argtypes = [ctypes.c_int]
     lib.addresses = tuple(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name, _ in _ENTRIES)
     if _native_call is None:
         try:
-            from ._host_call import (call as _native_call, rows as _native_rows, spans as _native_spans,
-                                     vectors as _native_vectors, written as _native_written)
+            from ._host_call import (call as _native_call, describe as _native_describe, rows as _native_rows,
+                                     spans as _native_spans, vectors as _native_vectors, written as _native_written)
         except ImportError as e:  # not built, or for another Python or torch
             warnings.warn(f"calls are marshalled by ctypes, about 5 us slower each: {e}; build the native marshalling "
                           "with `python -m paper_2609_34325_amd.build`")
             _native_call = _native_spans = _native_rows = _native_vectors = _native_written = _leave_to_ctypes
+            _native_describe = _leave_to_ctypes
     if path is None:
         _lib = lib
     return lib
@@ -905,3 +951,303 @@ def dora_grad_clip(grads, max_norm: float, out=None, eps: float = 1e-6, norm_out
     scaled = grads if out is None else out
     _written([] if out is None and max_norm == math.inf else scaled, norm_out)
     return scaled, norm_out
+
+
+def _describe(names, *tensors):
+    """Descriptions (dora_rows) of tensors [rows, heads, dim] or [rows, dim], the
+    address of each (0 for None) and their device, which is the current one."""
+    load_library()
+    rows = (Rows * len(tensors))()
+    at = ctypes.addressof(rows)
+    device = _native_describe(at, *tensors)
+    if device is NotImplemented:
+        device = -1
+        for i, (name, t) in enumerate(zip(names, tensors)):
+            if t is None:
+                continue
+            if not isinstance(t, torch.Tensor):
+                raise TypeError(f"{name} must be a torch tensor")
+            if t.layout != torch.strided or t.is_nested:
+                raise ValueError(f"{name} must be a strided tensor, not a sparse or nested one")
+            if t.dim() not in (2, 3):
+                raise ValueError(f"{name} must be [rows, dim] or [rows, heads, dim]")
+            if not t.is_cuda:
+                raise ValueError(f"{name} must be on the GPU")
+            if t.shape[-1] > 1 and t.stride(-1) != 1:
+                raise ValueError(f"{name} must have adjacent elements in each row")
+            if max(t.shape[1:]) > 0x7FFFFFFF:
+                raise ValueError(f"{name} is too wide")
+            if device >= 0 and t.get_device() != device:
+                raise ValueError(f"tensors on devices {device} and {t.get_device()}: {name}")
+            device = t.get_device()
+            heads = int(t.shape[1]) if t.dim() == 3 else 1
+            rows[i] = Rows(t.data_ptr(), t.shape[0], heads, t.shape[-1], t.stride(0), t.stride(1) if t.dim() == 3 else 0,
+                           _dtype_code(t), 0)
+    if device >= 0 and device != torch._C._cuda_getDevice():
+        raise ValueError(f"tensors on device {device}, which is not the current one")
+    size = ctypes.sizeof(Rows)
+    return rows, [0 if t is None else at + i * size for i, t in enumerate(tensors)], device
+
+
+def _like(t: torch.Tensor) -> torch.Tensor:
+    """A contiguous tensor of t's shape and type."""
+    return torch.empty(t.shape, dtype=t.dtype, device=t.device)
+
+
+def _heads(names, *tensors) -> None:
+    for name, t in zip(names, tensors):
+        if t is not None and not isinstance(t, torch.Tensor):
+            raise TypeError(f"{name} must be a torch tensor")
+        if t is not None and t.dim() != 3:
+            raise ValueError(f"{name} must be [rows, heads, dim]")
+
+
+def rope_frequencies(R: int, base: float = 10000.0, factor: float = 1.0, trained: Optional[int] = None,
+                     few: float = 1.0, many: float = 32.0, device=None) -> torch.Tensor:
+    """Angles a position for dora_rope: float64 [R / 2], base^(-2 i / R).
+
+    For contexts `factor` times the `trained` length, pairs are interpolated
+    (divided by factor) where they turn fewer than `few` times in that length,
+    left alone where more than `many` times, and blended linearly between; all
+    are interpolated without `trained`."""
+    if R < 2 or R % 2 or base <= 0 or factor <= 0 or (trained is not None and (trained < 1 or few >= many)):
+        raise ValueError("R must be even, base and factor positive, trained at least 1 and few below many")
+    freq = torch.tensor(float(base), dtype=torch.float64) ** (-2.0 * torch.arange(R // 2, dtype=torch.float64) / R)
+    if factor != 1.0:
+        keep = 0.0
+        if trained is not None:
+            keep = ((trained * freq / (2 * math.pi) - few) / (many - few)).clamp(0.0, 1.0)
+        freq = freq * keep + freq / factor * (1.0 - keep)
+    return freq.to(device or "cuda")
+
+
+def dora_rope(q: torch.Tensor, positions: torch.Tensor, freq: torch.Tensor, k: Optional[torch.Tensor] = None,
+              interleaved: bool = False, inverse: bool = False, scale: float = 1.0, q_out: Optional[torch.Tensor] = None,
+              k_out: Optional[torch.Tensor] = None, stream=None):
+    """Rotary positions of q [rows, H, D] and k [rows, Hk, D] (bf16 or fp32, any
+    strides between rows and heads).
+
+    positions: int32 [rows] or [rows, axes], each axis for its share of the pairs
+    in turn; freq: float64 [R / 2], radians per position (rope_frequencies); the
+    first R elements of each head are turned, in pairs (i, i + R / 2) or,
+    interleaved, (2 i, 2 i + 1), and multiplied by scale.  inverse turns back:
+    the gradient.  q_out and k_out may be q and k.  Returns (q_out, k_out)."""
+    if stream is not None:
+        with _in_stream(stream):
+            return dora_rope(q, positions, freq, k, interleaved, inverse, scale, q_out, k_out)
+    _heads(("q", "k"), q, k)
+    if k is None and k_out is not None:
+        raise ValueError("k_out goes with k")
+    q_out = _like(q) if q_out is None else q_out
+    k_out = _like(k) if k is not None and k_out is None else k_out
+    rows, at, device = _describe(("q", "k", "q_out", "k_out"), q, k, q_out, k_out)
+    axes = 1 if positions.dim() == 1 else int(positions.shape[-1])
+    if positions.dim() not in (1, 2) or int(positions.shape[0]) != int(q.shape[0]) or freq.dim() != 1:
+        raise ValueError("positions must be [rows] or [rows, axes], freq [R / 2]")
+    if freq.dtype != torch.float64:
+        raise TypeError(f"freq must be {torch.float64}, got {freq.dtype}")
+    _vectors(("positions", "freq"), device, -1, positions, -1, freq)
+    _call("dora_rope", None, at[0], at[1], positions, axes, freq, 2 * freq.numel(), int(bool(interleaved)),
+          int(bool(inverse)), float(scale), at[2], at[3])
+    _written(q_out) if k_out is None else _written(q_out, k_out)
+    return q_out, k_out
+
+
+def dora_grouped_attn_workspace_size(B: int, H: int, Hk: int, D: int, max_q: int, total_q: int, total_k: int) -> int:
+    return int(load_library().dora_grouped_attn_workspace_size(B, H, Hk, D, max_q, total_q, total_k))
+
+
+def dora_grouped_attn_backward_workspace_size(B: int, H: int, Hk: int, D: int, max_q: int, total_q: int,
+                                              total_k: int) -> int:
+    return int(load_library().dora_grouped_attn_backward_workspace_size(B, H, Hk, D, max_q, total_q, total_k))
+
+
+def new_grouped_attn_workspace(B: int, H: int, Hk: int, D: int, max_q: int, total_q: int, total_k: int,
+                               backward: bool = False, device=None) -> torch.Tensor:
+    """A workspace for dora_grouped_attn, and with `backward` for its backward pass too (no required contents)."""
+    sizes = (int(B), int(H), int(Hk), int(D), int(max_q), int(total_q), int(total_k))
+    n = dora_grouped_attn_workspace_size(*sizes)
+    if backward:
+        n = max(n, dora_grouped_attn_backward_workspace_size(*sizes))
+    return _new_bytes("dora_grouped_attn_workspace_size", n, device)
+
+
+def _sequences(cu_q, cu_k):
+    if not isinstance(cu_q, torch.Tensor) or cu_q.dim() != 1 or cu_q.numel() < 2:
+        raise ValueError("cu_q must be [B + 1]")
+    return int(cu_q.shape[0]) - 1, cu_q if cu_k is None else cu_k
+
+
+def dora_grouped_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.Tensor, max_q: int,
+                      cu_k: Optional[torch.Tensor] = None, causal: bool = False, softmax_scale: float = 0.0,
+                      out: Optional[torch.Tensor] = None, lse_out: Optional[torch.Tensor] = None, keep_lse: bool = True,
+                      workspace: Optional[torch.Tensor] = None, dev_status: Optional[torch.Tensor] = None, stream=None):
+    """softmax(scale q k^T) v inside packed sequences with grouped heads.
+
+    q: [total_q, H, D]; k, v: [total_k, Hk, D], H a multiple of Hk, D 32, 64 or
+    128, bf16 or fp32, any strides of 16 bytes; cu_q, cu_k (cu_q when None):
+    int32 [B + 1]; max_q: no sequence has more queries.  causal: query i of nq
+    sees the keys j <= i + nk - nq, so one new token sees all.  Returns (out
+    [total_q, H, D], lse [total_q, H] fp32 or None without keep_lse, dev_status)."""
+    if stream is not None:
+        with _in_stream(stream):
+            return dora_grouped_attn(q, k, v, cu_q, max_q, cu_k, causal, softmax_scale, out, lse_out, keep_lse,
+                                     workspace, dev_status)
+    _heads(("q", "k", "v"), q, k, v)
+    B, cu_k = _sequences(cu_q, cu_k)
+    dev = q.device
+    out = _like(q) if out is None else out
+    total_q, H, D = q.shape
+    if lse_out is None and keep_lse:
+        lse_out = torch.empty((total_q, H), dtype=torch.float32, device=dev)
+    if lse_out is not None and lse_out.shape != q.shape[:2]:
+        raise ValueError("lse_out must be [total_q, H]")
+    if workspace is None:
+        workspace = new_grouped_attn_workspace(B, H, k.shape[1], D, max_q, total_q, k.shape[0], device=dev)
+    dev_status = new_status(dev) if dev_status is None else dev_status
+    rows, at, device = _describe(("q", "k", "v", "out"), q, k, v, out)
+    _vectors(("cu_q", "cu_k", "lse_out", "workspace", "dev_status"), device, B + 1, cu_q, B + 1, cu_k, -1, lse_out,
+             -1, workspace, -1, dev_status)
+    _call("dora_grouped_attn", None, at[0], at[1], at[2], cu_q, cu_k, B, int(max_q), int(bool(causal)),
+          float(softmax_scale), at[3], lse_out, workspace, _bytes(workspace), dev_status)
+    _written(out) if lse_out is None else _written(out, lse_out)
+    return out, lse_out, dev_status
+
+
+def dora_grouped_attn_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                               out: torch.Tensor, lse: torch.Tensor, cu_q: torch.Tensor, max_q: int,
+                               cu_k: Optional[torch.Tensor] = None, causal: bool = False, softmax_scale: float = 0.0,
+                               dq: Optional[torch.Tensor] = None, dk: Optional[torch.Tensor] = None,
+                               dv: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                               dev_status: Optional[torch.Tensor] = None, stream=None):
+    """Gradients of dora_grouped_attn from the output's, dout: out and lse as the
+    forward call returned them, the other arguments as it had them.  dq, dk and
+    dv may be slices of one tensor.  Returns (dq, dk, dv, dev_status)."""
+    if stream is not None:
+        with _in_stream(stream):
+            return dora_grouped_attn_backward(dout, q, k, v, out, lse, cu_q, max_q, cu_k, causal, softmax_scale, dq, dk,
+                                              dv, workspace, dev_status)
+    _heads(("q", "k", "v"), q, k, v)
+    B, cu_k = _sequences(cu_q, cu_k)
+    dev = q.device
+    dq, dk, dv = (_like(t) if g is None else g for t, g in ((q, dq), (k, dk), (v, dv)))
+    total_q, H, D = q.shape
+    if not isinstance(lse, torch.Tensor) or lse.shape != q.shape[:2]:
+        raise ValueError("lse must be [total_q, H]")
+    if workspace is None:
+        n = dora_grouped_attn_backward_workspace_size(B, H, k.shape[1], D, int(max_q), total_q, k.shape[0])
+        workspace = _new_bytes("dora_grouped_attn_backward_workspace_size", n, dev)
+    dev_status = new_status(dev) if dev_status is None else dev_status
+    rows, at, device = _describe(("dout", "q", "k", "v", "out", "dq", "dk", "dv"), dout, q, k, v, out, dq, dk, dv)
+    _vectors(("lse", "cu_q", "cu_k", "workspace", "dev_status"), device, -1, lse, B + 1, cu_q, B + 1, cu_k, -1, workspace,
+             -1, dev_status)
+    _call("dora_grouped_attn_backward", None, *at[:5], lse, cu_q, cu_k, B, int(max_q), int(bool(causal)),
+          float(softmax_scale), *at[5:], workspace, _bytes(workspace), dev_status)
+    _written(dq, dk, dv)
+    return dq, dk, dv, dev_status
+
+
+def dora_residual_norm_workspace_size(T: int, C: int) -> int:
+    return int(load_library().dora_residual_norm_workspace_size(int(T), int(C)))
+
+
+def new_residual_norm_workspace(T: int, C: int, device=None) -> torch.Tensor:
+    """A workspace for dora_residual_norm_backward (no required contents)."""
+    return _new_bytes("dora_residual_norm_workspace_size", dora_residual_norm_workspace_size(T, C), device)
+
+
+_NORM_KINDS = {"layer": DORA_NORM_LAYER, "rms": DORA_NORM_RMS}
+
+
+def _norm_kind(kind: str) -> int:
+    if kind not in _NORM_KINDS:
+        raise ValueError(f"kind must be 'layer' or 'rms', not {kind!r}")
+    return _NORM_KINDS[kind]
+
+
+def _matrix(t, name: str):
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor")
+    if t.dim() != 2:
+        raise ValueError(f"{name} must be [T, C]")
+    return int(t.shape[0]), int(t.shape[1])
+
+
+def dora_residual_norm(x: torch.Tensor, a: Optional[torch.Tensor], gamma: torch.Tensor,
+                       beta: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
+                       gate: Optional[torch.Tensor] = None, post_gamma: Optional[torch.Tensor] = None,
+                       post_beta: Optional[torch.Tensor] = None, kind: str = "layer", eps: float = 1e-6,
+                       h_out: Optional[torch.Tensor] = None, y_out: Optional[torch.Tensor] = None, stream=None):
+    """h = x + gate scale u and y = norm(h), u the branch's output a or (with
+    post_gamma) its norm.
+
+    x, a: [T, C] bf16 or fp32, rows any distance apart; a None: the norm of x
+    alone.  gamma, beta, scale (layer scale), post_gamma, post_beta: fp32 [C];
+    gate: fp32 [T], 0 drops a row's branch.  kind: "layer" or "rms".  h_out and
+    y_out may be x or a.  Returns (h, y); h is x itself without a."""
+    if stream is not None:
+        with _in_stream(stream):
+            return dora_residual_norm(x, a, gamma, beta, scale, gate, post_gamma, post_beta, kind, eps, h_out, y_out)
+    T, C = _matrix(x, "x")
+    code = _norm_kind(kind)
+    h_out = _like(x) if h_out is None and a is not None else h_out
+    y_out = _like(x) if y_out is None else y_out
+    rows, at, device = _describe(("x", "a", "h_out", "y_out"), x, a, h_out, y_out)
+    _vectors(_NORM, device, C, gamma, C, beta, C, scale, T, gate, C, post_gamma, C, post_beta)
+    _call("dora_residual_norm", None, at[0], at[1], gamma, beta, scale, gate, post_gamma, post_beta, code, float(eps),
+          at[2], at[3])
+    _written(y_out) if h_out is None else _written(h_out, y_out)
+    return x if h_out is None else h_out, y_out
+
+
+class ResidualNormGrads(NamedTuple):
+    """Gradients of dora_residual_norm's arguments; None where it had none."""
+    dx: torch.Tensor
+    da: Optional[torch.Tensor]
+    dgamma: torch.Tensor
+    dbeta: Optional[torch.Tensor]
+    dscale: Optional[torch.Tensor]
+    dgate: Optional[torch.Tensor]
+    dpost_gamma: Optional[torch.Tensor]
+    dpost_beta: Optional[torch.Tensor]
+
+
+def dora_residual_norm_backward(dy: Optional[torch.Tensor], h: torch.Tensor, a: Optional[torch.Tensor],
+                                gamma: torch.Tensor, beta: Optional[torch.Tensor] = None,
+                                scale: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None,
+                                post_gamma: Optional[torch.Tensor] = None, post_beta: Optional[torch.Tensor] = None,
+                                dh: Optional[torch.Tensor] = None, kind: str = "layer", eps: float = 1e-6,
+                                dx: Optional[torch.Tensor] = None, da: Optional[torch.Tensor] = None,
+                                dgamma: Optional[torch.Tensor] = None, dbeta: Optional[torch.Tensor] = None,
+                                dscale: Optional[torch.Tensor] = None, dgate: Optional[torch.Tensor] = None,
+                                dpost_gamma: Optional[torch.Tensor] = None, dpost_beta: Optional[torch.Tensor] = None,
+                                workspace: Optional[torch.Tensor] = None, stream=None) -> ResidualNormGrads:
+    """Gradients of dora_residual_norm from those of y (dy) and of h (dh; either
+    may be None), for the h that it returned.  The branch's gradient is dx itself
+    where it has neither scale, gate nor norm (and da is None).  dx and da may be
+    dy, dh, h or a.  The parameters' gradients are fp32 in their shapes."""
+    if stream is not None:
+        with _in_stream(stream):
+            return dora_residual_norm_backward(dy, h, a, gamma, beta, scale, gate, post_gamma, post_beta, dh, kind, eps, dx,
+                                               da, dgamma, dbeta, dscale, dgate, dpost_gamma, dpost_beta, workspace)
+    T, C = _matrix(h, "h")
+    code = _norm_kind(kind)
+    dx = _like(h) if dx is None else dx
+    same = a is not None and da is None and scale is None and gate is None and post_gamma is None
+    if a is not None and da is None and not same:
+        da = _like(h)
+    workspace = new_residual_norm_workspace(T, C, h.device) if workspace is None else workspace
+    grads = [dgamma, dbeta, dscale, dgate, dpost_gamma, dpost_beta]
+    sizes = (C, C, C, T, C, C)
+    for i, (t, name) in enumerate(zip((gamma, beta, scale, gate, post_gamma, post_beta), _NORM_GRADS)):
+        if t is None and grads[i] is not None:
+            raise ValueError(f"{name} without {name[1:]}")
+        if t is not None and grads[i] is None:
+            grads[i] = torch.empty(sizes[i], dtype=torch.float32, device=h.device)
+    rows, at, device = _describe(("dy", "dh", "h", "a", "dx", "da"), dy, dh, h, None if same else a, dx, da)
+    _vectors(_NORM + ("workspace",) + _NORM_GRADS, device, C, gamma, C, beta, C, scale, T, gate, C, post_gamma, C,
+             post_beta, -1, workspace, *(x for pair in zip(sizes, grads) for x in pair))
+    _call("dora_residual_norm_backward", None, *at[:4], gamma, scale, gate, post_gamma, post_beta, code,
+          float(eps), at[4], at[5], *grads, workspace, _bytes(workspace))
+    _written(*(t for t in (dx, da, *grads) if t is not None))
+    return ResidualNormGrads(dx, dx if same else da, *grads)

@@ -21,6 +21,8 @@ CALIB_LIB = os.path.join(PKG, "libdora_calibrate.so")
 CALIB_SOURCES = ["calibrate.hip"]
 SOURCES = ["select_pack.hip", "varlen_attn.hip", "actor_decode.hip", "pl_sample.hip", "lc1_readout.hip", "flops.hip"]
 POLICY_SOURCES = ["policy_loss.hip", "pl_policy.hip", "grad_clip.hip"]
+# The transformer block's operators, built as the policy kernels are.
+BLOCK_SOURCES = ["grouped_attn.hip", "rope.hip", "residual_norm.hip"]
 # Native marshalling of the Python binding (host code only).
 HOST_LIB = os.path.join(PKG, "_host_call.so")
 ARCH = "gfx950"
@@ -61,7 +63,8 @@ def hipcc() -> str:
 
 
 def build(verbose: bool = False) -> str:
-    _build_lib([(s, HIPCC_FLAGS) for s in SOURCES] + [(s, POLICY_FLAGS) for s in POLICY_SOURCES], LIB, verbose)
+    _build_lib([(s, HIPCC_FLAGS) for s in SOURCES] + [(s, POLICY_FLAGS) for s in POLICY_SOURCES + BLOCK_SOURCES],
+               LIB, verbose)
     _build_lib([(s, HIPCC_FLAGS) for s in CALIB_SOURCES], CALIB_LIB, verbose)
     _build_host(verbose)
     return LIB

@@ -1,0 +1,916 @@
+// Attention over packed sequences with grouped heads, forward and backward: the
+// training and language-model form of varlen_attn.hip (own boundaries for
+// queries and keys, causal or full, 32/64/128-wide heads, bf16 or fp32).
+//
+// The G = H / Hk heads that read one key head are stacked: sequence b and key
+// head hk make one problem of nq G rows (row r = query r / G of head hk G + r %
+// G) against nk keys, with limit(r) = the keys that row r sees, nk or, causal,
+// r / G + 1 + nk - nq.  Keys and values are then read once for the G heads, dk
+// and dv are sums over rows like any other, and one query of many heads fills a
+// tile.  With c = softmax_scale log2(e):
+//   s = c q k^T,  m = max s,  p = 2^(s - m),  l = sum p
+//   out = p v / l,  lse = (m + log2 l) ln 2
+// in one pass over the keys, m, l and the products' sums in fp32.  Backward,
+// P = 2^(s - lse log2 e), delta = rowsum(dout out):
+//   grad_q   a tile of rows over the keys:  dS = P (dout v^T - delta), dq += dS k
+//   grad_kv  a tile of keys over the rows:  dv += P^T dout, dk += dS^T q
+// Each forms P and dS for itself (seven products in place of five), so that no
+// sum goes through memory and results do not depend on timing.
+//
+// Tiles of sequences are found without a plan: tile t of all belongs to the last
+// b with floor(cu[b] G / tile) + b <= t.  That leaves each sequence at least its
+// tiles' numbers, and at most total / tile + B numbers in all, which the host
+// knows; every wave looks its sequence up with ballots over 64 boundaries.
+#include <math.h>
+
+#include <algorithm>
+
+#include "dora_internal.h"
+#include "rows.h"
+
+namespace dora {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kTile = 64;  // rows (keys in grad_kv) of a workgroup, 16 a wave
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+struct AttnArgs {
+  RowView q, k, v, out, dout, dq, dk, dv;
+  const int32_t* cu_q;
+  const int32_t* cu_k;
+  int32_t B, H, Hk, G;
+  uint32_t g_mul, g_shift;  // r / G = mulhi(r, g_mul) >> g_shift for r < 2^31, G > 1
+  int64_t total_q, total_k;
+  int32_t max_q, causal;
+  float scale, c2;  // softmax_scale, softmax_scale * log2(e)
+  float* lse;
+  float* delta;
+  float* part;       // split sums
+  float2* part_ml;   // of a row's part: m and l
+  int32_t part_rows;  // rows of a part
+  int32_t splits;     // parts of a tile's keys (forward) or of a tile's rows (grad_kv)
+  int32_t chunk;      // or: keys of a part, every sequence one tile of rows
+  int32_t blocks;
+  int32_t* status;
+};
+
+__device__ __forceinline__ int div_group(const AttnArgs& a, int r) {
+  return a.G == 1 ? r : static_cast<int>(__umulhi(static_cast<uint32_t>(r), a.g_mul) >> a.g_shift);
+}
+
+// First tile number of sequence b.
+__device__ __forceinline__ int64_t first_tile(const int32_t* cu, int b, int mul, int tile) {
+  return static_cast<int64_t>(max(cu[b], 0)) * mul / tile + b;
+}
+
+// The last b with first(b) <= t; every lane of the wave calls it.
+template <class F>
+__device__ __forceinline__ int last_at_most(int B, int64_t t, F first) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, n = B;
+  while (n > 1) {
+    const int stride = (n + 63) >> 6, at = lane * stride;
+    const uint64_t hit = __ballot(at < n && first(lo + at) <= t);
+    const int step = hit ? (63 - __builtin_clzll(hit)) * stride : 0;
+    lo += step;
+    n = min(stride, n - step);
+  }
+  return __builtin_amdgcn_readfirstlane(lo);
+}
+
+struct Seq {
+  int q0, nq, k0, nk;
+};
+
+// Sequence b; nothing of it where its boundaries are no good.
+__device__ __forceinline__ bool sequence(const AttnArgs& a, int b, Seq* s) {
+  const int q0 = a.cu_q[b], q1 = a.cu_q[b + 1], k0 = a.cu_k[b], k1 = a.cu_k[b + 1];
+  if (q0 < 0 || q1 < q0 || q1 > a.total_q || k0 < 0 || k1 < k0 || k1 > a.total_k || q1 - q0 > a.max_q) return false;
+  *s = Seq{q0, q1 - q0, k0, k1 - k0};
+  return true;
+}
+
+// The grid's last workgroup looks at every boundary.
+__device__ __forceinline__ bool check_block(const AttnArgs& a) {
+  if (static_cast<int>(blockIdx.x) < a.blocks) return false;
+  bool bad = false;
+  Seq s;
+  for (int b = threadIdx.x; b < a.B; b += kThreads) bad |= !sequence(a, b, &s);
+  if (bad) atomicOr(a.status, DORA_DEV_CU_SEQLENS);
+  return true;
+}
+
+// Keys that row r sees.
+__device__ __forceinline__ int limit_of(const AttnArgs& a, const Seq& s, int r) {
+  if (r >= s.nq * a.G) return 0;
+  return a.causal ? max(0, min(s.nk, div_group(a, r) + 1 + s.nk - s.nq)) : s.nk;
+}
+
+__device__ __forceinline__ const char* query_row(const AttnArgs& a, const RowView& x, const Seq& s, int hk, int r) {
+  const int i = div_group(a, r);
+  return x.at + (static_cast<int64_t>(s.q0) + i) * x.row + static_cast<int64_t>(hk * a.G + r - i * a.G) * x.head;
+}
+__device__ __forceinline__ int64_t stat_at(const AttnArgs& a, const Seq& s, int hk, int r) {
+  const int i = div_group(a, r);
+  return (static_cast<int64_t>(s.q0) + i) * a.H + hk * a.G + r - i * a.G;
+}
+
+// Operands of a 16x16 product in steps of 32: lane l (g = l / 16, c = l % 16)
+// holds eight elements of row or column c, at 8g .. 8g + 7 of the step; the
+// result's lane holds column c, rows 4g .. 4g + 3.
+template <class E>
+struct Op;
+
+template <>
+struct Op<__bf16> {
+  typedef bf16x8 Frag;
+  static constexpr int kKeys = 64;  // rows of a staged tile
+  static constexpr int kPad = 8;    // elements after a staged row: its 16-byte pieces move on by one bank group a row
+  static __device__ __forceinline__ floatx4 mma(Frag a, Frag b, floatx4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+  }
+  // Two results of 16 rows as the eight elements of a step (in the order of columns()).
+  static __device__ __forceinline__ Frag pack(floatx4 x, floatx4 y) {
+    Frag f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = static_cast<__bf16>(x[i]), f[4 + i] = static_cast<__bf16>(y[i]);
+    return f;
+  }
+  // Column d0 + c of staged rows 4g .. 4g + 3 and 16 + 4g .. 16 + 4g + 3: the transposing read hands
+  // lane j of a group element j of the rows that lanes 4e + j / 4 point at.
+  template <int LD>
+  static __device__ __forceinline__ Frag columns(const __bf16* rows, int d0) {
+    typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
+    const int lane = threadIdx.x & 63, g = lane >> 4, e = (lane & 15) >> 2, r = lane & 3;
+    __bf16* p = const_cast<__bf16*>(rows) + (4 * g + e) * LD + d0 + 4 * r;
+    const bf16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)p);
+    const bf16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(p + 16 * LD));
+    return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+  }
+};
+
+struct alignas(16) float8 {
+  float v[8];
+};
+template <>
+struct Op<float> {
+  typedef float8 Frag;
+  static constexpr int kKeys = 32;
+  static constexpr int kPad = 4;
+  // Eight fp32 products of four: the step's element 8g + j is term g of product j, on both sides.
+  static __device__ __forceinline__ floatx4 mma(const Frag& a, const Frag& b, floatx4 c) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[j], b.v[j], c, 0, 0, 0);
+    return c;
+  }
+  static __device__ __forceinline__ Frag pack(floatx4 x, floatx4 y) {
+    Frag f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f.v[i] = x[i], f.v[4 + i] = y[i];
+    return f;
+  }
+  template <int LD>
+  static __device__ __forceinline__ Frag columns(const float* rows, int d0) {
+    const int lane = threadIdx.x & 63, g = lane >> 4;
+    const float* p = rows + 4 * g * LD + d0 + (lane & 15);
+    Frag f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f.v[i] = p[i * LD], f.v[4 + i] = p[(16 + i) * LD];
+    return f;
+  }
+};
+
+template <class E>
+__device__ __forceinline__ typename Op<E>::Frag zero_frag() {
+  typename Op<E>::Frag f;
+  __builtin_memset(&f, 0, sizeof f);
+  return f;
+}
+// Eight adjacent elements.
+template <class E>
+__device__ __forceinline__ typename Op<E>::Frag load_frag(const void* p) {
+  return *static_cast<const typename Op<E>::Frag*>(p);
+}
+
+template <class E>
+__device__ __forceinline__ bool finite_piece(u32x4 w) {
+  bool ok = true;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (sizeof(E) == 4) ok = ok && (w[i] & 0x7F800000u) != 0x7F800000u;
+    else ok = ok && (w[i] & 0x7F80u) != 0x7F80u && (w[i] & 0x7F800000u) != 0x7F800000u;
+  }
+  return ok;
+}
+
+// A tile of rows on its way from memory to LDS, through registers: asked for
+// while the tile before it is worked on.  Rows at n and past it are 0.
+template <class E, int D>
+struct Staged {
+  static constexpr int kRows = Op<E>::kKeys, kLd = D + Op<E>::kPad;
+  static constexpr int kRowPieces = D * sizeof(E) / 16, kPieces = kRows * kRowPieces / kThreads;
+  static_assert(kPieces >= 1, "every thread moves a piece");
+  u32x4 w[kPieces];
+  // address(row of the tile): its first element
+  template <class F>
+  __device__ __forceinline__ void load(int n, F address) {
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const int p = threadIdx.x + i * kThreads, row = p / kRowPieces;
+      w[i] = row < n ? *reinterpret_cast<const u32x4*>(address(row) + p % kRowPieces * 16) : u32x4{0u, 0u, 0u, 0u};
+    }
+  }
+  __device__ __forceinline__ void store(E* lds) const {
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const int p = threadIdx.x + i * kThreads;
+      *reinterpret_cast<u32x4*>(reinterpret_cast<char*>(lds + p / kRowPieces * kLd) + p % kRowPieces * 16) = w[i];
+    }
+  }
+  __device__ __forceinline__ bool finite() const {
+    bool ok = true;
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) ok = ok && finite_piece<E>(w[i]);
+    return ok;
+  }
+};
+
+// Four adjacent elements, rounded once.
+template <class E>
+__device__ __forceinline__ void store4(char* p, floatx4 x) {
+  if (sizeof(E) == 4) {
+    *reinterpret_cast<floatx4*>(p) = x;
+  } else {
+    bf16x4 y;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = static_cast<__bf16>(x[i]);
+    *reinterpret_cast<bf16x4*>(p) = y;
+  }
+}
+
+__device__ __forceinline__ float over_groups_max(float x) {
+  x = fmaxf(x, __shfl_xor(x, 16));
+  return fmaxf(x, __shfl_xor(x, 32));
+}
+__device__ __forceinline__ float over_groups_sum(float x) {
+  x += __shfl_xor(x, 16);
+  return x + __shfl_xor(x, 32);
+}
+
+// ------------------------------- forward ----------------------------------
+
+// One tile of 64 rows against a range of its keys.  s^T = k q^T leaves each lane
+// one row's column, so its maximum and sum are mostly in the lane, and p goes
+// into out^T += v^T p^T from the registers where it stands.
+template <class E, int D, bool SPLIT>
+__global__ __launch_bounds__(kThreads) void attn_kernel(AttnArgs a) {
+  typedef typename Op<E>::Frag Frag;
+  typedef Staged<E, D> Tile;
+  constexpr int kKeys = Tile::kRows, kLd = Tile::kLd, kSteps = kKeys / 16;
+  __shared__ alignas(16) E ks[kKeys * kLd];
+  __shared__ alignas(16) E vs[kKeys * kLd];
+  if (check_block(a)) return;
+  const int lane = threadIdx.x & 63, c16 = lane & 15, g = lane >> 4, wave = threadIdx.x >> 6;
+  const int hk = blockIdx.x % a.Hk, rest = blockIdx.x / a.Hk;
+  const int split = SPLIT && !a.chunk ? rest % a.splits : 0, t = SPLIT && !a.chunk ? rest / a.splits : rest;
+  Seq s;
+  int tile = 0, key_lo = 0, key_hi;
+  if (SPLIT && a.chunk) {
+    const int b = last_at_most(a.B, t, [&](int i) { return first_tile(a.cu_k, i, 1, a.chunk); });
+    if (!sequence(a, b, &s)) return;
+    const int64_t part = t - first_tile(a.cu_k, b, 1, a.chunk);
+    if (part < 0 || part * a.chunk >= s.nk || s.nq == 0) return;
+    key_lo = static_cast<int>(part) * a.chunk;
+    key_hi = min(s.nk, key_lo + a.chunk);
+  } else {
+    const int b = last_at_most(a.B, t, [&](int i) { return first_tile(a.cu_q, i, a.G, kTile); });
+    if (!sequence(a, b, &s)) return;
+    const int64_t at = t - first_tile(a.cu_q, b, a.G, kTile);
+    if (at < 0 || at * kTile >= static_cast<int64_t>(s.nq) * a.G) return;
+    tile = static_cast<int>(at);
+    key_hi = limit_of(a, s, min((tile + 1) * kTile, s.nq * a.G) - 1);
+    if (SPLIT) {
+      const int each = ((key_hi + a.splits - 1) / a.splits + kKeys - 1) / kKeys * kKeys;
+      key_lo = min(key_hi, split * each);
+      key_hi = min(key_hi, key_lo + each);
+    }
+  }
+  const int row = tile * kTile + wave * 16 + c16;
+  const bool real = row < s.nq * a.G;
+  const int limit = limit_of(a, s, row);
+  // Keys below this are seen by every row of the tile that exists.
+  const int open = limit_of(a, s, tile * kTile);
+  Frag qf[D / 32];
+#pragma unroll
+  for (int ks32 = 0; ks32 < D / 32; ++ks32)
+    qf[ks32] = real ? load_frag<E>(query_row(a, a.q, s, hk, row) + (32 * ks32 + 8 * g) * sizeof(E)) : zero_frag<E>();
+  floatx4 o[D / 16];
+#pragma unroll
+  for (int dt = 0; dt < D / 16; ++dt) o[dt] = floatx4{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;
+  const char* kbase = a.k.at + static_cast<int64_t>(s.k0) * a.k.row + hk * a.k.head;
+  const char* vbase = a.v.at + static_cast<int64_t>(s.k0) * a.v.row + hk * a.v.head;
+  Tile kt, vt;
+  const auto ask = [&](int key) {
+    kt.load(s.nk - key, [&](int i) { return kbase + static_cast<int64_t>(key + i) * a.k.row; });
+    vt.load(s.nk - key, [&](int i) { return vbase + static_cast<int64_t>(key + i) * a.v.row; });
+  };
+  if (key_lo < key_hi) ask(key_lo);
+  for (int key = key_lo; key < key_hi; key += kKeys) {
+    const bool masked = key + kKeys > open || key + kKeys > key_hi;
+    bool odd = false;  // a value that is not finite where some row may not see it
+    __syncthreads();
+    kt.store(ks);
+    vt.store(vs);
+    if (masked) odd = __syncthreads_or(!vt.finite());
+    else __syncthreads();
+    if (key + kKeys < key_hi) ask(key + kKeys);
+    floatx4 sc[kSteps];
+#pragma unroll
+    for (int kt16 = 0; kt16 < kSteps; ++kt16) {
+      sc[kt16] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ks32 = 0; ks32 < D / 32; ++ks32)
+        sc[kt16] = Op<E>::mma(load_frag<E>(ks + (kt16 * 16 + c16) * kLd + 32 * ks32 + 8 * g), qf[ks32], sc[kt16]);
+    }
+    const int end = min(limit, key_hi) - key;
+    if (masked) {
+#pragma unroll
+      for (int kt16 = 0; kt16 < kSteps; ++kt16)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (kt16 * 16 + 4 * g + i >= end) sc[kt16][i] = -INFINITY;
+    }
+    float top = -INFINITY;
+#pragma unroll
+    for (int kt16 = 0; kt16 < kSteps; ++kt16)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) top = fmaxf(top, sc[kt16][i]);
+    top = over_groups_max(top) * a.c2;
+    const float next = fmaxf(m, top), ref = next == -INFINITY ? 0.f : next;
+    const float keep = __builtin_amdgcn_exp2f(m - ref);
+    m = next;
+    float sum = 0.f;
+#pragma unroll
+    for (int kt16 = 0; kt16 < kSteps; ++kt16)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        sc[kt16][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[kt16][i], a.c2, -ref));
+        sum += sc[kt16][i];
+      }
+    l = l * keep + sum;
+#pragma unroll
+    for (int dt = 0; dt < D / 16; ++dt) o[dt] *= keep;
+    if (!odd) {
+#pragma unroll
+      for (int st = 0; st < kSteps / 2; ++st) {
+        const Frag p = Op<E>::pack(sc[2 * st], sc[2 * st + 1]);
+#pragma unroll
+        for (int dt = 0; dt < D / 16; ++dt)
+          o[dt] = Op<E>::mma(Op<E>::template columns<kLd>(vs + st * 32 * kLd, dt * 16), p, o[dt]);
+      }
+    } else {  // 0 times such a value is NaN: key by key, and only those that the row sees
+#pragma unroll
+      for (int kt16 = 0; kt16 < kSteps; ++kt16)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          for (int og = 0; og < 4; ++og) {
+            const float p = __shfl(sc[kt16][i], og * 16 + c16);
+            const int at = kt16 * 16 + 4 * og + i;
+            if (at < end) {
+#pragma unroll
+              for (int dt = 0; dt < D / 16; ++dt)
+#pragma unroll
+                for (int x = 0; x < 4; ++x)
+                  o[dt][x] = __builtin_fmaf(p, static_cast<float>(vs[at * kLd + dt * 16 + 4 * g + x]), o[dt][x]);
+            }
+          }
+    }
+  }
+  l = over_groups_sum(l);
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  if (!real) return;
+  if (SPLIT) {
+    const int64_t at = (static_cast<int64_t>(rest) * a.Hk + hk) * a.part_rows + row - tile * kTile;
+    if (g == 0) a.part_ml[at] = make_float2(m, l);
+#pragma unroll
+    for (int dt = 0; dt < D / 16; ++dt) *reinterpret_cast<floatx4*>(a.part + at * D + dt * 16 + 4 * g) = o[dt];
+    return;
+  }
+  if (g == 0 && a.lse) a.lse[stat_at(a, s, hk, row)] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+  char* to = const_cast<char*>(query_row(a, a.out, s, hk, row));
+#pragma unroll
+  for (int dt = 0; dt < D / 16; ++dt) store4<E>(to + (dt * 16 + 4 * g) * sizeof(E), o[dt] * inv);
+}
+
+// The parts of a row joined: one wave a row, out = sum w o / sum w l with w =
+// 2^(m - max m).
+template <class E, int D>
+__global__ __launch_bounds__(kThreads) void join_kernel(AttnArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int64_t at = static_cast<int64_t>(blockIdx.x) * (kThreads / 64) + (threadIdx.x >> 6);
+  if (at >= a.total_q * a.H) return;
+  const int64_t n = at / a.H;
+  const int h = static_cast<int>(at - n * a.H), hk = h / a.G;
+  const int b = last_at_most(a.B, n, [&](int i) { return static_cast<int64_t>(a.cu_q[i]); });
+  Seq s;
+  if (!sequence(a, b, &s) || n < s.q0 || n >= static_cast<int64_t>(s.q0) + s.nq) return;
+  const int row = static_cast<int>(n - s.q0) * a.G + h - hk * a.G;
+  int64_t first;
+  int parts, in = row;
+  if (a.chunk) {
+    first = first_tile(a.cu_k, b, 1, a.chunk);
+    parts = (s.nk + a.chunk - 1) / a.chunk;
+  } else {
+    first = (first_tile(a.cu_q, b, a.G, kTile) + row / kTile) * a.splits;
+    parts = a.splits;
+    in = row % kTile;
+  }
+  const auto slot = [&](int p) { return ((first + p) * a.Hk + hk) * a.part_rows + in; };
+  float top = -INFINITY;
+  for (int p = lane; p < parts; p += 64) top = fmaxf(top, a.part_ml[slot(p)].x);
+#pragma unroll
+  for (int x = 1; x < 64; x *= 2) top = fmaxf(top, __shfl_xor(top, x));
+  const float ref = top == -INFINITY ? 0.f : top;
+  constexpr int kEach = D >= 64 ? D / 64 : 1;
+  float sum = 0.f, o[kEach] = {};
+  const int d = lane * kEach;
+  for (int p = 0; p < parts; ++p) {
+    const int64_t i = slot(p);
+    const float2 ml = a.part_ml[i];
+    if (ml.x == -INFINITY && ml.y == 0.f) continue;  // sees none of these keys
+    const float w = __builtin_amdgcn_exp2f(ml.x - ref);
+    sum = __builtin_fmaf(w, ml.y, sum);
+    if (d < D)
+#pragma unroll
+      for (int x = 0; x < kEach; ++x) o[x] = __builtin_fmaf(w, a.part[i * D + d + x], o[x]);
+  }
+  // NaN scores: the parts' l are NaN and pass through the sums.
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  if (lane == 0 && a.lse) a.lse[at] = sum == 0.f ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * kLn2;
+  if (d < D) {
+    E* to = reinterpret_cast<E*>(a.out.at + n * a.out.row + h * a.out.head) + d;
+#pragma unroll
+    for (int x = 0; x < kEach; ++x) to[x] = static_cast<E>(o[x] * inv);
+  }
+}
+
+// ------------------------------- backward ---------------------------------
+
+// log2 of the row's sum of exponentials; a row without any gets one that makes every P 0.
+__device__ __forceinline__ float row_lse2(const AttnArgs& a, const Seq& s, int hk, int row, bool real) {
+  const float lse = real ? a.lse[stat_at(a, s, hk, row)] : -INFINITY;
+  return lse == -INFINITY ? INFINITY : lse * kLog2e;
+}
+
+// dq of 64 rows over their keys; also delta of each row, for grad_kv.
+template <class E, int D>
+__global__ __launch_bounds__(kThreads) void grad_q_kernel(AttnArgs a) {
+  typedef typename Op<E>::Frag Frag;
+  typedef Staged<E, D> Tile;
+  constexpr int kKeys = Tile::kRows, kLd = Tile::kLd;
+  __shared__ alignas(16) E ks[kKeys * kLd];
+  __shared__ alignas(16) E vs[kKeys * kLd];
+  if (check_block(a)) return;
+  const int lane = threadIdx.x & 63, c16 = lane & 15, g = lane >> 4, wave = threadIdx.x >> 6;
+  const int hk = blockIdx.x % a.Hk, t = blockIdx.x / a.Hk;
+  const int b = last_at_most(a.B, t, [&](int i) { return first_tile(a.cu_q, i, a.G, kTile); });
+  Seq s;
+  if (!sequence(a, b, &s)) return;
+  const int64_t tile = t - first_tile(a.cu_q, b, a.G, kTile);
+  const int rows = s.nq * a.G;
+  if (tile < 0 || tile * kTile >= rows) return;
+  const int row0 = static_cast<int>(tile) * kTile, row = row0 + wave * 16 + c16;
+  const bool real = row < rows;
+  const int limit = limit_of(a, s, row), open = limit_of(a, s, row0);
+  const int key_hi = limit_of(a, s, min(row0 + kTile, rows) - 1);
+  Frag qf[D / 32], gf[D / 32];
+  float delta = 0.f;
+#pragma unroll
+  for (int st = 0; st < D / 32; ++st) {
+    const int off = (32 * st + 8 * g) * sizeof(E);
+    qf[st] = real ? load_frag<E>(query_row(a, a.q, s, hk, row) + off) : zero_frag<E>();
+    gf[st] = real ? load_frag<E>(query_row(a, a.dout, s, hk, row) + off) : zero_frag<E>();
+    const Frag of = real ? load_frag<E>(query_row(a, a.out, s, hk, row) + off) : zero_frag<E>();
+    const E* x = reinterpret_cast<const E*>(&gf[st]);
+    const E* y = reinterpret_cast<const E*>(&of);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) delta = __builtin_fmaf(static_cast<float>(x[i]), static_cast<float>(y[i]), delta);
+  }
+  delta = over_groups_sum(delta);
+  if (real && g == 0) a.delta[stat_at(a, s, hk, row)] = delta;
+  const float lse2 = row_lse2(a, s, hk, row, real);
+  floatx4 dq[D / 16];
+#pragma unroll
+  for (int dt = 0; dt < D / 16; ++dt) dq[dt] = floatx4{0.f, 0.f, 0.f, 0.f};
+  const char* kbase = a.k.at + static_cast<int64_t>(s.k0) * a.k.row + hk * a.k.head;
+  const char* vbase = a.v.at + static_cast<int64_t>(s.k0) * a.v.row + hk * a.v.head;
+  Tile kt, vt;
+  const auto ask = [&](int key) {
+    kt.load(s.nk - key, [&](int i) { return kbase + static_cast<int64_t>(key + i) * a.k.row; });
+    vt.load(s.nk - key, [&](int i) { return vbase + static_cast<int64_t>(key + i) * a.v.row; });
+  };
+  if (key_hi > 0) ask(0);
+  for (int key = 0; key < key_hi; key += kKeys) {
+    const bool masked = key + kKeys > open;
+    __syncthreads();
+    kt.store(ks);
+    vt.store(vs);
+    __syncthreads();
+    if (key + kKeys < key_hi) ask(key + kKeys);
+#pragma unroll
+    for (int st32 = 0; st32 < kKeys / 32; ++st32) {
+      floatx4 ds[2];
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const int r0 = st32 * 32 + half * 16;
+        floatx4 sc = {0.f, 0.f, 0.f, 0.f}, dp = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int st = 0; st < D / 32; ++st) {
+          sc = Op<E>::mma(load_frag<E>(ks + (r0 + c16) * kLd + 32 * st + 8 * g), qf[st], sc);
+          dp = Op<E>::mma(load_frag<E>(vs + (r0 + c16) * kLd + 32 * st + 8 * g), gf[st], dp);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i], a.c2, -lse2));
+          ds[half][i] = masked && key + r0 + 4 * g + i >= limit ? 0.f : p * (dp[i] - delta);
+        }
+      }
+      const Frag f = Op<E>::pack(ds[0], ds[1]);
+#pragma unroll
+      for (int dt = 0; dt < D / 16; ++dt)
+        dq[dt] = Op<E>::mma(Op<E>::template columns<kLd>(ks + st32 * 32 * kLd, dt * 16), f, dq[dt]);
+    }
+  }
+  if (!real) return;
+  char* to = const_cast<char*>(query_row(a, a.dq, s, hk, row));
+#pragma unroll
+  for (int dt = 0; dt < D / 16; ++dt) store4<E>(to + (dt * 16 + 4 * g) * sizeof(E), dq[dt] * a.scale);
+}
+
+// dk and dv of 64 keys over the rows that see them.
+template <class E, int D, bool SPLIT>
+__global__ __launch_bounds__(kThreads) void grad_kv_kernel(AttnArgs a) {
+  typedef typename Op<E>::Frag Frag;
+  typedef Staged<E, D> Tile;
+  constexpr int kRows = Tile::kRows, kLd = Tile::kLd;
+  __shared__ alignas(16) E qs[kRows * kLd];
+  __shared__ alignas(16) E gs[kRows * kLd];
+  __shared__ floatx4 lse_s[kRows / 4], delta_s[kRows / 4];
+  __shared__ int4 limit_s[kRows / 4];
+  const int lane = threadIdx.x & 63, c16 = lane & 15, g = lane >> 4, wave = threadIdx.x >> 6;
+  const int hk = blockIdx.x % a.Hk, rest = blockIdx.x / a.Hk;
+  const int split = SPLIT ? rest % a.splits : 0, t = SPLIT ? rest / a.splits : rest;
+  const int b = last_at_most(a.B, t, [&](int i) { return first_tile(a.cu_k, i, 1, kTile); });
+  Seq s;
+  if (!sequence(a, b, &s)) return;
+  const int64_t tile = t - first_tile(a.cu_k, b, 1, kTile);
+  if (tile < 0 || tile * kTile >= s.nk) return;
+  const int key0 = static_cast<int>(tile) * kTile, key = key0 + wave * 16 + c16;
+  const bool real = key < s.nk;
+  const int rows = s.nq * a.G;
+  // The first row that sees a key of the tile.
+  int row_lo = a.causal ? min(rows, max(0, key0 - s.nk + s.nq) * a.G) : 0, row_hi = rows;
+  if (SPLIT) {
+    const int each = ((rows - row_lo + a.splits - 1) / a.splits + kRows - 1) / kRows * kRows;
+    row_lo = min(rows, row_lo + split * each);
+    row_hi = min(rows, row_lo + each);
+  }
+  const char* krow = a.k.at + (static_cast<int64_t>(s.k0) + key) * a.k.row + hk * a.k.head;
+  const char* vrow = a.v.at + (static_cast<int64_t>(s.k0) + key) * a.v.row + hk * a.v.head;
+  Frag kf[D / 32], vf[D / 32];
+#pragma unroll
+  for (int st = 0; st < D / 32; ++st) {
+    const int off = (32 * st + 8 * g) * sizeof(E);
+    kf[st] = real ? load_frag<E>(krow + off) : zero_frag<E>();
+    vf[st] = real ? load_frag<E>(vrow + off) : zero_frag<E>();
+  }
+  floatx4 dk[D / 16], dv[D / 16];
+#pragma unroll
+  for (int dt = 0; dt < D / 16; ++dt) dk[dt] = dv[dt] = floatx4{0.f, 0.f, 0.f, 0.f};
+  Tile qt, gt;
+  float lse2 = 0.f, delta = 0.f;
+  int limit = 0;
+  const auto ask = [&](int r) {
+    qt.load(row_hi - r, [&](int i) { return query_row(a, a.q, s, hk, r + i); });
+    gt.load(row_hi - r, [&](int i) { return query_row(a, a.dout, s, hk, r + i); });
+    if (threadIdx.x < kRows) {
+      const int row = r + threadIdx.x;
+      const bool here = row < row_hi;
+      lse2 = row_lse2(a, s, hk, row, here);
+      delta = here ? a.delta[stat_at(a, s, hk, row)] : 0.f;
+      limit = here ? limit_of(a, s, row) : 0;
+    }
+  };
+  if (row_lo < row_hi) ask(row_lo);
+  for (int r = row_lo; r < row_hi; r += kRows) {
+    __syncthreads();
+    qt.store(qs);
+    gt.store(gs);
+    if (threadIdx.x < kRows) {
+      reinterpret_cast<float*>(lse_s)[threadIdx.x] = lse2;
+      reinterpret_cast<float*>(delta_s)[threadIdx.x] = delta;
+      reinterpret_cast<int*>(limit_s)[threadIdx.x] = limit;
+    }
+    __syncthreads();
+    if (r + kRows < row_hi) ask(r + kRows);
+#pragma unroll
+    for (int st32 = 0; st32 < kRows / 32; ++st32) {
+      floatx4 p[2], ds[2];
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const int r0 = st32 * 32 + half * 16;
+        floatx4 sc = {0.f, 0.f, 0.f, 0.f}, dp = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int st = 0; st < D / 32; ++st) {
+          sc = Op<E>::mma(load_frag<E>(qs + (r0 + c16) * kLd + 32 * st + 8 * g), kf[st], sc);
+          dp = Op<E>::mma(load_frag<E>(gs + (r0 + c16) * kLd + 32 * st + 8 * g), vf[st], dp);
+        }
+        const floatx4 l4 = lse_s[r0 / 4 + g], d4 = delta_s[r0 / 4 + g];
+        const int4 m4 = limit_s[r0 / 4 + g];
+        const int lim[4] = {m4.x, m4.y, m4.z, m4.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const bool seen = key < lim[i];
+          p[half][i] = seen ? __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i], a.c2, -l4[i])) : 0.f;
+          ds[half][i] = seen ? p[half][i] * (dp[i] - d4[i]) : 0.f;
+        }
+      }
+      const Frag pf = Op<E>::pack(p[0], p[1]), df = Op<E>::pack(ds[0], ds[1]);
+#pragma unroll
+      for (int dt = 0; dt < D / 16; ++dt) {
+        dv[dt] = Op<E>::mma(Op<E>::template columns<kLd>(gs + st32 * 32 * kLd, dt * 16), pf, dv[dt]);
+        dk[dt] = Op<E>::mma(Op<E>::template columns<kLd>(qs + st32 * 32 * kLd, dt * 16), df, dk[dt]);
+      }
+    }
+  }
+  if (!real) return;
+  const int64_t at = static_cast<int64_t>(s.k0) + key;
+  if (SPLIT) {
+    float* to = a.part + ((split * a.Hk + hk) * a.total_k + at) * 2 * D;
+#pragma unroll
+    for (int dt = 0; dt < D / 16; ++dt) {
+      *reinterpret_cast<floatx4*>(to + dt * 16 + 4 * g) = dk[dt];
+      *reinterpret_cast<floatx4*>(to + D + dt * 16 + 4 * g) = dv[dt];
+    }
+    return;
+  }
+  char* kto = a.dk.at + at * a.dk.row + hk * a.dk.head;
+  char* vto = a.dv.at + at * a.dv.row + hk * a.dv.head;
+#pragma unroll
+  for (int dt = 0; dt < D / 16; ++dt) {
+    store4<E>(kto + (dt * 16 + 4 * g) * sizeof(E), dk[dt] * a.scale);
+    store4<E>(vto + (dt * 16 + 4 * g) * sizeof(E), dv[dt]);
+  }
+}
+
+// The parts of dk and dv added in their order: four elements a thread.
+template <class E, int D>
+__global__ __launch_bounds__(kThreads) void join_kv_kernel(AttnArgs a) {
+  constexpr int kQuads = 2 * D / 4, kKeysHere = kThreads / kQuads;
+  const int64_t at = static_cast<int64_t>(blockIdx.x / a.Hk) * kKeysHere + threadIdx.x / kQuads;
+  const int hk = blockIdx.x % a.Hk, d = threadIdx.x % kQuads * 4;
+  const bool here = at < a.total_k;
+  const int64_t key = here ? at : a.total_k - 1;
+  // Each wave holds one key at D 128, else several: the search is for the wave, so each of them in turn.
+  constexpr int kPerWave = 64 / kQuads > 1 ? 64 / kQuads : 1;
+  bool mine = false;
+  for (int i = 0; i < kPerWave; ++i) {
+    const int64_t n = __shfl(static_cast<int>(key), i * (64 / kPerWave));
+    const int b = last_at_most(a.B, n, [&](int j) { return static_cast<int64_t>(a.cu_k[j]); });
+    Seq s;
+    const bool in = sequence(a, b, &s) && n >= s.k0 && n < static_cast<int64_t>(s.k0) + s.nk;
+    if ((threadIdx.x & 63) / (64 / kPerWave) == i) mine = in;
+  }
+  if (!here || !mine) return;
+  floatx4 sum = {0.f, 0.f, 0.f, 0.f};
+  for (int p = 0; p < a.splits; ++p)
+    sum += *reinterpret_cast<const floatx4*>(a.part + ((p * a.Hk + hk) * a.total_k + at) * 2 * D + d);
+  if (d < D) store4<E>(a.dk.at + at * a.dk.row + hk * a.dk.head + d * sizeof(E), sum * a.scale);
+  else store4<E>(a.dv.at + at * a.dv.row + hk * a.dv.head + (d - D) * sizeof(E), sum);
+}
+
+// --------------------------------- host -----------------------------------
+
+struct Sizes {
+  int32_t B, H, Hk, D, max_q;
+  int64_t total_q, total_k;
+};
+
+bool good_sizes(const Sizes& z) {
+  return z.B >= 1 && z.B <= DORA_MAX_SEQUENCES && z.H >= 1 && z.H <= 256 && z.Hk >= 1 && z.H % z.Hk == 0 &&
+         (z.D == 32 || z.D == 64 || z.D == 128) && z.max_q >= 0 && z.total_q >= 0 && z.total_k >= 0 &&
+         z.total_k <= 0x7FFFFFFF && z.total_q * (z.H / z.Hk) <= 0x7FFFFFFF;
+}
+
+int64_t tiles(int64_t total, int32_t B, int64_t tile) { return total / tile + B; }
+
+// Workgroups of 64 rows that the GPU holds at a time, about.
+constexpr int kFill = 512;
+
+// How the forward pass splits its keys.
+struct Split {
+  int32_t splits, chunk, part_rows;
+  int64_t blocks;  // without heads
+};
+Split forward_split(const Sizes& z) {
+  const int32_t G = z.H / z.Hk;
+  const int64_t rows = static_cast<int64_t>(std::min<int64_t>(z.max_q, z.total_q)) * G;
+  if (rows <= kTile && z.total_k > 0) {
+    // every sequence is one tile: parts of the same number of keys
+    const int64_t want = z.total_k * z.Hk / (4 * kFill);
+    const int64_t chunk = std::min<int64_t>(4096, std::max<int64_t>(256, (want + 63) / 64 * 64));
+    if (z.total_k / z.B > chunk) return Split{1, static_cast<int32_t>(chunk), static_cast<int32_t>(rows), tiles(z.total_k, z.B, chunk)};
+  }
+  const int64_t n = tiles(z.total_q * G, z.B, kTile), keys = z.total_k / z.B;
+  int32_t splits = 1;
+  while (splits < 16 && n * z.Hk * splits < kFill && keys / (splits * 2) >= 512) splits *= 2;
+  return Split{splits, 0, kTile, n * splits};
+}
+
+int32_t backward_splits(const Sizes& z) {
+  const int64_t n = tiles(z.total_k, z.B, kTile) * z.Hk, rows = z.total_q / z.B * (z.H / z.Hk);
+  int32_t splits = 1;
+  while (splits < 16 && n * splits < kFill && rows / (splits * 2) >= 512) splits *= 2;
+  return splits;
+}
+
+size_t round256(size_t n) { return (n + 255) & ~size_t(255); }
+
+size_t forward_bytes(const Sizes& z) {
+  const Split p = forward_split(z);
+  if (p.splits == 1 && !p.chunk) return 256;
+  return round256(static_cast<size_t>(p.blocks) * z.Hk * p.part_rows * (z.D + 2) * sizeof(float));
+}
+size_t delta_bytes(const Sizes& z) { return round256(static_cast<size_t>(z.total_q) * z.H * sizeof(float)); }
+size_t backward_bytes(const Sizes& z) {
+  const int32_t splits = backward_splits(z);
+  return delta_bytes(z) + 256 +
+         (splits == 1 ? 0 : round256(static_cast<size_t>(splits) * z.Hk * z.total_k * 2 * z.D * sizeof(float)));
+}
+
+bool same_sizes(const dora_rows* s, const dora_rows* t) {
+  return s->rows == t->rows && s->heads == t->heads && s->dim == t->dim && s->dtype == t->dtype;
+}
+
+// Everything but the outputs and the workspace; fills the kernels' arguments.
+int check_attn(const dora_rows* q, const dora_rows* k, const dora_rows* v, const int32_t* cu_q, const int32_t* cu_k,
+               int32_t B, int32_t max_q, int32_t causal, float softmax_scale, int32_t* dev_status, Sizes* z,
+               AttnArgs* a) {
+  if (!q || !k || !v || !cu_q || !cu_k || !dev_status) return DORA_ERR_NULL;
+  for (const dora_rows* t : {q, k, v}) {
+    const int rc = check_rows(t, 16);
+    if (rc != DORA_OK) return rc;
+  }
+  if (q->dtype != k->dtype) return DORA_ERR_DTYPE;
+  if (!same_sizes(k, v) || k->dim != q->dim) return DORA_ERR_SHAPE;
+  *z = Sizes{B, q->heads, k->heads, q->dim, max_q, q->rows, k->rows};
+  if (!good_sizes(*z) || !(softmax_scale < INFINITY)) return DORA_ERR_SHAPE;
+  *a = AttnArgs{};
+  a->q = row_view(q), a->k = row_view(k), a->v = row_view(v);
+  a->cu_q = cu_q, a->cu_k = cu_k;
+  a->B = B, a->H = z->H, a->Hk = z->Hk, a->G = z->H / z->Hk;
+  int bits = 0;
+  while ((1 << bits) < a->G) ++bits;
+  // mul = ceil(2^(31 + bits) / G) < 2^32: r mul / 2^(31 + bits) lies less than 1 / G above r / G for r < 2^31
+  a->g_mul = bits ? static_cast<uint32_t>(((uint64_t{1} << (31 + bits)) + a->G - 1) / a->G) : 0;
+  a->g_shift = bits ? bits - 1 : 0;
+  a->total_q = z->total_q, a->total_k = z->total_k;
+  a->max_q = max_q, a->causal = causal != 0;
+  a->scale = softmax_scale > 0.f ? softmax_scale : static_cast<float>(1.0 / std::sqrt(static_cast<double>(z->D)));
+  a->c2 = a->scale * kLog2e;
+  a->status = dev_status;
+  return DORA_OK;
+}
+
+bool too_small(const void* ws, size_t bytes, size_t need) {
+  return !ws || reinterpret_cast<uintptr_t>(ws) & 255u || bytes < need;
+}
+
+constexpr int64_t kMaxBlocks = (int64_t{1} << 32) / kThreads - 2;  // threads of a launch in 32 bits
+
+// The launch for an element type and a head width: f(E{}, integral_constant D).
+template <class F>
+void with_type(int dtype, int D, F f) {
+  const auto width = [&](auto e) {
+    if (D == 32) f(e, std::integral_constant<int, 32>{});
+    else if (D == 64) f(e, std::integral_constant<int, 64>{});
+    else f(e, std::integral_constant<int, 128>{});
+  };
+  if (dtype == DORA_BF16) width(__bf16{});
+  else width(float{});
+}
+
+}  // namespace
+}  // namespace dora
+
+extern "C" size_t dora_grouped_attn_workspace_size(int32_t B, int32_t H, int32_t Hk, int32_t D, int32_t max_q,
+                                                   int64_t total_q, int64_t total_k) {
+  const dora::Sizes z{B, H, Hk, D, max_q, total_q, total_k};
+  return dora::good_sizes(z) ? dora::forward_bytes(z) : 0;
+}
+
+extern "C" size_t dora_grouped_attn_backward_workspace_size(int32_t B, int32_t H, int32_t Hk, int32_t D, int32_t max_q,
+                                                            int64_t total_q, int64_t total_k) {
+  const dora::Sizes z{B, H, Hk, D, max_q, total_q, total_k};
+  return dora::good_sizes(z) ? dora::backward_bytes(z) : 0;
+}
+
+extern "C" int dora_grouped_attn(const dora_rows* q, const dora_rows* k, const dora_rows* v, const int32_t* cu_q,
+                                 const int32_t* cu_k, int32_t B, int32_t max_q, int32_t causal, float softmax_scale,
+                                 const dora_rows* out, float* lse_out, void* workspace, size_t workspace_bytes,
+                                 int32_t* dev_status, void* stream) {
+  using namespace dora;
+  if (!out) return DORA_ERR_NULL;
+  Sizes z;
+  AttnArgs a;
+  int rc = check_attn(q, k, v, cu_q, cu_k, B, max_q, causal, softmax_scale, dev_status, &z, &a);
+  if (rc == DORA_OK) rc = check_rows(out, 16);
+  if (rc != DORA_OK) return rc;
+  if (!same_sizes(out, q)) return DORA_ERR_SHAPE;
+  if (too_small(workspace, workspace_bytes, forward_bytes(z))) return DORA_ERR_WORKSPACE;
+  const size_t cu_bytes = (static_cast<size_t>(B) + 1) * sizeof(int32_t);
+  if (rows_clash({out}, {q, k, v}, {},
+                 {{lse_out, static_cast<size_t>(z.total_q) * z.H * sizeof(float)},
+                  {workspace, forward_bytes(z)},
+                  {dev_status, sizeof(int32_t)}},
+                 {{cu_q, cu_bytes}, {cu_k, cu_bytes}}))
+    return DORA_ERR_OVERLAP;
+  if (z.total_q == 0) return DORA_OK;
+  const Split p = forward_split(z);
+  const bool split = p.splits > 1 || p.chunk;
+  const int64_t blocks = p.blocks * z.Hk, join = (z.total_q * z.H + kThreads / 64 - 1) / (kThreads / 64);
+  if (blocks > kMaxBlocks || (split && join > kMaxBlocks)) return DORA_ERR_UNSUPPORTED;
+  a.out = row_view(out);
+  a.lse = lse_out;
+  // 16-byte rows first
+  a.part = static_cast<float*>(workspace);
+  a.part_ml = reinterpret_cast<float2*>(a.part + p.blocks * z.Hk * p.part_rows * z.D);
+  a.splits = p.splits, a.chunk = p.chunk, a.part_rows = p.part_rows;
+  a.blocks = static_cast<int32_t>(blocks);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  with_type(q->dtype, z.D, [&](auto e, auto d) {
+    typedef decltype(e) E;
+    constexpr int D = decltype(d)::value;
+    if (split) {
+      hipLaunchKernelGGL((attn_kernel<E, D, true>), dim3(a.blocks + 1), dim3(kThreads), 0, st, a);
+      hipLaunchKernelGGL((join_kernel<E, D>), dim3(static_cast<uint32_t>(join)), dim3(kThreads), 0, st, a);
+    } else {
+      hipLaunchKernelGGL((attn_kernel<E, D, false>), dim3(a.blocks + 1), dim3(kThreads), 0, st, a);
+    }
+  });
+  return hipGetLastError() == hipSuccess ? DORA_OK : DORA_ERR_HIP;
+}
+
+extern "C" int dora_grouped_attn_backward(const dora_rows* dout, const dora_rows* q, const dora_rows* k,
+                                          const dora_rows* v, const dora_rows* out, const float* lse,
+                                          const int32_t* cu_q, const int32_t* cu_k, int32_t B, int32_t max_q,
+                                          int32_t causal, float softmax_scale, const dora_rows* dq,
+                                          const dora_rows* dk, const dora_rows* dv, void* workspace,
+                                          size_t workspace_bytes, int32_t* dev_status, void* stream) {
+  using namespace dora;
+  if (!q || !dout || !out || (!lse && q->rows > 0) || !dq || !dk || !dv) return DORA_ERR_NULL;
+  Sizes z;
+  AttnArgs a;
+  int rc = check_attn(q, k, v, cu_q, cu_k, B, max_q, causal, softmax_scale, dev_status, &z, &a);
+  for (const dora_rows* t : {dout, out, dq, dk, dv})
+    if (rc == DORA_OK) rc = check_rows(t, 16);
+  if (rc != DORA_OK) return rc;
+  if (!same_sizes(dout, q) || !same_sizes(out, q) || !same_sizes(dq, q) || !same_sizes(dk, k) || !same_sizes(dv, k))
+    return DORA_ERR_SHAPE;
+  if (too_small(workspace, workspace_bytes, backward_bytes(z))) return DORA_ERR_WORKSPACE;
+  const size_t cu_bytes = (static_cast<size_t>(B) + 1) * sizeof(int32_t);
+  if (rows_clash({dq, dk, dv}, {q, k, v, out, dout}, {},
+                 {{workspace, backward_bytes(z)}, {dev_status, sizeof(int32_t)}},
+                 {{cu_q, cu_bytes}, {cu_k, cu_bytes}, {lse, static_cast<size_t>(z.total_q) * z.H * sizeof(float)}}))
+    return DORA_ERR_OVERLAP;
+  const int64_t q_blocks = tiles(z.total_q * a.G, B, kTile) * z.Hk;
+  const int32_t splits = backward_splits(z);
+  const int64_t kv_blocks = tiles(z.total_k, B, kTile) * z.Hk * splits;
+  const int keys_here = kThreads / (2 * z.D / 4);
+  const int64_t join = (z.total_k + keys_here - 1) / keys_here * z.Hk;
+  if (q_blocks > kMaxBlocks || kv_blocks > kMaxBlocks || join > kMaxBlocks) return DORA_ERR_UNSUPPORTED;
+  a.out = row_view(out), a.dout = row_view(dout);
+  a.dq = row_view(dq), a.dk = row_view(dk), a.dv = row_view(dv);
+  a.lse = const_cast<float*>(lse);
+  a.delta = static_cast<float*>(workspace);
+  a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + delta_bytes(z));
+  a.splits = splits;
+  a.blocks = static_cast<int32_t>(q_blocks);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  with_type(q->dtype, z.D, [&](auto e, auto d) {
+    typedef decltype(e) E;
+    constexpr int D = decltype(d)::value;
+    hipLaunchKernelGGL((grad_q_kernel<E, D>), dim3(a.blocks + 1), dim3(kThreads), 0, st, a);
+    if (z.total_k == 0) return;
+    if (splits > 1) {
+      hipLaunchKernelGGL((grad_kv_kernel<E, D, true>), dim3(static_cast<uint32_t>(kv_blocks)), dim3(kThreads), 0, st, a);
+      hipLaunchKernelGGL((join_kv_kernel<E, D>), dim3(static_cast<uint32_t>(join)), dim3(kThreads), 0, st, a);
+    } else {
+      hipLaunchKernelGGL((grad_kv_kernel<E, D, false>), dim3(static_cast<uint32_t>(kv_blocks)), dim3(kThreads), 0, st, a);
+    }
+  });
+  return hipGetLastError() == hipSuccess ? DORA_OK : DORA_ERR_HIP;
+}

@@ -42,6 +42,7 @@ F* at_address(F&, void* fn) {
   return reinterpret_cast<F*>(fn);
 }
 int32_t i32(const Arg& a) { return static_cast<int32_t>(a.n); }
+const dora_rows* rows_of(const Arg& a) { return ptr<const dora_rows>(a); }
 dora_dtype type_of(const Arg& a) { return static_cast<dora_dtype>(a.n); }
 
 // The order is that of _ENTRIES in the binding.
@@ -141,6 +142,40 @@ const Entry kEntries[] = {
      [](void* fn, const Arg* a) {
        return at_address(dora_grad_clip, fn)(ptr<dora_span>(a[0]), ptr<dora_span>(a[1]), i32(a[2]), a[3].f, a[4].f,
                              ptr<float>(a[5]), a[6].p, static_cast<size_t>(a[7].n), a[8].p);
+     }},
+    {"ssInAnnnesss",
+     [](void* fn, const Arg* a) {
+       return at_address(dora_rope, fn)(rows_of(a[0]), rows_of(a[1]), ptr<int32_t>(a[2]), i32(a[3]), ptr<double>(a[4]),
+                         i32(a[5]), i32(a[6]), i32(a[7]), a[8].f, rows_of(a[9]), rows_of(a[10]), a[11].p);
+     }},
+    {"sssIInnnesfAnIs",
+     [](void* fn, const Arg* a) {
+       return at_address(dora_grouped_attn, fn)(rows_of(a[0]), rows_of(a[1]), rows_of(a[2]), ptr<int32_t>(a[3]),
+                                ptr<int32_t>(a[4]), i32(a[5]), i32(a[6]), i32(a[7]), a[8].f, rows_of(a[9]),
+                                ptr<float>(a[10]), a[11].p, static_cast<size_t>(a[12].n), ptr<int32_t>(a[13]), a[14].p);
+     }},
+    {"sssssFIInnnesssAnIs",
+     [](void* fn, const Arg* a) {
+       return at_address(dora_grouped_attn_backward, fn)(rows_of(a[0]), rows_of(a[1]), rows_of(a[2]), rows_of(a[3]),
+                                         rows_of(a[4]), ptr<float>(a[5]), ptr<int32_t>(a[6]), ptr<int32_t>(a[7]),
+                                         i32(a[8]), i32(a[9]), i32(a[10]), a[11].f, rows_of(a[12]), rows_of(a[13]),
+                                         rows_of(a[14]), a[15].p, static_cast<size_t>(a[16].n), ptr<int32_t>(a[17]),
+                                         a[18].p);
+     }},
+    {"ssFfffffnesss",
+     [](void* fn, const Arg* a) {
+       return at_address(dora_residual_norm, fn)(rows_of(a[0]), rows_of(a[1]), ptr<float>(a[2]), ptr<float>(a[3]),
+                                 ptr<float>(a[4]), ptr<float>(a[5]), ptr<float>(a[6]), ptr<float>(a[7]), i32(a[8]),
+                                 a[9].f, rows_of(a[10]), rows_of(a[11]), a[12].p);
+     }},
+    {"ssssFffffnessffffffans",
+     [](void* fn, const Arg* a) {
+       return at_address(dora_residual_norm_backward, fn)(rows_of(a[0]), rows_of(a[1]), rows_of(a[2]), rows_of(a[3]),
+                                          ptr<float>(a[4]), ptr<float>(a[5]), ptr<float>(a[6]), ptr<float>(a[7]),
+                                          ptr<float>(a[8]), i32(a[9]), a[10].f, rows_of(a[11]), rows_of(a[12]),
+                                          ptr<float>(a[13]), ptr<float>(a[14]), ptr<float>(a[15]), ptr<float>(a[16]),
+                                          ptr<float>(a[17]), ptr<float>(a[18]), a[19].p, static_cast<size_t>(a[20].n),
+                                          a[21].p);
      }},
 };
 constexpr int kMaxArgs = 24;
@@ -256,6 +291,39 @@ PyObject* rows(PyObject*, PyObject* o) {
   }
 }
 
+// describe(address, t, ...): writes a dora_rows per tensor ([rows, heads, dim] or
+// [rows, dim], elements of a row's head adjacent; None: no data) at the address
+// and returns the device that holds them all, or NotImplemented.
+PyObject* describe(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  if (nargs < 2 || at::impl::torch_function_mode_enabled()) Py_RETURN_NOTIMPLEMENTED;
+  dora_rows* out = static_cast<dora_rows*>(PyLong_AsVoidPtr(args[0]));
+  if (out == nullptr) {
+    if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "no room for the descriptions");
+    return nullptr;
+  }
+  long device = -1;
+  try {
+    for (Py_ssize_t i = 1; i < nargs; ++i, ++out) {
+      *out = dora_rows{};
+      if (args[i] == Py_None) continue;
+      if (!THPVariable_CheckExact(args[i])) Py_RETURN_NOTIMPLEMENTED;
+      const at::Tensor& t = THPVariable_Unpack(args[i]);
+      const at::ScalarType type = t.scalar_type();
+      if (t.layout() != at::kStrided || t.is_nested() || !t.is_cuda() || (t.dim() != 2 && t.dim() != 3) ||
+          (type != at::kFloat && type != at::kBFloat16) || (device >= 0 && t.get_device() != device))
+        Py_RETURN_NOTIMPLEMENTED;
+      const int64_t last = t.dim() - 1, dim = t.size(last), heads = last == 2 ? t.size(1) : 1;
+      if ((dim > 1 && t.stride(last) != 1) || dim > INT32_MAX || heads > INT32_MAX) Py_RETURN_NOTIMPLEMENTED;
+      device = t.get_device();
+      *out = dora_rows{t.data_ptr(), t.size(0), static_cast<int32_t>(heads), static_cast<int32_t>(dim), t.stride(0),
+                       last == 2 ? t.stride(1) : 0, type == at::kFloat ? DORA_F32 : DORA_BF16, 0};
+    }
+  } catch (...) {
+    Py_RETURN_NOTIMPLEMENTED;
+  }
+  return PyLong_FromLong(device);
+}
+
 // vectors(device, n, t, n, t, ...): True where every t is None or a vector of
 // n elements (n < 0: any tensor) on the device, else NotImplemented.
 PyObject* vectors(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
@@ -310,6 +378,8 @@ PyObject* written(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
 PyMethodDef kMethods[] = {
     {"written", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(written)), METH_FASTCALL,
      "written(tensor or list, ...): True, or NotImplemented"},
+    {"describe", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(describe)), METH_FASTCALL,
+     "describe(address, tensor or None, ...): the device, or NotImplemented"},
     {"rows", rows, METH_O, "rows(tensor): address, leading dimension, sizes, type and device, or NotImplemented"},
     {"vectors", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(vectors)), METH_FASTCALL,
      "vectors(device, n, tensor, ...): True, or NotImplemented"},
