@@ -26,6 +26,7 @@
 #include <algorithm>
 
 #include "dora_internal.h"
+#include "lanes.h"
 #include "rows.h"
 
 namespace dora {
@@ -250,14 +251,8 @@ __device__ __forceinline__ void store4(char* p, floatx4 x) {
   }
 }
 
-__device__ __forceinline__ float over_groups_max(float x) {
-  x = fmaxf(x, __shfl_xor(x, 16));
-  return fmaxf(x, __shfl_xor(x, 32));
-}
-__device__ __forceinline__ float over_groups_sum(float x) {
-  x += __shfl_xor(x, 16);
-  return x + __shfl_xor(x, 32);
-}
+__device__ __forceinline__ float over_groups_max(float x) { return max32(max16(x)); }
+__device__ __forceinline__ float over_groups_sum(float x) { return add32(add16(x)); }
 
 // ------------------------------- forward ----------------------------------
 

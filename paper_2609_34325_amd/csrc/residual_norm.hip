@@ -17,6 +17,7 @@
 #include <algorithm>
 
 #include "dora_internal.h"
+#include "lanes.h"
 #include "rows.h"
 
 namespace dora {
@@ -24,7 +25,7 @@ namespace {
 
 constexpr int kMaxC = 8192;
 constexpr int kParams = 5;  // dgamma, dbeta, dscale, dpost_gamma, dpost_beta
-constexpr int kFinishCols = 64, kFinishThreads = 1024;
+constexpr int kFinishCols = 16, kFinishThreads = 512;
 
 struct NormArgs {
   RowView x, a, h, y;            // backward: x is h
@@ -47,7 +48,6 @@ template <class E>
 struct Vec {
   static constexpr int kE = 16 / sizeof(E);
   float v[kE];
-  __device__ __forceinline__ void load(const char* p) { unpack(*reinterpret_cast<const u32x4*>(p)); }
   __device__ __forceinline__ void unpack(u32x4 w) {
     if (sizeof(E) == 4) {
 #pragma unroll
@@ -76,9 +76,10 @@ struct Vec {
 template <int L, int N>
 __device__ __forceinline__ void row_sum(float (&s)[N], float* lds) {
 #pragma unroll
-  for (int x = 1; x < (L < 64 ? L : 64); x *= 2)
-#pragma unroll
-    for (int n = 0; n < N; ++n) s[n] += __shfl_xor(s[n], x);
+  for (int n = 0; n < N; ++n) {
+    s[n] = sum16(s[n]);
+    if (L > 16) s[n] = add32(add16(s[n]));
+  }
   if (L > 64) {  // the row is the workgroup
     constexpr int kWaves = L / 64;
     __syncthreads();  // the last sums have been read
@@ -95,23 +96,33 @@ __device__ __forceinline__ void row_sum(float (&s)[N], float* lds) {
   }
 }
 
+// A row's pieces as they lie in memory, 0 past its end: asked for one row ahead.
+template <int L, int NP>
+struct Raw {
+  u32x4 w[NP];
+  __device__ __forceinline__ void load(const RowView& v, int64_t t, int lane, int pieces) {
+    if (!v.at) return;
+    const char* row = v.at + t * v.row;
+#pragma unroll
+    for (int j = 0; j < NP; ++j)
+      w[j] = lane + j * L < pieces ? *reinterpret_cast<const u32x4*>(row + static_cast<uint32_t>(lane + j * L) * 16u)
+                                   : u32x4{0u, 0u, 0u, 0u};
+  }
+};
+
 // A row's pieces in the lanes' registers.
 template <class E, int L, int NP>
 struct Row {
   static constexpr int kE = Vec<E>::kE;
   Vec<E> p[NP];
-  // Lanes past the row's end hold 0.
-  __device__ __forceinline__ void load(const char* row, int lane, int pieces) {
+  __device__ __forceinline__ void unpack(const Raw<L, NP>& raw) {
 #pragma unroll
-    for (int j = 0; j < NP; ++j) {
-      if (lane + j * L < pieces) p[j].load(row + (lane + j * L) * 16);
-      else p[j].fill(0.f);
-    }
+    for (int j = 0; j < NP; ++j) p[j].unpack(raw.w[j]);
   }
   __device__ __forceinline__ void store(char* row, int lane, int pieces) const {
 #pragma unroll
     for (int j = 0; j < NP; ++j)
-      if (lane + j * L < pieces) p[j].store(row + (lane + j * L) * 16);
+      if (lane + j * L < pieces) p[j].store(row + static_cast<uint32_t>(lane + j * L) * 16u);
   }
   // A parameter's values at the lane's columns, x where there is none; 0 past the row's end, which makes what
   // is multiplied by it 0 there.
@@ -119,9 +130,12 @@ struct Row {
 #pragma unroll
     for (int j = 0; j < NP; ++j) {
       p[j].fill(lane + j * L < pieces ? x : 0.f);
-      if (q && lane + j * L < pieces)
+      if (q && lane + j * L < pieces) {
+        // a 32-bit offset from the parameter's address: one register for all of them
+        const char* at = reinterpret_cast<const char*>(q) + static_cast<uint32_t>((lane + j * L) * kE) * 4u;
 #pragma unroll
-        for (int i = 0; i < kE; ++i) p[j].v[i] = q[(lane + j * L) * kE + i];
+        for (int i = 0; i < kE; ++i) p[j].v[i] = reinterpret_cast<const float*>(at)[i];
+      }
     }
   }
   template <class F>
@@ -147,6 +161,7 @@ struct Param {
   }
   __device__ __forceinline__ Row<E, L, NP> row(int lane, int pieces) const {
     if constexpr (kHeld) return held;
+    asm volatile("" : "+v"(lane));  // addresses are formed here, not kept in registers for every row
     Row<E, L, NP> r;
     r.param(q, none, lane, pieces);
     return r;
@@ -203,13 +218,21 @@ __global__ __launch_bounds__(threads_of<L>()) void residual_norm_kernel(NormArgs
   const int lane = threadIdx.x % L, group = threadIdx.x / L, pieces = a.C / kE;
   const P gamma(a.gamma, 1.f, lane, pieces), beta(a.beta, 0.f, lane, pieces), scale(a.scale, 1.f, lane, pieces),
       pg(POST ? a.post_gamma : nullptr, 1.f, lane, pieces), pb(POST ? a.post_beta : nullptr, 0.f, lane, pieces);
+  const int64_t step = static_cast<int64_t>(gridDim.x) * kGroups;
+  int64_t t = static_cast<int64_t>(blockIdx.x) * kGroups + group;
+  Raw<L, NP> rx, ra;
+  const auto ask = [&](int64_t row) {
+    rx.load(a.x, row, lane, pieces);
+    ra.load(a.a, row, lane, pieces);
+  };
+  if (t < a.T) ask(t);
   // A row of many lanes is its workgroup's alone: its barriers are reached by all of them.
-  for (int64_t t = static_cast<int64_t>(blockIdx.x) * kGroups + group; t < a.T; t += static_cast<int64_t>(gridDim.x) * kGroups) {
-    R h;
-    h.load(a.x.at + t * a.x.row, lane, pieces);
+  for (; t < a.T; t += step) {
+    R h, u;
+    h.unpack(rx);
+    if (a.a.at) u.unpack(ra);
+    if (t + step < a.T) ask(t + step);
     if (a.a.at) {
-      R u;
-      u.load(a.a.at + t * a.a.row, lane, pieces);
       const float gate = a.gate ? a.gate[t] : 1.f;
       if (POST) {
         to_hat(u, a, lane, pieces, lds);
@@ -237,23 +260,41 @@ __global__ __launch_bounds__(threads_of<L>()) void residual_norm_grad_kernel(Nor
   const int lane = threadIdx.x % L, group = threadIdx.x / L, pieces = a.C / kE;
   const P gamma(a.gamma, 1.f, lane, pieces), scale(a.scale, 1.f, lane, pieces),
       pg(POST ? a.post_gamma : nullptr, 1.f, lane, pieces), pb(POST ? a.post_beta : nullptr, 0.f, lane, pieces);
-  // The branch norm's sums of the widest lanes stand in LDS, a slot for each lane: with them the registers spill.
+  // The branch's sums of the widest lanes stand in LDS, a slot for each lane: with them the registers spill.
   constexpr bool kLdsSums = POST && NP * kE > 8;
-  constexpr int kSums = POST && !kLdsSums ? 5 : 3;
-  __shared__ float2 post_sums[kLdsSums ? NP * kE * kThreads : 1];
+  constexpr int kSums = kLdsSums ? 2 : POST ? 5 : 3;
+  __shared__ float lds_sums[kLdsSums ? (5 - kSums) * NP * kE * kThreads : 1];
+  const auto slot = [&](int n, int j, int i) -> float& {
+    return lds_sums[((n - kSums) * NP * kE + j * kE + i) * kThreads + threadIdx.x];
+  };
   R sum[kSums];
 #pragma unroll
   for (int n = 0; n < kSums; ++n) sum[n].param(nullptr, 0.f, lane, pieces);
   if constexpr (kLdsSums)
-    for (int n = 0; n < NP * kE; ++n) post_sums[n * kThreads + threadIdx.x] = make_float2(0.f, 0.f);
-  for (int64_t t = static_cast<int64_t>(blockIdx.x) * kGroups + group; t < a.T; t += static_cast<int64_t>(gridDim.x) * kGroups) {
-    R g, u, dh;
-    if (a.a.at) u.load(a.a.at + t * a.a.row, lane, pieces);
-    if (a.dh.at) dh.load(a.dh.at + t * a.dh.row, lane, pieces);
+    for (int n = 0; n < (5 - kSums) * NP * kE; ++n) lds_sums[n * kThreads + threadIdx.x] = 0.f;
+  const int64_t step = static_cast<int64_t>(gridDim.x) * kGroups;
+  int64_t t = static_cast<int64_t>(blockIdx.x) * kGroups + group;
+  Raw<L, NP> ry, rdh, rh, ra;
+  const auto ask = [&](int64_t row) {
+    if (a.dy.at) rh.load(a.x, row, lane, pieces);
+    ry.load(a.dy, row, lane, pieces);
+    rdh.load(a.dh, row, lane, pieces);
+    ra.load(a.a, row, lane, pieces);
+  };
+  constexpr bool kAhead = NP <= 2;  // one row ahead, where the registers hold two
+  if (kAhead && t < a.T) ask(t);
+  for (; t < a.T; t += step) {
+    Raw<L, NP> cy = ry, cdh = rdh, ch = rh, ca = ra;
+    if (kAhead && t + step < a.T) ask(t + step);
+    if (!kAhead && a.dy.at) {
+      ch.load(a.x, t, lane, pieces);
+      cy.load(a.dy, t, lane, pieces);
+    }
+    R g, u;
     if (a.dy.at) {
       R hat;
-      hat.load(a.x.at + t * a.x.row, lane, pieces);
-      g.load(a.dy.at + t * a.dy.row, lane, pieces);
+      hat.unpack(ch);
+      g.unpack(cy);
       const float r = to_hat(hat, a, lane, pieces, lds);
       const R w = gamma.row(lane, pieces);
       g.each([&](float& v, int j, int i) {
@@ -265,10 +306,17 @@ __global__ __launch_bounds__(threads_of<L>()) void residual_norm_grad_kernel(Nor
     } else {
       g.param(nullptr, 0.f, lane, pieces);
     }
-    if (a.dh.at) g.each([&](float& v, int j, int i) { v += dh.p[j].v[i]; });
+    if (a.dh.at) {
+      R dh;
+      if (!kAhead) cdh.load(a.dh, t, lane, pieces);
+      dh.unpack(cdh);
+      g.each([&](float& v, int j, int i) { v += dh.p[j].v[i]; });
+    }
+    if (!kAhead) ca.load(a.a, t, lane, pieces);  // before dx, which may take its place
     g.store(a.dx.at + t * a.dx.row, lane, pieces);
     if (!a.a.at) continue;
     const float gate = a.gate ? a.gate[t] : 1.f;
+    u.unpack(ca);
     R ahat;
     float ar = 0.f;
     if constexpr (POST) {
@@ -283,7 +331,10 @@ __global__ __launch_bounds__(threads_of<L>()) void residual_norm_grad_kernel(Nor
     u.each([&](float& v, int j, int i) {
       const float d = g.p[j].v[i], gated = d * gate;
       s[0] = __builtin_fmaf(d, v * sc.p[j].v[i], s[0]);
-      if (gate != 0.f) sum[2].p[j].v[i] = __builtin_fmaf(gated, v, sum[2].p[j].v[i]);
+      if (gate != 0.f) {
+        if constexpr (kLdsSums) slot(2, j, i) = __builtin_fmaf(gated, v, slot(2, j, i));
+        else sum[2].p[j].v[i] = __builtin_fmaf(gated, v, sum[2].p[j].v[i]);
+      }
       v = gated * sc.p[j].v[i];
     });
     if (a.dgate) {
@@ -295,8 +346,8 @@ __global__ __launch_bounds__(threads_of<L>()) void residual_norm_grad_kernel(Nor
       if (gate != 0.f)
         u.each([&](float& v, int j, int i) {
           if constexpr (kLdsSums) {
-            float2& s2 = post_sums[(j * kE + i) * kThreads + threadIdx.x];
-            s2 = make_float2(__builtin_fmaf(v, ahat.p[j].v[i], s2.x), s2.y + v);
+            slot(3, j, i) = __builtin_fmaf(v, ahat.p[j].v[i], slot(3, j, i));
+            slot(4, j, i) += v;
           } else {
             sum[3].p[j].v[i] = __builtin_fmaf(v, ahat.p[j].v[i], sum[3].p[j].v[i]);
             sum[4].p[j].v[i] += v;
@@ -314,10 +365,7 @@ __global__ __launch_bounds__(threads_of<L>()) void residual_norm_grad_kernel(Nor
   for (int n = 0; n < (POST ? 5 : 3); ++n) {
     R all;
     if (n < kSums) all = sum[n < kSums ? n : 0];
-    else all.each([&](float& v, int j, int i) {
-      const float2 s2 = post_sums[(j * kE + i) * kThreads + threadIdx.x];
-      v = n == 3 ? s2.x : s2.y;
-    });
+    else all.each([&](float& v, int j, int i) { v = slot(n, j, i); });
     if (kGroups > 1) {
       constexpr int kCols = L * NP * kE;
       __syncthreads();
@@ -345,7 +393,8 @@ struct FinishArgs {
   int32_t parts, C;
 };
 
-// The workgroups' sums added in 64 bits: 64 columns of one parameter a workgroup.
+// The workgroups' sums added in 64 bits: 16 columns of one parameter a workgroup, 32 parts side by side, eight
+// loads of each on their way at a time.
 __global__ __launch_bounds__(kFinishThreads) void norm_finish_kernel(FinishArgs f) {
   constexpr int kRows = kFinishThreads / kFinishCols;
   __shared__ double meet[kRows][kFinishCols];
@@ -354,7 +403,16 @@ __global__ __launch_bounds__(kFinishThreads) void norm_finish_kernel(FinishArgs 
   const int col = blockIdx.x * kFinishCols + threadIdx.x % kFinishCols, row = threadIdx.x / kFinishCols;
   double s = 0.0;
   if (col < f.C)
-    for (int p = row; p < f.parts; p += kRows) s += f.part[(static_cast<int64_t>(p) * kParams + blockIdx.y) * f.C + col];
+    for (int p = row; p < f.parts; p += 8 * kRows) {
+      float x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int64_t at = static_cast<int64_t>(min(p + i * kRows, f.parts - 1)) * kParams + blockIdx.y;
+        x[i] = f.part[at * f.C + col];
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s += p + i * kRows < f.parts ? x[i] : 0.f;
+    }
   meet[row][threadIdx.x % kFinishCols] = s;
   __syncthreads();
   if (row == 0 && col < f.C) {
@@ -368,8 +426,9 @@ int lanes_of(int pieces) { return pieces <= 32 ? 16 : pieces <= 128 ? 64 : piece
 
 // Workgroups of a launch: what the GPU holds a few times over, each with rows to spare.
 int64_t groups_of(int64_t T, int32_t C, int dtype, int64_t most) {
-  const int L = lanes_of(C * elem_bytes(dtype) / 16), rows = L >= 256 ? 1 : 256 / L;
-  return std::min((T + rows - 1) / rows, L == 512 ? most / 2 : most);
+  const int pieces = C * elem_bytes(dtype) / 16, L = lanes_of(pieces), rows = L >= 256 ? 1 : 256 / L;
+  const bool wide = L == 512 || (dtype == DORA_BF16 && pieces > L);  // 16 elements a lane: half as many fit
+  return std::min((T + rows - 1) / rows, wide ? most / 2 : most);
 }
 constexpr int64_t kForwardGroups = 2048, kBackwardGroups = 1024;
 

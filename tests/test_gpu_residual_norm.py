@@ -130,8 +130,8 @@ def test_far_means(gpu, dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
-def test_in_place_and_strided(gpu, dtype):
-    T, C = 50, 264
+@pytest.mark.parametrize("T,C", [(50, 264), (700, 8192), (3000, 128)])
+def test_in_place_and_strided(gpu, dtype, T, C):
     t, p = inputs(T, C, dtype, "layer", True, True, True, 6)
     d, q = cuda(t), cuda(p)
     h, y = gpu.dora_residual_norm(d["x"], d["a"], **q)
