@@ -400,6 +400,232 @@ __global__ __launch_bounds__(kThreads) void attn_kernel(AttnArgs a) {
   for (int dt = 0; dt < D / 16; ++dt) store4<E>(to + (dt * 16 + 4 * g) * sizeof(E), o[dt] * inv);
 }
 
+// ------------------------- bf16 in tiles of 128 ---------------------------
+
+// Products of 32 x 32 in steps of 16: lane l (c = l % 32, hi = l / 32) holds
+// elements 8 hi .. 8 hi + 7 of row or column c, the result's lane column c, rows
+// 8 (i / 4) + 4 hi + i % 4.  One operand read from LDS serves 32 columns in place
+// of 16, which halves the LDS reads, what bounds the 16-wide kernels.
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+typedef __attribute__((address_space(3))) void lds_void;
+
+__device__ __attribute__((aligned(256))) const uint4 zero_row[16] = {};
+
+constexpr int kWide = 128;      // rows of a workgroup, 32 a wave
+constexpr int kWideKeys = 64;   // rows of a staged tile
+
+// Staged rows stand unpadded, the 16-byte pieces of row r moved by turn(r): eight
+// rows' reads of one piece, and the transposing reads of four rows by two pieces,
+// fall on banks of their own.
+__device__ __forceinline__ int turn(int r) { return (r & 3) << 1 | (r >> 2 & 1); }
+
+// 64 rows on their way to LDS by DMA, rows at n and past it zeros; address(row) the first byte of a real row.
+template <int D, class F>
+__device__ __forceinline__ void stage_rows(__bf16* to, int n, F address) {
+  constexpr int kPieces = D / 8, kRows = 64 / kPieces;  // of an instruction's rows
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
+#pragma unroll
+  for (int i = 0; i < kWideKeys / kRows / 4; ++i) {
+    const int row0 = (i * 4 + wave) * kRows, row = row0 + lane / kPieces, piece = (lane % kPieces) ^ turn(row);
+    const char* from = row < n ? address(row) : reinterpret_cast<const char*>(zero_row);
+    __builtin_amdgcn_global_load_lds(from + piece * 16, (lds_void*)(to + row0 * D), 16, 0, 0);
+  }
+}
+
+// Everything that this workgroup staged has arrived, and every wave is done with what stood there.
+__device__ __forceinline__ void staged() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+__device__ __forceinline__ floatx16 mma32(bf16x8 a, bf16x8 b, floatx16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+
+// Row r0 + c of a staged tile, elements 16 st + 8 hi .. + 7 (r0 a multiple of 32).
+template <int D>
+__device__ __forceinline__ bf16x8 wide_row(const __bf16* tile, int r0, int st) {
+  const int lane = threadIdx.x & 63, c = lane & 31, hi = lane >> 5;
+  return *reinterpret_cast<const bf16x8*>(tile + (r0 + c) * D + ((2 * st + hi) ^ turn(c)) * 8);
+}
+// Column d0 + c (d0 a multiple of 32) of staged rows r0 + 4 hi .. + 3 and r0 + 8 + 4 hi .. + 3 (r0 a multiple of 16).
+template <int D>
+__device__ __forceinline__ bf16x8 wide_column(const __bf16* tile, int r0, int d0) {
+  typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
+  const int lane = threadIdx.x & 63, hi = lane >> 5, half = lane >> 4 & 1, e = (lane & 15) >> 2, r = lane & 3;
+  const int row = 4 * hi + e, piece = d0 / 8 + 2 * half + (r >> 1);
+  // turn(row + 8) = turn(row): the second read is eight rows on
+  __bf16* p = const_cast<__bf16*>(tile) + (r0 + row) * D + (piece ^ turn(row)) * 8 + (r & 1) * 4;
+  const bf16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)p);
+  const bf16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(p + 8 * D));
+  return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+// Elements 8t .. 8t + 7 of a result as the operand of 16 rows, in the order of wide_column.
+__device__ __forceinline__ bf16x8 wide_pack(const floatx16& x, int t) {
+  bf16x8 f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f[i] = static_cast<__bf16>(x[8 * t + i]);
+  return f;
+}
+__device__ __forceinline__ floatx16 zero16() {
+  floatx16 z;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) z[i] = 0.f;
+  return z;
+}
+__device__ __forceinline__ int wide_place(int i) { return 8 * (i / 4) + i % 4; }  // + 4 hi
+
+template <int D>
+struct WideTiles {
+  __bf16 a0[kWideKeys * D], b0[kWideKeys * D], a1[kWideKeys * D], b1[kWideKeys * D];
+};
+
+template <int D>
+struct WideForward {
+  bf16x8 q[D / 16];
+  floatx16 o[D / 32];
+  float m, l;
+  int limit;
+};
+
+// Values that are not finite among keys that some rows do not see: 0 times them is NaN.  The rows that see them take
+// them here (an infinite or NaN sum is what p times them gives), and zeros stand in their place.
+template <int D>
+__device__ __forceinline__ void take_odd(WideForward<D>& f, __bf16* vs, int end) {
+  const int hi = (threadIdx.x & 63) >> 5;
+  for (int at = 0; at < min(end, kWideKeys); ++at)
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+      for (int x = 0; x < 16; ++x) {
+        const int d = 32 * dt + wide_place(x) + 4 * hi;
+        const float v = static_cast<float>(vs[at * D + ((d / 8) ^ turn(at)) * 8 + d % 8]);
+        if (!(__builtin_fabsf(v) < INFINITY)) f.o[dt][x] += v;
+      }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kWideKeys * D / 8 / kThreads; ++i) {
+    __bf16* p = vs + (i * kThreads + threadIdx.x) * 8;
+    for (int x = 0; x < 8; ++x)
+      if (!(__builtin_fabsf(static_cast<float>(p[x])) < INFINITY)) p[x] = static_cast<__bf16>(0.f);
+  }
+  __syncthreads();
+}
+
+// 64 staged keys.  The maximum that p is taken against rises only when a score passes it by 2^8: p, l and the
+// products' sums stay far inside their range, and the sums are multiplied a few times in place of every tile.
+template <int D>
+__device__ __forceinline__ void wide_keys(const AttnArgs& a, WideForward<D>& f, const __bf16* ks, __bf16* vs, int end,
+                                          bool masked, bool odd) {
+  const int hi = (threadIdx.x & 63) >> 5;
+  floatx16 s[2];
+#pragma unroll
+  for (int n = 0; n < 2; ++n) {
+    s[n] = zero16();
+#pragma unroll
+    for (int st = 0; st < D / 16; ++st) s[n] = mma32(wide_row<D>(ks, 32 * n, st), f.q[st], s[n]);
+  }
+  if (masked) {
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (32 * n + wide_place(i) + 4 * hi >= end) s[n][i] = -INFINITY;
+  }
+  float top = -INFINITY;
+#pragma unroll
+  for (int n = 0; n < 2; ++n)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) top = fmaxf(top, s[n][i]);
+  top = max32(top) * a.c2;
+  if (__any(top > f.m + 8.f)) {
+    const float next = fmaxf(f.m, top), keep = __builtin_amdgcn_exp2f(next == -INFINITY ? 0.f : f.m - next);
+    f.m = next;
+    f.l *= keep;
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt) f.o[dt] *= keep;
+  }
+  const float ref = f.m == -INFINITY ? 0.f : f.m;
+#pragma unroll
+  for (int n = 0; n < 2; ++n)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      s[n][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][i], a.c2, -ref));
+      f.l += s[n][i];
+    }
+  if (odd) take_odd<D>(f, vs, end);
+#pragma unroll
+  for (int n = 0; n < 2; ++n)
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const bf16x8 p = wide_pack(s[n], t);
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt) f.o[dt] = mma32(wide_column<D>(vs, 32 * n + 16 * t, 32 * dt), p, f.o[dt]);
+    }
+}
+
+// Some value of the staged tile is not finite.
+template <int D>
+__device__ __forceinline__ bool odd_tile(const __bf16* tile) {
+  bool ok = true;
+#pragma unroll
+  for (int i = 0; i < kWideKeys * D / 8 / kThreads; ++i)
+    ok = ok && finite_piece<__bf16>(*reinterpret_cast<const u32x4*>(tile + (i * kThreads + threadIdx.x) * 8));
+  return __syncthreads_or(!ok);
+}
+
+template <int D>
+__global__ __launch_bounds__(kThreads, 2) void attn_wide_kernel(AttnArgs a) {
+  __shared__ __attribute__((aligned(1024))) WideTiles<D> tiles;
+  if (check_block(a)) return;
+  const int lane = threadIdx.x & 63, c = lane & 31, hi = lane >> 5, wave = threadIdx.x >> 6;
+  const int hk = blockIdx.x % a.Hk, t = a.blocks / a.Hk - 1 - blockIdx.x / a.Hk;  // long tiles first
+  const int b = last_at_most(a.B, t, [&](int i) { return first_tile(a.cu_q, i, a.G, kWide); });
+  Seq s;
+  if (!sequence(a, b, &s)) return;
+  const int64_t tile = t - first_tile(a.cu_q, b, a.G, kWide);
+  const int rows = s.nq * a.G;
+  if (tile < 0 || tile * kWide >= rows) return;
+  const int row0 = static_cast<int>(tile) * kWide, row = row0 + wave * 32 + c;
+  const bool real = row < rows;
+  const int key_hi = limit_of(a, s, min(row0 + kWide, rows) - 1), open = limit_of(a, s, row0);
+  WideForward<D> f;
+  f.limit = limit_of(a, s, row);
+  f.m = -INFINITY, f.l = 0.f;
+#pragma unroll
+  for (int st = 0; st < D / 16; ++st)
+    f.q[st] = real ? load_frag<__bf16>(query_row(a, a.q, s, hk, row) + (16 * st + 8 * hi) * 2) : zero_frag<__bf16>();
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt) f.o[dt] = zero16();
+  const char* kbase = a.k.at + static_cast<int64_t>(s.k0) * a.k.row + hk * a.k.head;
+  const char* vbase = a.v.at + static_cast<int64_t>(s.k0) * a.v.row + hk * a.v.head;
+  const auto ask = [&](int key, __bf16* kt, __bf16* vt) {
+    stage_rows<D>(kt, s.nk - key, [&](int i) { return kbase + static_cast<int64_t>(key + i) * a.k.row; });
+    stage_rows<D>(vt, s.nk - key, [&](int i) { return vbase + static_cast<int64_t>(key + i) * a.v.row; });
+  };
+  // One tile in these buffers while the next comes into the others.
+  const auto step = [&](int key, __bf16* kt, __bf16* vt, __bf16* kn, __bf16* vn) {
+    staged();
+    if (key + kWideKeys < key_hi) ask(key + kWideKeys, kn, vn);
+    const bool masked = key + kWideKeys > open;
+    wide_keys<D>(a, f, kt, vt, f.limit - key, masked, masked && a.causal && odd_tile<D>(vt));
+  };
+  if (key_hi > 0) ask(0, tiles.a0, tiles.b0);
+  for (int key = 0; key < key_hi; key += 2 * kWideKeys) {
+    step(key, tiles.a0, tiles.b0, tiles.a1, tiles.b1);
+    if (key + kWideKeys >= key_hi) break;
+    step(key + kWideKeys, tiles.a1, tiles.b1, tiles.a0, tiles.b0);
+  }
+  const float l = add32(f.l), inv = l == 0.f ? 0.f : 1.f / l;
+  if (!real) return;
+  if (hi == 0 && a.lse) a.lse[stat_at(a, s, hk, row)] = l == 0.f ? -INFINITY : (f.m + __builtin_amdgcn_logf(l)) * kLn2;
+  char* to = const_cast<char*>(query_row(a, a.out, s, hk, row));
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      const floatx4 x = {f.o[dt][4 * n], f.o[dt][4 * n + 1], f.o[dt][4 * n + 2], f.o[dt][4 * n + 3]};
+      store4<__bf16>(to + (32 * dt + 8 * n + 4 * hi) * 2, x * inv);
+    }
+}
+
 // The parts of a row joined: one wave a row, out = sum w o / sum w l with w =
 // 2^(m - max m).
 template <class E, int D>
@@ -732,6 +958,10 @@ int32_t backward_splits(const Sizes& z) {
   return splits;
 }
 
+bool use_wide(const Sizes& z, int dtype) {
+  return dtype == DORA_BF16 && z.D >= 64 && z.total_q * (z.H / z.Hk) / z.B >= 96;
+}
+
 size_t round256(size_t n) { return (n + 255) & ~size_t(255); }
 
 size_t forward_bytes(const Sizes& z) {
@@ -836,7 +1066,8 @@ extern "C" int dora_grouped_attn(const dora_rows* q, const dora_rows* k, const d
   if (z.total_q == 0) return DORA_OK;
   const Split p = forward_split(z);
   const bool split = p.splits > 1 || p.chunk;
-  const int64_t blocks = p.blocks * z.Hk, join = (z.total_q * z.H + kThreads / 64 - 1) / (kThreads / 64);
+  const bool wide = !split && use_wide(z, q->dtype);
+  const int64_t blocks = (wide ? tiles(z.total_q * a.G, B, kWide) : p.blocks) * z.Hk, join = (z.total_q * z.H + kThreads / 64 - 1) / (kThreads / 64);
   if (blocks > kMaxBlocks || (split && join > kMaxBlocks)) return DORA_ERR_UNSUPPORTED;
   a.out = row_view(out);
   a.lse = lse_out;
@@ -852,6 +1083,9 @@ extern "C" int dora_grouped_attn(const dora_rows* q, const dora_rows* k, const d
     if (split) {
       hipLaunchKernelGGL((attn_kernel<E, D, true>), dim3(a.blocks + 1), dim3(kThreads), 0, st, a);
       hipLaunchKernelGGL((join_kernel<E, D>), dim3(static_cast<uint32_t>(join)), dim3(kThreads), 0, st, a);
+    } else if constexpr (sizeof(E) == 2 && D >= 64) {
+      if (wide) hipLaunchKernelGGL((attn_wide_kernel<D>), dim3(a.blocks + 1), dim3(kThreads), 0, st, a);
+      else hipLaunchKernelGGL((attn_kernel<E, D, false>), dim3(a.blocks + 1), dim3(kThreads), 0, st, a);
     } else {
       hipLaunchKernelGGL((attn_kernel<E, D, false>), dim3(a.blocks + 1), dim3(kThreads), 0, st, a);
     }
