@@ -47,7 +47,7 @@ struct AttnArgs {
   int32_t max_q, causal;
   float scale, c2;  // softmax_scale, softmax_scale * log2(e)
   float* lse;
-  float* delta;
+  float2* stat;  // of a row: log2 of its sum of exponentials, delta
   float* part;       // split sums
   float2* part_ml;   // of a row's part: m and l
   int32_t part_rows;  // rows of a part
@@ -409,8 +409,6 @@ __global__ __launch_bounds__(kThreads) void attn_kernel(AttnArgs a) {
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 typedef __attribute__((address_space(3))) void lds_void;
 
-__device__ __attribute__((aligned(256))) const uint4 zero_row[16] = {};
-
 constexpr int kWide = 128;      // rows of a workgroup, 32 a wave
 constexpr int kWideKeys = 64;   // rows of a staged tile
 
@@ -419,18 +417,63 @@ constexpr int kWideKeys = 64;   // rows of a staged tile
 // fall on banks of their own.
 __device__ __forceinline__ int turn(int r) { return (r & 3) << 1 | (r >> 2 & 1); }
 
-// 64 rows on their way to LDS by DMA, rows at n and past it zeros; address(row) the first byte of a real row.
-template <int D, class F>
-__device__ __forceinline__ void stage_rows(__bf16* to, int n, F address) {
-  constexpr int kPieces = D / 8, kRows = 64 / kPieces;  // of an instruction's rows
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
-#pragma unroll
-  for (int i = 0; i < kWideKeys / kRows / 4; ++i) {
-    const int row0 = (i * 4 + wave) * kRows, row = row0 + lane / kPieces, piece = (lane % kPieces) ^ turn(row);
-    const char* from = row < n ? address(row) : reinterpret_cast<const char*>(zero_row);
-    __builtin_amdgcn_global_load_lds(from + piece * 16, (lds_void*)(to + row0 * D), 16, 0, 0);
+// A lane's share of staging tiles of ROWS rows by DMA: an instruction moves 1 KB, whole rows; its address is one that all
+// lanes share and a 32-bit offset, formed once, so that a tile costs next to no vector arithmetic.  Rows at n and past it
+// are copies of row n - 1: what they are multiplied by is 0, and that they may not be finite is looked after.
+template <int D, int ROWS>
+struct Stage {
+  static constexpr int kPieces = D / 8, kRows = 64 / kPieces, kCount = ROWS / kRows / 4;
+  static __device__ __forceinline__ int first_row() {
+    return static_cast<int>(threadIdx.x >> 6) * kRows + (threadIdx.x & 63) / kPieces;
   }
-}
+  // Byte of the row that the lane moves (turn() of row 4 kRows i + r is that of row r).
+  static __device__ __forceinline__ uint32_t piece() { return ((threadIdx.x & 63) % kPieces ^ turn(first_row())) * 16; }
+  // address(i) of instruction i's first row, the same in all lanes; lane(i) the lane's offset from it, last(i) that of row
+  // n - 1.
+  template <class A, class L, class Z>
+  static __device__ __forceinline__ void run(__bf16* to, int n, A address, L lane, Z last) {
+    const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
+#pragma unroll
+    for (int i = 0; i < kCount; ++i) {
+      uint32_t off = lane(i);
+      if (n < ROWS) off = first_row() + i * 4 * kRows < n ? off : last(i);
+      __builtin_amdgcn_global_load_lds(address(i) + off, (lds_void*)(to + (i * 4 + wave) * kRows * D), 16, 0, 0);
+    }
+  }
+};
+// Rows one after another, `row` bytes apart.
+template <int D, int ROWS>
+struct KeyStage : Stage<D, ROWS> {
+  typedef Stage<D, ROWS> S;
+  uint32_t off, row;
+  __device__ __forceinline__ KeyStage(int64_t bytes)
+      : off(S::first_row() * static_cast<uint32_t>(bytes) + S::piece()), row(static_cast<uint32_t>(bytes)) {}
+  __device__ __forceinline__ void stage(__bf16* to, const char* tile, int n) const {
+    S::run(to, n, [&](int) { return tile; }, [&](int i) { return off + i * 4 * S::kRows * row; },
+           [&](int) { return (n - 1) * row + S::piece(); });
+  }
+};
+// The rows of whole queries: row r is query r / G of head r % G (G divides ROWS).
+template <int D, int ROWS>
+struct QueryStage : Stage<D, ROWS> {
+  typedef Stage<D, ROWS> S;
+  uint32_t off[S::kCount];
+  uint32_t row, head;
+  int group;
+  __device__ __forceinline__ QueryStage(const AttnArgs& a, const RowView& x)
+      : row(static_cast<uint32_t>(x.row)), head(static_cast<uint32_t>(x.head)), group(a.G) {
+#pragma unroll
+    for (int i = 0; i < S::kCount; ++i) off[i] = place(a, S::first_row() + i * 4 * S::kRows) + S::piece();
+  }
+  __device__ __forceinline__ uint32_t place(const AttnArgs& a, int r) const {
+    const int q = div_group(a, r);
+    return q * row + (r - q * group) * head;
+  }
+  __device__ __forceinline__ void stage(const AttnArgs& a, __bf16* to, const char* tile, int n) const {
+    S::run(to, n, [&](int) { return tile; }, [&](int i) { return off[i]; },
+           [&](int) { return place(a, n - 1) + S::piece(); });
+  }
+};
 
 // Everything that this workgroup staged has arrived, and every wave is done with what stood there.
 __device__ __forceinline__ void staged() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
@@ -439,20 +482,35 @@ __device__ __forceinline__ floatx16 mma32(bf16x8 a, bf16x8 b, floatx16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
 
+// A lane's places in a staged tile, in elements.  turn() moves pieces within groups of eight, so that pieces 64 or 128
+// elements on, and rows 16 on, lie at a constant distance, which the reads hold as their immediate.
+struct WidePlaces {
+  uint32_t row[4];     // row c, elements 16 st + 8 hi .. + 7, st 0 .. 3
+  uint32_t column[2];  // for the transposing read of columns 0 .. 31 and 32 .. 63: lane m = 4 e + r of sixteen points at row 4 hi + e
+};
+template <int D>
+__device__ __forceinline__ WidePlaces wide_places() {
+  const int lane = threadIdx.x & 63, c = lane & 31, hi = lane >> 5, half = lane >> 4 & 1, e = (lane & 15) >> 2, r = lane & 3;
+  const int row = 4 * hi + e;
+  WidePlaces w;
+#pragma unroll
+  for (int st = 0; st < 4; ++st) w.row[st] = c * D + ((2 * st + hi) ^ turn(c)) * 8;
+#pragma unroll
+  for (int n = 0; n < 2; ++n) w.column[n] = row * D + ((4 * n + 2 * half + (r >> 1)) ^ turn(row)) * 8 + (r & 1) * 4;
+  return w;
+}
+
 // Row r0 + c of a staged tile, elements 16 st + 8 hi .. + 7 (r0 a multiple of 32).
 template <int D>
-__device__ __forceinline__ bf16x8 wide_row(const __bf16* tile, int r0, int st) {
-  const int lane = threadIdx.x & 63, c = lane & 31, hi = lane >> 5;
-  return *reinterpret_cast<const bf16x8*>(tile + (r0 + c) * D + ((2 * st + hi) ^ turn(c)) * 8);
+__device__ __forceinline__ bf16x8 wide_row(const __bf16* tile, const WidePlaces& w, int r0, int st) {
+  return *reinterpret_cast<const bf16x8*>(tile + w.row[st % 4] + st / 4 * 64 + r0 * D);
 }
 // Column d0 + c (d0 a multiple of 32) of staged rows r0 + 4 hi .. + 3 and r0 + 8 + 4 hi .. + 3 (r0 a multiple of 16).
 template <int D>
-__device__ __forceinline__ bf16x8 wide_column(const __bf16* tile, int r0, int d0) {
+__device__ __forceinline__ bf16x8 wide_column(const __bf16* tile, const WidePlaces& w, int r0, int d0) {
   typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
-  const int lane = threadIdx.x & 63, hi = lane >> 5, half = lane >> 4 & 1, e = (lane & 15) >> 2, r = lane & 3;
-  const int row = 4 * hi + e, piece = d0 / 8 + 2 * half + (r >> 1);
   // turn(row + 8) = turn(row): the second read is eight rows on
-  __bf16* p = const_cast<__bf16*>(tile) + (r0 + row) * D + (piece ^ turn(row)) * 8 + (r & 1) * 4;
+  __bf16* p = const_cast<__bf16*>(tile) + w.column[d0 / 32 % 2] + d0 / 64 * 64 + r0 * D;
   const bf16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)p);
   const bf16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(p + 8 * D));
   return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
@@ -512,15 +570,15 @@ __device__ __forceinline__ void take_odd(WideForward<D>& f, __bf16* vs, int end)
 // 64 staged keys.  The maximum that p is taken against rises only when a score passes it by 2^8: p, l and the
 // products' sums stay far inside their range, and the sums are multiplied a few times in place of every tile.
 template <int D>
-__device__ __forceinline__ void wide_keys(const AttnArgs& a, WideForward<D>& f, const __bf16* ks, __bf16* vs, int end,
-                                          bool masked, bool odd) {
+__device__ __forceinline__ void wide_keys(const AttnArgs& a, WideForward<D>& f, const __bf16* ks, __bf16* vs,
+                                          const WidePlaces& w, int end, bool masked, bool odd) {
   const int hi = (threadIdx.x & 63) >> 5;
   floatx16 s[2];
 #pragma unroll
   for (int n = 0; n < 2; ++n) {
     s[n] = zero16();
 #pragma unroll
-    for (int st = 0; st < D / 16; ++st) s[n] = mma32(wide_row<D>(ks, 32 * n, st), f.q[st], s[n]);
+    for (int st = 0; st < D / 16; ++st) s[n] = mma32(wide_row<D>(ks, w, 32 * n, st), f.q[st], s[n]);
   }
   if (masked) {
 #pragma unroll
@@ -557,7 +615,7 @@ __device__ __forceinline__ void wide_keys(const AttnArgs& a, WideForward<D>& f, 
     for (int t = 0; t < 2; ++t) {
       const bf16x8 p = wide_pack(s[n], t);
 #pragma unroll
-      for (int dt = 0; dt < D / 32; ++dt) f.o[dt] = mma32(wide_column<D>(vs, 32 * n + 16 * t, 32 * dt), p, f.o[dt]);
+      for (int dt = 0; dt < D / 32; ++dt) f.o[dt] = mma32(wide_column<D>(vs, w, 32 * n + 16 * t, 32 * dt), p, f.o[dt]);
     }
 }
 
@@ -586,6 +644,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_wide_kernel(AttnArgs a) {
   const int row0 = static_cast<int>(tile) * kWide, row = row0 + wave * 32 + c;
   const bool real = row < rows;
   const int key_hi = limit_of(a, s, min(row0 + kWide, rows) - 1), open = limit_of(a, s, row0);
+  const WidePlaces w = wide_places<D>();
   WideForward<D> f;
   f.limit = limit_of(a, s, row);
   f.m = -INFINITY, f.l = 0.f;
@@ -596,16 +655,17 @@ __global__ __launch_bounds__(kThreads, 2) void attn_wide_kernel(AttnArgs a) {
   for (int dt = 0; dt < D / 32; ++dt) f.o[dt] = zero16();
   const char* kbase = a.k.at + static_cast<int64_t>(s.k0) * a.k.row + hk * a.k.head;
   const char* vbase = a.v.at + static_cast<int64_t>(s.k0) * a.v.row + hk * a.v.head;
+  const KeyStage<D, kWideKeys> kst(a.k.row), vst(a.v.row);
   const auto ask = [&](int key, __bf16* kt, __bf16* vt) {
-    stage_rows<D>(kt, s.nk - key, [&](int i) { return kbase + static_cast<int64_t>(key + i) * a.k.row; });
-    stage_rows<D>(vt, s.nk - key, [&](int i) { return vbase + static_cast<int64_t>(key + i) * a.v.row; });
+    kst.stage(kt, kbase + key * a.k.row, s.nk - key);
+    vst.stage(vt, vbase + key * a.v.row, s.nk - key);
   };
   // One tile in these buffers while the next comes into the others.
   const auto step = [&](int key, __bf16* kt, __bf16* vt, __bf16* kn, __bf16* vn) {
     staged();
     if (key + kWideKeys < key_hi) ask(key + kWideKeys, kn, vn);
     const bool masked = key + kWideKeys > open;
-    wide_keys<D>(a, f, kt, vt, f.limit - key, masked, masked && a.causal && odd_tile<D>(vt));
+    wide_keys<D>(a, f, kt, vt, w, f.limit - key, masked, masked && odd_tile<D>(vt));
   };
   if (key_hi > 0) ask(0, tiles.a0, tiles.b0);
   for (int key = 0; key < key_hi; key += 2 * kWideKeys) {
@@ -721,8 +781,8 @@ __global__ __launch_bounds__(kThreads) void grad_q_kernel(AttnArgs a) {
     for (int i = 0; i < 8; ++i) delta = __builtin_fmaf(static_cast<float>(x[i]), static_cast<float>(y[i]), delta);
   }
   delta = over_groups_sum(delta);
-  if (real && g == 0) a.delta[stat_at(a, s, hk, row)] = delta;
   const float lse2 = row_lse2(a, s, hk, row, real);
+  if (real && g == 0) a.stat[stat_at(a, s, hk, row)] = make_float2(lse2, delta);
   floatx4 dq[D / 16];
 #pragma unroll
   for (int dt = 0; dt < D / 16; ++dt) dq[dt] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -771,6 +831,306 @@ __global__ __launch_bounds__(kThreads) void grad_q_kernel(AttnArgs a) {
   for (int dt = 0; dt < D / 16; ++dt) store4<E>(to + (dt * 16 + 4 * g) * sizeof(E), dq[dt] * a.scale);
 }
 
+// The products that make x come before what follows: left alone, the compiler reads their operands here and forms them
+// where x is used, which takes the registers of all operands at once.
+__device__ __forceinline__ void formed(floatx16& x) { asm volatile("" : "+v"(x)); }
+
+// grad_q in tiles of 128 rows.
+template <int D>
+struct WideGradQ {
+  bf16x8 q[D / 16], g[D / 16];
+  floatx16 dq[D / 32];
+  float lse2, delta;
+};
+
+template <int D>
+__device__ __forceinline__ void wide_grad_q_keys(const AttnArgs& a, WideGradQ<D>& f, const __bf16* ks, const __bf16* vs,
+                                                 const WidePlaces& w, int end, bool masked) {
+  const int hi = (threadIdx.x & 63) >> 5;
+#pragma unroll
+  for (int n = 0; n < 2; ++n) {
+    floatx16 s = zero16(), dp = zero16();
+#pragma unroll
+    for (int st = 0; st < D / 16; ++st) s = mma32(wide_row<D>(ks, w, 32 * n, st), f.q[st], s);
+    formed(s);
+#pragma unroll
+    for (int st = 0; st < D / 16; ++st) dp = mma32(wide_row<D>(vs, w, 32 * n, st), f.g[st], dp);
+    formed(dp);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], a.c2, -f.lse2));
+      dp[i] = p * (dp[i] - f.delta);
+    }
+    if (masked) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (32 * n + wide_place(i) + 4 * hi >= end) dp[i] = 0.f;
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const bf16x8 ds = wide_pack(dp, t);
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt) f.dq[dt] = mma32(wide_column<D>(ks, w, 32 * n + 16 * t, 32 * dt), ds, f.dq[dt]);
+    }
+  }
+}
+
+template <int D>
+__global__ __launch_bounds__(kThreads, 2) void grad_q_wide_kernel(AttnArgs a) {
+  __shared__ __attribute__((aligned(1024))) WideTiles<D> tiles;
+  if (check_block(a)) return;
+  const int lane = threadIdx.x & 63, c = lane & 31, hi = lane >> 5, wave = threadIdx.x >> 6;
+  const int hk = blockIdx.x % a.Hk, t = a.blocks / a.Hk - 1 - blockIdx.x / a.Hk;  // long tiles first
+  const int b = last_at_most(a.B, t, [&](int i) { return first_tile(a.cu_q, i, a.G, kWide); });
+  Seq s;
+  if (!sequence(a, b, &s)) return;
+  const int64_t tile = t - first_tile(a.cu_q, b, a.G, kWide);
+  const int rows = s.nq * a.G;
+  if (tile < 0 || tile * kWide >= rows) return;
+  const int row0 = static_cast<int>(tile) * kWide, row = row0 + wave * 32 + c;
+  const bool real = row < rows;
+  const int key_hi = limit_of(a, s, min(row0 + kWide, rows) - 1), open = limit_of(a, s, row0);
+  const int limit = limit_of(a, s, row);
+  const WidePlaces w = wide_places<D>();
+  WideGradQ<D> f;
+  float delta = 0.f;
+#pragma unroll
+  for (int st = 0; st < D / 16; ++st) {
+    const int off = (16 * st + 8 * hi) * 2;
+    f.q[st] = real ? load_frag<__bf16>(query_row(a, a.q, s, hk, row) + off) : zero_frag<__bf16>();
+    f.g[st] = real ? load_frag<__bf16>(query_row(a, a.dout, s, hk, row) + off) : zero_frag<__bf16>();
+    const bf16x8 o = real ? load_frag<__bf16>(query_row(a, a.out, s, hk, row) + off) : zero_frag<__bf16>();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) delta = __builtin_fmaf(static_cast<float>(f.g[st][i]), static_cast<float>(o[i]), delta);
+  }
+  f.delta = add32(delta);
+  f.lse2 = row_lse2(a, s, hk, row, real);
+  if (real && hi == 0) a.stat[stat_at(a, s, hk, row)] = make_float2(f.lse2, f.delta);
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt) f.dq[dt] = zero16();
+  const char* kbase = a.k.at + static_cast<int64_t>(s.k0) * a.k.row + hk * a.k.head;
+  const char* vbase = a.v.at + static_cast<int64_t>(s.k0) * a.v.row + hk * a.v.head;
+  const KeyStage<D, kWideKeys> kst(a.k.row), vst(a.v.row);
+  const auto ask = [&](int key, __bf16* kt, __bf16* vt) {
+    kst.stage(kt, kbase + key * a.k.row, s.nk - key);
+    vst.stage(vt, vbase + key * a.v.row, s.nk - key);
+  };
+  const auto step = [&](int key, const __bf16* kt, const __bf16* vt, __bf16* kn, __bf16* vn) {
+    staged();
+    if (key + kWideKeys < key_hi) ask(key + kWideKeys, kn, vn);
+    wide_grad_q_keys<D>(a, f, kt, vt, w, limit - key, key + kWideKeys > open);
+  };
+  if (key_hi > 0) ask(0, tiles.a0, tiles.b0);
+  for (int key = 0; key < key_hi; key += 2 * kWideKeys) {
+    step(key, tiles.a0, tiles.b0, tiles.a1, tiles.b1);
+    if (key + kWideKeys >= key_hi) break;
+    step(key + kWideKeys, tiles.a1, tiles.b1, tiles.a0, tiles.b0);
+  }
+  if (!real) return;
+  char* to = const_cast<char*>(query_row(a, a.dq, s, hk, row));
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      const floatx4 x = {f.dq[dt][4 * n], f.dq[dt][4 * n + 1], f.dq[dt][4 * n + 2], f.dq[dt][4 * n + 3]};
+      store4<__bf16>(to + (32 * dt + 8 * n + 4 * hi) * 2, x * a.scale);
+    }
+}
+
+// grad_kv in tiles of 128 keys, 32 a wave.  The sums of dk and dv of 128-wide heads, the keys' and the values' operands
+// take 192 of the 256 registers that two waves a SIMD leave, too many beside the scores: there, half of the workgroups form
+// dv and half dk, each with its own scores (five products in place of four).
+enum Part { kBoth, kDv, kDk };
+
+template <int D, Part PART>
+struct WideGradKv {
+  bf16x8 k[D / 16], v[PART == kDv ? 1 : D / 16];
+  floatx16 dk[PART == kDv ? 1 : D / 32], dv[PART == kDk ? 1 : D / 32];
+};
+
+template <int D>
+struct WideKvLds {
+  struct Stats {
+    float lse2[kWideKeys], delta[kWideKeys];
+    int limit[kWideKeys];
+  } stats[2];  // in front: their reads' offsets fit the instructions
+  __attribute__((aligned(1024))) __bf16 q0[kWideKeys * D], g0[kWideKeys * D], q1[kWideKeys * D], g1[kWideKeys * D];
+};
+
+template <int D, Part PART>
+__device__ __forceinline__ void wide_grad_kv_rows(const AttnArgs& a, WideGradKv<D, PART>& f, const __bf16* qs,
+                                                  const __bf16* gs, const WidePlaces& w,
+                                                  const typename WideKvLds<D>::Stats& stats, int key, bool masked) {
+  const int hi = (threadIdx.x & 63) >> 5;
+#pragma unroll
+  for (int n = 0; n < 2; ++n) {
+    floatx16 s = zero16(), dp = zero16();
+#pragma unroll
+    for (int st = 0; st < D / 16; ++st) s = mma32(wide_row<D>(qs, w, 32 * n, st), f.k[st], s);
+    formed(s);
+    if constexpr (PART != kDv) {
+#pragma unroll
+      for (int st = 0; st < D / 16; ++st) dp = mma32(wide_row<D>(gs, w, 32 * n, st), f.v[st], dp);
+      formed(dp);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int at = 32 * n + 8 * j + 4 * hi;
+      const floatx4 l4 = *reinterpret_cast<const floatx4*>(stats.lse2 + at);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[4 * j + i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[4 * j + i], a.c2, -l4[i]));
+      if constexpr (PART != kDv) {
+        const floatx4 d4 = *reinterpret_cast<const floatx4*>(stats.delta + at);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) dp[4 * j + i] = s[4 * j + i] * (dp[4 * j + i] - d4[i]);
+      }
+    }
+    if (masked) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int4 m4 = *reinterpret_cast<const int4*>(stats.limit + 32 * n + 8 * j + 4 * hi);
+        const int lim[4] = {m4.x, m4.y, m4.z, m4.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (key >= lim[i]) s[4 * j + i] = dp[4 * j + i] = 0.f;
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      if constexpr (PART != kDk) {
+        const bf16x8 p = wide_pack(s, t);
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt) f.dv[dt] = mma32(wide_column<D>(gs, w, 32 * n + 16 * t, 32 * dt), p, f.dv[dt]);
+      }
+      if constexpr (PART != kDv) {
+        const bf16x8 ds = wide_pack(dp, t);
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt) f.dk[dt] = mma32(wide_column<D>(qs, w, 32 * n + 16 * t, 32 * dt), ds, f.dk[dt]);
+      }
+    }
+  }
+}
+
+template <int D, bool SPLIT, Part PART>
+__device__ __forceinline__ void grad_kv_wide(const AttnArgs& a, int block, WideKvLds<D>& lds) {
+  constexpr int kRows = kWideKeys;
+  const int lane = threadIdx.x & 63, c = lane & 31, hi = lane >> 5, wave = threadIdx.x >> 6;
+  const int hk = block % a.Hk, rest = block / a.Hk;
+  const int split = SPLIT ? rest % a.splits : 0, t = SPLIT ? rest / a.splits : rest;
+  const int b = last_at_most(a.B, t, [&](int i) { return first_tile(a.cu_k, i, 1, kWide); });
+  Seq s;
+  if (!sequence(a, b, &s)) return;
+  const int64_t tile = t - first_tile(a.cu_k, b, 1, kWide);
+  if (tile < 0 || tile * kWide >= s.nk) return;
+  const int key0 = static_cast<int>(tile) * kWide, key = key0 + wave * 32 + c;
+  const bool real = key < s.nk;
+  const int rows = s.nq * a.G;
+  int row_lo = a.causal ? min(rows, max(0, key0 - s.nk + s.nq) * a.G) : 0, row_hi = rows;
+  // Rows from here on see every key of the tile that exists.
+  const int open = a.causal ? max(0, min(key0 + kWide, s.nk) - 1 - s.nk + s.nq) * a.G : 0;
+  if (SPLIT) {
+    const int each = ((rows - row_lo + a.splits - 1) / a.splits + kRows - 1) / kRows * kRows;
+    row_lo = min(rows, row_lo + split * each);
+    row_hi = min(rows, row_lo + each);
+  }
+  const char* kbase = a.k.at + (static_cast<int64_t>(s.k0) + key0) * a.k.row + hk * a.k.head;
+  const char* vbase = a.v.at + (static_cast<int64_t>(s.k0) + key0) * a.v.row + hk * a.v.head;
+  const WidePlaces w = wide_places<D>();
+  WideGradKv<D, PART> f;
+#pragma unroll
+  for (int st = 0; st < D / 16; ++st) {
+    const int64_t own = wave * 32 + c;
+    const int off = (16 * st + 8 * hi) * 2;
+    f.k[st] = real ? load_frag<__bf16>(kbase + own * a.k.row + off) : zero_frag<__bf16>();
+    if constexpr (PART != kDv) f.v[st] = real ? load_frag<__bf16>(vbase + own * a.v.row + off) : zero_frag<__bf16>();
+  }
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt) {
+    if constexpr (PART != kDv) f.dk[dt] = zero16();
+    if constexpr (PART != kDk) f.dv[dt] = zero16();
+  }
+  float2 stat = {};
+  // A tile's rows are whole queries (G divides the tile, and row_lo is a multiple of it).
+  const QueryStage<D, kRows> qst(a, a.q), gst(a, a.dout);
+  const char* qbase = a.q.at + s.q0 * a.q.row + hk * a.G * a.q.head;
+  const char* gbase = a.dout.at + s.q0 * a.dout.row + hk * a.G * a.dout.head;
+  const auto ask = [&](int r, __bf16* qt, __bf16* gt) {
+    const int64_t n = div_group(a, r);
+    qst.stage(a, qt, qbase + n * a.q.row, row_hi - r);
+    gst.stage(a, gt, gbase + n * a.dout.row, row_hi - r);
+  };
+  // The rows' statistics go through a register, one tile ahead of their LDS.
+  const auto ask_stat = [&](int r) {
+    const int row = min(r + static_cast<int>(threadIdx.x), row_hi - 1);
+    if (threadIdx.x < kRows) stat = a.stat[stat_at(a, s, hk, row)];
+  };
+  const auto put_stat = [&](int r, typename WideKvLds<D>::Stats& x) {
+    if (threadIdx.x >= kRows) return;
+    const int row = r + threadIdx.x;
+    const bool here = row < row_hi;
+    x.lse2[threadIdx.x] = here ? stat.x : INFINITY;
+    x.delta[threadIdx.x] = here ? stat.y : 0.f;
+    x.limit[threadIdx.x] = here ? limit_of(a, s, row) : 0;
+  };
+  const auto step = [&](int r, const __bf16* qt, const __bf16* gt, const typename WideKvLds<D>::Stats& here, __bf16* qn,
+                        __bf16* gn, typename WideKvLds<D>::Stats& next) {
+    staged();
+    const bool more = r > row_lo;
+    if (more) {
+      ask_stat(r - kRows);
+      ask(r - kRows, qn, gn);
+    }
+    wide_grad_kv_rows<D, PART>(a, f, qt, gt, w, here, key, r < open || r + kRows > row_hi);
+    if (more) put_stat(r - kRows, next);
+  };
+  // From the last rows back: every tile of keys begins with the same rows, and the tiles at work share them in the L2
+  // (forward, each begins at its own: 4050 us in place of LATER).
+  const int last = row_lo + max(row_hi - row_lo - 1, 0) / kRows * kRows;
+  if (row_lo < row_hi) {
+    ask_stat(last);
+    ask(last, lds.q0, lds.g0);
+    put_stat(last, lds.stats[0]);
+    for (int r = last; r >= row_lo; r -= 2 * kRows) {
+      step(r, lds.q0, lds.g0, lds.stats[0], lds.q1, lds.g1, lds.stats[1]);
+      if (r == row_lo) break;
+      step(r - kRows, lds.q1, lds.g1, lds.stats[1], lds.q0, lds.g0, lds.stats[0]);
+    }
+  }
+  if (!real) return;
+  const int64_t at = static_cast<int64_t>(s.k0) + key;
+  float* part = SPLIT ? a.part + ((split * a.Hk + hk) * a.total_k + at) * 2 * D : nullptr;
+  char* kto = a.dk.at + at * a.dk.row + hk * a.dk.head;
+  char* vto = a.dv.at + at * a.dv.row + hk * a.dv.head;
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      const int d = 32 * dt + 8 * n + 4 * hi;
+      if constexpr (PART != kDv) {
+        const floatx4 x = {f.dk[dt][4 * n], f.dk[dt][4 * n + 1], f.dk[dt][4 * n + 2], f.dk[dt][4 * n + 3]};
+        if (SPLIT) *reinterpret_cast<floatx4*>(part + d) = x;
+        else store4<__bf16>(kto + d * 2, x * a.scale);
+      }
+      if constexpr (PART != kDk) {
+        const floatx4 y = {f.dv[dt][4 * n], f.dv[dt][4 * n + 1], f.dv[dt][4 * n + 2], f.dv[dt][4 * n + 3]};
+        if (SPLIT) *reinterpret_cast<floatx4*>(part + D + d) = y;
+        else store4<__bf16>(vto + d * 2, y);
+      }
+    }
+}
+
+template <int D, bool SPLIT>
+__global__ __launch_bounds__(kThreads, 2) void grad_kv_wide_kernel(AttnArgs a) {
+  __shared__ __attribute__((aligned(1024))) WideKvLds<D> lds;
+  if constexpr (D == 64) {
+    grad_kv_wide<D, SPLIT, kBoth>(a, blockIdx.x, lds);
+  } else {
+    const int hk = blockIdx.x % a.Hk, rest = blockIdx.x / a.Hk, block = rest / 2 * a.Hk + hk;
+    if (rest % 2) grad_kv_wide<D, SPLIT, kDv>(a, block, lds);
+    else grad_kv_wide<D, SPLIT, kDk>(a, block, lds);
+  }
+}
+
 // dk and dv of 64 keys over the rows that see them.
 template <class E, int D, bool SPLIT>
 __global__ __launch_bounds__(kThreads) void grad_kv_kernel(AttnArgs a) {
@@ -812,7 +1172,7 @@ __global__ __launch_bounds__(kThreads) void grad_kv_kernel(AttnArgs a) {
 #pragma unroll
   for (int dt = 0; dt < D / 16; ++dt) dk[dt] = dv[dt] = floatx4{0.f, 0.f, 0.f, 0.f};
   Tile qt, gt;
-  float lse2 = 0.f, delta = 0.f;
+  float2 stat = {};
   int limit = 0;
   const auto ask = [&](int r) {
     qt.load(row_hi - r, [&](int i) { return query_row(a, a.q, s, hk, r + i); });
@@ -820,8 +1180,7 @@ __global__ __launch_bounds__(kThreads) void grad_kv_kernel(AttnArgs a) {
     if (threadIdx.x < kRows) {
       const int row = r + threadIdx.x;
       const bool here = row < row_hi;
-      lse2 = row_lse2(a, s, hk, row, here);
-      delta = here ? a.delta[stat_at(a, s, hk, row)] : 0.f;
+      stat = here ? a.stat[stat_at(a, s, hk, row)] : make_float2(INFINITY, 0.f);
       limit = here ? limit_of(a, s, row) : 0;
     }
   };
@@ -831,8 +1190,8 @@ __global__ __launch_bounds__(kThreads) void grad_kv_kernel(AttnArgs a) {
     qt.store(qs);
     gt.store(gs);
     if (threadIdx.x < kRows) {
-      reinterpret_cast<float*>(lse_s)[threadIdx.x] = lse2;
-      reinterpret_cast<float*>(delta_s)[threadIdx.x] = delta;
+      reinterpret_cast<float*>(lse_s)[threadIdx.x] = stat.x;
+      reinterpret_cast<float*>(delta_s)[threadIdx.x] = stat.y;
       reinterpret_cast<int*>(limit_s)[threadIdx.x] = limit;
     }
     __syncthreads();
@@ -958,8 +1317,15 @@ int32_t backward_splits(const Sizes& z) {
   return splits;
 }
 
-bool use_wide(const Sizes& z, int dtype) {
-  return dtype == DORA_BF16 && z.D >= 64 && z.total_q * (z.H / z.Hk) / z.B >= 96;
+// The 128-row kernels: where a tile is mostly rows that exist, and the bytes from a staged tile's first row to its last
+// fit the 32-bit offsets (a stride of 2^23 bytes on).
+bool near(const RowView& x, int64_t rows, int64_t heads) { return x.row * rows + x.head * heads < (int64_t{1} << 31); }
+bool use_wide(const Sizes& z, int dtype, const AttnArgs& a) {
+  return dtype == DORA_BF16 && z.D >= 64 && z.total_q * a.G / z.B >= 96 && near(a.k, 128, 0) && near(a.v, 128, 0);
+}
+bool use_wide_kv(const Sizes& z, int dtype, const AttnArgs& a) {
+  return dtype == DORA_BF16 && z.D >= 64 && z.total_k / z.B >= 96 && 32 % a.G == 0 && near(a.v, 128, 0) &&
+         near(a.q, 64, a.G) && near(a.dout, 64, a.G);
 }
 
 size_t round256(size_t n) { return (n + 255) & ~size_t(255); }
@@ -969,10 +1335,10 @@ size_t forward_bytes(const Sizes& z) {
   if (p.splits == 1 && !p.chunk) return 256;
   return round256(static_cast<size_t>(p.blocks) * z.Hk * p.part_rows * (z.D + 2) * sizeof(float));
 }
-size_t delta_bytes(const Sizes& z) { return round256(static_cast<size_t>(z.total_q) * z.H * sizeof(float)); }
+size_t stat_bytes(const Sizes& z) { return round256(static_cast<size_t>(z.total_q) * z.H * sizeof(float2)); }
 size_t backward_bytes(const Sizes& z) {
   const int32_t splits = backward_splits(z);
-  return delta_bytes(z) + 256 +
+  return stat_bytes(z) + 256 +
          (splits == 1 ? 0 : round256(static_cast<size_t>(splits) * z.Hk * z.total_k * 2 * z.D * sizeof(float)));
 }
 
@@ -1066,7 +1432,7 @@ extern "C" int dora_grouped_attn(const dora_rows* q, const dora_rows* k, const d
   if (z.total_q == 0) return DORA_OK;
   const Split p = forward_split(z);
   const bool split = p.splits > 1 || p.chunk;
-  const bool wide = !split && use_wide(z, q->dtype);
+  const bool wide = !split && use_wide(z, q->dtype, a);
   const int64_t blocks = (wide ? tiles(z.total_q * a.G, B, kWide) : p.blocks) * z.Hk, join = (z.total_q * z.H + kThreads / 64 - 1) / (kThreads / 64);
   if (blocks > kMaxBlocks || (split && join > kMaxBlocks)) return DORA_ERR_UNSUPPORTED;
   a.out = row_view(out);
@@ -1115,31 +1481,44 @@ extern "C" int dora_grouped_attn_backward(const dora_rows* dout, const dora_rows
                  {{workspace, backward_bytes(z)}, {dev_status, sizeof(int32_t)}},
                  {{cu_q, cu_bytes}, {cu_k, cu_bytes}, {lse, static_cast<size_t>(z.total_q) * z.H * sizeof(float)}}))
     return DORA_ERR_OVERLAP;
-  const int64_t q_blocks = tiles(z.total_q * a.G, B, kTile) * z.Hk;
+  a.dout = row_view(dout);
+  const bool wide_q = use_wide(z, q->dtype, a), wide_kv = use_wide_kv(z, q->dtype, a);
+  const int64_t q_blocks = tiles(z.total_q * a.G, B, wide_q ? kWide : kTile) * z.Hk;
   const int32_t splits = backward_splits(z);
-  const int64_t kv_blocks = tiles(z.total_k, B, kTile) * z.Hk * splits;
+  const int64_t kv_blocks = tiles(z.total_k, B, wide_kv ? kWide : kTile) * z.Hk * splits * (wide_kv && z.D == 128 ? 2 : 1);
   const int keys_here = kThreads / (2 * z.D / 4);
   const int64_t join = (z.total_k + keys_here - 1) / keys_here * z.Hk;
   if (q_blocks > kMaxBlocks || kv_blocks > kMaxBlocks || join > kMaxBlocks) return DORA_ERR_UNSUPPORTED;
-  a.out = row_view(out), a.dout = row_view(dout);
+  a.out = row_view(out);
   a.dq = row_view(dq), a.dk = row_view(dk), a.dv = row_view(dv);
   a.lse = const_cast<float*>(lse);
-  a.delta = static_cast<float*>(workspace);
-  a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + delta_bytes(z));
+  a.stat = static_cast<float2*>(workspace);
+  a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + stat_bytes(z));
   a.splits = splits;
   a.blocks = static_cast<int32_t>(q_blocks);
   hipStream_t st = static_cast<hipStream_t>(stream);
   with_type(q->dtype, z.D, [&](auto e, auto d) {
     typedef decltype(e) E;
     constexpr int D = decltype(d)::value;
-    hipLaunchKernelGGL((grad_q_kernel<E, D>), dim3(a.blocks + 1), dim3(kThreads), 0, st, a);
-    if (z.total_k == 0) return;
-    if (splits > 1) {
-      hipLaunchKernelGGL((grad_kv_kernel<E, D, true>), dim3(static_cast<uint32_t>(kv_blocks)), dim3(kThreads), 0, st, a);
-      hipLaunchKernelGGL((join_kv_kernel<E, D>), dim3(static_cast<uint32_t>(join)), dim3(kThreads), 0, st, a);
-    } else {
-      hipLaunchKernelGGL((grad_kv_kernel<E, D, false>), dim3(static_cast<uint32_t>(kv_blocks)), dim3(kThreads), 0, st, a);
+    const dim3 gq(a.blocks + 1), gkv(static_cast<uint32_t>(kv_blocks)), block(kThreads);
+    bool launched_q = false, launched_kv = z.total_k == 0;
+    if constexpr (sizeof(E) == 2 && D >= 64) {
+      if (wide_q) hipLaunchKernelGGL((grad_q_wide_kernel<D>), gq, block, 0, st, a);
+      if (wide_kv && !launched_kv) {
+        if (!wide_q) hipLaunchKernelGGL((grad_q_kernel<E, D>), gq, block, 0, st, a);
+        launched_q = launched_kv = true;
+        if (splits > 1) hipLaunchKernelGGL((grad_kv_wide_kernel<D, true>), gkv, block, 0, st, a);
+        else hipLaunchKernelGGL((grad_kv_wide_kernel<D, false>), gkv, block, 0, st, a);
+      }
+      launched_q = launched_q || wide_q;
     }
+    if (!launched_q) hipLaunchKernelGGL((grad_q_kernel<E, D>), gq, block, 0, st, a);
+    if (!launched_kv) {
+      if (splits > 1) hipLaunchKernelGGL((grad_kv_kernel<E, D, true>), gkv, block, 0, st, a);
+      else hipLaunchKernelGGL((grad_kv_kernel<E, D, false>), gkv, block, 0, st, a);
+    }
+    if (splits > 1 && z.total_k > 0)
+      hipLaunchKernelGGL((join_kv_kernel<E, D>), dim3(static_cast<uint32_t>(join)), block, 0, st, a);
   });
   return hipGetLastError() == hipSuccess ? DORA_OK : DORA_ERR_HIP;
 }
