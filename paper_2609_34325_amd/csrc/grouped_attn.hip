@@ -412,66 +412,64 @@ typedef __attribute__((address_space(3))) void lds_void;
 constexpr int kWide = 128;      // rows of a workgroup, 32 a wave
 constexpr int kWideKeys = 64;   // rows of a staged tile
 
-// Staged rows stand unpadded, the 16-byte pieces of row r moved by turn(r): eight
-// rows' reads of one piece, and the transposing reads of four rows by two pieces,
-// fall on banks of their own.
-__device__ __forceinline__ int turn(int r) { return (r & 3) << 1 | (r >> 2 & 1); }
+// A staged tile stands as D / 64 blocks of 64 columns, [64 rows][64 columns] each, the eight 16-byte pieces of row r at
+// piece ^ turn(r).  Two rows fill the 256 bytes of all banks: sixteen rows' reads of one piece, and the transposing reads
+// of 64 bytes from four rows, each fall on banks of their own (with rows of 256 bytes and another turn half of them met:
+// a third of the LDS's cycles).
+__device__ __forceinline__ int turn(int r) { return (r >> 1 & 1) << 2 | (r >> 2 & 3); }
 
-// A lane's share of staging tiles of ROWS rows by DMA: an instruction moves 1 KB, whole rows; its address is one that all
+// A lane's share of staging a tile by DMA: an instruction moves 1 KB, eight rows of a block; its address is one that all
 // lanes share and a 32-bit offset, formed once, so that a tile costs next to no vector arithmetic.  Rows at n and past it
 // are copies of row n - 1: what they are multiplied by is 0, and that they may not be finite is looked after.
-template <int D, int ROWS>
+template <int D>
 struct Stage {
-  static constexpr int kPieces = D / 8, kRows = 64 / kPieces, kCount = ROWS / kRows / 4;
-  static __device__ __forceinline__ int first_row() {
-    return static_cast<int>(threadIdx.x >> 6) * kRows + (threadIdx.x & 63) / kPieces;
+  static constexpr int kBlocks = D / 64, kCount = kWideKeys * kBlocks / 8 / 4;  // instructions of a wave
+  // Row that the lane moves in instruction i, and the byte of it (turn() does not change over 32 rows).
+  static __device__ __forceinline__ int row_of(int i) {
+    return static_cast<int>(threadIdx.x >> 6) * 8 + (threadIdx.x & 63) / 8 + i / kBlocks * 32;
   }
-  // Byte of the row that the lane moves (turn() of row 4 kRows i + r is that of row r).
-  static __device__ __forceinline__ uint32_t piece() { return ((threadIdx.x & 63) % kPieces ^ turn(first_row())) * 16; }
-  // address(i) of instruction i's first row, the same in all lanes; lane(i) the lane's offset from it, last(i) that of row
-  // n - 1.
-  template <class A, class L, class Z>
-  static __device__ __forceinline__ void run(__bf16* to, int n, A address, L lane, Z last) {
+  static __device__ __forceinline__ uint32_t piece() { return ((threadIdx.x & 7) ^ turn(row_of(0))) * 16; }
+  // lane(row): its offset from the tile's address; last(): that of row n - 1
+  template <class L, class Z>
+  static __device__ __forceinline__ void run(__bf16* to, const char* tile, int n, L lane, Z last) {
     const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
 #pragma unroll
     for (int i = 0; i < kCount; ++i) {
-      uint32_t off = lane(i);
-      if (n < ROWS) off = first_row() + i * 4 * kRows < n ? off : last(i);
-      __builtin_amdgcn_global_load_lds(address(i) + off, (lds_void*)(to + (i * 4 + wave) * kRows * D), 16, 0, 0);
+      uint32_t off = lane(i / kBlocks);
+      if (n < kWideKeys) off = row_of(i) < n ? off : last();
+      __bf16* at = to + i % kBlocks * kWideKeys * 64 + (i / kBlocks * 4 + wave) * 8 * 64;
+      __builtin_amdgcn_global_load_lds(tile + i % kBlocks * 128 + off, (lds_void*)at, 16, 0, 0);
     }
   }
 };
 // Rows one after another, `row` bytes apart.
-template <int D, int ROWS>
-struct KeyStage : Stage<D, ROWS> {
-  typedef Stage<D, ROWS> S;
+template <int D>
+struct KeyStage : Stage<D> {
+  typedef Stage<D> S;
   uint32_t off, row;
   __device__ __forceinline__ KeyStage(int64_t bytes)
-      : off(S::first_row() * static_cast<uint32_t>(bytes) + S::piece()), row(static_cast<uint32_t>(bytes)) {}
+      : off(S::row_of(0) * static_cast<uint32_t>(bytes) + S::piece()), row(static_cast<uint32_t>(bytes)) {}
   __device__ __forceinline__ void stage(__bf16* to, const char* tile, int n) const {
-    S::run(to, n, [&](int) { return tile; }, [&](int i) { return off + i * 4 * S::kRows * row; },
-           [&](int) { return (n - 1) * row + S::piece(); });
+    S::run(to, tile, n, [&](int k) { return off + k * 32 * row; }, [&] { return (n - 1) * row + S::piece(); });
   }
 };
-// The rows of whole queries: row r is query r / G of head r % G (G divides ROWS).
-template <int D, int ROWS>
-struct QueryStage : Stage<D, ROWS> {
-  typedef Stage<D, ROWS> S;
-  uint32_t off[S::kCount];
+// The rows of whole queries: row r is query r / G of head r % G (G divides 32).
+template <int D>
+struct QueryStage : Stage<D> {
+  typedef Stage<D> S;
+  uint32_t off[2];
   uint32_t row, head;
-  int group;
   __device__ __forceinline__ QueryStage(const AttnArgs& a, const RowView& x)
-      : row(static_cast<uint32_t>(x.row)), head(static_cast<uint32_t>(x.head)), group(a.G) {
+      : row(static_cast<uint32_t>(x.row)), head(static_cast<uint32_t>(x.head)) {
 #pragma unroll
-    for (int i = 0; i < S::kCount; ++i) off[i] = place(a, S::first_row() + i * 4 * S::kRows) + S::piece();
+    for (int k = 0; k < 2; ++k) off[k] = place(a, S::row_of(0) + k * 32) + S::piece();
   }
   __device__ __forceinline__ uint32_t place(const AttnArgs& a, int r) const {
     const int q = div_group(a, r);
-    return q * row + (r - q * group) * head;
+    return q * row + (r - q * a.G) * head;
   }
   __device__ __forceinline__ void stage(const AttnArgs& a, __bf16* to, const char* tile, int n) const {
-    S::run(to, n, [&](int) { return tile; }, [&](int i) { return off[i]; },
-           [&](int) { return place(a, n - 1) + S::piece(); });
+    S::run(to, tile, n, [&](int k) { return off[k]; }, [&] { return place(a, n - 1) + S::piece(); });
   }
 };
 
@@ -482,38 +480,43 @@ __device__ __forceinline__ floatx16 mma32(bf16x8 a, bf16x8 b, floatx16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
 
-// A lane's places in a staged tile, in elements.  turn() moves pieces within groups of eight, so that pieces 64 or 128
-// elements on, and rows 16 on, lie at a constant distance, which the reads hold as their immediate.
+// A lane's places in a block of a staged tile, in elements; blocks, and rows 16 on, lie at constant distances, which the
+// reads hold as their immediate.
 struct WidePlaces {
-  uint32_t row[4];     // row c, elements 16 st + 8 hi .. + 7, st 0 .. 3
-  uint32_t column[2];  // for the transposing read of columns 0 .. 31 and 32 .. 63: lane m = 4 e + r of sixteen points at row 4 hi + e
+  uint32_t row[4];        // row c, columns 16 st + 8 hi .. + 7 of the block
+  uint32_t column[2][2];  // for the transposing read of columns 0 .. 31 and 32 .. 63, of rows 4 hi + e and 8 further: lane
+                          // 4 e + r of sixteen points at four columns of row e
 };
-template <int D>
 __device__ __forceinline__ WidePlaces wide_places() {
   const int lane = threadIdx.x & 63, c = lane & 31, hi = lane >> 5, half = lane >> 4 & 1, e = (lane & 15) >> 2, r = lane & 3;
-  const int row = 4 * hi + e;
   WidePlaces w;
 #pragma unroll
-  for (int st = 0; st < 4; ++st) w.row[st] = c * D + ((2 * st + hi) ^ turn(c)) * 8;
+  for (int st = 0; st < 4; ++st) w.row[st] = c * 64 + ((2 * st + hi) ^ turn(c)) * 8;
 #pragma unroll
-  for (int n = 0; n < 2; ++n) w.column[n] = row * D + ((4 * n + 2 * half + (r >> 1)) ^ turn(row)) * 8 + (r & 1) * 4;
+  for (int n = 0; n < 2; ++n)
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int row = 8 * k + 4 * hi + e;
+      w.column[n][k] = row * 64 + ((4 * n + 2 * half + (r >> 1)) ^ turn(row)) * 8 + (r & 1) * 4;
+    }
   return w;
 }
 
-// Row r0 + c of a staged tile, elements 16 st + 8 hi .. + 7 (r0 a multiple of 32).
-template <int D>
+// Row r0 + c of a staged tile, columns 16 st + 8 hi .. + 7 (r0 a multiple of 32).
 __device__ __forceinline__ bf16x8 wide_row(const __bf16* tile, const WidePlaces& w, int r0, int st) {
-  return *reinterpret_cast<const bf16x8*>(tile + w.row[st % 4] + st / 4 * 64 + r0 * D);
+  return *reinterpret_cast<const bf16x8*>(tile + w.row[st % 4] + st / 4 * kWideKeys * 64 + r0 * 64);
 }
 // Column d0 + c (d0 a multiple of 32) of staged rows r0 + 4 hi .. + 3 and r0 + 8 + 4 hi .. + 3 (r0 a multiple of 16).
-template <int D>
 __device__ __forceinline__ bf16x8 wide_column(const __bf16* tile, const WidePlaces& w, int r0, int d0) {
   typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
-  // turn(row + 8) = turn(row): the second read is eight rows on
-  __bf16* p = const_cast<__bf16*>(tile) + w.column[d0 / 32 % 2] + d0 / 64 * 64 + r0 * D;
-  const bf16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)p);
-  const bf16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(p + 8 * D));
+  __bf16* block = const_cast<__bf16*>(tile) + d0 / 64 * kWideKeys * 64 + r0 * 64;
+  const bf16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(block + w.column[d0 / 32 % 2][0]));
+  const bf16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(block + w.column[d0 / 32 % 2][1]));
   return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+// Row `at`, column d.
+__device__ __forceinline__ int wide_at(int at, int d) {
+  return d / 64 * kWideKeys * 64 + at * 64 + ((d / 8 % 8) ^ turn(at)) * 8 + d % 8;
 }
 // Elements 8t .. 8t + 7 of a result as the operand of 16 rows, in the order of wide_column.
 __device__ __forceinline__ bf16x8 wide_pack(const floatx16& x, int t) {
@@ -554,7 +557,7 @@ __device__ __forceinline__ void take_odd(WideForward<D>& f, __bf16* vs, int end)
 #pragma unroll
       for (int x = 0; x < 16; ++x) {
         const int d = 32 * dt + wide_place(x) + 4 * hi;
-        const float v = static_cast<float>(vs[at * D + ((d / 8) ^ turn(at)) * 8 + d % 8]);
+        const float v = static_cast<float>(vs[wide_at(at, d)]);
         if (!(__builtin_fabsf(v) < INFINITY)) f.o[dt][x] += v;
       }
   __syncthreads();
@@ -578,7 +581,7 @@ __device__ __forceinline__ void wide_keys(const AttnArgs& a, WideForward<D>& f, 
   for (int n = 0; n < 2; ++n) {
     s[n] = zero16();
 #pragma unroll
-    for (int st = 0; st < D / 16; ++st) s[n] = mma32(wide_row<D>(ks, w, 32 * n, st), f.q[st], s[n]);
+    for (int st = 0; st < D / 16; ++st) s[n] = mma32(wide_row(ks, w, 32 * n, st), f.q[st], s[n]);
   }
   if (masked) {
 #pragma unroll
@@ -615,7 +618,7 @@ __device__ __forceinline__ void wide_keys(const AttnArgs& a, WideForward<D>& f, 
     for (int t = 0; t < 2; ++t) {
       const bf16x8 p = wide_pack(s[n], t);
 #pragma unroll
-      for (int dt = 0; dt < D / 32; ++dt) f.o[dt] = mma32(wide_column<D>(vs, w, 32 * n + 16 * t, 32 * dt), p, f.o[dt]);
+      for (int dt = 0; dt < D / 32; ++dt) f.o[dt] = mma32(wide_column(vs, w, 32 * n + 16 * t, 32 * dt), p, f.o[dt]);
     }
 }
 
@@ -644,7 +647,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_wide_kernel(AttnArgs a) {
   const int row0 = static_cast<int>(tile) * kWide, row = row0 + wave * 32 + c;
   const bool real = row < rows;
   const int key_hi = limit_of(a, s, min(row0 + kWide, rows) - 1), open = limit_of(a, s, row0);
-  const WidePlaces w = wide_places<D>();
+  const WidePlaces w = wide_places();
   WideForward<D> f;
   f.limit = limit_of(a, s, row);
   f.m = -INFINITY, f.l = 0.f;
@@ -655,7 +658,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_wide_kernel(AttnArgs a) {
   for (int dt = 0; dt < D / 32; ++dt) f.o[dt] = zero16();
   const char* kbase = a.k.at + static_cast<int64_t>(s.k0) * a.k.row + hk * a.k.head;
   const char* vbase = a.v.at + static_cast<int64_t>(s.k0) * a.v.row + hk * a.v.head;
-  const KeyStage<D, kWideKeys> kst(a.k.row), vst(a.v.row);
+  const KeyStage<D> kst(a.k.row), vst(a.v.row);
   const auto ask = [&](int key, __bf16* kt, __bf16* vt) {
     kst.stage(kt, kbase + key * a.k.row, s.nk - key);
     vst.stage(vt, vbase + key * a.v.row, s.nk - key);
@@ -851,10 +854,10 @@ __device__ __forceinline__ void wide_grad_q_keys(const AttnArgs& a, WideGradQ<D>
   for (int n = 0; n < 2; ++n) {
     floatx16 s = zero16(), dp = zero16();
 #pragma unroll
-    for (int st = 0; st < D / 16; ++st) s = mma32(wide_row<D>(ks, w, 32 * n, st), f.q[st], s);
+    for (int st = 0; st < D / 16; ++st) s = mma32(wide_row(ks, w, 32 * n, st), f.q[st], s);
     formed(s);
 #pragma unroll
-    for (int st = 0; st < D / 16; ++st) dp = mma32(wide_row<D>(vs, w, 32 * n, st), f.g[st], dp);
+    for (int st = 0; st < D / 16; ++st) dp = mma32(wide_row(vs, w, 32 * n, st), f.g[st], dp);
     formed(dp);
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
@@ -870,7 +873,7 @@ __device__ __forceinline__ void wide_grad_q_keys(const AttnArgs& a, WideGradQ<D>
     for (int t = 0; t < 2; ++t) {
       const bf16x8 ds = wide_pack(dp, t);
 #pragma unroll
-      for (int dt = 0; dt < D / 32; ++dt) f.dq[dt] = mma32(wide_column<D>(ks, w, 32 * n + 16 * t, 32 * dt), ds, f.dq[dt]);
+      for (int dt = 0; dt < D / 32; ++dt) f.dq[dt] = mma32(wide_column(ks, w, 32 * n + 16 * t, 32 * dt), ds, f.dq[dt]);
     }
   }
 }
@@ -891,7 +894,7 @@ __global__ __launch_bounds__(kThreads, 2) void grad_q_wide_kernel(AttnArgs a) {
   const bool real = row < rows;
   const int key_hi = limit_of(a, s, min(row0 + kWide, rows) - 1), open = limit_of(a, s, row0);
   const int limit = limit_of(a, s, row);
-  const WidePlaces w = wide_places<D>();
+  const WidePlaces w = wide_places();
   WideGradQ<D> f;
   float delta = 0.f;
 #pragma unroll
@@ -910,7 +913,7 @@ __global__ __launch_bounds__(kThreads, 2) void grad_q_wide_kernel(AttnArgs a) {
   for (int dt = 0; dt < D / 32; ++dt) f.dq[dt] = zero16();
   const char* kbase = a.k.at + static_cast<int64_t>(s.k0) * a.k.row + hk * a.k.head;
   const char* vbase = a.v.at + static_cast<int64_t>(s.k0) * a.v.row + hk * a.v.head;
-  const KeyStage<D, kWideKeys> kst(a.k.row), vst(a.v.row);
+  const KeyStage<D> kst(a.k.row), vst(a.v.row);
   const auto ask = [&](int key, __bf16* kt, __bf16* vt) {
     kst.stage(kt, kbase + key * a.k.row, s.nk - key);
     vst.stage(vt, vbase + key * a.v.row, s.nk - key);
@@ -966,11 +969,11 @@ __device__ __forceinline__ void wide_grad_kv_rows(const AttnArgs& a, WideGradKv<
   for (int n = 0; n < 2; ++n) {
     floatx16 s = zero16(), dp = zero16();
 #pragma unroll
-    for (int st = 0; st < D / 16; ++st) s = mma32(wide_row<D>(qs, w, 32 * n, st), f.k[st], s);
+    for (int st = 0; st < D / 16; ++st) s = mma32(wide_row(qs, w, 32 * n, st), f.k[st], s);
     formed(s);
     if constexpr (PART != kDv) {
 #pragma unroll
-      for (int st = 0; st < D / 16; ++st) dp = mma32(wide_row<D>(gs, w, 32 * n, st), f.v[st], dp);
+      for (int st = 0; st < D / 16; ++st) dp = mma32(wide_row(gs, w, 32 * n, st), f.v[st], dp);
       formed(dp);
     }
 #pragma unroll
@@ -1000,12 +1003,12 @@ __device__ __forceinline__ void wide_grad_kv_rows(const AttnArgs& a, WideGradKv<
       if constexpr (PART != kDk) {
         const bf16x8 p = wide_pack(s, t);
 #pragma unroll
-        for (int dt = 0; dt < D / 32; ++dt) f.dv[dt] = mma32(wide_column<D>(gs, w, 32 * n + 16 * t, 32 * dt), p, f.dv[dt]);
+        for (int dt = 0; dt < D / 32; ++dt) f.dv[dt] = mma32(wide_column(gs, w, 32 * n + 16 * t, 32 * dt), p, f.dv[dt]);
       }
       if constexpr (PART != kDv) {
         const bf16x8 ds = wide_pack(dp, t);
 #pragma unroll
-        for (int dt = 0; dt < D / 32; ++dt) f.dk[dt] = mma32(wide_column<D>(qs, w, 32 * n + 16 * t, 32 * dt), ds, f.dk[dt]);
+        for (int dt = 0; dt < D / 32; ++dt) f.dk[dt] = mma32(wide_column(qs, w, 32 * n + 16 * t, 32 * dt), ds, f.dk[dt]);
       }
     }
   }
@@ -1035,7 +1038,7 @@ __device__ __forceinline__ void grad_kv_wide(const AttnArgs& a, int block, WideK
   }
   const char* kbase = a.k.at + (static_cast<int64_t>(s.k0) + key0) * a.k.row + hk * a.k.head;
   const char* vbase = a.v.at + (static_cast<int64_t>(s.k0) + key0) * a.v.row + hk * a.v.head;
-  const WidePlaces w = wide_places<D>();
+  const WidePlaces w = wide_places();
   WideGradKv<D, PART> f;
 #pragma unroll
   for (int st = 0; st < D / 16; ++st) {
@@ -1051,7 +1054,7 @@ __device__ __forceinline__ void grad_kv_wide(const AttnArgs& a, int block, WideK
   }
   float2 stat = {};
   // A tile's rows are whole queries (G divides the tile, and row_lo is a multiple of it).
-  const QueryStage<D, kRows> qst(a, a.q), gst(a, a.dout);
+  const QueryStage<D> qst(a, a.q), gst(a, a.dout);
   const char* qbase = a.q.at + s.q0 * a.q.row + hk * a.G * a.q.head;
   const char* gbase = a.dout.at + s.q0 * a.dout.row + hk * a.G * a.dout.head;
   const auto ask = [&](int r, __bf16* qt, __bf16* gt) {
