@@ -423,22 +423,24 @@ __device__ __forceinline__ int turn(int r) { return (r >> 1 & 1) << 2 | (r >> 2 
 // are copies of row n - 1: what they are multiplied by is 0, and that they may not be finite is looked after.
 template <int D>
 struct Stage {
-  static constexpr int kBlocks = D / 64, kCount = kWideKeys * kBlocks / 8 / 4;  // instructions of a wave
-  // Row that the lane moves in instruction i, and the byte of it (turn() does not change over 32 rows).
-  static __device__ __forceinline__ int row_of(int i) {
-    return static_cast<int>(threadIdx.x >> 6) * 8 + (threadIdx.x & 63) / 8 + i / kBlocks * 32;
-  }
-  static __device__ __forceinline__ uint32_t piece() { return ((threadIdx.x & 7) ^ turn(row_of(0))) * 16; }
-  // lane(row): its offset from the tile's address; last(): that of row n - 1
+  static constexpr int kBlocks = D / 64, kCount = 2 * kBlocks;  // instructions of a wave
+  // The lane moves rows row() and row() + 32, from this byte on (turn() is the same for both).
+  static __device__ __forceinline__ int row() { return static_cast<int>(threadIdx.x / 8); }
+  static __device__ __forceinline__ uint32_t piece() { return ((threadIdx.x & 7) ^ turn(row())) * 16; }
+  // lane(k): row row() + 32 k's offset from the tile's address; last(): that of row n - 1
   template <class L, class Z>
   static __device__ __forceinline__ void run(__bf16* to, const char* tile, int n, L lane, Z last) {
     const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
+    uint32_t off[2] = {lane(0), lane(1)};
+    if (n < kWideKeys) {
+      const uint32_t end = last();
+      off[0] = row() < n ? off[0] : end;
+      off[1] = row() + 32 < n ? off[1] : end;
+    }
 #pragma unroll
     for (int i = 0; i < kCount; ++i) {
-      uint32_t off = lane(i / kBlocks);
-      if (n < kWideKeys) off = row_of(i) < n ? off : last();
       __bf16* at = to + i % kBlocks * kWideKeys * 64 + (i / kBlocks * 4 + wave) * 8 * 64;
-      __builtin_amdgcn_global_load_lds(tile + i % kBlocks * 128 + off, (lds_void*)at, 16, 0, 0);
+      __builtin_amdgcn_global_load_lds(tile + i % kBlocks * 128 + off[i / kBlocks], (lds_void*)at, 16, 0, 0);
     }
   }
 };
@@ -446,11 +448,11 @@ struct Stage {
 template <int D>
 struct KeyStage : Stage<D> {
   typedef Stage<D> S;
-  uint32_t off, row;
+  uint32_t off, step;
   __device__ __forceinline__ KeyStage(int64_t bytes)
-      : off(S::row_of(0) * static_cast<uint32_t>(bytes) + S::piece()), row(static_cast<uint32_t>(bytes)) {}
+      : off(S::row() * static_cast<uint32_t>(bytes) + S::piece()), step(static_cast<uint32_t>(bytes)) {}
   __device__ __forceinline__ void stage(__bf16* to, const char* tile, int n) const {
-    S::run(to, tile, n, [&](int k) { return off + k * 32 * row; }, [&] { return (n - 1) * row + S::piece(); });
+    S::run(to, tile, n, [&](int k) { return off + k * 32 * step; }, [&] { return (n - 1) * step + S::piece(); });
   }
 };
 // The rows of whole queries: row r is query r / G of head r % G (G divides 32).
@@ -458,15 +460,15 @@ template <int D>
 struct QueryStage : Stage<D> {
   typedef Stage<D> S;
   uint32_t off[2];
-  uint32_t row, head;
+  uint32_t step, head;
   __device__ __forceinline__ QueryStage(const AttnArgs& a, const RowView& x)
-      : row(static_cast<uint32_t>(x.row)), head(static_cast<uint32_t>(x.head)) {
+      : step(static_cast<uint32_t>(x.row)), head(static_cast<uint32_t>(x.head)) {
 #pragma unroll
-    for (int k = 0; k < 2; ++k) off[k] = place(a, S::row_of(0) + k * 32) + S::piece();
+    for (int k = 0; k < 2; ++k) off[k] = place(a, S::row() + k * 32) + S::piece();
   }
   __device__ __forceinline__ uint32_t place(const AttnArgs& a, int r) const {
     const int q = div_group(a, r);
-    return q * row + (r - q * a.G) * head;
+    return q * step + (r - q * a.G) * head;
   }
   __device__ __forceinline__ void stage(const AttnArgs& a, __bf16* to, const char* tile, int n) const {
     S::run(to, tile, n, [&](int k) { return off[k]; }, [&] { return place(a, n - 1) + S::piece(); });
@@ -532,6 +534,14 @@ __device__ __forceinline__ floatx16 zero16() {
   return z;
 }
 __device__ __forceinline__ int wide_place(int i) { return 8 * (i / 4) + i % 4; }  // + 4 hi
+
+// The thread's number, where the compiler does not know that it has it already: what is formed from it after a loop is
+// not held in registers, or spilled, through the loop.
+__device__ __forceinline__ int thread_again() {
+  int t = threadIdx.x;
+  asm volatile("" : "+v"(t));
+  return t;
+}
 
 template <int D>
 struct WideTiles {
@@ -677,15 +687,17 @@ __global__ __launch_bounds__(kThreads, 2) void attn_wide_kernel(AttnArgs a) {
     step(key + kWideKeys, tiles.a1, tiles.b1, tiles.a0, tiles.b0);
   }
   const float l = add32(f.l), inv = l == 0.f ? 0.f : 1.f / l;
-  if (!real) return;
-  if (hi == 0 && a.lse) a.lse[stat_at(a, s, hk, row)] = l == 0.f ? -INFINITY : (f.m + __builtin_amdgcn_logf(l)) * kLn2;
-  char* to = const_cast<char*>(query_row(a, a.out, s, hk, row));
+  const int thread = thread_again(), out_row = row0 + thread / 64 * 32 + thread % 32, out_hi = thread % 64 / 32;
+  if (out_row >= rows) return;
+  if (out_hi == 0 && a.lse)
+    a.lse[stat_at(a, s, hk, out_row)] = l == 0.f ? -INFINITY : (f.m + __builtin_amdgcn_logf(l)) * kLn2;
+  char* to = const_cast<char*>(query_row(a, a.out, s, hk, out_row)) + out_hi * 8;
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
       const floatx4 x = {f.o[dt][4 * n], f.o[dt][4 * n + 1], f.o[dt][4 * n + 2], f.o[dt][4 * n + 3]};
-      store4<__bf16>(to + (32 * dt + 8 * n + 4 * hi) * 2, x * inv);
+      store4<__bf16>(to + (32 * dt + 8 * n) * 2, x * inv);
     }
 }
 
@@ -853,12 +865,14 @@ __device__ __forceinline__ void wide_grad_q_keys(const AttnArgs& a, WideGradQ<D>
 #pragma unroll
   for (int n = 0; n < 2; ++n) {
     floatx16 s = zero16(), dp = zero16();
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int st = 0; st < D / 16; ++st) s = mma32(wide_row(ks, w, 32 * n, st), f.q[st], s);
     formed(s);
 #pragma unroll
     for (int st = 0; st < D / 16; ++st) dp = mma32(wide_row(vs, w, 32 * n, st), f.g[st], dp);
     formed(dp);
+    __builtin_amdgcn_s_setprio(0);
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], a.c2, -f.lse2));
@@ -929,14 +943,15 @@ __global__ __launch_bounds__(kThreads, 2) void grad_q_wide_kernel(AttnArgs a) {
     if (key + kWideKeys >= key_hi) break;
     step(key + kWideKeys, tiles.a1, tiles.b1, tiles.a0, tiles.b0);
   }
-  if (!real) return;
-  char* to = const_cast<char*>(query_row(a, a.dq, s, hk, row));
+  const int thread = thread_again(), out_row = row0 + thread / 64 * 32 + thread % 32;
+  if (out_row >= rows) return;
+  char* to = const_cast<char*>(query_row(a, a.dq, s, hk, out_row)) + (thread % 64 / 32) * 8;
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
       const floatx4 x = {f.dq[dt][4 * n], f.dq[dt][4 * n + 1], f.dq[dt][4 * n + 2], f.dq[dt][4 * n + 3]};
-      store4<__bf16>(to + (32 * dt + 8 * n + 4 * hi) * 2, x * a.scale);
+      store4<__bf16>(to + (32 * dt + 8 * n) * 2, x * a.scale);
     }
 }
 
@@ -968,14 +983,22 @@ __device__ __forceinline__ void wide_grad_kv_rows(const AttnArgs& a, WideGradKv<
 #pragma unroll
   for (int n = 0; n < 2; ++n) {
     floatx16 s = zero16(), dp = zero16();
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-    for (int st = 0; st < D / 16; ++st) s = mma32(wide_row(qs, w, 32 * n, st), f.k[st], s);
+    for (int st = 0; st < D / 16; ++st) {
+      s = mma32(wide_row(qs, w, 32 * n, st), f.k[st], s);
+      if (D == 128 && st == 3) __builtin_amdgcn_sched_barrier(0);
+    }
     formed(s);
     if constexpr (PART != kDv) {
 #pragma unroll
-      for (int st = 0; st < D / 16; ++st) dp = mma32(wide_row(gs, w, 32 * n, st), f.v[st], dp);
+      for (int st = 0; st < D / 16; ++st) {
+        dp = mma32(wide_row(gs, w, 32 * n, st), f.v[st], dp);
+        if (D == 128 && st == 3) __builtin_amdgcn_sched_barrier(0);
+      }
       formed(dp);
     }
+    __builtin_amdgcn_s_setprio(0);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int at = 32 * n + 8 * j + 4 * hi;
@@ -1009,6 +1032,7 @@ __device__ __forceinline__ void wide_grad_kv_rows(const AttnArgs& a, WideGradKv<
         const bf16x8 ds = wide_pack(dp, t);
 #pragma unroll
         for (int dt = 0; dt < D / 32; ++dt) f.dk[dt] = mma32(wide_column(qs, w, 32 * n + 16 * t, 32 * dt), ds, f.dk[dt]);
+        if (D == 128) __builtin_amdgcn_sched_barrier(0);
       }
     }
   }
@@ -1052,7 +1076,6 @@ __device__ __forceinline__ void grad_kv_wide(const AttnArgs& a, int block, WideK
     if constexpr (PART != kDv) f.dk[dt] = zero16();
     if constexpr (PART != kDk) f.dv[dt] = zero16();
   }
-  float2 stat = {};
   // A tile's rows are whole queries (G divides the tile, and row_lo is a multiple of it).
   const QueryStage<D> qst(a, a.q), gst(a, a.dout);
   const char* qbase = a.q.at + s.q0 * a.q.row + hk * a.G * a.q.head;
@@ -1062,53 +1085,58 @@ __device__ __forceinline__ void grad_kv_wide(const AttnArgs& a, int block, WideK
     qst.stage(a, qt, qbase + n * a.q.row, row_hi - r);
     gst.stage(a, gt, gbase + n * a.dout.row, row_hi - r);
   };
-  // The rows' statistics go through a register, one tile ahead of their LDS.
+  // The rows' statistics go through a register, one tile ahead of their LDS; thread t < 64 moves row t's.
+  const int own_query = div_group(a, threadIdx.x % kRows), own_head = threadIdx.x % kRows - own_query * a.G;
+  const float2* const stats = a.stat + static_cast<int64_t>(s.q0) * a.H + hk * a.G;
   const auto ask_stat = [&](int r) {
-    const int row = min(r + static_cast<int>(threadIdx.x), row_hi - 1);
-    if (threadIdx.x < kRows) stat = a.stat[stat_at(a, s, hk, row)];
+    const int n = div_group(a, r);
+    const uint32_t off = min(own_query, s.nq - 1 - n) * a.H + own_head;
+    return threadIdx.x < kRows ? (stats + static_cast<int64_t>(n) * a.H)[off] : make_float2(0.f, 0.f);
   };
-  const auto put_stat = [&](int r, typename WideKvLds<D>::Stats& x) {
+  const auto put_stat = [&](int r, float2 stat, typename WideKvLds<D>::Stats& x) {
     if (threadIdx.x >= kRows) return;
-    const int row = r + threadIdx.x;
-    const bool here = row < row_hi;
+    const int query = div_group(a, r) + own_query;
+    const bool here = r + static_cast<int>(threadIdx.x) < row_hi;
     x.lse2[threadIdx.x] = here ? stat.x : INFINITY;
     x.delta[threadIdx.x] = here ? stat.y : 0.f;
-    x.limit[threadIdx.x] = here ? limit_of(a, s, row) : 0;
+    x.limit[threadIdx.x] = !here ? 0 : a.causal ? max(0, min(s.nk, query + 1 + s.nk - s.nq)) : s.nk;
   };
   const auto step = [&](int r, const __bf16* qt, const __bf16* gt, const typename WideKvLds<D>::Stats& here, __bf16* qn,
                         __bf16* gn, typename WideKvLds<D>::Stats& next) {
     staged();
     const bool more = r > row_lo;
+    float2 stat;
     if (more) {
-      ask_stat(r - kRows);
+      stat = ask_stat(r - kRows);
       ask(r - kRows, qn, gn);
     }
     wide_grad_kv_rows<D, PART>(a, f, qt, gt, w, here, key, r < open || r + kRows > row_hi);
-    if (more) put_stat(r - kRows, next);
+    if (more) put_stat(r - kRows, stat, next);
   };
   // From the last rows back: every tile of keys begins with the same rows, and the tiles at work share them in the L2
   // (forward, each begins at its own: 4050 us in place of LATER).
   const int last = row_lo + max(row_hi - row_lo - 1, 0) / kRows * kRows;
   if (row_lo < row_hi) {
-    ask_stat(last);
+    const float2 stat = ask_stat(last);
     ask(last, lds.q0, lds.g0);
-    put_stat(last, lds.stats[0]);
+    put_stat(last, stat, lds.stats[0]);
     for (int r = last; r >= row_lo; r -= 2 * kRows) {
       step(r, lds.q0, lds.g0, lds.stats[0], lds.q1, lds.g1, lds.stats[1]);
       if (r == row_lo) break;
       step(r - kRows, lds.q1, lds.g1, lds.stats[1], lds.q0, lds.g0, lds.stats[0]);
     }
   }
-  if (!real) return;
-  const int64_t at = static_cast<int64_t>(s.k0) + key;
-  float* part = SPLIT ? a.part + ((split * a.Hk + hk) * a.total_k + at) * 2 * D : nullptr;
-  char* kto = a.dk.at + at * a.dk.row + hk * a.dk.head;
-  char* vto = a.dv.at + at * a.dv.row + hk * a.dv.head;
+  const int thread = thread_again(), out_key = key0 + thread / 64 * 32 + thread % 32, hi4 = thread % 64 / 32 * 4;
+  if (out_key >= s.nk) return;
+  const int64_t at = static_cast<int64_t>(s.k0) + out_key;
+  float* part = SPLIT ? a.part + ((split * a.Hk + hk) * a.total_k + at) * 2 * D + hi4 : nullptr;
+  char* kto = a.dk.at + at * a.dk.row + hk * a.dk.head + hi4 * 2;
+  char* vto = a.dv.at + at * a.dv.row + hk * a.dv.head + hi4 * 2;
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
-      const int d = 32 * dt + 8 * n + 4 * hi;
+      const int d = 32 * dt + 8 * n;
       if constexpr (PART != kDv) {
         const floatx4 x = {f.dk[dt][4 * n], f.dk[dt][4 * n + 1], f.dk[dt][4 * n + 2], f.dk[dt][4 * n + 3]};
         if (SPLIT) *reinterpret_cast<floatx4*>(part + d) = x;
