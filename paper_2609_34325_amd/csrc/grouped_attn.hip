@@ -643,7 +643,7 @@ __device__ __forceinline__ bool odd_tile(const __bf16* tile) {
 }
 
 template <int D>
-__global__ __launch_bounds__(kThreads, 2) void attn_wide_kernel(AttnArgs a) {
+__global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void attn_wide_kernel(AttnArgs a) {
   __shared__ __attribute__((aligned(1024))) WideTiles<D> tiles;
   if (check_block(a)) return;
   const int lane = threadIdx.x & 63, c = lane & 31, hi = lane >> 5, wave = threadIdx.x >> 6;
@@ -871,7 +871,6 @@ __device__ __forceinline__ void wide_grad_q_keys(const AttnArgs& a, WideGradQ<D>
     formed(s);
 #pragma unroll
     for (int st = 0; st < D / 16; ++st) dp = mma32(wide_row(vs, w, 32 * n, st), f.g[st], dp);
-    formed(dp);
     __builtin_amdgcn_s_setprio(0);
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
@@ -893,7 +892,7 @@ __device__ __forceinline__ void wide_grad_q_keys(const AttnArgs& a, WideGradQ<D>
 }
 
 template <int D>
-__global__ __launch_bounds__(kThreads, 2) void grad_q_wide_kernel(AttnArgs a) {
+__global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void grad_q_wide_kernel(AttnArgs a) {
   __shared__ __attribute__((aligned(1024))) WideTiles<D> tiles;
   if (check_block(a)) return;
   const int lane = threadIdx.x & 63, c = lane & 31, hi = lane >> 5, wave = threadIdx.x >> 6;
@@ -996,7 +995,6 @@ __device__ __forceinline__ void wide_grad_kv_rows(const AttnArgs& a, WideGradKv<
         dp = mma32(wide_row(gs, w, 32 * n, st), f.v[st], dp);
         if (D == 128 && st == 3) __builtin_amdgcn_sched_barrier(0);
       }
-      formed(dp);
     }
     __builtin_amdgcn_s_setprio(0);
 #pragma unroll
@@ -1086,16 +1084,16 @@ __device__ __forceinline__ void grad_kv_wide(const AttnArgs& a, int block, WideK
     gst.stage(a, gt, gbase + n * a.dout.row, row_hi - r);
   };
   // The rows' statistics go through a register, one tile ahead of their LDS; thread t < 64 moves row t's.
-  const int own_query = div_group(a, threadIdx.x % kRows), own_head = threadIdx.x % kRows - own_query * a.G;
   const float2* const stats = a.stat + static_cast<int64_t>(s.q0) * a.H + hk * a.G;
   const auto ask_stat = [&](int r) {
-    const int n = div_group(a, r);
-    const uint32_t off = min(own_query, s.nq - 1 - n) * a.H + own_head;
-    return threadIdx.x < kRows ? (stats + static_cast<int64_t>(n) * a.H)[off] : make_float2(0.f, 0.f);
+    if (threadIdx.x >= kRows) return make_float2(0.f, 0.f);
+    const int n = div_group(a, r), t = thread_again(), query = div_group(a, t);
+    const uint32_t off = min(query, s.nq - 1 - n) * a.H + t - query * a.G;
+    return (stats + static_cast<int64_t>(n) * a.H)[off];
   };
   const auto put_stat = [&](int r, float2 stat, typename WideKvLds<D>::Stats& x) {
     if (threadIdx.x >= kRows) return;
-    const int query = div_group(a, r) + own_query;
+    const int query = div_group(a, r) + div_group(a, thread_again());
     const bool here = r + static_cast<int>(threadIdx.x) < row_hi;
     x.lse2[threadIdx.x] = here ? stat.x : INFINITY;
     x.delta[threadIdx.x] = here ? stat.y : 0.f;
