@@ -61,9 +61,9 @@ __device__ __forceinline__ int div_group(const AttnArgs& a, int r) {
   return a.G == 1 ? r : static_cast<int>(__umulhi(static_cast<uint32_t>(r), a.g_mul) >> a.g_shift);
 }
 
-// First tile number of sequence b.
-__device__ __forceinline__ int64_t first_tile(const int32_t* cu, int b, int mul, int tile) {
-  return static_cast<int64_t>(max(cu[b], 0)) * mul / tile + b;
+// First tile number of sequence b, which begins at `boundary`.
+__device__ __forceinline__ int64_t first_tile(int boundary, int b, int mul, int tile) {
+  return static_cast<int64_t>(max(boundary, 0)) * mul / tile + b;
 }
 
 // The last b with first(b) <= t; every lane of the wave calls it.
@@ -93,12 +93,34 @@ __device__ __forceinline__ bool sequence(const AttnArgs& a, int b, Seq* s) {
   return true;
 }
 
+// The last sequence b with first(boundary, b) <= t, boundary = cu_q[b] (QUERIES) or cu_k[b]; false where its boundaries
+// are no good.  Every lane of the wave calls it.  Fewer than 64 sequences take one trip to memory, each lane holding a
+// boundary of both lists (a trip on cold lines is 1 to 2 us, of a small call's 10).
+template <bool QUERIES, class F>
+__device__ __forceinline__ bool locate(const AttnArgs& a, int64_t t, F first, int* found, Seq* s) {
+  if (a.B >= 64) {
+    const int32_t* cu = QUERIES ? a.cu_q : a.cu_k;
+    *found = last_at_most(a.B, t, [&](int b) { return first(cu[b], b); });
+    return sequence(a, *found, s);
+  }
+  const int lane = threadIdx.x & 63, at = min(lane, a.B);
+  const int q = a.cu_q[at], k = a.cu_k[at];
+  const uint64_t hit = __ballot(lane < a.B && first(QUERIES ? q : k, lane) <= t);
+  const int b = hit ? 63 - __builtin_clzll(hit) : 0;
+  *found = b;
+  const int q0 = __builtin_amdgcn_readlane(q, b), q1 = __builtin_amdgcn_readlane(q, b + 1);
+  const int k0 = __builtin_amdgcn_readlane(k, b), k1 = __builtin_amdgcn_readlane(k, b + 1);
+  if (q0 < 0 || q1 < q0 || q1 > a.total_q || k0 < 0 || k1 < k0 || k1 > a.total_k || q1 - q0 > a.max_q) return false;
+  *s = Seq{q0, q1 - q0, k0, k1 - k0};
+  return true;
+}
+
 // The grid's last workgroup looks at every boundary.
 __device__ __forceinline__ bool check_block(const AttnArgs& a) {
   if (static_cast<int>(blockIdx.x) < a.blocks) return false;
   bool bad = false;
   Seq s;
-  for (int b = threadIdx.x; b < a.B; b += kThreads) bad |= !sequence(a, b, &s);
+  for (int b = threadIdx.x; b < a.B; b += blockDim.x) bad |= !sequence(a, b, &s);
   if (bad) atomicOr(a.status, DORA_DEV_CU_SEQLENS);
   return true;
 }
@@ -273,16 +295,16 @@ __global__ __launch_bounds__(kThreads) void attn_kernel(AttnArgs a) {
   Seq s;
   int tile = 0, key_lo = 0, key_hi;
   if (SPLIT && a.chunk) {
-    const int b = last_at_most(a.B, t, [&](int i) { return first_tile(a.cu_k, i, 1, a.chunk); });
-    if (!sequence(a, b, &s)) return;
-    const int64_t part = t - first_tile(a.cu_k, b, 1, a.chunk);
+    int b;
+    if (!locate<false>(a, t, [&](int cu, int i) { return first_tile(cu, i, 1, a.chunk); }, &b, &s)) return;
+    const int64_t part = t - first_tile(s.k0, b, 1, a.chunk);
     if (part < 0 || part * a.chunk >= s.nk || s.nq == 0) return;
     key_lo = static_cast<int>(part) * a.chunk;
     key_hi = min(s.nk, key_lo + a.chunk);
   } else {
-    const int b = last_at_most(a.B, t, [&](int i) { return first_tile(a.cu_q, i, a.G, kTile); });
-    if (!sequence(a, b, &s)) return;
-    const int64_t at = t - first_tile(a.cu_q, b, a.G, kTile);
+    int b;
+    if (!locate<true>(a, t, [&](int cu, int i) { return first_tile(cu, i, a.G, kTile); }, &b, &s)) return;
+    const int64_t at = t - first_tile(s.q0, b, a.G, kTile);
     if (at < 0 || at * kTile >= static_cast<int64_t>(s.nq) * a.G) return;
     tile = static_cast<int>(at);
     key_hi = limit_of(a, s, min((tile + 1) * kTile, s.nq * a.G) - 1);
@@ -648,10 +670,11 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void attn_wide_kernel(At
   if (check_block(a)) return;
   const int lane = threadIdx.x & 63, c = lane & 31, hi = lane >> 5, wave = threadIdx.x >> 6;
   const int hk = blockIdx.x % a.Hk, t = a.blocks / a.Hk - 1 - blockIdx.x / a.Hk;  // long tiles first
-  const int b = last_at_most(a.B, t, [&](int i) { return first_tile(a.cu_q, i, a.G, kWide); });
   Seq s;
-  if (!sequence(a, b, &s)) return;
-  const int64_t tile = t - first_tile(a.cu_q, b, a.G, kWide);
+  int b;
+  const bool good = locate<true>(a, t, [&](int cu, int i) { return first_tile(cu, i, a.G, kWide); }, &b, &s);
+  if (!good) return;
+  const int64_t tile = t - first_tile(s.q0, b, a.G, kWide);
   const int rows = s.nq * a.G;
   if (tile < 0 || tile * kWide >= rows) return;
   const int row0 = static_cast<int>(tile) * kWide, row = row0 + wave * 32 + c;
@@ -701,6 +724,203 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void attn_wide_kernel(At
     }
 }
 
+// ------------------------- bf16, at most 16 rows --------------------------
+
+// One new token for each sequence: the G heads of a key head are one 16-wide tile, and the keys are all the work.  Eight
+// waves each take 32 keys of every 256 of a part: keys straight into registers as the product's operand, values by DMA
+// into LDS of the wave's own for the transposing read, both a round ahead, no barrier among the waves before their
+// sums meet at the end.
+constexpr int kFewThreads = 512, kFewWaves = kFewThreads / 64, kFewKeys = 32, kFewRound = kFewWaves * kFewKeys;
+
+template <int D>
+struct FewLds {
+  __bf16 v0[kFewWaves][kFewKeys * D], v1[kFewWaves][kFewKeys * D];
+};
+
+template <int D>
+struct FewState {
+  bf16x8 q[D / 32];
+  floatx4 o[D / 16];
+  float m, l;
+};
+
+// 32 keys: k their operands, v the staged values [D / 64 blocks][32 rows][64 columns], pieces turned as in a wide tile.
+template <int D>
+__device__ __forceinline__ void few_keys(const AttnArgs& a, FewState<D>& f, const bf16x8 (&k)[2][D / 32], __bf16* v, int end,
+                                         bool masked) {
+  const int lane = threadIdx.x & 63, g = lane >> 4, e = (lane & 15) >> 2, r = lane & 3;
+  floatx4 s[2];
+#pragma unroll
+  for (int n = 0; n < 2; ++n) {
+    s[n] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int st = 0; st < D / 32; ++st) s[n] = Op<__bf16>::mma(k[n][st], f.q[st], s[n]);
+  }
+  if (masked) {
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (16 * n + 4 * g + i >= end) s[n][i] = -INFINITY;
+  }
+  float top = -INFINITY;
+#pragma unroll
+  for (int n = 0; n < 2; ++n)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top = fmaxf(top, s[n][i]);
+  top = over_groups_max(top) * a.c2;
+  const float next = fmaxf(f.m, top), ref = next == -INFINITY ? 0.f : next, keep = __builtin_amdgcn_exp2f(f.m - ref);
+  f.m = next;
+  f.l *= keep;
+#pragma unroll
+  for (int dt = 0; dt < D / 16; ++dt) f.o[dt] *= keep;
+#pragma unroll
+  for (int n = 0; n < 2; ++n)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      s[n][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][i], a.c2, -ref));
+      f.l += s[n][i];
+    }
+  if (masked) {  // values that are not finite where some row does not see them (take_odd)
+    bool ok = true;
+#pragma unroll
+    for (int i = 0; i < kFewKeys * D / 8 / 64; ++i)
+      ok = ok && finite_piece<__bf16>(*reinterpret_cast<const u32x4*>(v + (i * 64 + lane) * 8));
+    if (__any(!ok)) {
+      for (int at = 0; at < min(end, kFewKeys); ++at)
+#pragma unroll
+        for (int dt = 0; dt < D / 16; ++dt)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const int d = 16 * dt + 4 * g + x;
+            const float y = static_cast<float>(v[d / 64 * kFewKeys * 64 + at * 64 + ((d / 8 % 8) ^ turn(at)) * 8 + d % 8]);
+            if (!(__builtin_fabsf(y) < INFINITY)) f.o[dt][x] += y;
+          }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // one wave: in order once its reads are done
+      for (int i = lane; i < kFewKeys * D; i += 64)
+        if (!(__builtin_fabsf(static_cast<float>(v[i])) < INFINITY)) v[i] = static_cast<__bf16>(0.f);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+  }
+  const bf16x8 p = Op<__bf16>::pack(s[0], s[1]);
+  typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
+#pragma unroll
+  for (int dt = 0; dt < D / 16; ++dt) {
+    __bf16* block = v + dt / 4 * kFewKeys * 64 + (4 * g + e) * 64 + (r & 1) * 4;
+    const int piece = dt % 4 * 2 + (r >> 1);
+    // turn() is the same 16 rows on
+    __bf16* at = block + (piece ^ turn(4 * g + e)) * 8;
+    const bf16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)at);
+    const bf16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(at + 16 * 64));
+    f.o[dt] = Op<__bf16>::mma(__builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7), p, f.o[dt]);
+  }
+}
+
+template <int D, bool SPLIT>
+__global__ __launch_bounds__(kFewThreads, 1) void attn_few_kernel(AttnArgs a) {
+  __shared__ union {
+    FewLds<D> v;
+    struct {
+      floatx4 o[kFewWaves][16][D / 4];
+      float m[kFewWaves][16], l[kFewWaves][16];
+    } meet;
+  } __attribute__((aligned(1024))) lds;
+  if (check_block(a)) return;
+  const int lane = threadIdx.x & 63, c16 = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
+  const int hk = blockIdx.x % a.Hk, rest = blockIdx.x / a.Hk;
+  Seq s;
+  int key_lo = 0, key_hi;
+  if (SPLIT) {
+    int b;
+    if (!locate<false>(a, rest, [&](int cu, int i) { return first_tile(cu, i, 1, a.chunk); }, &b, &s)) return;
+    const int64_t part = rest - first_tile(s.k0, b, 1, a.chunk);
+    if (part < 0 || part * a.chunk >= s.nk) return;
+    key_lo = static_cast<int>(part) * a.chunk;
+    key_hi = min(s.nk, key_lo + a.chunk);
+  } else {
+    if (!sequence(a, rest, &s)) return;
+    key_hi = s.nk;
+  }
+  const int rows = s.nq * a.G;
+  if (rows == 0) return;
+  const bool real = c16 < rows;
+  const int limit = limit_of(a, s, c16), open = limit_of(a, s, 0);
+  FewState<D> f;
+#pragma unroll
+  for (int st = 0; st < D / 32; ++st)
+    f.q[st] = real ? load_frag<__bf16>(query_row(a, a.q, s, hk, c16) + (32 * st + 8 * g) * 2) : zero_frag<__bf16>();
+#pragma unroll
+  for (int dt = 0; dt < D / 16; ++dt) f.o[dt] = floatx4{0.f, 0.f, 0.f, 0.f};
+  f.m = -INFINITY, f.l = 0.f;
+  const char* kbase = a.k.at + static_cast<int64_t>(s.k0) * a.k.row + hk * a.k.head;
+  const char* vbase = a.v.at + static_cast<int64_t>(s.k0) * a.v.row + hk * a.v.head;
+  const uint32_t krow = static_cast<uint32_t>(a.k.row), vrow = static_cast<uint32_t>(a.v.row);
+  const auto piece = [&](int row) { return static_cast<uint32_t>(((lane & 7) ^ turn(row)) * 16); };
+  const auto ask = [&](int key, bf16x8 (&k)[2][D / 32], __bf16* v) {
+    const char* kt = kbase + key * a.k.row;
+    const char* vt = vbase + key * a.v.row;
+    const int last = s.nk - 1 - key;  // rows past it are copies of it
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      const uint32_t off = min(16 * n + c16, last) * krow + 16 * g;
+#pragma unroll
+      for (int st = 0; st < D / 32; ++st) k[n][st] = load_frag<__bf16>(kt + off + 64 * st);
+    }
+#pragma unroll
+    for (int i = 0; i < kFewKeys / 8; ++i) {
+      const int row = 8 * i + lane / 8;
+      const uint32_t off = min(row, last) * vrow + piece(row);
+#pragma unroll
+      for (int n = 0; n < D / 64; ++n)
+        __builtin_amdgcn_global_load_lds(vt + off + 128 * n, (lds_void*)(v + n * kFewKeys * 64 + 8 * i * 64), 16, 0, 0);
+    }
+  };
+  bf16x8 k0[2][D / 32], k1[2][D / 32];
+  const auto step = [&](int key, const bf16x8 (&k)[2][D / 32], __bf16* v, bf16x8 (&kn)[2][D / 32], __bf16* vn) {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    if (key + kFewRound < key_hi) ask(key + kFewRound, kn, vn);
+    few_keys<D>(a, f, k, v, min(limit, key_hi) - key, key + kFewKeys > min(open, key_hi));
+  };
+  const int first = key_lo + wave * kFewKeys;
+  if (first < key_hi) ask(first, k0, lds.v.v0[wave]);
+  for (int key = first; key < key_hi; key += 2 * kFewRound) {
+    step(key, k0, lds.v.v0[wave], k1, lds.v.v1[wave]);
+    if (key + kFewRound >= key_hi) break;
+    step(key + kFewRound, k1, lds.v.v1[wave], k0, lds.v.v0[wave]);
+  }
+  // The waves' sums meet: w = 2^(m - max m).
+  f.l = over_groups_sum(f.l);
+  __syncthreads();
+#pragma unroll
+  for (int dt = 0; dt < D / 16; ++dt) lds.meet.o[wave][c16][4 * dt + g] = f.o[dt];
+  if (g == 0) lds.meet.m[wave][c16] = f.m, lds.meet.l[wave][c16] = f.l;
+  __syncthreads();
+  for (int i = threadIdx.x; i < rows * (D / 4); i += kFewThreads) {
+    const int row = i / (D / 4), d4 = i % (D / 4);
+    float top = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int x = 0; x < kFewWaves; ++x) top = fmaxf(top, lds.meet.m[x][row]);
+    const float ref = top == -INFINITY ? 0.f : top;
+    floatx4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int x = 0; x < kFewWaves; ++x) {
+      const float w = __builtin_amdgcn_exp2f(lds.meet.m[x][row] - ref);
+      l = __builtin_fmaf(w, lds.meet.l[x][row], l);
+      o += lds.meet.o[x][row][d4] * w;
+    }
+    if (SPLIT) {
+      const int64_t at = (static_cast<int64_t>(rest) * a.Hk + hk) * a.part_rows + row;
+      if (d4 == 0) a.part_ml[at] = make_float2(top, l);
+      *reinterpret_cast<floatx4*>(a.part + at * D + 4 * d4) = o;
+    } else {
+      if (d4 == 0 && a.lse)
+        a.lse[stat_at(a, s, hk, row)] = l == 0.f ? -INFINITY : (ref + __builtin_amdgcn_logf(l)) * kLn2;
+      store4<__bf16>(const_cast<char*>(query_row(a, a.out, s, hk, row)) + d4 * 8, o * (l == 0.f ? 0.f : 1.f / l));
+    }
+  }
+}
+
 // The parts of a row joined: one wave a row, out = sum w o / sum w l with w =
 // 2^(m - max m).
 template <class E, int D>
@@ -710,39 +930,55 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttnArgs a) {
   if (at >= a.total_q * a.H) return;
   const int64_t n = at / a.H;
   const int h = static_cast<int>(at - n * a.H), hk = h / a.G;
-  const int b = last_at_most(a.B, n, [&](int i) { return static_cast<int64_t>(a.cu_q[i]); });
   Seq s;
-  if (!sequence(a, b, &s) || n < s.q0 || n >= static_cast<int64_t>(s.q0) + s.nq) return;
+  int b;
+  const bool good = locate<true>(a, n, [](int cu, int) { return static_cast<int64_t>(cu); }, &b, &s);
+  if (!good || n < s.q0 || n >= static_cast<int64_t>(s.q0) + s.nq) return;
   const int row = static_cast<int>(n - s.q0) * a.G + h - hk * a.G;
   int64_t first;
   int parts, in = row;
   if (a.chunk) {
-    first = first_tile(a.cu_k, b, 1, a.chunk);
+    first = first_tile(s.k0, b, 1, a.chunk);
     parts = (s.nk + a.chunk - 1) / a.chunk;
   } else {
-    first = (first_tile(a.cu_q, b, a.G, kTile) + row / kTile) * a.splits;
+    first = (first_tile(s.q0, b, a.G, kTile) + row / kTile) * a.splits;
     parts = a.splits;
     in = row % kTile;
   }
-  const auto slot = [&](int p) { return ((first + p) * a.Hk + hk) * a.part_rows + in; };
-  float top = -INFINITY;
-  for (int p = lane; p < parts; p += 64) top = fmaxf(top, a.part_ml[slot(p)].x);
-#pragma unroll
-  for (int x = 1; x < 64; x *= 2) top = fmaxf(top, __shfl_xor(top, x));
-  const float ref = top == -INFINITY ? 0.f : top;
-  constexpr int kEach = D >= 64 ? D / 64 : 1;
-  float sum = 0.f, o[kEach] = {};
+  constexpr int kEach = D >= 64 ? D / 64 : 1, kAtOnce = 8;
   const int d = lane * kEach;
-  for (int p = 0; p < parts; ++p) {
-    const int64_t i = slot(p);
-    const float2 ml = a.part_ml[i];
-    if (ml.x == -INFINITY && ml.y == 0.f) continue;  // sees none of these keys
-    const float w = __builtin_amdgcn_exp2f(ml.x - ref);
-    sum = __builtin_fmaf(w, ml.y, sum);
-    if (d < D)
+  float top = -INFINITY, sum = 0.f, o[kEach] = {};
+  for (int p = 0; p < parts; p += kAtOnce) {
+    float2 ml[kAtOnce];
+    float x[kAtOnce][kEach];
 #pragma unroll
-      for (int x = 0; x < kEach; ++x) o[x] = __builtin_fmaf(w, a.part[i * D + d + x], o[x]);
+    for (int i = 0; i < kAtOnce; ++i) {
+      const int64_t slot = ((first + min(p + i, parts - 1)) * a.Hk + hk) * a.part_rows + in;
+      ml[i] = a.part_ml[slot];
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) x[i][e] = a.part[slot * D + (d < D ? d + e : 0)];
+    }
+    float next = top;
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      if (p + i >= parts) ml[i] = make_float2(-INFINITY, 0.f);
+      next = fmaxf(next, ml[i].x);
+    }
+    const float ref = next == -INFINITY ? 0.f : next, keep = __builtin_amdgcn_exp2f(top - ref);
+    top = next;
+    sum *= keep;
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) o[e] *= keep;
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      if (ml[i].x == -INFINITY && ml[i].y == 0.f) continue;  // sees none of these keys
+      const float w = __builtin_amdgcn_exp2f(ml[i].x - ref);
+      sum = __builtin_fmaf(w, ml[i].y, sum);
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) o[e] = __builtin_fmaf(w, x[i][e], o[e]);
+    }
   }
+  const float ref = top == -INFINITY ? 0.f : top;
   // NaN scores: the parts' l are NaN and pass through the sums.
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
   if (lane == 0 && a.lse) a.lse[at] = sum == 0.f ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * kLn2;
@@ -772,10 +1008,11 @@ __global__ __launch_bounds__(kThreads) void grad_q_kernel(AttnArgs a) {
   if (check_block(a)) return;
   const int lane = threadIdx.x & 63, c16 = lane & 15, g = lane >> 4, wave = threadIdx.x >> 6;
   const int hk = blockIdx.x % a.Hk, t = blockIdx.x / a.Hk;
-  const int b = last_at_most(a.B, t, [&](int i) { return first_tile(a.cu_q, i, a.G, kTile); });
   Seq s;
-  if (!sequence(a, b, &s)) return;
-  const int64_t tile = t - first_tile(a.cu_q, b, a.G, kTile);
+  int b;
+  const bool good = locate<true>(a, t, [&](int cu, int i) { return first_tile(cu, i, a.G, kTile); }, &b, &s);
+  if (!good) return;
+  const int64_t tile = t - first_tile(s.q0, b, a.G, kTile);
   const int rows = s.nq * a.G;
   if (tile < 0 || tile * kTile >= rows) return;
   const int row0 = static_cast<int>(tile) * kTile, row = row0 + wave * 16 + c16;
@@ -897,10 +1134,11 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void grad_q_wide_kernel(
   if (check_block(a)) return;
   const int lane = threadIdx.x & 63, c = lane & 31, hi = lane >> 5, wave = threadIdx.x >> 6;
   const int hk = blockIdx.x % a.Hk, t = a.blocks / a.Hk - 1 - blockIdx.x / a.Hk;  // long tiles first
-  const int b = last_at_most(a.B, t, [&](int i) { return first_tile(a.cu_q, i, a.G, kWide); });
   Seq s;
-  if (!sequence(a, b, &s)) return;
-  const int64_t tile = t - first_tile(a.cu_q, b, a.G, kWide);
+  int b;
+  const bool good = locate<true>(a, t, [&](int cu, int i) { return first_tile(cu, i, a.G, kWide); }, &b, &s);
+  if (!good) return;
+  const int64_t tile = t - first_tile(s.q0, b, a.G, kWide);
   const int rows = s.nq * a.G;
   if (tile < 0 || tile * kWide >= rows) return;
   const int row0 = static_cast<int>(tile) * kWide, row = row0 + wave * 32 + c;
@@ -1042,10 +1280,11 @@ __device__ __forceinline__ void grad_kv_wide(const AttnArgs& a, int block, WideK
   const int lane = threadIdx.x & 63, c = lane & 31, hi = lane >> 5, wave = threadIdx.x >> 6;
   const int hk = block % a.Hk, rest = block / a.Hk;
   const int split = SPLIT ? rest % a.splits : 0, t = SPLIT ? rest / a.splits : rest;
-  const int b = last_at_most(a.B, t, [&](int i) { return first_tile(a.cu_k, i, 1, kWide); });
   Seq s;
-  if (!sequence(a, b, &s)) return;
-  const int64_t tile = t - first_tile(a.cu_k, b, 1, kWide);
+  int b;
+  const bool good = locate<false>(a, t, [&](int cu, int i) { return first_tile(cu, i, 1, kWide); }, &b, &s);
+  if (!good) return;
+  const int64_t tile = t - first_tile(s.k0, b, 1, kWide);
   if (tile < 0 || tile * kWide >= s.nk) return;
   const int key0 = static_cast<int>(tile) * kWide, key = key0 + wave * 32 + c;
   const bool real = key < s.nk;
@@ -1173,10 +1412,11 @@ __global__ __launch_bounds__(kThreads) void grad_kv_kernel(AttnArgs a) {
   const int lane = threadIdx.x & 63, c16 = lane & 15, g = lane >> 4, wave = threadIdx.x >> 6;
   const int hk = blockIdx.x % a.Hk, rest = blockIdx.x / a.Hk;
   const int split = SPLIT ? rest % a.splits : 0, t = SPLIT ? rest / a.splits : rest;
-  const int b = last_at_most(a.B, t, [&](int i) { return first_tile(a.cu_k, i, 1, kTile); });
   Seq s;
-  if (!sequence(a, b, &s)) return;
-  const int64_t tile = t - first_tile(a.cu_k, b, 1, kTile);
+  int b;
+  const bool good = locate<false>(a, t, [&](int cu, int i) { return first_tile(cu, i, 1, kTile); }, &b, &s);
+  if (!good) return;
+  const int64_t tile = t - first_tile(s.k0, b, 1, kTile);
   if (tile < 0 || tile * kTile >= s.nk) return;
   const int key0 = static_cast<int>(tile) * kTile, key = key0 + wave * 16 + c16;
   const bool real = key < s.nk;
@@ -1318,25 +1558,33 @@ int64_t tiles(int64_t total, int32_t B, int64_t tile) { return total / tile + B;
 
 // Workgroups of 64 rows that the GPU holds at a time, about.
 constexpr int kFill = 512;
+constexpr int64_t kFewFill = 768, kFewWhole = 512;
 
 // How the forward pass splits its keys.
 struct Split {
   int32_t splits, chunk, part_rows;
   int64_t blocks;  // without heads
+  bool few;        // at most 16 rows a sequence and key head
 };
-Split forward_split(const Sizes& z) {
+Split forward_split(const Sizes& z, bool bf16) {
   const int32_t G = z.H / z.Hk;
   const int64_t rows = static_cast<int64_t>(std::min<int64_t>(z.max_q, z.total_q)) * G;
+  if (rows <= 16 && bf16 && z.D >= 64 && z.total_k > 0) {
+    const int64_t want = z.total_k * z.Hk / kFewFill;
+    const int64_t chunk = std::min<int64_t>(4096, std::max<int64_t>(kFewRound, (want + kFewRound - 1) / kFewRound * kFewRound));
+    if (z.total_k <= kFewWhole || z.total_k / z.B <= kFewRound) return Split{1, 0, static_cast<int32_t>(rows), z.B, true};
+    return Split{1, static_cast<int32_t>(chunk), static_cast<int32_t>(rows), tiles(z.total_k, z.B, chunk), true};
+  }
   if (rows <= kTile && z.total_k > 0) {
     // every sequence is one tile: parts of the same number of keys
     const int64_t want = z.total_k * z.Hk / (4 * kFill);
     const int64_t chunk = std::min<int64_t>(4096, std::max<int64_t>(256, (want + 63) / 64 * 64));
-    if (z.total_k / z.B > chunk) return Split{1, static_cast<int32_t>(chunk), static_cast<int32_t>(rows), tiles(z.total_k, z.B, chunk)};
+    if (z.total_k / z.B > chunk) return Split{1, static_cast<int32_t>(chunk), static_cast<int32_t>(rows), tiles(z.total_k, z.B, chunk), false};
   }
   const int64_t n = tiles(z.total_q * G, z.B, kTile), keys = z.total_k / z.B;
   int32_t splits = 1;
   while (splits < 16 && n * z.Hk * splits < kFill && keys / (splits * 2) >= 512) splits *= 2;
-  return Split{splits, 0, kTile, n * splits};
+  return Split{splits, 0, kTile, n * splits, false};
 }
 
 int32_t backward_splits(const Sizes& z) {
@@ -1359,8 +1607,8 @@ bool use_wide_kv(const Sizes& z, int dtype, const AttnArgs& a) {
 
 size_t round256(size_t n) { return (n + 255) & ~size_t(255); }
 
-size_t forward_bytes(const Sizes& z) {
-  const Split p = forward_split(z);
+size_t forward_bytes(const Sizes& z, bool bf16) {
+  const Split p = forward_split(z, bf16);
   if (p.splits == 1 && !p.chunk) return 256;
   return round256(static_cast<size_t>(p.blocks) * z.Hk * p.part_rows * (z.D + 2) * sizeof(float));
 }
@@ -1429,7 +1677,7 @@ void with_type(int dtype, int D, F f) {
 extern "C" size_t dora_grouped_attn_workspace_size(int32_t B, int32_t H, int32_t Hk, int32_t D, int32_t max_q,
                                                    int64_t total_q, int64_t total_k) {
   const dora::Sizes z{B, H, Hk, D, max_q, total_q, total_k};
-  return dora::good_sizes(z) ? dora::forward_bytes(z) : 0;
+  return dora::good_sizes(z) ? std::max(dora::forward_bytes(z, false), dora::forward_bytes(z, true)) : 0;
 }
 
 extern "C" size_t dora_grouped_attn_backward_workspace_size(int32_t B, int32_t H, int32_t Hk, int32_t D, int32_t max_q,
@@ -1450,18 +1698,21 @@ extern "C" int dora_grouped_attn(const dora_rows* q, const dora_rows* k, const d
   if (rc == DORA_OK) rc = check_rows(out, 16);
   if (rc != DORA_OK) return rc;
   if (!same_sizes(out, q)) return DORA_ERR_SHAPE;
-  if (too_small(workspace, workspace_bytes, forward_bytes(z))) return DORA_ERR_WORKSPACE;
+  const size_t need = dora_grouped_attn_workspace_size(B, z.H, z.Hk, z.D, max_q, z.total_q, z.total_k);
+  if (too_small(workspace, workspace_bytes, need)) return DORA_ERR_WORKSPACE;
   const size_t cu_bytes = (static_cast<size_t>(B) + 1) * sizeof(int32_t);
   if (rows_clash({out}, {q, k, v}, {},
                  {{lse_out, static_cast<size_t>(z.total_q) * z.H * sizeof(float)},
-                  {workspace, forward_bytes(z)},
+                  {workspace, need},
                   {dev_status, sizeof(int32_t)}},
                  {{cu_q, cu_bytes}, {cu_k, cu_bytes}}))
     return DORA_ERR_OVERLAP;
   if (z.total_q == 0) return DORA_OK;
-  const Split p = forward_split(z);
+  // 32-bit offsets to 32 rows on
+  const bool lean = near(a.k, 128, 0) && near(a.v, 128, 0);
+  Split p = forward_split(z, q->dtype == DORA_BF16 && lean);
   const bool split = p.splits > 1 || p.chunk;
-  const bool wide = !split && use_wide(z, q->dtype, a);
+  const bool wide = !split && !p.few && use_wide(z, q->dtype, a);
   const int64_t blocks = (wide ? tiles(z.total_q * a.G, B, kWide) : p.blocks) * z.Hk, join = (z.total_q * z.H + kThreads / 64 - 1) / (kThreads / 64);
   if (blocks > kMaxBlocks || (split && join > kMaxBlocks)) return DORA_ERR_UNSUPPORTED;
   a.out = row_view(out);
@@ -1475,8 +1726,19 @@ extern "C" int dora_grouped_attn(const dora_rows* q, const dora_rows* k, const d
   with_type(q->dtype, z.D, [&](auto e, auto d) {
     typedef decltype(e) E;
     constexpr int D = decltype(d)::value;
+    if constexpr (sizeof(E) == 2 && D >= 64) {
+      if (p.few && !split) {
+        hipLaunchKernelGGL((attn_few_kernel<D, false>), dim3(a.blocks + 1), dim3(kFewThreads), 0, st, a);
+        return;
+      }
+    }
     if (split) {
-      hipLaunchKernelGGL((attn_kernel<E, D, true>), dim3(a.blocks + 1), dim3(kThreads), 0, st, a);
+      bool launched = false;
+      if constexpr (sizeof(E) == 2 && D >= 64) {
+        launched = p.few;
+        if (launched) hipLaunchKernelGGL((attn_few_kernel<D, true>), dim3(a.blocks + 1), dim3(kFewThreads), 0, st, a);
+      }
+      if (!launched) hipLaunchKernelGGL((attn_kernel<E, D, true>), dim3(a.blocks + 1), dim3(kThreads), 0, st, a);
       hipLaunchKernelGGL((join_kernel<E, D>), dim3(static_cast<uint32_t>(join)), dim3(kThreads), 0, st, a);
     } else if constexpr (sizeof(E) == 2 && D >= 64) {
       if (wide) hipLaunchKernelGGL((attn_wide_kernel<D>), dim3(a.blocks + 1), dim3(kThreads), 0, st, a);

@@ -97,6 +97,34 @@ def test_split_keys(gpu, dtype, nq, H, Hk, D):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("nq,H,Hk,D", [(1, 8, 1, 128), (1, 3, 3, 64), (4, 8, 2, 128), (2, 5, 1, 64), (1, 16, 1, 64)])
+def test_few_rows(gpu, dtype, nq, H, Hk, D):
+    """At most 16 rows a key head: whole and split, lengths on both sides of a wave's 32 keys, a round's 256 and a part's,
+    queries that see none of a part, values that the last query alone sees."""
+    for causal in (False, True):
+        for nk in ([1, 2, 31, 32, 33, 255, 256, 257, 0, 511, 513, 3], [9000, 300, 0, 2500, 1, 4097], [8000, 1, 193]):
+            t, cu_q, cu_k = make([nq] * len(nk), nk, H, Hk, D, dtype, nk[0] + nq)
+            d = cuda(t)
+            args = (d["q"], d["k"], d["v"], dev_cu(cu_q), nq)
+            out, lse, st = gpu.dora_grouped_attn(*args, cu_k=dev_cu(cu_k), causal=causal)
+            want, bound = ref.attention(t["q"], t["k"], t["v"], cu_q, cu_k, causal)
+            assert int(st) == 0
+            ref.check(out, want["out"], bound["out"], f"{nk} out")
+            ref.check(lse, want["lse"], bound["lse"], f"{nk} lse")
+            if causal and nq > 1:
+                ends = torch.tensor([b - 1 for a, b in zip(cu_k, cu_k[1:]) if b - a > 1])
+                d["v"][ends, :, 2] = float("inf")
+                d["v"][ends, :, 5] = float("nan")
+                out, _, _ = gpu.dora_grouped_attn(*args, cu_k=dev_cu(cu_k), causal=True)
+                for b in range(len(nk)):
+                    rows = slice(cu_q[b], cu_q[b + 1] - 1)
+                    ref.check(out[rows], want["out"][rows], bound["out"][rows], f"{nk} {b} odd")
+                    if nk[b] > 1:
+                        assert bool((out[cu_q[b + 1] - 1, :, 2] == float("inf")).all())
+                        assert bool(torch.isnan(out[cu_q[b + 1] - 1, :, 5]).all())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 def test_split_tiles(gpu, dtype):
     """Several tiles of queries, still few: keys split, causal and not; dk and dv split over many rows."""
     for causal, nq, nk, H, Hk, D in ((True, [150], [5000], 4, 2, 64), (False, [90, 40], [4000, 3500], 4, 1, 128),
