@@ -131,6 +131,12 @@ __device__ __forceinline__ int limit_of(const AttnArgs& a, const Seq& s, int r) 
   return a.causal ? max(0, min(s.nk, div_group(a, r) + 1 + s.nk - s.nq)) : s.nk;
 }
 
+// Keys that any of n rows from row r on sees: a wave is idle past them.
+__device__ __forceinline__ int wave_limit(const AttnArgs& a, const Seq& s, int r, int n) {
+  const int rows = s.nq * a.G;
+  return __builtin_amdgcn_readfirstlane(r < rows ? limit_of(a, s, min(r + n, rows) - 1) : 0);
+}
+
 __device__ __forceinline__ const char* query_row(const AttnArgs& a, const RowView& x, const Seq& s, int hk, int r) {
   const int i = div_group(a, r);
   return x.at + (static_cast<int64_t>(s.q0) + i) * x.row + static_cast<int64_t>(hk * a.G + r - i * a.G) * x.head;
@@ -318,7 +324,7 @@ __global__ __launch_bounds__(kThreads) void attn_kernel(AttnArgs a) {
   const bool real = row < s.nq * a.G;
   const int limit = limit_of(a, s, row);
   // Keys below this are seen by every row of the tile that exists.
-  const int open = limit_of(a, s, tile * kTile);
+  const int open = limit_of(a, s, tile * kTile), wave_hi = wave_limit(a, s, tile * kTile + wave * 16, 16);
   Frag qf[D / 32];
 #pragma unroll
   for (int ks32 = 0; ks32 < D / 32; ++ks32)
@@ -344,6 +350,7 @@ __global__ __launch_bounds__(kThreads) void attn_kernel(AttnArgs a) {
     if (masked) odd = __syncthreads_or(!vt.finite());
     else __syncthreads();
     if (key + kKeys < key_hi) ask(key + kKeys);
+    if (key >= wave_hi) continue;
     floatx4 sc[kSteps];
 #pragma unroll
     for (int kt16 = 0; kt16 < kSteps; ++kt16) {
@@ -606,8 +613,12 @@ __device__ __forceinline__ void take_odd(WideForward<D>& f, __bf16* vs, int end)
 // products' sums stay far inside their range, and the sums are multiplied a few times in place of every tile.
 template <int D>
 __device__ __forceinline__ void wide_keys(const AttnArgs& a, WideForward<D>& f, const __bf16* ks, __bf16* vs,
-                                          const WidePlaces& w, int end, bool masked, bool odd) {
+                                          const WidePlaces& w, int end, bool masked, bool odd, bool idle) {
   const int hi = (threadIdx.x & 63) >> 5;
+  if (idle) {
+    if (odd) take_odd<D>(f, vs, 0);
+    return;
+  }
   floatx16 s[2];
 #pragma unroll
   for (int n = 0; n < 2; ++n) {
@@ -680,6 +691,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void attn_wide_kernel(At
   const int row0 = static_cast<int>(tile) * kWide, row = row0 + wave * 32 + c;
   const bool real = row < rows;
   const int key_hi = limit_of(a, s, min(row0 + kWide, rows) - 1), open = limit_of(a, s, row0);
+  const int wave_hi = wave_limit(a, s, row0 + wave * 32, 32);
   const WidePlaces w = wide_places();
   WideForward<D> f;
   f.limit = limit_of(a, s, row);
@@ -701,7 +713,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void attn_wide_kernel(At
     staged();
     if (key + kWideKeys < key_hi) ask(key + kWideKeys, kn, vn);
     const bool masked = key + kWideKeys > open;
-    wide_keys<D>(a, f, kt, vt, w, f.limit - key, masked, masked && odd_tile<D>(vt));
+    wide_keys<D>(a, f, kt, vt, w, f.limit - key, masked, masked && odd_tile<D>(vt), key >= wave_hi);
   };
   if (key_hi > 0) ask(0, tiles.a0, tiles.b0);
   for (int key = 0; key < key_hi; key += 2 * kWideKeys) {
@@ -1018,7 +1030,7 @@ __global__ __launch_bounds__(kThreads) void grad_q_kernel(AttnArgs a) {
   const int row0 = static_cast<int>(tile) * kTile, row = row0 + wave * 16 + c16;
   const bool real = row < rows;
   const int limit = limit_of(a, s, row), open = limit_of(a, s, row0);
-  const int key_hi = limit_of(a, s, min(row0 + kTile, rows) - 1);
+  const int key_hi = limit_of(a, s, min(row0 + kTile, rows) - 1), wave_hi = wave_limit(a, s, row0 + wave * 16, 16);
   Frag qf[D / 32], gf[D / 32];
   float delta = 0.f;
 #pragma unroll
@@ -1053,6 +1065,7 @@ __global__ __launch_bounds__(kThreads) void grad_q_kernel(AttnArgs a) {
     vt.store(vs);
     __syncthreads();
     if (key + kKeys < key_hi) ask(key + kKeys);
+    if (key >= wave_hi) continue;
 #pragma unroll
     for (int st32 = 0; st32 < kKeys / 32; ++st32) {
       floatx4 ds[2];
@@ -1144,7 +1157,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void grad_q_wide_kernel(
   const int row0 = static_cast<int>(tile) * kWide, row = row0 + wave * 32 + c;
   const bool real = row < rows;
   const int key_hi = limit_of(a, s, min(row0 + kWide, rows) - 1), open = limit_of(a, s, row0);
-  const int limit = limit_of(a, s, row);
+  const int limit = limit_of(a, s, row), wave_hi = wave_limit(a, s, row0 + wave * 32, 32);
   const WidePlaces w = wide_places();
   WideGradQ<D> f;
   float delta = 0.f;
@@ -1172,7 +1185,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void grad_q_wide_kernel(
   const auto step = [&](int key, const __bf16* kt, const __bf16* vt, __bf16* kn, __bf16* vn) {
     staged();
     if (key + kWideKeys < key_hi) ask(key + kWideKeys, kn, vn);
-    wide_grad_q_keys<D>(a, f, kt, vt, w, limit - key, key + kWideKeys > open);
+    if (key < wave_hi) wide_grad_q_keys<D>(a, f, kt, vt, w, limit - key, key + kWideKeys > open);
   };
   if (key_hi > 0) ask(0, tiles.a0, tiles.b0);
   for (int key = 0; key < key_hi; key += 2 * kWideKeys) {
@@ -1287,6 +1300,7 @@ __device__ __forceinline__ void grad_kv_wide(const AttnArgs& a, int block, WideK
   const int64_t tile = t - first_tile(s.k0, b, 1, kWide);
   if (tile < 0 || tile * kWide >= s.nk) return;
   const int key0 = static_cast<int>(tile) * kWide, key = key0 + wave * 32 + c;
+  const int wave_key = __builtin_amdgcn_readfirstlane(key0 + wave * 32);
   const bool real = key < s.nk;
   const int rows = s.nq * a.G;
   int row_lo = a.causal ? min(rows, max(0, key0 - s.nk + s.nq) * a.G) : 0, row_hi = rows;
@@ -1347,7 +1361,8 @@ __device__ __forceinline__ void grad_kv_wide(const AttnArgs& a, int block, WideK
       stat = ask_stat(r - kRows);
       ask(r - kRows, qn, gn);
     }
-    wide_grad_kv_rows<D, PART>(a, f, qt, gt, w, here, key, r < open || r + kRows > row_hi);
+    if (wave_key < wave_limit(a, s, r, kRows))
+      wide_grad_kv_rows<D, PART>(a, f, qt, gt, w, here, key, r < open || r + kRows > row_hi);
     if (more) put_stat(r - kRows, stat, next);
   };
   // From the last rows back: every tile of keys begins with the same rows, and the tiles at work share them in the L2
@@ -1419,6 +1434,7 @@ __global__ __launch_bounds__(kThreads) void grad_kv_kernel(AttnArgs a) {
   const int64_t tile = t - first_tile(s.k0, b, 1, kTile);
   if (tile < 0 || tile * kTile >= s.nk) return;
   const int key0 = static_cast<int>(tile) * kTile, key = key0 + wave * 16 + c16;
+  const int wave_key = __builtin_amdgcn_readfirstlane(key0 + wave * 16);
   const bool real = key < s.nk;
   const int rows = s.nq * a.G;
   // The first row that sees a key of the tile.
@@ -1465,6 +1481,7 @@ __global__ __launch_bounds__(kThreads) void grad_kv_kernel(AttnArgs a) {
     }
     __syncthreads();
     if (r + kRows < row_hi) ask(r + kRows);
+    if (wave_key >= wave_limit(a, s, r, kRows)) continue;
 #pragma unroll
     for (int st32 = 0; st32 < kRows / 32; ++st32) {
       floatx4 p[2], ds[2];
