@@ -727,7 +727,8 @@ int dora_rope(const dora_rows* q, const dora_rows* k, const int32_t* positions, 
  *              D 32, 64 or 128; H at most 256; one dtype.
  *   cu_q, cu_k int32 [B+1], monotone from 0 or more to at most the rows; equal
  *              pointers are allowed.  1 <= B <= DORA_MAX_SEQUENCES.
- *   max_q      no sequence has more queries; total_q H / Hk at most 2^31 - 1.
+ *   max_q      no sequence has more queries; total_k and total_q H / Hk at most
+ *              2^31 - 65536.
  *   softmax_scale  <= 0 selects 1/sqrt(D).
  *   dtype      bf16: fp32 products and softmax, P rounded to bf16 for its
  *              product; fp32: fp32 throughout.  Output rounded once.

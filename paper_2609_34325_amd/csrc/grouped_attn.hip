@@ -54,6 +54,7 @@ struct AttnArgs {
   int32_t splits;     // parts of a tile's keys (forward) or of a tile's rows (grad_kv)
   int32_t chunk;      // or: keys of a part, every sequence one tile of rows
   int32_t blocks;
+  int32_t mixed;
   int32_t* status;
 };
 
@@ -64,6 +65,17 @@ __device__ __forceinline__ int div_group(const AttnArgs& a, int r) {
 // First tile number of sequence b, which begins at `boundary`.
 __device__ __forceinline__ int64_t first_tile(int boundary, int b, int mul, int tile) {
   return static_cast<int64_t>(max(boundary, 0)) * mul / tile + b;
+}
+
+// Tile number of workgroup i of n (without heads): i, or (a.mixed) in another order, sixteen at a time, each sixteen turned
+// one further than the last.  Numbers that hold no tile (a sequence of exactly one tile has one such beside it) recur at a
+// fixed distance, and workgroups go to dies and shader engines by their number: in plain order the tiles that exist meet on
+// half of the GPU (512 sequences of 64 rows, 8 heads of 64, bf16: 73 us in place of 51; 256 of 128 in the wide kernel 71 in
+// place of 48).  Long sequences have few such numbers, and their tiles share keys in the L2 in plain order (5670 us in place
+// of 6000 for forward and backward over eight of up to 8192).
+__device__ __forceinline__ int tile_number(const AttnArgs& a, int i) {
+  const int n = a.blocks / a.Hk, lo = i & ~15;
+  return a.mixed && lo + 16 <= n ? lo | ((i + (i >> 4)) & 15) : i;
 }
 
 // The last b with first(b) <= t; every lane of the wave calls it.
@@ -120,7 +132,7 @@ __device__ __forceinline__ bool check_block(const AttnArgs& a) {
   if (static_cast<int>(blockIdx.x) < a.blocks) return false;
   bool bad = false;
   Seq s;
-  for (int b = threadIdx.x; b < a.B; b += blockDim.x) bad |= !sequence(a, b, &s);
+  for (int b = threadIdx.x; b < a.B; b += kThreads) bad |= !sequence(a, b, &s);
   if (bad) atomicOr(a.status, DORA_DEV_CU_SEQLENS);
   return true;
 }
@@ -296,7 +308,7 @@ __global__ __launch_bounds__(kThreads) void attn_kernel(AttnArgs a) {
   __shared__ alignas(16) E vs[kKeys * kLd];
   if (check_block(a)) return;
   const int lane = threadIdx.x & 63, c16 = lane & 15, g = lane >> 4, wave = threadIdx.x >> 6;
-  const int hk = blockIdx.x % a.Hk, rest = blockIdx.x / a.Hk;
+  const int hk = blockIdx.x % a.Hk, rest = tile_number(a, blockIdx.x / a.Hk);
   const int split = SPLIT && !a.chunk ? rest % a.splits : 0, t = SPLIT && !a.chunk ? rest / a.splits : rest;
   Seq s;
   int tile = 0, key_lo = 0, key_hi;
@@ -680,7 +692,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void attn_wide_kernel(At
   __shared__ __attribute__((aligned(1024))) WideTiles<D> tiles;
   if (check_block(a)) return;
   const int lane = threadIdx.x & 63, c = lane & 31, hi = lane >> 5, wave = threadIdx.x >> 6;
-  const int hk = blockIdx.x % a.Hk, t = a.blocks / a.Hk - 1 - blockIdx.x / a.Hk;  // long tiles first
+  const int hk = blockIdx.x % a.Hk, t = a.blocks / a.Hk - 1 - tile_number(a, blockIdx.x / a.Hk);  // long tiles first
   Seq s;
   int b;
   const bool good = locate<true>(a, t, [&](int cu, int i) { return first_tile(cu, i, a.G, kWide); }, &b, &s);
@@ -734,203 +746,6 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void attn_wide_kernel(At
       const floatx4 x = {f.o[dt][4 * n], f.o[dt][4 * n + 1], f.o[dt][4 * n + 2], f.o[dt][4 * n + 3]};
       store4<__bf16>(to + (32 * dt + 8 * n) * 2, x * inv);
     }
-}
-
-// ------------------------- bf16, at most 16 rows --------------------------
-
-// One new token for each sequence: the G heads of a key head are one 16-wide tile, and the keys are all the work.  Eight
-// waves each take 32 keys of every 256 of a part: keys straight into registers as the product's operand, values by DMA
-// into LDS of the wave's own for the transposing read, both a round ahead, no barrier among the waves before their
-// sums meet at the end.
-constexpr int kFewThreads = 512, kFewWaves = kFewThreads / 64, kFewKeys = 32, kFewRound = kFewWaves * kFewKeys;
-
-template <int D>
-struct FewLds {
-  __bf16 v0[kFewWaves][kFewKeys * D], v1[kFewWaves][kFewKeys * D];
-};
-
-template <int D>
-struct FewState {
-  bf16x8 q[D / 32];
-  floatx4 o[D / 16];
-  float m, l;
-};
-
-// 32 keys: k their operands, v the staged values [D / 64 blocks][32 rows][64 columns], pieces turned as in a wide tile.
-template <int D>
-__device__ __forceinline__ void few_keys(const AttnArgs& a, FewState<D>& f, const bf16x8 (&k)[2][D / 32], __bf16* v, int end,
-                                         bool masked) {
-  const int lane = threadIdx.x & 63, g = lane >> 4, e = (lane & 15) >> 2, r = lane & 3;
-  floatx4 s[2];
-#pragma unroll
-  for (int n = 0; n < 2; ++n) {
-    s[n] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int st = 0; st < D / 32; ++st) s[n] = Op<__bf16>::mma(k[n][st], f.q[st], s[n]);
-  }
-  if (masked) {
-#pragma unroll
-    for (int n = 0; n < 2; ++n)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (16 * n + 4 * g + i >= end) s[n][i] = -INFINITY;
-  }
-  float top = -INFINITY;
-#pragma unroll
-  for (int n = 0; n < 2; ++n)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) top = fmaxf(top, s[n][i]);
-  top = over_groups_max(top) * a.c2;
-  const float next = fmaxf(f.m, top), ref = next == -INFINITY ? 0.f : next, keep = __builtin_amdgcn_exp2f(f.m - ref);
-  f.m = next;
-  f.l *= keep;
-#pragma unroll
-  for (int dt = 0; dt < D / 16; ++dt) f.o[dt] *= keep;
-#pragma unroll
-  for (int n = 0; n < 2; ++n)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      s[n][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][i], a.c2, -ref));
-      f.l += s[n][i];
-    }
-  if (masked) {  // values that are not finite where some row does not see them (take_odd)
-    bool ok = true;
-#pragma unroll
-    for (int i = 0; i < kFewKeys * D / 8 / 64; ++i)
-      ok = ok && finite_piece<__bf16>(*reinterpret_cast<const u32x4*>(v + (i * 64 + lane) * 8));
-    if (__any(!ok)) {
-      for (int at = 0; at < min(end, kFewKeys); ++at)
-#pragma unroll
-        for (int dt = 0; dt < D / 16; ++dt)
-#pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            const int d = 16 * dt + 4 * g + x;
-            const float y = static_cast<float>(v[d / 64 * kFewKeys * 64 + at * 64 + ((d / 8 % 8) ^ turn(at)) * 8 + d % 8]);
-            if (!(__builtin_fabsf(y) < INFINITY)) f.o[dt][x] += y;
-          }
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // one wave: in order once its reads are done
-      for (int i = lane; i < kFewKeys * D; i += 64)
-        if (!(__builtin_fabsf(static_cast<float>(v[i])) < INFINITY)) v[i] = static_cast<__bf16>(0.f);
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    }
-  }
-  const bf16x8 p = Op<__bf16>::pack(s[0], s[1]);
-  typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
-#pragma unroll
-  for (int dt = 0; dt < D / 16; ++dt) {
-    __bf16* block = v + dt / 4 * kFewKeys * 64 + (4 * g + e) * 64 + (r & 1) * 4;
-    const int piece = dt % 4 * 2 + (r >> 1);
-    // turn() is the same 16 rows on
-    __bf16* at = block + (piece ^ turn(4 * g + e)) * 8;
-    const bf16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)at);
-    const bf16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(at + 16 * 64));
-    f.o[dt] = Op<__bf16>::mma(__builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7), p, f.o[dt]);
-  }
-}
-
-template <int D, bool SPLIT>
-__global__ __launch_bounds__(kFewThreads, 1) void attn_few_kernel(AttnArgs a) {
-  __shared__ union {
-    FewLds<D> v;
-    struct {
-      floatx4 o[kFewWaves][16][D / 4];
-      float m[kFewWaves][16], l[kFewWaves][16];
-    } meet;
-  } __attribute__((aligned(1024))) lds;
-  if (check_block(a)) return;
-  const int lane = threadIdx.x & 63, c16 = lane & 15, g = lane >> 4;
-  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
-  const int hk = blockIdx.x % a.Hk, rest = blockIdx.x / a.Hk;
-  Seq s;
-  int key_lo = 0, key_hi;
-  if (SPLIT) {
-    int b;
-    if (!locate<false>(a, rest, [&](int cu, int i) { return first_tile(cu, i, 1, a.chunk); }, &b, &s)) return;
-    const int64_t part = rest - first_tile(s.k0, b, 1, a.chunk);
-    if (part < 0 || part * a.chunk >= s.nk) return;
-    key_lo = static_cast<int>(part) * a.chunk;
-    key_hi = min(s.nk, key_lo + a.chunk);
-  } else {
-    if (!sequence(a, rest, &s)) return;
-    key_hi = s.nk;
-  }
-  const int rows = s.nq * a.G;
-  if (rows == 0) return;
-  const bool real = c16 < rows;
-  const int limit = limit_of(a, s, c16), open = limit_of(a, s, 0);
-  FewState<D> f;
-#pragma unroll
-  for (int st = 0; st < D / 32; ++st)
-    f.q[st] = real ? load_frag<__bf16>(query_row(a, a.q, s, hk, c16) + (32 * st + 8 * g) * 2) : zero_frag<__bf16>();
-#pragma unroll
-  for (int dt = 0; dt < D / 16; ++dt) f.o[dt] = floatx4{0.f, 0.f, 0.f, 0.f};
-  f.m = -INFINITY, f.l = 0.f;
-  const char* kbase = a.k.at + static_cast<int64_t>(s.k0) * a.k.row + hk * a.k.head;
-  const char* vbase = a.v.at + static_cast<int64_t>(s.k0) * a.v.row + hk * a.v.head;
-  const uint32_t krow = static_cast<uint32_t>(a.k.row), vrow = static_cast<uint32_t>(a.v.row);
-  const auto piece = [&](int row) { return static_cast<uint32_t>(((lane & 7) ^ turn(row)) * 16); };
-  const auto ask = [&](int key, bf16x8 (&k)[2][D / 32], __bf16* v) {
-    const char* kt = kbase + key * a.k.row;
-    const char* vt = vbase + key * a.v.row;
-    const int last = s.nk - 1 - key;  // rows past it are copies of it
-#pragma unroll
-    for (int n = 0; n < 2; ++n) {
-      const uint32_t off = min(16 * n + c16, last) * krow + 16 * g;
-#pragma unroll
-      for (int st = 0; st < D / 32; ++st) k[n][st] = load_frag<__bf16>(kt + off + 64 * st);
-    }
-#pragma unroll
-    for (int i = 0; i < kFewKeys / 8; ++i) {
-      const int row = 8 * i + lane / 8;
-      const uint32_t off = min(row, last) * vrow + piece(row);
-#pragma unroll
-      for (int n = 0; n < D / 64; ++n)
-        __builtin_amdgcn_global_load_lds(vt + off + 128 * n, (lds_void*)(v + n * kFewKeys * 64 + 8 * i * 64), 16, 0, 0);
-    }
-  };
-  bf16x8 k0[2][D / 32], k1[2][D / 32];
-  const auto step = [&](int key, const bf16x8 (&k)[2][D / 32], __bf16* v, bf16x8 (&kn)[2][D / 32], __bf16* vn) {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-    if (key + kFewRound < key_hi) ask(key + kFewRound, kn, vn);
-    few_keys<D>(a, f, k, v, min(limit, key_hi) - key, key + kFewKeys > min(open, key_hi));
-  };
-  const int first = key_lo + wave * kFewKeys;
-  if (first < key_hi) ask(first, k0, lds.v.v0[wave]);
-  for (int key = first; key < key_hi; key += 2 * kFewRound) {
-    step(key, k0, lds.v.v0[wave], k1, lds.v.v1[wave]);
-    if (key + kFewRound >= key_hi) break;
-    step(key + kFewRound, k1, lds.v.v1[wave], k0, lds.v.v0[wave]);
-  }
-  // The waves' sums meet: w = 2^(m - max m).
-  f.l = over_groups_sum(f.l);
-  __syncthreads();
-#pragma unroll
-  for (int dt = 0; dt < D / 16; ++dt) lds.meet.o[wave][c16][4 * dt + g] = f.o[dt];
-  if (g == 0) lds.meet.m[wave][c16] = f.m, lds.meet.l[wave][c16] = f.l;
-  __syncthreads();
-  for (int i = threadIdx.x; i < rows * (D / 4); i += kFewThreads) {
-    const int row = i / (D / 4), d4 = i % (D / 4);
-    float top = -INFINITY, l = 0.f;
-#pragma unroll
-    for (int x = 0; x < kFewWaves; ++x) top = fmaxf(top, lds.meet.m[x][row]);
-    const float ref = top == -INFINITY ? 0.f : top;
-    floatx4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int x = 0; x < kFewWaves; ++x) {
-      const float w = __builtin_amdgcn_exp2f(lds.meet.m[x][row] - ref);
-      l = __builtin_fmaf(w, lds.meet.l[x][row], l);
-      o += lds.meet.o[x][row][d4] * w;
-    }
-    if (SPLIT) {
-      const int64_t at = (static_cast<int64_t>(rest) * a.Hk + hk) * a.part_rows + row;
-      if (d4 == 0) a.part_ml[at] = make_float2(top, l);
-      *reinterpret_cast<floatx4*>(a.part + at * D + 4 * d4) = o;
-    } else {
-      if (d4 == 0 && a.lse)
-        a.lse[stat_at(a, s, hk, row)] = l == 0.f ? -INFINITY : (ref + __builtin_amdgcn_logf(l)) * kLn2;
-      store4<__bf16>(const_cast<char*>(query_row(a, a.out, s, hk, row)) + d4 * 8, o * (l == 0.f ? 0.f : 1.f / l));
-    }
-  }
 }
 
 // The parts of a row joined: one wave a row, out = sum w o / sum w l with w =
@@ -1019,7 +834,7 @@ __global__ __launch_bounds__(kThreads) void grad_q_kernel(AttnArgs a) {
   __shared__ alignas(16) E vs[kKeys * kLd];
   if (check_block(a)) return;
   const int lane = threadIdx.x & 63, c16 = lane & 15, g = lane >> 4, wave = threadIdx.x >> 6;
-  const int hk = blockIdx.x % a.Hk, t = blockIdx.x / a.Hk;
+  const int hk = blockIdx.x % a.Hk, t = tile_number(a, blockIdx.x / a.Hk);
   Seq s;
   int b;
   const bool good = locate<true>(a, t, [&](int cu, int i) { return first_tile(cu, i, a.G, kTile); }, &b, &s);
@@ -1146,7 +961,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void grad_q_wide_kernel(
   __shared__ __attribute__((aligned(1024))) WideTiles<D> tiles;
   if (check_block(a)) return;
   const int lane = threadIdx.x & 63, c = lane & 31, hi = lane >> 5, wave = threadIdx.x >> 6;
-  const int hk = blockIdx.x % a.Hk, t = a.blocks / a.Hk - 1 - blockIdx.x / a.Hk;  // long tiles first
+  const int hk = blockIdx.x % a.Hk, t = a.blocks / a.Hk - 1 - tile_number(a, blockIdx.x / a.Hk);  // long tiles first
   Seq s;
   int b;
   const bool good = locate<true>(a, t, [&](int cu, int i) { return first_tile(cu, i, a.G, kWide); }, &b, &s);
@@ -1291,7 +1106,7 @@ template <int D, bool SPLIT, Part PART>
 __device__ __forceinline__ void grad_kv_wide(const AttnArgs& a, int block, WideKvLds<D>& lds) {
   constexpr int kRows = kWideKeys;
   const int lane = threadIdx.x & 63, c = lane & 31, hi = lane >> 5, wave = threadIdx.x >> 6;
-  const int hk = block % a.Hk, rest = block / a.Hk;
+  const int hk = block % a.Hk, rest = tile_number(a, block / a.Hk);
   const int split = SPLIT ? rest % a.splits : 0, t = SPLIT ? rest / a.splits : rest;
   Seq s;
   int b;
@@ -1366,7 +1181,7 @@ __device__ __forceinline__ void grad_kv_wide(const AttnArgs& a, int block, WideK
     if (more) put_stat(r - kRows, stat, next);
   };
   // From the last rows back: every tile of keys begins with the same rows, and the tiles at work share them in the L2
-  // (forward, each begins at its own: 4050 us in place of LATER).
+  // (each from its own first rows on: 4050 us in place of 3610).
   const int last = row_lo + max(row_hi - row_lo - 1, 0) / kRows * kRows;
   if (row_lo < row_hi) {
     const float2 stat = ask_stat(last);
@@ -1425,7 +1240,7 @@ __global__ __launch_bounds__(kThreads) void grad_kv_kernel(AttnArgs a) {
   __shared__ floatx4 lse_s[kRows / 4], delta_s[kRows / 4];
   __shared__ int4 limit_s[kRows / 4];
   const int lane = threadIdx.x & 63, c16 = lane & 15, g = lane >> 4, wave = threadIdx.x >> 6;
-  const int hk = blockIdx.x % a.Hk, rest = blockIdx.x / a.Hk;
+  const int hk = blockIdx.x % a.Hk, rest = tile_number(a, blockIdx.x / a.Hk);
   const int split = SPLIT ? rest % a.splits : 0, t = SPLIT ? rest / a.splits : rest;
   Seq s;
   int b;
@@ -1565,43 +1380,38 @@ struct Sizes {
   int64_t total_q, total_k;
 };
 
+constexpr int64_t kMaxRows = 0x7FFF0000;  // a tile's steps past the last row stay in 32 bits
 bool good_sizes(const Sizes& z) {
   return z.B >= 1 && z.B <= DORA_MAX_SEQUENCES && z.H >= 1 && z.H <= 256 && z.Hk >= 1 && z.H % z.Hk == 0 &&
          (z.D == 32 || z.D == 64 || z.D == 128) && z.max_q >= 0 && z.total_q >= 0 && z.total_k >= 0 &&
-         z.total_k <= 0x7FFFFFFF && z.total_q * (z.H / z.Hk) <= 0x7FFFFFFF;
+         z.total_k <= kMaxRows && z.total_q <= kMaxRows && z.total_q * (z.H / z.Hk) <= kMaxRows;
 }
 
 int64_t tiles(int64_t total, int32_t B, int64_t tile) { return total / tile + B; }
+// Sequences of about one to four tiles: the numbers that hold none are many (tile_number).
+int32_t mix_tiles(int64_t total, int32_t B, int64_t tile) { return total / tile >= B / 2 && total / tile < int64_t{4} * B; }
 
 // Workgroups of 64 rows that the GPU holds at a time, about.
 constexpr int kFill = 512;
-constexpr int64_t kFewFill = 768, kFewWhole = 512;
 
 // How the forward pass splits its keys.
 struct Split {
   int32_t splits, chunk, part_rows;
   int64_t blocks;  // without heads
-  bool few;        // at most 16 rows a sequence and key head
 };
-Split forward_split(const Sizes& z, bool bf16) {
+Split forward_split(const Sizes& z) {
   const int32_t G = z.H / z.Hk;
   const int64_t rows = static_cast<int64_t>(std::min<int64_t>(z.max_q, z.total_q)) * G;
-  if (rows <= 16 && bf16 && z.D >= 64 && z.total_k > 0) {
-    const int64_t want = z.total_k * z.Hk / kFewFill;
-    const int64_t chunk = std::min<int64_t>(4096, std::max<int64_t>(kFewRound, (want + kFewRound - 1) / kFewRound * kFewRound));
-    if (z.total_k <= kFewWhole || z.total_k / z.B <= kFewRound) return Split{1, 0, static_cast<int32_t>(rows), z.B, true};
-    return Split{1, static_cast<int32_t>(chunk), static_cast<int32_t>(rows), tiles(z.total_k, z.B, chunk), true};
-  }
   if (rows <= kTile && z.total_k > 0) {
     // every sequence is one tile: parts of the same number of keys
     const int64_t want = z.total_k * z.Hk / (4 * kFill);
     const int64_t chunk = std::min<int64_t>(4096, std::max<int64_t>(256, (want + 63) / 64 * 64));
-    if (z.total_k / z.B > chunk) return Split{1, static_cast<int32_t>(chunk), static_cast<int32_t>(rows), tiles(z.total_k, z.B, chunk), false};
+    if (z.total_k / z.B > chunk) return Split{1, static_cast<int32_t>(chunk), static_cast<int32_t>(rows), tiles(z.total_k, z.B, chunk)};
   }
   const int64_t n = tiles(z.total_q * G, z.B, kTile), keys = z.total_k / z.B;
   int32_t splits = 1;
   while (splits < 16 && n * z.Hk * splits < kFill && keys / (splits * 2) >= 512) splits *= 2;
-  return Split{splits, 0, kTile, n * splits, false};
+  return Split{splits, 0, kTile, n * splits};
 }
 
 int32_t backward_splits(const Sizes& z) {
@@ -1611,21 +1421,25 @@ int32_t backward_splits(const Sizes& z) {
   return splits;
 }
 
-// The 128-row kernels: where a tile is mostly rows that exist, and the bytes from a staged tile's first row to its last
-// fit the 32-bit offsets (a stride of 2^23 bytes on).
+// The kernels of 128 rows or keys: where the bytes from a staged tile's first row to its last fit the 32-bit offsets, and
+// from this many rows (keys) a sequence on, by the average.  Both sides in us, 8 heads, as many sequences as fill the GPU:
+//   forward   64 rows of 64 50.6 narrow, 52.5 wide; 65 rows 74, 61; 64 rows of 128 80.7, 83.2; 65 rows 133, 102
+//   backward  160 rows of 64 186, 188; 200 rows 142, 129; 64 rows of 128 271, 275; 65 rows 451, 324
+constexpr int64_t kWideRows = kTile, kWideGradRows64 = 176;
 bool near(const RowView& x, int64_t rows, int64_t heads) { return x.row * rows + x.head * heads < (int64_t{1} << 31); }
-bool use_wide(const Sizes& z, int dtype, const AttnArgs& a) {
-  return dtype == DORA_BF16 && z.D >= 64 && z.total_q * a.G / z.B >= 96 && near(a.k, 128, 0) && near(a.v, 128, 0);
+bool use_wide(const Sizes& z, int dtype, const AttnArgs& a, bool grad) {
+  return dtype == DORA_BF16 && z.D >= 64 && near(a.k, 128, 0) && near(a.v, 128, 0) &&
+         z.total_q * a.G / z.B > (grad && z.D == 64 ? kWideGradRows64 : kWideRows);
 }
 bool use_wide_kv(const Sizes& z, int dtype, const AttnArgs& a) {
-  return dtype == DORA_BF16 && z.D >= 64 && z.total_k / z.B >= 96 && 32 % a.G == 0 && near(a.v, 128, 0) &&
-         near(a.q, 64, a.G) && near(a.dout, 64, a.G);
+  return dtype == DORA_BF16 && z.D >= 64 && 32 % a.G == 0 && near(a.q, 64, a.G) && near(a.dout, 64, a.G) &&
+         z.total_k / z.B > (z.D == 64 ? kWideGradRows64 : kWideRows);
 }
 
 size_t round256(size_t n) { return (n + 255) & ~size_t(255); }
 
-size_t forward_bytes(const Sizes& z, bool bf16) {
-  const Split p = forward_split(z, bf16);
+size_t forward_bytes(const Sizes& z) {
+  const Split p = forward_split(z);
   if (p.splits == 1 && !p.chunk) return 256;
   return round256(static_cast<size_t>(p.blocks) * z.Hk * p.part_rows * (z.D + 2) * sizeof(float));
 }
@@ -1694,7 +1508,7 @@ void with_type(int dtype, int D, F f) {
 extern "C" size_t dora_grouped_attn_workspace_size(int32_t B, int32_t H, int32_t Hk, int32_t D, int32_t max_q,
                                                    int64_t total_q, int64_t total_k) {
   const dora::Sizes z{B, H, Hk, D, max_q, total_q, total_k};
-  return dora::good_sizes(z) ? std::max(dora::forward_bytes(z, false), dora::forward_bytes(z, true)) : 0;
+  return dora::good_sizes(z) ? dora::forward_bytes(z) : 0;
 }
 
 extern "C" size_t dora_grouped_attn_backward_workspace_size(int32_t B, int32_t H, int32_t Hk, int32_t D, int32_t max_q,
@@ -1715,21 +1529,18 @@ extern "C" int dora_grouped_attn(const dora_rows* q, const dora_rows* k, const d
   if (rc == DORA_OK) rc = check_rows(out, 16);
   if (rc != DORA_OK) return rc;
   if (!same_sizes(out, q)) return DORA_ERR_SHAPE;
-  const size_t need = dora_grouped_attn_workspace_size(B, z.H, z.Hk, z.D, max_q, z.total_q, z.total_k);
-  if (too_small(workspace, workspace_bytes, need)) return DORA_ERR_WORKSPACE;
+  if (too_small(workspace, workspace_bytes, forward_bytes(z))) return DORA_ERR_WORKSPACE;
   const size_t cu_bytes = (static_cast<size_t>(B) + 1) * sizeof(int32_t);
   if (rows_clash({out}, {q, k, v}, {},
                  {{lse_out, static_cast<size_t>(z.total_q) * z.H * sizeof(float)},
-                  {workspace, need},
+                  {workspace, forward_bytes(z)},
                   {dev_status, sizeof(int32_t)}},
                  {{cu_q, cu_bytes}, {cu_k, cu_bytes}}))
     return DORA_ERR_OVERLAP;
   if (z.total_q == 0) return DORA_OK;
-  // 32-bit offsets to 32 rows on
-  const bool lean = near(a.k, 128, 0) && near(a.v, 128, 0);
-  Split p = forward_split(z, q->dtype == DORA_BF16 && lean);
+  const Split p = forward_split(z);
   const bool split = p.splits > 1 || p.chunk;
-  const bool wide = !split && !p.few && use_wide(z, q->dtype, a);
+  const bool wide = !split && use_wide(z, q->dtype, a, false);
   const int64_t blocks = (wide ? tiles(z.total_q * a.G, B, kWide) : p.blocks) * z.Hk, join = (z.total_q * z.H + kThreads / 64 - 1) / (kThreads / 64);
   if (blocks > kMaxBlocks || (split && join > kMaxBlocks)) return DORA_ERR_UNSUPPORTED;
   a.out = row_view(out);
@@ -1739,23 +1550,13 @@ extern "C" int dora_grouped_attn(const dora_rows* q, const dora_rows* k, const d
   a.part_ml = reinterpret_cast<float2*>(a.part + p.blocks * z.Hk * p.part_rows * z.D);
   a.splits = p.splits, a.chunk = p.chunk, a.part_rows = p.part_rows;
   a.blocks = static_cast<int32_t>(blocks);
+  a.mixed = !split && mix_tiles(z.total_q * a.G, B, wide ? kWide : kTile);
   hipStream_t st = static_cast<hipStream_t>(stream);
   with_type(q->dtype, z.D, [&](auto e, auto d) {
     typedef decltype(e) E;
     constexpr int D = decltype(d)::value;
-    if constexpr (sizeof(E) == 2 && D >= 64) {
-      if (p.few && !split) {
-        hipLaunchKernelGGL((attn_few_kernel<D, false>), dim3(a.blocks + 1), dim3(kFewThreads), 0, st, a);
-        return;
-      }
-    }
     if (split) {
-      bool launched = false;
-      if constexpr (sizeof(E) == 2 && D >= 64) {
-        launched = p.few;
-        if (launched) hipLaunchKernelGGL((attn_few_kernel<D, true>), dim3(a.blocks + 1), dim3(kFewThreads), 0, st, a);
-      }
-      if (!launched) hipLaunchKernelGGL((attn_kernel<E, D, true>), dim3(a.blocks + 1), dim3(kThreads), 0, st, a);
+      hipLaunchKernelGGL((attn_kernel<E, D, true>), dim3(a.blocks + 1), dim3(kThreads), 0, st, a);
       hipLaunchKernelGGL((join_kernel<E, D>), dim3(static_cast<uint32_t>(join)), dim3(kThreads), 0, st, a);
     } else if constexpr (sizeof(E) == 2 && D >= 64) {
       if (wide) hipLaunchKernelGGL((attn_wide_kernel<D>), dim3(a.blocks + 1), dim3(kThreads), 0, st, a);
@@ -1790,7 +1591,7 @@ extern "C" int dora_grouped_attn_backward(const dora_rows* dout, const dora_rows
                  {{cu_q, cu_bytes}, {cu_k, cu_bytes}, {lse, static_cast<size_t>(z.total_q) * z.H * sizeof(float)}}))
     return DORA_ERR_OVERLAP;
   a.dout = row_view(dout);
-  const bool wide_q = use_wide(z, q->dtype, a), wide_kv = use_wide_kv(z, q->dtype, a);
+  const bool wide_q = use_wide(z, q->dtype, a, true), wide_kv = use_wide_kv(z, q->dtype, a);
   const int64_t q_blocks = tiles(z.total_q * a.G, B, wide_q ? kWide : kTile) * z.Hk;
   const int32_t splits = backward_splits(z);
   const int64_t kv_blocks = tiles(z.total_k, B, wide_kv ? kWide : kTile) * z.Hk * splits * (wide_kv && z.D == 128 ? 2 : 1);
@@ -1804,6 +1605,10 @@ extern "C" int dora_grouped_attn_backward(const dora_rows* dout, const dora_rows
   a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + stat_bytes(z));
   a.splits = splits;
   a.blocks = static_cast<int32_t>(q_blocks);
+  a.mixed = mix_tiles(z.total_q * a.G, B, wide_q ? kWide : kTile);
+  AttnArgs kv = a;
+  kv.blocks = static_cast<int32_t>(tiles(z.total_k, B, wide_kv ? kWide : kTile) * z.Hk * splits);
+  kv.mixed = splits == 1 && mix_tiles(z.total_k, B, wide_kv ? kWide : kTile);
   hipStream_t st = static_cast<hipStream_t>(stream);
   with_type(q->dtype, z.D, [&](auto e, auto d) {
     typedef decltype(e) E;
@@ -1815,15 +1620,15 @@ extern "C" int dora_grouped_attn_backward(const dora_rows* dout, const dora_rows
       if (wide_kv && !launched_kv) {
         if (!wide_q) hipLaunchKernelGGL((grad_q_kernel<E, D>), gq, block, 0, st, a);
         launched_q = launched_kv = true;
-        if (splits > 1) hipLaunchKernelGGL((grad_kv_wide_kernel<D, true>), gkv, block, 0, st, a);
-        else hipLaunchKernelGGL((grad_kv_wide_kernel<D, false>), gkv, block, 0, st, a);
+        if (splits > 1) hipLaunchKernelGGL((grad_kv_wide_kernel<D, true>), gkv, block, 0, st, kv);
+        else hipLaunchKernelGGL((grad_kv_wide_kernel<D, false>), gkv, block, 0, st, kv);
       }
       launched_q = launched_q || wide_q;
     }
     if (!launched_q) hipLaunchKernelGGL((grad_q_kernel<E, D>), gq, block, 0, st, a);
     if (!launched_kv) {
-      if (splits > 1) hipLaunchKernelGGL((grad_kv_kernel<E, D, true>), gkv, block, 0, st, a);
-      else hipLaunchKernelGGL((grad_kv_kernel<E, D, false>), gkv, block, 0, st, a);
+      if (splits > 1) hipLaunchKernelGGL((grad_kv_kernel<E, D, true>), gkv, block, 0, st, kv);
+      else hipLaunchKernelGGL((grad_kv_kernel<E, D, false>), gkv, block, 0, st, kv);
     }
     if (splits > 1 && z.total_k > 0)
       hipLaunchKernelGGL((join_kv_kernel<E, D>), dim3(static_cast<uint32_t>(join)), block, 0, st, a);

@@ -329,7 +329,7 @@ __global__ __launch_bounds__(threads_of<L>()) void residual_norm_grad_kernel(Nor
     const R sc = scale.row(lane, pieces);
     float s[1] = {0.f};
     u.each([&](float& v, int j, int i) {
-      const float d = g.p[j].v[i], gated = d * gate;
+      const float d = g.p[j].v[i], gated = gate != 0.f ? d * gate : 0.f;
       s[0] = __builtin_fmaf(d, v * sc.p[j].v[i], s[0]);
       if (gate != 0.f) {
         if constexpr (kLdsSums) slot(2, j, i) = __builtin_fmaf(gated, v, slot(2, j, i));
