@@ -729,6 +729,8 @@ int dora_rope(const dora_rows* q, const dora_rows* k, const int32_t* positions, 
  *              pointers are allowed.  1 <= B <= DORA_MAX_SEQUENCES.
  *   max_q      no sequence has more queries; total_k and total_q H / Hk at most
  *              2^31 - 65536.
+ *   max_k      0, or no sequence has more keys: few queries against short lists
+ *              of keys then take one launch.
  *   softmax_scale  <= 0 selects 1/sqrt(D).
  *   dtype      bf16: fp32 products and softmax, P rounded to bf16 for its
  *              product; fp32: fp32 throughout.  Output rounded once.
@@ -740,7 +742,7 @@ int dora_rope(const dora_rows* q, const dora_rows* k, const int32_t* positions, 
  *              joined in a fixed order.  Calls that share it must not overlap
  *              in time.
  *   dev_status DORA_DEV_CU_SEQLENS for invalid offsets or a sequence of more
- *              than max_q queries; such sequences are skipped.
+ *              than max_q queries or max_k keys; such sequences are skipped.
  * Outputs, workspace and dev_status share no memory with each other or with an
  * input (DORA_ERR_OVERLAP).  Results do not depend on timing.
  *
@@ -766,7 +768,7 @@ size_t dora_grouped_attn_workspace_size(int32_t B, int32_t H, int32_t Hk, int32_
 size_t dora_grouped_attn_backward_workspace_size(int32_t B, int32_t H, int32_t Hk, int32_t D, int32_t max_q,
                                                  int64_t total_q, int64_t total_k);
 int dora_grouped_attn(const dora_rows* q, const dora_rows* k, const dora_rows* v, const int32_t* cu_q,
-                      const int32_t* cu_k, int32_t B, int32_t max_q, int32_t causal, float softmax_scale,
+                      const int32_t* cu_k, int32_t B, int32_t max_q, int32_t max_k, int32_t causal, float softmax_scale,
                       const dora_rows* out, float* lse_out, void* workspace, size_t workspace_bytes,
                       int32_t* dev_status, void* stream);
 int dora_grouped_attn_backward(const dora_rows* dout, const dora_rows* q, const dora_rows* k, const dora_rows* v,

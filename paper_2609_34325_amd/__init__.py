@@ -137,7 +137,7 @@ _ENTRIES = (
     ("dora_grad_clip", (None,) * 5 + (("norm_out", _F32), ("workspace", _ANY), None, None)),
     # Rows go by the address of their description (strided views are allowed).
     ("dora_rope", (None, None, ("positions", _I32), None, ("freq", torch.float64)) + (None,) * 7),
-    ("dora_grouped_attn", (None,) * 3 + (("cu_q", _I32), ("cu_k", _I32)) + (None,) * 5 +
+    ("dora_grouped_attn", (None,) * 3 + (("cu_q", _I32), ("cu_k", _I32)) + (None,) * 6 +
      (("lse_out", _F32), ("workspace", _ANY), None) + _STATUS),
     ("dora_grouped_attn_backward", (None,) * 5 + (("lse", _F32), ("cu_q", _I32), ("cu_k", _I32)) + (None,) * 7 +
      (("workspace", _ANY), None) + _STATUS),
@@ -262,7 +262,7 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
         getattr(lib, name).restype = sz
         getattr(lib, name).argtypes = [i32, i32, i32, i32, i32, i64, i64]
     lib.dora_grouped_attn.restype = ctypes.c_int
-    lib.dora_grouped_attn.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, f32, vp, vp, vp, sz, vp, vp]
+    lib.dora_grouped_attn.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, i32, f32, vp, vp, vp, sz, vp, vp]
     lib.dora_grouped_attn_backward.restype = ctypes.c_int
     lib.dora_grouped_attn_backward.argtypes = [vp] * 8 + [i32, i32, i32, f32, vp, vp, vp, vp, sz, vp, vp]
     lib.dora_residual_norm.restype = ctypes.c_int
@@ -1081,18 +1081,20 @@ def _sequences(cu_q, cu_k):
 def dora_grouped_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.Tensor, max_q: int,
                       cu_k: Optional[torch.Tensor] = None, causal: bool = False, softmax_scale: float = 0.0,
                       out: Optional[torch.Tensor] = None, lse_out: Optional[torch.Tensor] = None, keep_lse: bool = True,
-                      workspace: Optional[torch.Tensor] = None, dev_status: Optional[torch.Tensor] = None, stream=None):
+                      workspace: Optional[torch.Tensor] = None, dev_status: Optional[torch.Tensor] = None, stream=None,
+                      max_k: int = 0):
     """softmax(scale q k^T) v inside packed sequences with grouped heads.
 
     q: [total_q, H, D]; k, v: [total_k, Hk, D], H a multiple of Hk, D 32, 64 or
     128, bf16 or fp32, any strides of 16 bytes; cu_q, cu_k (cu_q when None):
     int32 [B + 1]; max_q: no sequence has more queries.  causal: query i of nq
-    sees the keys j <= i + nk - nq, so one new token sees all.  Returns (out
+    sees the keys j <= i + nk - nq, so one new token sees all.  max_k: no
+    sequence has more keys (0: not known); short lists then take one launch.  Returns (out
     [total_q, H, D], lse [total_q, H] fp32 or None without keep_lse, dev_status)."""
     if stream is not None:
         with _in_stream(stream):
             return dora_grouped_attn(q, k, v, cu_q, max_q, cu_k, causal, softmax_scale, out, lse_out, keep_lse,
-                                     workspace, dev_status)
+                                     workspace, dev_status, max_k=max_k)
     _heads(("q", "k", "v"), q, k, v)
     B, cu_k = _sequences(cu_q, cu_k)
     dev = q.device
@@ -1108,8 +1110,8 @@ def dora_grouped_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: t
     rows, at, device = _describe(("q", "k", "v", "out"), q, k, v, out)
     _vectors(("cu_q", "cu_k", "lse_out", "workspace", "dev_status"), device, B + 1, cu_q, B + 1, cu_k, -1, lse_out,
              -1, workspace, -1, dev_status)
-    _call("dora_grouped_attn", None, at[0], at[1], at[2], cu_q, cu_k, B, int(max_q), int(bool(causal)),
-          float(softmax_scale), at[3], lse_out, workspace, _bytes(workspace), dev_status)
+    _call("dora_grouped_attn", None, at[0], at[1], at[2], cu_q, cu_k, B, int(max_q), int(max_k),
+          int(bool(causal)), float(softmax_scale), at[3], lse_out, workspace, _bytes(workspace), dev_status)
     _written(out) if lse_out is None else _written(out, lse_out)
     return out, lse_out, dev_status
 

@@ -44,7 +44,7 @@ struct AttnArgs {
   int32_t B, H, Hk, G;
   uint32_t g_mul, g_shift;  // r / G = mulhi(r, g_mul) >> g_shift for r < 2^31, G > 1
   int64_t total_q, total_k;
-  int32_t max_q, causal;
+  int32_t max_q, max_k, causal;
   float scale, c2;  // softmax_scale, softmax_scale * log2(e)
   float* lse;
   float2* stat;  // of a row: log2 of its sum of exponentials, delta
@@ -97,10 +97,15 @@ struct Seq {
   int q0, nq, k0, nk;
 };
 
+__device__ __forceinline__ bool good_boundaries(const AttnArgs& a, int q0, int q1, int k0, int k1) {
+  return q0 >= 0 && q1 >= q0 && q1 <= a.total_q && k0 >= 0 && k1 >= k0 && k1 <= a.total_k && q1 - q0 <= a.max_q &&
+         k1 - k0 <= a.max_k;
+}
+
 // Sequence b; nothing of it where its boundaries are no good.
 __device__ __forceinline__ bool sequence(const AttnArgs& a, int b, Seq* s) {
   const int q0 = a.cu_q[b], q1 = a.cu_q[b + 1], k0 = a.cu_k[b], k1 = a.cu_k[b + 1];
-  if (q0 < 0 || q1 < q0 || q1 > a.total_q || k0 < 0 || k1 < k0 || k1 > a.total_k || q1 - q0 > a.max_q) return false;
+  if (!good_boundaries(a, q0, q1, k0, k1)) return false;
   *s = Seq{q0, q1 - q0, k0, k1 - k0};
   return true;
 }
@@ -122,7 +127,7 @@ __device__ __forceinline__ bool locate(const AttnArgs& a, int64_t t, F first, in
   *found = b;
   const int q0 = __builtin_amdgcn_readlane(q, b), q1 = __builtin_amdgcn_readlane(q, b + 1);
   const int k0 = __builtin_amdgcn_readlane(k, b), k1 = __builtin_amdgcn_readlane(k, b + 1);
-  if (q0 < 0 || q1 < q0 || q1 > a.total_q || k0 < 0 || k1 < k0 || k1 > a.total_k || q1 - q0 > a.max_q) return false;
+  if (!good_boundaries(a, q0, q1, k0, k1)) return false;
   *s = Seq{q0, q1 - q0, k0, k1 - k0};
   return true;
 }
@@ -1399,14 +1404,19 @@ struct Split {
   int32_t splits, chunk, part_rows;
   int64_t blocks;  // without heads
 };
-Split forward_split(const Sizes& z) {
+// max_k: the longest sequence's keys; 0: not known; -1: as if it were long (for the workspace, which serves any).
+Split forward_split(const Sizes& z, int32_t max_k) {
   const int32_t G = z.H / z.Hk;
   const int64_t rows = static_cast<int64_t>(std::min<int64_t>(z.max_q, z.total_q)) * G;
   if (rows <= kTile && z.total_k > 0) {
-    // every sequence is one tile: parts of the same number of keys
-    const int64_t want = z.total_k * z.Hk / (4 * kFill);
-    const int64_t chunk = std::min<int64_t>(4096, std::max<int64_t>(256, (want + 63) / 64 * 64));
-    if (z.total_k / z.B > chunk) return Split{1, static_cast<int32_t>(chunk), static_cast<int32_t>(rows), tiles(z.total_k, z.B, chunk)};
+    // Every sequence is one tile: parts of the same number of keys, as many as fill the GPU once, 128 keys or more and at
+    // most 32 a sequence, by the average.  A part's 64 keys take 1.3 us one after another, the parts' join 4 to 5: whole
+    // sequences where the longest is short, 64 of 400 keys and 8 key heads of 128 25 us whole and 35 split, one of 512 12.5
+    // in two parts and 10 in four.  Where the longest is not known, an average can hide one that would be slow whole.
+    const int64_t keys = z.total_k / z.B, want = std::max(z.total_k * z.Hk / kFill, keys / 32);
+    const int64_t chunk = std::min<int64_t>(4096, std::max<int64_t>(128, (want + 63) / 64 * 64));
+    const bool whole = max_k > 0 ? max_k <= std::max<int64_t>(chunk, 256) : max_k == 0 && (keys <= 128 || z.total_k <= 512);
+    if (!whole) return Split{1, static_cast<int32_t>(chunk), static_cast<int32_t>(rows), tiles(z.total_k, z.B, chunk)};
   }
   const int64_t n = tiles(z.total_q * G, z.B, kTile), keys = z.total_k / z.B;
   int32_t splits = 1;
@@ -1439,7 +1449,7 @@ bool use_wide_kv(const Sizes& z, int dtype, const AttnArgs& a) {
 size_t round256(size_t n) { return (n + 255) & ~size_t(255); }
 
 size_t forward_bytes(const Sizes& z) {
-  const Split p = forward_split(z);
+  const Split p = forward_split(z, -1);
   if (p.splits == 1 && !p.chunk) return 256;
   return round256(static_cast<size_t>(p.blocks) * z.Hk * p.part_rows * (z.D + 2) * sizeof(float));
 }
@@ -1477,7 +1487,7 @@ int check_attn(const dora_rows* q, const dora_rows* k, const dora_rows* v, const
   a->g_mul = bits ? static_cast<uint32_t>(((uint64_t{1} << (31 + bits)) + a->G - 1) / a->G) : 0;
   a->g_shift = bits ? bits - 1 : 0;
   a->total_q = z->total_q, a->total_k = z->total_k;
-  a->max_q = max_q, a->causal = causal != 0;
+  a->max_q = max_q, a->max_k = 0x7FFFFFFF, a->causal = causal != 0;
   a->scale = softmax_scale > 0.f ? softmax_scale : static_cast<float>(1.0 / std::sqrt(static_cast<double>(z->D)));
   a->c2 = a->scale * kLog2e;
   a->status = dev_status;
@@ -1518,8 +1528,8 @@ extern "C" size_t dora_grouped_attn_backward_workspace_size(int32_t B, int32_t H
 }
 
 extern "C" int dora_grouped_attn(const dora_rows* q, const dora_rows* k, const dora_rows* v, const int32_t* cu_q,
-                                 const int32_t* cu_k, int32_t B, int32_t max_q, int32_t causal, float softmax_scale,
-                                 const dora_rows* out, float* lse_out, void* workspace, size_t workspace_bytes,
+                                 const int32_t* cu_k, int32_t B, int32_t max_q, int32_t max_k, int32_t causal,
+                                 float softmax_scale, const dora_rows* out, float* lse_out, void* workspace, size_t workspace_bytes,
                                  int32_t* dev_status, void* stream) {
   using namespace dora;
   if (!out) return DORA_ERR_NULL;
@@ -1528,7 +1538,8 @@ extern "C" int dora_grouped_attn(const dora_rows* q, const dora_rows* k, const d
   int rc = check_attn(q, k, v, cu_q, cu_k, B, max_q, causal, softmax_scale, dev_status, &z, &a);
   if (rc == DORA_OK) rc = check_rows(out, 16);
   if (rc != DORA_OK) return rc;
-  if (!same_sizes(out, q)) return DORA_ERR_SHAPE;
+  if (!same_sizes(out, q) || max_k < 0) return DORA_ERR_SHAPE;
+  if (max_k > 0) a.max_k = max_k;
   if (too_small(workspace, workspace_bytes, forward_bytes(z))) return DORA_ERR_WORKSPACE;
   const size_t cu_bytes = (static_cast<size_t>(B) + 1) * sizeof(int32_t);
   if (rows_clash({out}, {q, k, v}, {},
@@ -1538,7 +1549,7 @@ extern "C" int dora_grouped_attn(const dora_rows* q, const dora_rows* k, const d
                  {{cu_q, cu_bytes}, {cu_k, cu_bytes}}))
     return DORA_ERR_OVERLAP;
   if (z.total_q == 0) return DORA_OK;
-  const Split p = forward_split(z);
+  const Split p = forward_split(z, max_k);
   const bool split = p.splits > 1 || p.chunk;
   const bool wide = !split && use_wide(z, q->dtype, a, false);
   const int64_t blocks = (wide ? tiles(z.total_q * a.G, B, kWide) : p.blocks) * z.Hk, join = (z.total_q * z.H + kThreads / 64 - 1) / (kThreads / 64);

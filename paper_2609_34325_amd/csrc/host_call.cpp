@@ -148,11 +148,11 @@ const Entry kEntries[] = {
        return at_address(dora_rope, fn)(rows_of(a[0]), rows_of(a[1]), ptr<int32_t>(a[2]), i32(a[3]), ptr<double>(a[4]),
                          i32(a[5]), i32(a[6]), i32(a[7]), a[8].f, rows_of(a[9]), rows_of(a[10]), a[11].p);
      }},
-    {"sssIInnnesfAnIs",
+    {"sssIInnnnesfAnIs",
      [](void* fn, const Arg* a) {
        return at_address(dora_grouped_attn, fn)(rows_of(a[0]), rows_of(a[1]), rows_of(a[2]), ptr<int32_t>(a[3]),
-                                ptr<int32_t>(a[4]), i32(a[5]), i32(a[6]), i32(a[7]), a[8].f, rows_of(a[9]),
-                                ptr<float>(a[10]), a[11].p, static_cast<size_t>(a[12].n), ptr<int32_t>(a[13]), a[14].p);
+                                ptr<int32_t>(a[4]), i32(a[5]), i32(a[6]), i32(a[7]), i32(a[8]), a[9].f, rows_of(a[10]),
+                                ptr<float>(a[11]), a[12].p, static_cast<size_t>(a[13].n), ptr<int32_t>(a[14]), a[15].p);
      }},
     {"sssssFIInnnesssAnIs",
      [](void* fn, const Arg* a) {

@@ -69,8 +69,8 @@ def attn_names(dtype=dora.DORA_BF16, n=6, m=9, H=4, Hk=2, D=64):
                  ws=A + 7 * big, st=A + 8 * big, dout=r(9, n, H), dq=r(10, n, H), dk=r(11, m, Hk), dv=r(12, m, Hk))
 
 
-def attn(a, B=2, max_q=5, causal=1, scale=0.0, ws_bytes=1 << 27):
-    return dora.load_library().dora_grouped_attn(a.ref("q"), a.ref("k"), a.ref("v"), a["cq"], a["ck"], B, max_q, causal,
+def attn(a, B=2, max_q=5, causal=1, scale=0.0, ws_bytes=1 << 27, max_k=0):
+    return dora.load_library().dora_grouped_attn(a.ref("q"), a.ref("k"), a.ref("v"), a["cq"], a["ck"], B, max_q, max_k, causal,
                                                  scale, a.ref("out"), a["lse"], a["ws"], ws_bytes, a["st"], None)
 
 
@@ -98,6 +98,8 @@ def test_attention_refusals(call):
                dict(k=rows(A + big, n=9, heads=3), v=rows(A + 2 * big, n=9, heads=3)), dict(v=rows(A + 2 * big, n=8, heads=2)),
                dict(q=rows(A, dim=32)), dict(out=rows(A + 5 * big, n=5)), dict(out=rows(A + 5 * big, heads=2))):
         bad(dora.DORA_ERR_SHAPE, **kw)
+    if call is attn:
+        bad(dora.DORA_ERR_SHAPE, max_k=-1)
     for D in (16, 96, 256):
         a = attn_names(D=D)
         assert call(a) == dora.DORA_ERR_SHAPE

@@ -99,10 +99,11 @@ def test_split_keys(gpu, dtype, nq, H, Hk, D):
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("nq,H,Hk,D", [(1, 8, 1, 128), (1, 3, 3, 64), (4, 8, 2, 128), (2, 5, 1, 64), (1, 16, 1, 64)])
 def test_few_rows(gpu, dtype, nq, H, Hk, D):
-    """At most 16 rows a key head: whole and split, lengths on both sides of a wave's 32 keys, a round's 256 and a part's,
-    queries that see none of a part, values that the last query alone sees."""
+    """Few rows a key head: whole and split, lengths on both sides of a part's, the longest known and not, queries that see
+    none of a part, values that the last query alone sees."""
     for causal in (False, True):
-        for nk in ([1, 2, 31, 32, 33, 255, 256, 257, 0, 511, 513, 3], [9000, 300, 0, 2500, 1, 4097], [8000, 1, 193]):
+        for nk in ([1, 2, 31, 32, 33, 255, 256, 257, 0, 511, 513, 3], [9000, 300, 0, 2500, 1, 4097], [8000, 1, 193],
+                   [100, 256, 200, 0]):
             t, cu_q, cu_k = make([nq] * len(nk), nk, H, Hk, D, dtype, nk[0] + nq)
             d = cuda(t)
             args = (d["q"], d["k"], d["v"], dev_cu(cu_q), nq)
@@ -111,6 +112,10 @@ def test_few_rows(gpu, dtype, nq, H, Hk, D):
             assert int(st) == 0
             ref.check(out, want["out"], bound["out"], f"{nk} out")
             ref.check(lse, want["lse"], bound["lse"], f"{nk} lse")
+            whole, lse2, st = gpu.dora_grouped_attn(*args, cu_k=dev_cu(cu_k), causal=causal, max_k=max(nk))
+            assert int(st) == 0
+            ref.check(whole, want["out"], bound["out"], f"{nk} out, longest known")
+            ref.check(lse2, want["lse"], bound["lse"], f"{nk} lse, longest known")
             if causal and nq > 1:
                 ends = torch.tensor([b - 1 for a, b in zip(cu_k, cu_k[1:]) if b - a > 1])
                 d["v"][ends, :, 2] = float("inf")
@@ -309,6 +314,10 @@ def test_bad_boundaries(gpu):
         assert int(st) == gpu.DORA_DEV_CU_SEQLENS, bad
     out = torch.full_like(good, 5.0)
     _, _, st = gpu.dora_grouped_attn(d["q"], d["k"], d["v"], dev_cu(cu), 35, out=out)     # the first is too long
+    assert int(st) == gpu.DORA_DEV_CU_SEQLENS
+    assert torch.equal(out[40:], good[40:]) and bool((out[:40] == 5.0).all())
+    out = torch.full_like(good, 5.0)
+    _, _, st = gpu.dora_grouped_attn(d["q"], d["k"], d["v"], dev_cu(cu), 40, max_k=35, out=out)
     assert int(st) == gpu.DORA_DEV_CU_SEQLENS
     assert torch.equal(out[40:], good[40:]) and bool((out[:40] == 5.0).all())
     _, _, st = gpu.dora_grouped_attn(d["q"][:3], d["k"], d["v"], dev_cu([0, 1, 2, 3]), 1, cu_k=dev_cu([0, 95, 70, 90]))
