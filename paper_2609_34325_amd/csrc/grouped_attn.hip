@@ -26,6 +26,7 @@
 #include <algorithm>
 
 #include "dora_internal.h"
+#include "grouped_attn_split.h"
 #include "lanes.h"
 #include "rows.h"
 
@@ -33,7 +34,6 @@ namespace dora {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kTile = 64;  // rows (keys in grad_kv) of a workgroup, 16 a wave
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -1380,57 +1380,6 @@ __global__ __launch_bounds__(kThreads) void join_kv_kernel(AttnArgs a) {
 
 // --------------------------------- host -----------------------------------
 
-struct Sizes {
-  int32_t B, H, Hk, D, max_q;
-  int64_t total_q, total_k;
-};
-
-constexpr int64_t kMaxRows = 0x7FFF0000;  // a tile's steps past the last row stay in 32 bits
-bool good_sizes(const Sizes& z) {
-  return z.B >= 1 && z.B <= DORA_MAX_SEQUENCES && z.H >= 1 && z.H <= 256 && z.Hk >= 1 && z.H % z.Hk == 0 &&
-         (z.D == 32 || z.D == 64 || z.D == 128) && z.max_q >= 0 && z.total_q >= 0 && z.total_k >= 0 &&
-         z.total_k <= kMaxRows && z.total_q <= kMaxRows && z.total_q * (z.H / z.Hk) <= kMaxRows;
-}
-
-int64_t tiles(int64_t total, int32_t B, int64_t tile) { return total / tile + B; }
-// Sequences of about one to four tiles: the numbers that hold none are many (tile_number).
-int32_t mix_tiles(int64_t total, int32_t B, int64_t tile) { return total / tile >= B / 2 && total / tile < int64_t{4} * B; }
-
-// Workgroups of 64 rows that the GPU holds at a time, about.
-constexpr int kFill = 512;
-
-// How the forward pass splits its keys.
-struct Split {
-  int32_t splits, chunk, part_rows;
-  int64_t blocks;  // without heads
-};
-// max_k: the longest sequence's keys; 0: not known; -1: as if it were long (for the workspace, which serves any).
-Split forward_split(const Sizes& z, int32_t max_k) {
-  const int32_t G = z.H / z.Hk;
-  const int64_t rows = static_cast<int64_t>(std::min<int64_t>(z.max_q, z.total_q)) * G;
-  if (rows <= kTile && z.total_k > 0) {
-    // Every sequence is one tile: parts of the same number of keys, as many as fill the GPU once, 128 keys or more and at
-    // most 32 a sequence, by the average.  A part's 64 keys take 1.3 us one after another, the parts' join 4 to 5: whole
-    // sequences where the longest is short, 64 of 400 keys and 8 key heads of 128 25 us whole and 35 split, one of 512 12.5
-    // in two parts and 10 in four.  Where the longest is not known, an average can hide one that would be slow whole.
-    const int64_t keys = z.total_k / z.B, want = std::max(z.total_k * z.Hk / kFill, keys / 32);
-    const int64_t chunk = std::min<int64_t>(4096, std::max<int64_t>(128, (want + 63) / 64 * 64));
-    const bool whole = max_k > 0 ? max_k <= std::max<int64_t>(chunk, 256) : max_k == 0 && (keys <= 128 || z.total_k <= 512);
-    if (!whole) return Split{1, static_cast<int32_t>(chunk), static_cast<int32_t>(rows), tiles(z.total_k, z.B, chunk)};
-  }
-  const int64_t n = tiles(z.total_q * G, z.B, kTile), keys = z.total_k / z.B;
-  int32_t splits = 1;
-  while (splits < 16 && n * z.Hk * splits < kFill && keys / (splits * 2) >= 512) splits *= 2;
-  return Split{splits, 0, kTile, n * splits};
-}
-
-int32_t backward_splits(const Sizes& z) {
-  const int64_t n = tiles(z.total_k, z.B, kTile) * z.Hk, rows = z.total_q / z.B * (z.H / z.Hk);
-  int32_t splits = 1;
-  while (splits < 16 && n * splits < kFill && rows / (splits * 2) >= 512) splits *= 2;
-  return splits;
-}
-
 // The kernels of 128 rows or keys: where the bytes from a staged tile's first row to its last fit the 32-bit offsets, and
 // from this many rows (keys) a sequence on, by the average.  Both sides in us, 8 heads, as many sequences as fill the GPU:
 //   forward   64 rows of 64 50.6 narrow, 52.5 wide; 65 rows 74, 61; 64 rows of 128 80.7, 83.2; 65 rows 133, 102
@@ -1444,20 +1393,6 @@ bool use_wide(const Sizes& z, int dtype, const AttnArgs& a, bool grad) {
 bool use_wide_kv(const Sizes& z, int dtype, const AttnArgs& a) {
   return dtype == DORA_BF16 && z.D >= 64 && 32 % a.G == 0 && near(a.q, 64, a.G) && near(a.dout, 64, a.G) &&
          z.total_k / z.B > (z.D == 64 ? kWideGradRows64 : kWideRows);
-}
-
-size_t round256(size_t n) { return (n + 255) & ~size_t(255); }
-
-size_t forward_bytes(const Sizes& z) {
-  const Split p = forward_split(z, -1);
-  if (p.splits == 1 && !p.chunk) return 256;
-  return round256(static_cast<size_t>(p.blocks) * z.Hk * p.part_rows * (z.D + 2) * sizeof(float));
-}
-size_t stat_bytes(const Sizes& z) { return round256(static_cast<size_t>(z.total_q) * z.H * sizeof(float2)); }
-size_t backward_bytes(const Sizes& z) {
-  const int32_t splits = backward_splits(z);
-  return stat_bytes(z) + 256 +
-         (splits == 1 ? 0 : round256(static_cast<size_t>(splits) * z.Hk * z.total_k * 2 * z.D * sizeof(float)));
 }
 
 bool same_sizes(const dora_rows* s, const dora_rows* t) {

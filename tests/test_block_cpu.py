@@ -217,10 +217,18 @@ def test_norm_overlaps():
 
 
 PROBE = """
+#include "grouped_attn_split.h"
 #include "rows.h"
 extern "C" int pair(const dora_rows* s, const dora_rows* t) { return dora::rows_meet(s, t); }
 extern "C" int vector(const dora_rows* s, void* p, size_t n) { return dora::rows_meet(s, dora::Extent(p, n)); }
 extern "C" int itself(const dora_rows* s) { return dora::meets_itself(s); }
+// Bytes that a forward call's parts take beyond those of the workspace that any call of its sizes has to bring.
+extern "C" long beyond(int B, int H, int Hk, int D, int max_q, long total_q, long total_k, int max_k) {
+  const dora::Sizes z{B, H, Hk, D, max_q, total_q, total_k};
+  const dora::Split p = dora::forward_split(z, max_k);
+  if (p.splits == 1 && !p.chunk) return 0;
+  return p.blocks * Hk * p.part_rows * (D + 2) * 4L - static_cast<long>(dora::forward_bytes(z));
+}
 """
 
 
@@ -304,6 +312,24 @@ def test_outputs_over_themselves(probe):
         a = places(s)
         if len(set(a)) < len(a):
             assert probe.itself(ctypes.byref(s)), (s.rows, s.heads, s.dim, s.row_stride, s.head_stride)
+
+
+def test_parts_fit_the_workspace(probe):
+    """Whatever a call says of its longest sequence (right or not), its parts lie in the workspace of its sizes."""
+    probe.beyond.argtypes = [ctypes.c_int] * 5 + [ctypes.c_long] * 2 + [ctypes.c_int]
+    probe.beyond.restype = ctypes.c_long
+    # sequences that stay whole and have keys enough for tiles' parts: about 500 of them and a little over 1024 keys
+    # each, then a longest sequence said to be shorter than the average
+    assert probe.beyond(250, 2, 2, 64, 1, 250, 250 * 1050, 1050) <= 0
+    assert probe.beyond(4, 8, 8, 64, 1, 4, 4 * 100000, 128) <= 0
+    rng = random.Random(10)
+    log = lambda lo, hi: int(lo * (hi / lo) ** rng.random())  # noqa: E731
+    for _ in range(200000):
+        Hk, D = log(1, 32), rng.choice((32, 64, 128))
+        B, H, keys, max_q = log(1, 2000), Hk * rng.choice((1, 2, 4, 5, 8)), log(1, 20000), log(1, 300)
+        total_q, total_k = B * min(max_q, log(1, 300)), min(B * keys + rng.randint(0, B), 0x7FFF0000)
+        max_k = rng.choice((0, keys + 1, keys * 2, log(1, 5000)))
+        assert probe.beyond(B, H, Hk, D, max_q, total_q, total_k, max_k) <= 0, (B, H, Hk, D, max_q, total_q, total_k, max_k)
 
 
 def test_binding_refusals():
