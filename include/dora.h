@@ -739,8 +739,8 @@ int dora_rope(const dora_rows* q, const dora_rows* k, const int32_t* positions, 
  *   workspace  device, 256-byte aligned, dora_grouped_attn_workspace_size
  *              bytes, no required contents: where there are few queries against
  *              the GPU, the keys are split over workgroups and their parts
- *              joined in a fixed order.  Calls that share it must not overlap
- *              in time.
+ *              joined in a fixed order.  Smaller sizes can need more of it than
+ *              larger ones.  Calls that share it must not overlap in time.
  *   dev_status DORA_DEV_CU_SEQLENS for invalid offsets or a sequence of more
  *              than max_q queries or max_k keys; such sequences are skipped.
  * Outputs, workspace and dev_status share no memory with each other or with an

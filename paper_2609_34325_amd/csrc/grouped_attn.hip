@@ -14,8 +14,16 @@
 // P = 2^(s - lse log2 e), delta = rowsum(dout out):
 //   grad_q   a tile of rows over the keys:  dS = P (dout v^T - delta), dq += dS k
 //   grad_kv  a tile of keys over the rows:  dv += P^T dout, dk += dS^T q
-// Each forms P and dS for itself (seven products in place of five), so that no
-// sum goes through memory and results do not depend on timing.
+// Each forms P and dS for itself (seven products in place of five, eight for bf16
+// heads of 128), so that no sum goes through memory and results do not depend on
+// timing.  Eight packed sequences of up to 8192, 30497 rows, 32 query and 8 key
+// heads of 128, bf16, causal: forward 1.2 ms, grad_q 1.6, grad_kv 3.0; 660 to 700
+// TFLOP/s of seven products, 930 to 1000 of the ten that are formed, where a large
+// library product reaches 1254 on the same card.  Sums of dq by atomics would save
+// three of the ten, and depend on timing.
+//
+// Kernels of 64 rows (16 a wave) take every type and width; those of 128 rows (32
+// a wave) longer sequences of bf16 heads of 64 and 128.
 //
 // Tiles of sequences are found without a plan: tile t of all belongs to the last
 // b with floor(cu[b] G / tile) + b <= t.  That leaves each sequence at least its
@@ -53,6 +61,7 @@ struct AttnArgs {
   int32_t part_rows;  // rows of a part
   int32_t splits;     // parts of a tile's keys (forward) or of a tile's rows (grad_kv)
   int32_t chunk;      // or: keys of a part, every sequence one tile of rows
+  int32_t step;       // rows of whole queries in 64 (grad_kv_wide)
   int32_t blocks;
   int32_t mixed;
   int32_t* status;
@@ -304,6 +313,12 @@ __device__ __forceinline__ float over_groups_sum(float x) { return add32(add16(x
 // One tile of 64 rows against a range of its keys.  s^T = k q^T leaves each lane
 // one row's column, so its maximum and sum are mostly in the lane, and p goes
 // into out^T += v^T p^T from the registers where it stands.
+// One query a sequence is bound by the caches' bytes (32 of 1000 to 65000 keys, 8
+// key heads of 128, bf16: 839 us and 6 for the join, 5.6 TB/s of reads) or, few of
+// them, by the chain from boundaries to keys to products (four of 321 to 1205: 7.6
+// and 4.5).  fp32 by its matrix rate, 154 TFLOP/s (256 sequences of 60 to 197, four
+// heads of 32: 45 us, matrix units busy 43 %, a sixth of that in places past a
+// sequence).
 template <class E, int D, bool SPLIT>
 __global__ __launch_bounds__(kThreads) void attn_kernel(AttnArgs a) {
   typedef typename Op<E>::Frag Frag;
@@ -451,7 +466,13 @@ __global__ __launch_bounds__(kThreads) void attn_kernel(AttnArgs a) {
 // Products of 32 x 32 in steps of 16: lane l (c = l % 32, hi = l / 32) holds
 // elements 8 hi .. 8 hi + 7 of row or column c, the result's lane column c, rows
 // 8 (i / 4) + 4 hi + i % 4.  One operand read from LDS serves 32 columns in place
-// of 16, which halves the LDS reads, what bounds the 16-wide kernels.
+// of 16.  Two waves a SIMD at 128, three at 64, on the sequences
+// above: matrix units busy 45 % of the cycles forward, 56 % in grad_q, 45 % in
+// grad_kv, vector instructions a third to two fifths, LDS a fifth and no conflicts;
+// a wave waits for its own products, exponentials or operands the rest.  Heads of
+// 64 have the same exponentials for half the products: 64 sequences of 46 to 577,
+// 20337 rows, 12 heads, take 56 us forward, 69 in grad_q and 84 in grad_kv, with
+// matrix units busy 22 to 30 %.
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 typedef __attribute__((address_space(3))) void lds_void;
 
@@ -501,7 +522,7 @@ struct KeyStage : Stage<D> {
     S::run(to, tile, n, [&](int k) { return off + k * 32 * step; }, [&] { return (n - 1) * step + S::piece(); });
   }
 };
-// The rows of whole queries: row r is query r / G of head r % G (G divides 32).
+// The rows of whole queries: row r is query r / G of head r % G.
 template <int D>
 struct QueryStage : Stage<D> {
   typedef Stage<D> S;
@@ -829,7 +850,8 @@ __device__ __forceinline__ float row_lse2(const AttnArgs& a, const Seq& s, int h
   return lse == -INFINITY ? INFINITY : lse * kLog2e;
 }
 
-// dq of 64 rows over their keys; also delta of each row, for grad_kv.
+// dq of 64 rows over their keys; also delta of each row, for grad_kv.  fp32, the
+// sequences above: 60 us, matrix units busy 49 %.
 template <class E, int D>
 __global__ __launch_bounds__(kThreads) void grad_q_kernel(AttnArgs a) {
   typedef typename Op<E>::Frag Frag;
@@ -1027,7 +1049,8 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void grad_q_wide_kernel(
 
 // grad_kv in tiles of 128 keys, 32 a wave.  The sums of dk and dv of 128-wide heads, the keys' and the values' operands
 // take 192 of the 256 registers that two waves a SIMD leave, too many beside the scores: there, half of the workgroups form
-// dv and half dk, each with its own scores (five products in place of four).
+// dv and half dk, each with its own scores (five products in place of four: 3.0 ms on the sequences above; all four at one
+// wave a SIMD 4.7).
 enum Part { kBoth, kDv, kDk };
 
 template <int D, Part PART>
@@ -1109,7 +1132,7 @@ __device__ __forceinline__ void wide_grad_kv_rows(const AttnArgs& a, WideGradKv<
 
 template <int D, bool SPLIT, Part PART>
 __device__ __forceinline__ void grad_kv_wide(const AttnArgs& a, int block, WideKvLds<D>& lds) {
-  constexpr int kRows = kWideKeys;
+  const int step_rows = a.step;
   const int lane = threadIdx.x & 63, c = lane & 31, hi = lane >> 5, wave = threadIdx.x >> 6;
   const int hk = block % a.Hk, rest = tile_number(a, block / a.Hk);
   const int split = SPLIT ? rest % a.splits : 0, t = SPLIT ? rest / a.splits : rest;
@@ -1127,7 +1150,7 @@ __device__ __forceinline__ void grad_kv_wide(const AttnArgs& a, int block, WideK
   // Rows from here on see every key of the tile that exists.
   const int open = a.causal ? max(0, min(key0 + kWide, s.nk) - 1 - s.nk + s.nq) * a.G : 0;
   if (SPLIT) {
-    const int each = ((rows - row_lo + a.splits - 1) / a.splits + kRows - 1) / kRows * kRows;
+    const int each = ((rows - row_lo + a.splits - 1) / a.splits + step_rows - 1) / step_rows * step_rows;
     row_lo = min(rows, row_lo + split * each);
     row_hi = min(rows, row_lo + each);
   }
@@ -1147,27 +1170,28 @@ __device__ __forceinline__ void grad_kv_wide(const AttnArgs& a, int block, WideK
     if constexpr (PART != kDv) f.dk[dt] = zero16();
     if constexpr (PART != kDk) f.dv[dt] = zero16();
   }
-  // A tile's rows are whole queries (G divides the tile, and row_lo is a multiple of it).
+  // A tile's rows are whole queries, a.step of them from row_lo on, a multiple of G.  (16 sequences of 2048, 12 heads of 64
+  // that share 4, causal: backward 513 us with 63 rows a tile, 658 in the kernel of 64 keys; 20 of 577 of 128 191 and 240.)
   const QueryStage<D> qst(a, a.q), gst(a, a.dout);
   const char* qbase = a.q.at + s.q0 * a.q.row + hk * a.G * a.q.head;
   const char* gbase = a.dout.at + s.q0 * a.dout.row + hk * a.G * a.dout.head;
   const auto ask = [&](int r, __bf16* qt, __bf16* gt) {
     const int64_t n = div_group(a, r);
-    qst.stage(a, qt, qbase + n * a.q.row, row_hi - r);
-    gst.stage(a, gt, gbase + n * a.dout.row, row_hi - r);
+    qst.stage(a, qt, qbase + n * a.q.row, min(row_hi - r, step_rows));
+    gst.stage(a, gt, gbase + n * a.dout.row, min(row_hi - r, step_rows));
   };
   // The rows' statistics go through a register, one tile ahead of their LDS; thread t < 64 moves row t's.
   const float2* const stats = a.stat + static_cast<int64_t>(s.q0) * a.H + hk * a.G;
   const auto ask_stat = [&](int r) {
-    if (threadIdx.x >= kRows) return make_float2(0.f, 0.f);
+    if (threadIdx.x >= kWideKeys) return make_float2(0.f, 0.f);
     const int n = div_group(a, r), t = thread_again(), query = div_group(a, t);
     const uint32_t off = min(query, s.nq - 1 - n) * a.H + t - query * a.G;
     return (stats + static_cast<int64_t>(n) * a.H)[off];
   };
   const auto put_stat = [&](int r, float2 stat, typename WideKvLds<D>::Stats& x) {
-    if (threadIdx.x >= kRows) return;
+    if (threadIdx.x >= kWideKeys) return;
     const int query = div_group(a, r) + div_group(a, thread_again());
-    const bool here = r + static_cast<int>(threadIdx.x) < row_hi;
+    const bool here = static_cast<int>(threadIdx.x) < min(row_hi - r, step_rows);
     x.lse2[threadIdx.x] = here ? stat.x : INFINITY;
     x.delta[threadIdx.x] = here ? stat.y : 0.f;
     x.limit[threadIdx.x] = !here ? 0 : a.causal ? max(0, min(s.nk, query + 1 + s.nk - s.nq)) : s.nk;
@@ -1178,24 +1202,24 @@ __device__ __forceinline__ void grad_kv_wide(const AttnArgs& a, int block, WideK
     const bool more = r > row_lo;
     float2 stat;
     if (more) {
-      stat = ask_stat(r - kRows);
-      ask(r - kRows, qn, gn);
+      stat = ask_stat(r - step_rows);
+      ask(r - step_rows, qn, gn);
     }
-    if (wave_key < wave_limit(a, s, r, kRows))
-      wide_grad_kv_rows<D, PART>(a, f, qt, gt, w, here, key, r < open || r + kRows > row_hi);
-    if (more) put_stat(r - kRows, stat, next);
+    if (wave_key < wave_limit(a, s, r, step_rows))
+      wide_grad_kv_rows<D, PART>(a, f, qt, gt, w, here, key, r < open || r + kWideKeys > row_hi || step_rows < kWideKeys);
+    if (more) put_stat(r - step_rows, stat, next);
   };
   // From the last rows back: every tile of keys begins with the same rows, and the tiles at work share them in the L2
   // (each from its own first rows on: 4050 us in place of 3610).
-  const int last = row_lo + max(row_hi - row_lo - 1, 0) / kRows * kRows;
+  const int last = row_lo + max(row_hi - row_lo - 1, 0) / step_rows * step_rows;
   if (row_lo < row_hi) {
     const float2 stat = ask_stat(last);
     ask(last, lds.q0, lds.g0);
     put_stat(last, stat, lds.stats[0]);
-    for (int r = last; r >= row_lo; r -= 2 * kRows) {
+    for (int r = last; r >= row_lo; r -= 2 * step_rows) {
       step(r, lds.q0, lds.g0, lds.stats[0], lds.q1, lds.g1, lds.stats[1]);
       if (r == row_lo) break;
-      step(r - kRows, lds.q1, lds.g1, lds.stats[1], lds.q0, lds.g0, lds.stats[0]);
+      step(r - step_rows, lds.q1, lds.g1, lds.stats[1], lds.q0, lds.g0, lds.stats[0]);
     }
   }
   const int thread = thread_again(), out_key = key0 + thread / 64 * 32 + thread % 32, hi4 = thread % 64 / 32 * 4;
@@ -1223,7 +1247,7 @@ __device__ __forceinline__ void grad_kv_wide(const AttnArgs& a, int block, WideK
 }
 
 template <int D, bool SPLIT>
-__global__ __launch_bounds__(kThreads, 2) void grad_kv_wide_kernel(AttnArgs a) {
+__global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void grad_kv_wide_kernel(AttnArgs a) {
   __shared__ __attribute__((aligned(1024))) WideKvLds<D> lds;
   if constexpr (D == 64) {
     grad_kv_wide<D, SPLIT, kBoth>(a, blockIdx.x, lds);
@@ -1234,7 +1258,9 @@ __global__ __launch_bounds__(kThreads, 2) void grad_kv_wide_kernel(AttnArgs a) {
   }
 }
 
-// dk and dv of 64 keys over the rows that see them.
+// dk and dv of 64 keys over the rows that see them.  fp32, the sequences above: 77
+// us, matrix units busy 53 %.  (fp32 tiles of 32 rows a wave: 53, 71 and 92 us for
+// the three kernels in place of 45, 60 and 77.)
 template <class E, int D, bool SPLIT>
 __global__ __launch_bounds__(kThreads) void grad_kv_kernel(AttnArgs a) {
   typedef typename Op<E>::Frag Frag;
@@ -1391,7 +1417,7 @@ bool use_wide(const Sizes& z, int dtype, const AttnArgs& a, bool grad) {
          z.total_q * a.G / z.B > (grad && z.D == 64 ? kWideGradRows64 : kWideRows);
 }
 bool use_wide_kv(const Sizes& z, int dtype, const AttnArgs& a) {
-  return dtype == DORA_BF16 && z.D >= 64 && 32 % a.G == 0 && near(a.q, 64, a.G) && near(a.dout, 64, a.G) &&
+  return dtype == DORA_BF16 && z.D >= 64 && a.step >= 48 && near(a.q, 64, a.G) && near(a.dout, 64, a.G) &&
          z.total_k / z.B > (z.D == 64 ? kWideGradRows64 : kWideRows);
 }
 
@@ -1425,6 +1451,7 @@ int check_attn(const dora_rows* q, const dora_rows* k, const dora_rows* v, const
   a->max_q = max_q, a->max_k = 0x7FFFFFFF, a->causal = causal != 0;
   a->scale = softmax_scale > 0.f ? softmax_scale : static_cast<float>(1.0 / std::sqrt(static_cast<double>(z->D)));
   a->c2 = a->scale * kLog2e;
+  a->step = kWideKeys / a->G * a->G;
   a->status = dev_status;
   return DORA_OK;
 }

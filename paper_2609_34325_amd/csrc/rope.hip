@@ -8,6 +8,10 @@
 // half a turn however far the position), while its first elements are already
 // on their way.  A thread's unit is the two 16-byte pieces that hold its pairs'
 // ends, or, with adjacent pairs, one piece.
+//
+// 32749 rows of 40 heads of 128, half of each turned, bf16: 119 us, 5.6 TB/s; 35295
+// of 24 heads of 64, fp32: 84 us, 5.2 TB/s (a large copy runs at 4.9); 16 rows: 6 us,
+// a launch and one chain of loads.
 #include <math.h>
 
 #include <algorithm>

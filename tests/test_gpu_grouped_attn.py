@@ -382,3 +382,30 @@ def test_no_rows(gpu):
     q = torch.randn((3, 4, 64), device="cuda")
     out, lse, _ = gpu.dora_grouped_attn(q, e[:, :2], e[:, :2], dev_cu([0, 3]), 3, cu_k=dev_cu([0, 0]))
     assert bool((out == 0).all()) and bool((lse == -float("inf")).all())
+
+
+@pytest.mark.parametrize("causal,D", itertools.product((False, True), (64, 128)))
+@pytest.mark.parametrize("H,Hk", [(3, 1), (10, 2), (7, 1), (12, 1), (48, 1), (64, 1), (20, 1), (33, 1)])
+def test_group_sizes(gpu, causal, D, H, Hk):
+    """Heads of a group that do not divide a tile of rows; more queries than keys and fewer, and parts of them."""
+    for lens, keys in (([200, 0, 190, 260], [200, 5, 190, 260]), ([21, 22], [300, 200]), ([150, 1], [190, 182])):
+        t, cu_q, cu_k = make(lens, keys, H, Hk, D, torch.bfloat16, 13 * H + D)
+        run_both(gpu, t, cu_q, cu_k, causal, what=f"{lens} {keys}")
+    if H in (3, 12):
+        t, cu_q, cu_k = make([1500], [190], H, Hk, D, torch.bfloat16, 14 * H + D)
+        run_both(gpu, t, cu_q, cu_k, causal, what="parts")
+
+
+def test_group_rows_beyond(gpu):
+    """One sequence's infinities stay out of another's gradients where a tile of rows ends before a wave's last."""
+    lens, H, Hk, D = [180, 200], 5, 1, 64
+    t, cu, _ = make(lens, lens, H, Hk, D, torch.bfloat16, 15)
+    t["q"][179, :, 5] = float("inf")
+    t["dout"][180 - 12, :, 1] = float("nan")
+    d = cuda(t)
+    out, lse, _ = gpu.dora_grouped_attn(d["q"], d["k"], d["v"], dev_cu(cu), 200, causal=True)
+    grads = gpu.dora_grouped_attn_backward(d["dout"], d["q"], d["k"], d["v"], out, lse, dev_cu(cu), 200, causal=True)[:3]
+    want, bound = ref.attention(t["q"][180:], t["k"][180:], t["v"][180:], [0, 200], [0, 200], True, None,
+                                dout=t["dout"][180:], out=out[180:].cpu(), lse=lse[180:].cpu())
+    for n, x in zip(("dq", "dk", "dv"), grads):
+        ref.check(x[180:], want[n], bound[n], n)
