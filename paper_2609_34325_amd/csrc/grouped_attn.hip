@@ -63,7 +63,7 @@ struct AttnArgs {
   int32_t chunk;      // or: keys of a part, every sequence one tile of rows
   int32_t step;       // rows of whole queries in 64 (grad_kv_wide)
   int32_t blocks;
-  int32_t mixed;
+  int32_t mixed, ranked;
   int32_t* status;
 };
 
@@ -139,6 +139,63 @@ __device__ __forceinline__ bool locate(const AttnArgs& a, int64_t t, F first, in
   if (!good_boundaries(a, q0, q1, k0, k1)) return false;
   *s = Seq{q0, q1 - q0, k0, k1 - k0};
   return true;
+}
+
+// x summed over this lane and those before it.
+__device__ __forceinline__ int running(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);  // row_shr 1, 2, 4, 8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);  // row_bcast 15, 31
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);
+  return x;
+}
+
+// Tile i of at most 64 sequences, a sequence a lane: those whose tiles take longest first, in four bands of what their
+// tiles go over, so that the last to end are short.  Tiles that do not exist have the last numbers.
+template <bool QUERIES>
+__device__ __forceinline__ bool by_length(const AttnArgs& a, int i, int mul, int size, Seq* s, int* tile) {
+  const int lane = threadIdx.x & 63, at = min(lane, a.B), to = min(lane + 1, a.B);
+  const int q0 = a.cu_q[at], q1 = a.cu_q[to], k0 = a.cu_k[at], k1 = a.cu_k[to];
+  const bool good = lane < a.B && good_boundaries(a, q0, q1, k0, k1);
+  const int nq = good ? q1 - q0 : 0, nk = good ? k1 - k0 : 0;
+  const int tiles = static_cast<int>((static_cast<uint32_t>(QUERIES ? nq : nk) * mul + size - 1) / static_cast<uint32_t>(size));
+  const float work = tiles ? static_cast<float>(QUERIES ? nk : nq) : -1.f;
+  float most = fmaxf(work, dpp<0xB1>(work));
+  most = fmaxf(most, dpp<0x4E>(most));
+  most = fmaxf(most, dpp<0x141>(most));
+  most = fmaxf(most, dpp<0x140>(most));
+  most = max32(max16(most));
+  int start = 0, before = 0;
+#pragma unroll
+  for (int band = 0; band < 4; ++band) {
+    const bool in = work >= most * (0.75f - 0.25f * band) && (band == 0 || work < most * (1.f - 0.25f * band));
+    const int x = in ? tiles : 0, sum = running(x);
+    if (in) start = before + sum - x;
+    before += __builtin_amdgcn_readlane(sum, 63);
+  }
+  const uint64_t hit = __ballot(i >= start && i - start < tiles);
+  if (!hit) return false;
+  const int b = __builtin_ctzll(hit);
+  *s = Seq{__builtin_amdgcn_readlane(q0, b), __builtin_amdgcn_readlane(nq, b), __builtin_amdgcn_readlane(k0, b),
+           __builtin_amdgcn_readlane(nk, b)};
+  const int in_sequence = i - __builtin_amdgcn_readlane(start, b);
+  *tile = QUERIES ? __builtin_amdgcn_readlane(tiles, b) - 1 - in_sequence : in_sequence;
+  return true;
+}
+
+// Workgroup i's tile of `size` rows (keys) of a sequence; false: none.  Of a causal mask the long tiles first, the last rows'
+// and the first keys'.
+template <bool QUERIES>
+__device__ __forceinline__ bool find_tile(const AttnArgs& a, int i, int mul, int size, Seq* s, int* tile) {
+  if (a.ranked) return by_length<QUERIES>(a, i, mul, size, s, tile);
+  const int t = QUERIES ? a.blocks / a.Hk - 1 - tile_number(a, i) : tile_number(a, i);
+  int b;
+  if (!locate<QUERIES>(a, t, [&](int cu, int j) { return first_tile(cu, j, mul, size); }, &b, s)) return false;
+  const int64_t at = t - first_tile(QUERIES ? s->q0 : s->k0, b, mul, size);
+  *tile = static_cast<int>(at);
+  return at >= 0 && at * size < static_cast<int64_t>(QUERIES ? s->nq : s->nk) * mul;
 }
 
 // The grid's last workgroup looks at every boundary.
@@ -328,7 +385,7 @@ __global__ __launch_bounds__(kThreads) void attn_kernel(AttnArgs a) {
   __shared__ alignas(16) E vs[kKeys * kLd];
   if (check_block(a)) return;
   const int lane = threadIdx.x & 63, c16 = lane & 15, g = lane >> 4, wave = threadIdx.x >> 6;
-  const int hk = blockIdx.x % a.Hk, rest = tile_number(a, blockIdx.x / a.Hk);
+  const int hk = blockIdx.x % a.Hk, rest = blockIdx.x / a.Hk;
   const int split = SPLIT && !a.chunk ? rest % a.splits : 0, t = SPLIT && !a.chunk ? rest / a.splits : rest;
   Seq s;
   int tile = 0, key_lo = 0, key_hi;
@@ -340,11 +397,15 @@ __global__ __launch_bounds__(kThreads) void attn_kernel(AttnArgs a) {
     key_lo = static_cast<int>(part) * a.chunk;
     key_hi = min(s.nk, key_lo + a.chunk);
   } else {
-    int b;
-    if (!locate<true>(a, t, [&](int cu, int i) { return first_tile(cu, i, a.G, kTile); }, &b, &s)) return;
-    const int64_t at = t - first_tile(s.q0, b, a.G, kTile);
-    if (at < 0 || at * kTile >= static_cast<int64_t>(s.nq) * a.G) return;
-    tile = static_cast<int>(at);
+    if constexpr (SPLIT) {
+      int b;
+      if (!locate<true>(a, t, [&](int cu, int i) { return first_tile(cu, i, a.G, kTile); }, &b, &s)) return;
+      const int64_t at = t - first_tile(s.q0, b, a.G, kTile);
+      if (at < 0 || at * kTile >= static_cast<int64_t>(s.nq) * a.G) return;
+      tile = static_cast<int>(at);
+    } else if (!find_tile<true>(a, t, a.G, kTile, &s, &tile)) {
+      return;
+    }
     key_hi = limit_of(a, s, min((tile + 1) * kTile, s.nq * a.G) - 1);
     if (SPLIT) {
       const int each = ((key_hi + a.splits - 1) / a.splits + kKeys - 1) / kKeys * kKeys;
@@ -718,15 +779,11 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void attn_wide_kernel(At
   __shared__ __attribute__((aligned(1024))) WideTiles<D> tiles;
   if (check_block(a)) return;
   const int lane = threadIdx.x & 63, c = lane & 31, hi = lane >> 5, wave = threadIdx.x >> 6;
-  const int hk = blockIdx.x % a.Hk, t = a.blocks / a.Hk - 1 - tile_number(a, blockIdx.x / a.Hk);  // long tiles first
+  const int hk = blockIdx.x % a.Hk;
   Seq s;
-  int b;
-  const bool good = locate<true>(a, t, [&](int cu, int i) { return first_tile(cu, i, a.G, kWide); }, &b, &s);
-  if (!good) return;
-  const int64_t tile = t - first_tile(s.q0, b, a.G, kWide);
-  const int rows = s.nq * a.G;
-  if (tile < 0 || tile * kWide >= rows) return;
-  const int row0 = static_cast<int>(tile) * kWide, row = row0 + wave * 32 + c;
+  int tile;
+  if (!find_tile<true>(a, blockIdx.x / a.Hk, a.G, kWide, &s, &tile)) return;
+  const int rows = s.nq * a.G, row0 = tile * kWide, row = row0 + wave * 32 + c;
   const bool real = row < rows;
   const int key_hi = limit_of(a, s, min(row0 + kWide, rows) - 1), open = limit_of(a, s, row0);
   const int wave_hi = wave_limit(a, s, row0 + wave * 32, 32);
@@ -861,15 +918,11 @@ __global__ __launch_bounds__(kThreads) void grad_q_kernel(AttnArgs a) {
   __shared__ alignas(16) E vs[kKeys * kLd];
   if (check_block(a)) return;
   const int lane = threadIdx.x & 63, c16 = lane & 15, g = lane >> 4, wave = threadIdx.x >> 6;
-  const int hk = blockIdx.x % a.Hk, t = tile_number(a, blockIdx.x / a.Hk);
+  const int hk = blockIdx.x % a.Hk;
   Seq s;
-  int b;
-  const bool good = locate<true>(a, t, [&](int cu, int i) { return first_tile(cu, i, a.G, kTile); }, &b, &s);
-  if (!good) return;
-  const int64_t tile = t - first_tile(s.q0, b, a.G, kTile);
-  const int rows = s.nq * a.G;
-  if (tile < 0 || tile * kTile >= rows) return;
-  const int row0 = static_cast<int>(tile) * kTile, row = row0 + wave * 16 + c16;
+  int tile;
+  if (!find_tile<true>(a, blockIdx.x / a.Hk, a.G, kTile, &s, &tile)) return;
+  const int rows = s.nq * a.G, row0 = tile * kTile, row = row0 + wave * 16 + c16;
   const bool real = row < rows;
   const int limit = limit_of(a, s, row), open = limit_of(a, s, row0);
   const int key_hi = limit_of(a, s, min(row0 + kTile, rows) - 1), wave_hi = wave_limit(a, s, row0 + wave * 16, 16);
@@ -988,15 +1041,11 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void grad_q_wide_kernel(
   __shared__ __attribute__((aligned(1024))) WideTiles<D> tiles;
   if (check_block(a)) return;
   const int lane = threadIdx.x & 63, c = lane & 31, hi = lane >> 5, wave = threadIdx.x >> 6;
-  const int hk = blockIdx.x % a.Hk, t = a.blocks / a.Hk - 1 - tile_number(a, blockIdx.x / a.Hk);  // long tiles first
+  const int hk = blockIdx.x % a.Hk;
   Seq s;
-  int b;
-  const bool good = locate<true>(a, t, [&](int cu, int i) { return first_tile(cu, i, a.G, kWide); }, &b, &s);
-  if (!good) return;
-  const int64_t tile = t - first_tile(s.q0, b, a.G, kWide);
-  const int rows = s.nq * a.G;
-  if (tile < 0 || tile * kWide >= rows) return;
-  const int row0 = static_cast<int>(tile) * kWide, row = row0 + wave * 32 + c;
+  int tile;
+  if (!find_tile<true>(a, blockIdx.x / a.Hk, a.G, kWide, &s, &tile)) return;
+  const int rows = s.nq * a.G, row0 = tile * kWide, row = row0 + wave * 32 + c;
   const bool real = row < rows;
   const int key_hi = limit_of(a, s, min(row0 + kWide, rows) - 1), open = limit_of(a, s, row0);
   const int limit = limit_of(a, s, row), wave_hi = wave_limit(a, s, row0 + wave * 32, 32);
@@ -1134,15 +1183,12 @@ template <int D, bool SPLIT, Part PART>
 __device__ __forceinline__ void grad_kv_wide(const AttnArgs& a, int block, WideKvLds<D>& lds) {
   const int step_rows = a.step;
   const int lane = threadIdx.x & 63, c = lane & 31, hi = lane >> 5, wave = threadIdx.x >> 6;
-  const int hk = block % a.Hk, rest = tile_number(a, block / a.Hk);
+  const int hk = block % a.Hk, rest = block / a.Hk;
   const int split = SPLIT ? rest % a.splits : 0, t = SPLIT ? rest / a.splits : rest;
   Seq s;
-  int b;
-  const bool good = locate<false>(a, t, [&](int cu, int i) { return first_tile(cu, i, 1, kWide); }, &b, &s);
-  if (!good) return;
-  const int64_t tile = t - first_tile(s.k0, b, 1, kWide);
-  if (tile < 0 || tile * kWide >= s.nk) return;
-  const int key0 = static_cast<int>(tile) * kWide, key = key0 + wave * 32 + c;
+  int tile;
+  if (!find_tile<false>(a, t, 1, kWide, &s, &tile)) return;
+  const int key0 = tile * kWide, key = key0 + wave * 32 + c;
   const int wave_key = __builtin_amdgcn_readfirstlane(key0 + wave * 32);
   const bool real = key < s.nk;
   const int rows = s.nq * a.G;
@@ -1271,15 +1317,12 @@ __global__ __launch_bounds__(kThreads) void grad_kv_kernel(AttnArgs a) {
   __shared__ floatx4 lse_s[kRows / 4], delta_s[kRows / 4];
   __shared__ int4 limit_s[kRows / 4];
   const int lane = threadIdx.x & 63, c16 = lane & 15, g = lane >> 4, wave = threadIdx.x >> 6;
-  const int hk = blockIdx.x % a.Hk, rest = tile_number(a, blockIdx.x / a.Hk);
+  const int hk = blockIdx.x % a.Hk, rest = blockIdx.x / a.Hk;
   const int split = SPLIT ? rest % a.splits : 0, t = SPLIT ? rest / a.splits : rest;
   Seq s;
-  int b;
-  const bool good = locate<false>(a, t, [&](int cu, int i) { return first_tile(cu, i, 1, kTile); }, &b, &s);
-  if (!good) return;
-  const int64_t tile = t - first_tile(s.k0, b, 1, kTile);
-  if (tile < 0 || tile * kTile >= s.nk) return;
-  const int key0 = static_cast<int>(tile) * kTile, key = key0 + wave * 16 + c16;
+  int tile;
+  if (!find_tile<false>(a, t, 1, kTile, &s, &tile)) return;
+  const int key0 = tile * kTile, key = key0 + wave * 16 + c16;
   const int wave_key = __builtin_amdgcn_readfirstlane(key0 + wave * 16);
   const bool real = key < s.nk;
   const int rows = s.nq * a.G;
@@ -1452,6 +1495,7 @@ int check_attn(const dora_rows* q, const dora_rows* k, const dora_rows* v, const
   a->scale = softmax_scale > 0.f ? softmax_scale : static_cast<float>(1.0 / std::sqrt(static_cast<double>(z->D)));
   a->c2 = a->scale * kLog2e;
   a->step = kWideKeys / a->G * a->G;
+  a->ranked = B <= 64;
   a->status = dev_status;
   return DORA_OK;
 }
