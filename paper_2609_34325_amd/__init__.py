@@ -136,7 +136,7 @@ _ENTRIES = (
      _DECISIONS + (None,) * 5 + (("dscores", _F32),) + _LOSS_OUT),
     ("dora_grad_clip", (None,) * 5 + (("norm_out", _F32), ("workspace", _ANY), None, None)),
     # Rows go by the address of their description (strided views are allowed).
-    ("dora_rope", (None, None, ("positions", _I32), None, ("freq", torch.float64)) + (None,) * 7),
+    ("dora_rope", (None, None, ("positions", _I32), None, ("freq", _ANY)) + (None,) * 7),
     ("dora_grouped_attn", (None,) * 3 + (("cu_q", _I32), ("cu_k", _I32)) + (None,) * 6 +
      (("lse_out", _F32), ("workspace", _ANY), None) + _STATUS),
     ("dora_grouped_attn_backward", (None,) * 5 + (("lse", _F32), ("cu_q", _I32), ("cu_k", _I32)) + (None,) * 7 +
@@ -1038,14 +1038,17 @@ def dora_rope(q: torch.Tensor, positions: torch.Tensor, freq: torch.Tensor, k: O
     _heads(("q", "k"), q, k)
     if k is None and k_out is not None:
         raise ValueError("k_out goes with k")
-    q_out = _like(q) if q_out is None else q_out
-    k_out = _like(k) if k is not None and k_out is None else k_out
-    rows, at, device = _describe(("q", "k", "q_out", "k_out"), q, k, q_out, k_out)
+    for name, t in (("positions", positions), ("freq", freq)):
+        if not isinstance(t, torch.Tensor):
+            raise TypeError(f"{name} must be a torch tensor")
     axes = 1 if positions.dim() == 1 else int(positions.shape[-1])
     if positions.dim() not in (1, 2) or int(positions.shape[0]) != int(q.shape[0]) or freq.dim() != 1:
         raise ValueError("positions must be [rows] or [rows, axes], freq [R / 2]")
     if freq.dtype != torch.float64:
         raise TypeError(f"freq must be {torch.float64}, got {freq.dtype}")
+    q_out = _like(q) if q_out is None else q_out
+    k_out = _like(k) if k is not None and k_out is None else k_out
+    rows, at, device = _describe(("q", "k", "q_out", "k_out"), q, k, q_out, k_out)
     _vectors(("positions", "freq"), device, -1, positions, -1, freq)
     _call("dora_rope", None, at[0], at[1], positions, axes, freq, 2 * freq.numel(), int(bool(interleaved)),
           int(bool(inverse)), float(scale), at[2], at[3])

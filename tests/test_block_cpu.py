@@ -340,6 +340,12 @@ def test_binding_refusals():
         dora.dora_rope(q, pos, freq)
     with pytest.raises(ValueError, match="rows, heads, dim"):
         dora.dora_rope(q[:, 0], pos, freq)
+    with pytest.raises(TypeError, match="freq must be torch.float64"):
+        dora.dora_rope(q, pos, freq.float())
+    with pytest.raises(TypeError, match="positions must be a torch tensor"):
+        dora.dora_rope(q, [0, 1, 2, 3], freq)
+    with pytest.raises(ValueError, match="positions must be"):
+        dora.dora_rope(q, pos[:3], freq)
     with pytest.raises(ValueError, match="goes with k"):
         dora.dora_rope(q, pos, freq, k_out=q)
     with pytest.raises(ValueError, match="on the GPU"):
