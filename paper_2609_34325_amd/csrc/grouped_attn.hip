@@ -533,12 +533,12 @@ __global__ __launch_bounds__(kThreads) void attn_kernel(AttnArgs a) {
 // elements 8 hi .. 8 hi + 7 of row or column c, the result's lane column c, rows
 // 8 (i / 4) + 4 hi + i % 4.  One operand read from LDS serves 32 columns in place
 // of 16.  Two waves a SIMD at 128, three at 64, on the sequences
-// above: matrix units busy 45 % of the cycles forward, 56 % in grad_q, 45 % in
-// grad_kv, vector instructions a third to two fifths, LDS a fifth and no conflicts;
+// above: matrix units busy 45 % of the cycles forward, 56 % in grad_q, 46 % in
+// grad_kv, vector instructions a third to two fifths, LDS a quarter, no conflicts;
 // a wave waits for its own products, exponentials or operands the rest.  Heads of
 // 64 have the same exponentials for half the products: 64 sequences of 46 to 577,
-// 20337 rows, 12 heads, take 56 us forward, 69 in grad_q and 84 in grad_kv, with
-// matrix units busy 22 to 30 %.
+// 20337 rows, 12 heads, take 54 us forward, 67 in grad_q and 79 in grad_kv, with
+// matrix units busy 23 to 33 %.
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 typedef __attribute__((address_space(3))) void lds_void;
 
