@@ -912,6 +912,10 @@ __device__ __forceinline__ float row_lse2(const AttnArgs& a, const Seq& s, int h
   return lse == -INFINITY ? INFINITY : lse * kLog2e;
 }
 
+// delta from out carries out's rounding to bf16, which stands for as much as the roundings of dS and of the results where a
+// row has few keys (2^-9 of |dout||out|, and |out| falls as 1 / sqrt(keys)): 1.6 times the error of a form that rounds its
+// results alone, 1.4 without.  Where a tile's keys are staged at once (64, wide 128), delta is the sum of P dP instead.
+
 // dq of 64 rows over their keys; also delta of each row, for grad_kv.  fp32, the
 // sequences above: 60 us, matrix units busy 49 %.
 template <class E, int D>
@@ -946,7 +950,6 @@ __global__ __launch_bounds__(kThreads) void grad_q_kernel(AttnArgs a) {
   }
   delta = over_groups_sum(delta);
   const float lse2 = row_lse2(a, s, hk, row, real);
-  if (real && g == 0) a.stat[stat_at(a, s, hk, row)] = make_float2(lse2, delta);
   floatx4 dq[D / 16];
 #pragma unroll
   for (int dt = 0; dt < D / 16; ++dt) dq[dt] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -966,6 +969,22 @@ __global__ __launch_bounds__(kThreads) void grad_q_kernel(AttnArgs a) {
     __syncthreads();
     if (key + kKeys < key_hi) ask(key + kKeys);
     if (key >= wave_hi) continue;
+    if (sizeof(E) == 2 && key_hi <= kKeys) {
+      delta = 0.f;
+#pragma unroll
+      for (int r0 = 0; r0 < kKeys; r0 += 16) {
+        floatx4 sc = {0.f, 0.f, 0.f, 0.f}, dp = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int st = 0; st < D / 32; ++st) {
+          sc = Op<E>::mma(load_frag<E>(ks + (r0 + c16) * kLd + 32 * st + 8 * g), qf[st], sc);
+          dp = Op<E>::mma(load_frag<E>(vs + (r0 + c16) * kLd + 32 * st + 8 * g), gf[st], dp);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          delta += r0 + 4 * g + i >= limit ? 0.f : __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i], a.c2, -lse2)) * dp[i];
+      }
+      delta = over_groups_sum(delta);
+    }
 #pragma unroll
     for (int st32 = 0; st32 < kKeys / 32; ++st32) {
       floatx4 ds[2];
@@ -990,6 +1009,7 @@ __global__ __launch_bounds__(kThreads) void grad_q_kernel(AttnArgs a) {
         dq[dt] = Op<E>::mma(Op<E>::template columns<kLd>(ks + st32 * 32 * kLd, dt * 16), f, dq[dt]);
     }
   }
+  if (real && g == 0) a.stat[stat_at(a, s, hk, row)] = make_float2(lse2, delta);
   if (!real) return;
   char* to = const_cast<char*>(query_row(a, a.dq, s, hk, row));
 #pragma unroll
@@ -1007,6 +1027,29 @@ struct WideGradQ {
   floatx16 dq[D / 32];
   float lse2, delta;
 };
+
+// The lane's share of the sum of P dP over 64 staged keys.
+template <int D>
+__device__ __forceinline__ float wide_delta(const AttnArgs& a, const WideGradQ<D>& f, const __bf16* ks, const __bf16* vs,
+                                            const WidePlaces& w, int end) {
+  const int hi = (threadIdx.x & 63) >> 5;
+  float sum = 0.f;
+#pragma unroll
+  for (int n = 0; n < 2; ++n) {
+    floatx16 s = zero16(), dp = zero16();
+#pragma unroll
+    for (int st = 0; st < D / 16; ++st) s = mma32(wide_row(ks, w, 32 * n, st), f.q[st], s);
+    formed(s);
+#pragma unroll
+    for (int st = 0; st < D / 16; ++st) dp = mma32(wide_row(vs, w, 32 * n, st), f.g[st], dp);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], a.c2, -f.lse2));
+      sum += 32 * n + wide_place(i) + 4 * hi >= end ? 0.f : p * dp[i];
+    }
+  }
+  return sum;
+}
 
 template <int D>
 __device__ __forceinline__ void wide_grad_q_keys(const AttnArgs& a, WideGradQ<D>& f, const __bf16* ks, const __bf16* vs,
@@ -1068,9 +1111,6 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void grad_q_wide_kernel(
   }
   f.delta = add32(delta);
   f.lse2 = row_lse2(a, s, hk, row, real);
-  if (real && hi == 0) a.stat[stat_at(a, s, hk, row)] = make_float2(f.lse2, f.delta);
-#pragma unroll
-  for (int dt = 0; dt < D / 32; ++dt) f.dq[dt] = zero16();
   const char* kbase = a.k.at + static_cast<int64_t>(s.k0) * a.k.row + hk * a.k.head;
   const char* vbase = a.v.at + static_cast<int64_t>(s.k0) * a.v.row + hk * a.v.head;
   const KeyStage<D> kst(a.k.row), vst(a.v.row);
@@ -1078,12 +1118,23 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void grad_q_wide_kernel(
     kst.stage(kt, kbase + key * a.k.row, s.nk - key);
     vst.stage(vt, vbase + key * a.v.row, s.nk - key);
   };
+  const bool few = key_hi <= 2 * kWideKeys;
   const auto step = [&](int key, const __bf16* kt, const __bf16* vt, __bf16* kn, __bf16* vn) {
     staged();
-    if (key + kWideKeys < key_hi) ask(key + kWideKeys, kn, vn);
+    if (key + kWideKeys < key_hi && !few) ask(key + kWideKeys, kn, vn);
     if (key < wave_hi) wide_grad_q_keys<D>(a, f, kt, vt, w, limit - key, key + kWideKeys > open);
   };
   if (key_hi > 0) ask(0, tiles.a0, tiles.b0);
+  if (few) {
+    if (key_hi > kWideKeys) ask(kWideKeys, tiles.a1, tiles.b1);
+    staged();
+    float sum = wave_hi > 0 ? wide_delta<D>(a, f, tiles.a0, tiles.b0, w, limit) : 0.f;
+    if (wave_hi > kWideKeys) sum += wide_delta<D>(a, f, tiles.a1, tiles.b1, w, limit - kWideKeys);
+    f.delta = add32(sum);
+  }
+  if (real && hi == 0) a.stat[stat_at(a, s, hk, row)] = make_float2(f.lse2, f.delta);
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt) f.dq[dt] = zero16();
   for (int key = 0; key < key_hi; key += 2 * kWideKeys) {
     step(key, tiles.a0, tiles.b0, tiles.a1, tiles.b1);
     if (key + kWideKeys >= key_hi) break;

@@ -90,6 +90,11 @@ def attention(q, k, v, cu_q, cu_k, causal, scale=None, dout=None, out=None, lse=
             dP, delta = g @ vh.T, (g * o).sum(1, keepdim=True)
             T = P * (dP - delta)
             eT = T.abs() * (one + 2 * U) + P * (D + 4) * U * (g.abs() @ vh.abs().T + (g * o).abs().sum(1, keepdim=True))
+            if dtype == torch.bfloat16:
+                # Rows of few keys have delta as the sum of P dP, of which g . out differs by out's rounding, half a step of
+                # each element; P's own errors and those of the products (as above, P adds up to 1) come on top.
+                eT = eT + P * ((g * o).abs().sum(1, keepdim=True) * HALF[dtype] + (P * one * dP.abs()).sum(1, keepdim=True) +
+                               (P * (D + 4 + nk) * U * (g.abs() @ vh.abs().T)).sum(1, keepdim=True))
             eT = eT * (1 + held) + T.abs() * held
             r["dq"][rq, h] = c * T @ kh
             e["dq"][rq, h] = c * (eT + T.abs() * (nk + 24) * U) @ kh.abs()

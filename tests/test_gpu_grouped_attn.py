@@ -409,3 +409,24 @@ def test_group_rows_beyond(gpu):
                                 dout=t["dout"][180:], out=out[180:].cpu(), lse=lse[180:].cpu())
     for n, x in zip(("dq", "dk", "dv"), grads):
         ref.check(x[180:], want[n], bound[n], n)
+
+
+@pytest.mark.parametrize("dtype,D", itertools.product(DTYPES, (32, 64, 128)))
+@pytest.mark.parametrize("long", [False, True])
+def test_one_key_has_no_gradient(gpu, dtype, D, long):
+    """A row that sees one key has P 1 whatever its score: dq is 0 but for the roundings of fp32 sums, though the output
+    that goes in is rounded to its type."""
+    lens, H, Hk = [1, 1, 40, 1] + [300] * long, 4, 2
+    t, cu, _ = make(lens, lens, H, Hk, D, dtype, 16)
+    d = cuda(t)
+    out, lse, _ = gpu.dora_grouped_attn(d["q"], d["k"], d["v"], dev_cu(cu), max(lens), causal=True)
+    dq = gpu.dora_grouped_attn_backward(d["dout"], d["q"], d["k"], d["v"], out, lse, dev_cu(cu), max(lens), causal=True)[0]
+    u, c = 2.0 ** -24, D ** -0.5
+    for i in cu[:-1]:                                           # first rows
+        q, g = t["q"][i].double().abs(), t["dout"][i].double().abs()
+        k, v = (t[n][i].double().abs().repeat_interleave(H // Hk, 0) for n in ("k", "v"))
+        # P is 2 to a difference of two numbers of the score's size: roundings of the products' sum and of the two
+        one = (D + 4) * u * c * (q * k).sum(1) + 8 * u * (1 + c * (q * k).sum(1))
+        # dS = P (dP - delta), both sums of D products; its rounding, the product's and the result's come on top
+        ds = (one + 2 * (D + 4) * u) * (g * v).sum(1)
+        assert bool((dq[i].double().cpu().abs() <= 1.02 * c * ds[:, None] * k).all()), i
