@@ -754,8 +754,8 @@ int dora_rope(const dora_rows* q, const dora_rows* k, const int32_t* positions, 
  * that read them.
  *   P = exp(S - lse),  dS = P (dout v^T - rowsum(dout out))
  *   dq = softmax_scale dS k,  dk = softmax_scale dS^T q,  dv = P^T dout
- * (where few keys are seen, the sum of P dout v^T for rowsum(dout out), whose
- * rounding would count).
+ * (where few keys are seen, the mean of dout v^T under P for rowsum(dout out),
+ * whose rounding would count).  Of a query that sees one key dS is 0, exactly.
  * bf16: P and dS rounded to bf16 for their products, sums in fp32, gradients
  * rounded once.  Infinities and NaN stay inside their sequence.
  *   dout, out  q's sizes; dq, dk, dv those of q, k, v, any strides (slices of

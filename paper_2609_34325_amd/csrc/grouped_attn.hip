@@ -914,7 +914,16 @@ __device__ __forceinline__ float row_lse2(const AttnArgs& a, const Seq& s, int h
 
 // delta from out carries out's rounding to bf16, which stands for as much as the roundings of dS and of the results where a
 // row has few keys (2^-9 of |dout||out|, and |out| falls as 1 / sqrt(keys)): 1.6 times the error of a form that rounds its
-// results alone, 1.4 without.  Where a tile's keys are staged at once (64, wide 128), delta is the sum of P dP instead.
+// results alone, 1.4 without.  Where a tile's keys are staged at once (64, wide 128), delta is the sum of P dP over the sum
+// of P instead.  That sum is 1 but for lse's roundings, 2^-23 of its size: left out, dS of a row whose P is all on one key
+// keeps as much of dP (1e-4 of it at scores of 900), where it should vanish.
+__device__ __forceinline__ float mean_of(float sum, float weights) { return weights == 0.f ? 0.f : sum / weights; }
+
+// Keys whose dS counts, of `limit` that the row sees: of one key P is 1 whatever its score, and dS 0.
+__device__ __forceinline__ int gradient_limit(int limit) { return limit == 1 ? 0 : limit; }
+// Both limits of a row in one number, for dS and, without the sign bit, for P.
+__device__ __forceinline__ int both_limits(int limit) { return limit == 1 ? INT32_MIN | 1 : limit; }
+__device__ __forceinline__ int p_limit(int both) { return both & INT32_MAX; }
 
 // dq of 64 rows over their keys; also delta of each row, for grad_kv.  fp32, the
 // sequences above: 60 us, matrix units busy 49 %.
@@ -933,7 +942,7 @@ __global__ __launch_bounds__(kThreads) void grad_q_kernel(AttnArgs a) {
   if (!find_tile<true>(a, blockIdx.x / a.Hk, a.G, kTile, &s, &tile)) return;
   const int rows = s.nq * a.G, row0 = tile * kTile, row = row0 + wave * 16 + c16;
   const bool real = row < rows;
-  const int limit = limit_of(a, s, row), open = limit_of(a, s, row0);
+  const int limit = limit_of(a, s, row), open = limit_of(a, s, row0), ds_limit = gradient_limit(limit);
   const int key_hi = limit_of(a, s, min(row0 + kTile, rows) - 1), wave_hi = wave_limit(a, s, row0 + wave * 16, 16);
   Frag qf[D / 32], gf[D / 32];
   float delta = 0.f;
@@ -970,6 +979,7 @@ __global__ __launch_bounds__(kThreads) void grad_q_kernel(AttnArgs a) {
     if (key + kKeys < key_hi) ask(key + kKeys);
     if (key >= wave_hi) continue;
     if (sizeof(E) == 2 && key_hi <= kKeys) {
+      float sum = 0.f;
       delta = 0.f;
 #pragma unroll
       for (int r0 = 0; r0 < kKeys; r0 += 16) {
@@ -980,10 +990,14 @@ __global__ __launch_bounds__(kThreads) void grad_q_kernel(AttnArgs a) {
           dp = Op<E>::mma(load_frag<E>(vs + (r0 + c16) * kLd + 32 * st + 8 * g), gf[st], dp);
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          delta += r0 + 4 * g + i >= limit ? 0.f : __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i], a.c2, -lse2)) * dp[i];
+        for (int i = 0; i < 4; ++i) {
+          const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i], a.c2, -lse2));
+          const bool seen = r0 + 4 * g + i < limit;
+          sum += seen ? p : 0.f;
+          delta += seen ? p * dp[i] : 0.f;
+        }
       }
-      delta = over_groups_sum(delta);
+      delta = mean_of(over_groups_sum(delta), over_groups_sum(sum));
     }
 #pragma unroll
     for (int st32 = 0; st32 < kKeys / 32; ++st32) {
@@ -1000,7 +1014,7 @@ __global__ __launch_bounds__(kThreads) void grad_q_kernel(AttnArgs a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i], a.c2, -lse2));
-          ds[half][i] = masked && key + r0 + 4 * g + i >= limit ? 0.f : p * (dp[i] - delta);
+          ds[half][i] = masked && key + r0 + 4 * g + i >= ds_limit ? 0.f : p * (dp[i] - delta);
         }
       }
       const Frag f = Op<E>::pack(ds[0], ds[1]);
@@ -1028,12 +1042,12 @@ struct WideGradQ {
   float lse2, delta;
 };
 
-// The lane's share of the sum of P dP over 64 staged keys.
+// The lane's share of the sums of P dP and of P over 64 staged keys.
 template <int D>
-__device__ __forceinline__ float wide_delta(const AttnArgs& a, const WideGradQ<D>& f, const __bf16* ks, const __bf16* vs,
-                                            const WidePlaces& w, int end) {
+__device__ __forceinline__ float2 wide_delta(const AttnArgs& a, const WideGradQ<D>& f, const __bf16* ks, const __bf16* vs,
+                                             const WidePlaces& w, int end) {
   const int hi = (threadIdx.x & 63) >> 5;
-  float sum = 0.f;
+  float2 sum = {0.f, 0.f};
 #pragma unroll
   for (int n = 0; n < 2; ++n) {
     floatx16 s = zero16(), dp = zero16();
@@ -1045,7 +1059,9 @@ __device__ __forceinline__ float wide_delta(const AttnArgs& a, const WideGradQ<D
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], a.c2, -f.lse2));
-      sum += 32 * n + wide_place(i) + 4 * hi >= end ? 0.f : p * dp[i];
+      const bool seen = 32 * n + wide_place(i) + 4 * hi < end;
+      sum.x += seen ? p * dp[i] : 0.f;
+      sum.y += seen ? p : 0.f;
     }
   }
   return sum;
@@ -1122,15 +1138,18 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 3 : 2) void grad_q_wide_kernel(
   const auto step = [&](int key, const __bf16* kt, const __bf16* vt, __bf16* kn, __bf16* vn) {
     staged();
     if (key + kWideKeys < key_hi && !few) ask(key + kWideKeys, kn, vn);
-    if (key < wave_hi) wide_grad_q_keys<D>(a, f, kt, vt, w, limit - key, key + kWideKeys > open);
+    if (key < wave_hi) wide_grad_q_keys<D>(a, f, kt, vt, w, gradient_limit(limit) - key, key + kWideKeys > open);
   };
   if (key_hi > 0) ask(0, tiles.a0, tiles.b0);
   if (few) {
     if (key_hi > kWideKeys) ask(kWideKeys, tiles.a1, tiles.b1);
     staged();
-    float sum = wave_hi > 0 ? wide_delta<D>(a, f, tiles.a0, tiles.b0, w, limit) : 0.f;
-    if (wave_hi > kWideKeys) sum += wide_delta<D>(a, f, tiles.a1, tiles.b1, w, limit - kWideKeys);
-    f.delta = add32(sum);
+    float2 sum = wave_hi > 0 ? wide_delta<D>(a, f, tiles.a0, tiles.b0, w, limit) : make_float2(0.f, 0.f);
+    if (wave_hi > kWideKeys) {
+      const float2 more = wide_delta<D>(a, f, tiles.a1, tiles.b1, w, limit - kWideKeys);
+      sum.x += more.x, sum.y += more.y;
+    }
+    f.delta = mean_of(add32(sum.x), add32(sum.y));
   }
   if (real && hi == 0) a.stat[stat_at(a, s, hk, row)] = make_float2(f.lse2, f.delta);
 #pragma unroll
@@ -1214,8 +1233,10 @@ __device__ __forceinline__ void wide_grad_kv_rows(const AttnArgs& a, WideGradKv<
         const int4 m4 = *reinterpret_cast<const int4*>(stats.limit + 32 * n + 8 * j + 4 * hi);
         const int lim[4] = {m4.x, m4.y, m4.z, m4.w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (key >= lim[i]) s[4 * j + i] = dp[4 * j + i] = 0.f;
+        for (int i = 0; i < 4; ++i) {
+          if (PART != kDk && key >= p_limit(lim[i])) s[4 * j + i] = 0.f;
+          if (PART != kDv && key >= lim[i]) dp[4 * j + i] = 0.f;
+        }
       }
     }
 #pragma unroll
@@ -1249,8 +1270,8 @@ __device__ __forceinline__ void grad_kv_wide(const AttnArgs& a, int block, WideK
   const bool real = key < s.nk;
   const int rows = s.nq * a.G;
   int row_lo = a.causal ? min(rows, max(0, key0 - s.nk + s.nq) * a.G) : 0, row_hi = rows;
-  // Rows from here on see every key of the tile that exists.
-  const int open = a.causal ? max(0, min(key0 + kWide, s.nk) - 1 - s.nk + s.nq) * a.G : 0;
+  // Rows from here on see every key of the tile that exists, and more than one.
+  const int open = s.nk == 1 ? rows : a.causal ? max(0, min(key0 + kWide, s.nk) - 1 - s.nk + s.nq) * a.G : 0;
   if (SPLIT) {
     const int each = ((rows - row_lo + a.splits - 1) / a.splits + step_rows - 1) / step_rows * step_rows;
     row_lo = min(rows, row_lo + split * each);
@@ -1296,7 +1317,7 @@ __device__ __forceinline__ void grad_kv_wide(const AttnArgs& a, int block, WideK
     const bool here = static_cast<int>(threadIdx.x) < min(row_hi - r, step_rows);
     x.lse2[threadIdx.x] = here ? stat.x : INFINITY;
     x.delta[threadIdx.x] = here ? stat.y : 0.f;
-    x.limit[threadIdx.x] = !here ? 0 : a.causal ? max(0, min(s.nk, query + 1 + s.nk - s.nq)) : s.nk;
+    x.limit[threadIdx.x] = !here ? 0 : both_limits(a.causal ? max(0, min(s.nk, query + 1 + s.nk - s.nq)) : s.nk);
   };
   const auto step = [&](int r, const __bf16* qt, const __bf16* gt, const typename WideKvLds<D>::Stats& here, __bf16* qn,
                         __bf16* gn, typename WideKvLds<D>::Stats& next) {
@@ -1389,6 +1410,8 @@ __global__ __launch_bounds__(kThreads) void grad_kv_kernel(AttnArgs a) {
     row_lo = min(rows, row_lo + split * each);
     row_hi = min(rows, row_lo + each);
   }
+  // Rows before this one see at most one key, where that key is the tile's first.
+  const int one_key = key0 > 0 ? 0 : s.nk == 1 ? rows : a.causal ? max(0, s.nq - s.nk + 1) * a.G : 0;
   const char* krow = a.k.at + (static_cast<int64_t>(s.k0) + key) * a.k.row + hk * a.k.head;
   const char* vrow = a.v.at + (static_cast<int64_t>(s.k0) + key) * a.v.row + hk * a.v.head;
   Frag kf[D / 32], vf[D / 32];
@@ -1447,6 +1470,11 @@ __global__ __launch_bounds__(kThreads) void grad_kv_kernel(AttnArgs a) {
           const bool seen = key < lim[i];
           p[half][i] = seen ? __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i], a.c2, -l4[i])) : 0.f;
           ds[half][i] = seen ? p[half][i] * (dp[i] - d4[i]) : 0.f;
+        }
+        if (r < one_key) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (lim[i] == 1) ds[half][i] = 0.f;
         }
       }
       const Frag pf = Op<E>::pack(p[0], p[1]), df = Op<E>::pack(ds[0], ds[1]);
