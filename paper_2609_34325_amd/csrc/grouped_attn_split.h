@@ -73,7 +73,8 @@ inline size_t round256(size_t n) { return (n + 255) & ~size_t(255); }
 inline size_t forward_bytes(const Sizes& z) {
   const Split p = forward_split(z, -1);
   if (p.splits == 1 && !p.chunk) return 256;
-  return round256(static_cast<size_t>(p.blocks) * z.Hk * p.part_rows * (z.D + 2) * sizeof(float));
+  // 0 is for sizes out of range: no queries have parts of no rows
+  return std::max<size_t>(256, round256(static_cast<size_t>(p.blocks) * z.Hk * p.part_rows * (z.D + 2) * sizeof(float)));
 }
 inline size_t stat_bytes(const Sizes& z) { return round256(static_cast<size_t>(z.total_q) * z.H * sizeof(float2)); }
 inline size_t backward_bytes(const Sizes& z) {
