@@ -1249,7 +1249,11 @@ def dora_residual_norm_backward(dy: Optional[torch.Tensor], h: torch.Tensor, a: 
             raise ValueError(f"{name} without {name[1:]}")
         if t is not None and grads[i] is None:
             grads[i] = torch.empty(sizes[i], dtype=torch.float32, device=h.device)
-    rows, at, device = _describe(("dy", "dh", "h", "a", "dx", "da"), dy, dh, h, None if same else a, dx, da)
+    rows, at, device = _describe(("dy", "dh", "h", "a", "dx", "da"), dy, dh, h, a, dx, da)
+    if same:  # not read, but a's gradient has its sizes and type
+        if a.shape != h.shape or a.dtype != h.dtype:
+            raise DoraError("dora_residual_norm_backward", DORA_ERR_SHAPE if a.shape != h.shape else DORA_ERR_DTYPE)
+        at[3] = 0
     _vectors(_NORM + ("workspace",) + _NORM_GRADS, device, C, gamma, C, beta, C, scale, T, gate, C, post_gamma, C,
              post_beta, -1, workspace, *(x for pair in zip(sizes, grads) for x in pair))
     _call("dora_residual_norm_backward", None, *at[:4], gamma, scale, gate, post_gamma, post_beta, code,
