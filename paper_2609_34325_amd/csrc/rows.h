@@ -72,52 +72,72 @@ inline bool meets_itself(const dora_rows* t) {
   return (b.pieces > 1 && b.gap < b.len) || (b.n > 1 && b.step < b.block_bytes());
 }
 
-// Two tensors share memory.  Tensors whose rows lie between each other's (slices
-// of one product) need one and the same distance between rows to be told apart;
-// with different ones they count as sharing.
+// The same memory with what is read again and again (strides of 0) once.
+inline Blocks blocks_read(const dora_rows* t) {
+  Blocks b = blocks_of(t);
+  if (b.step == 0) b.n = 1;
+  if (b.gap == 0) b.pieces = 1;
+  return b;
+}
+
+// Some x = p gap, 0 <= p < n, lies in (lo, hi).
+inline bool step_between(int64_t n, int64_t gap, int64_t lo, int64_t hi) {
+  if (hi <= 0 || lo >= (n - 1) * gap || hi - lo < 2) return false;
+  if (lo < 0) return true;  // x = 0
+  return gap > 0 && (lo / gap + 1) * gap < hi;
+}
+
+// Two tensors share memory.  Tensors whose rows and heads lie between each other's
+// (slices of one product) need one and the same distance between the outer of the
+// two to be told apart; with different ones they count as sharing.
 inline bool rows_meet(const dora_rows* s, const dora_rows* t) {
   if (!s || !t || s->rows == 0 || t->rows == 0) return false;
-  Blocks a = blocks_of(s), b = blocks_of(t);
+  Blocks a = blocks_read(s), b = blocks_read(t);
   if (!Extent(reinterpret_cast<void*>(a.at), static_cast<size_t>(a.bytes()))
            .meets(Extent(reinterpret_cast<void*>(b.at), static_cast<size_t>(b.bytes()))))
     return false;
+  // Blocks of one piece each are the pieces of one block as well.
+  if (a.step != b.step && a.pieces == 1 && (b.pieces > 1 || a.n >= b.n)) a = Blocks{a.at, 1, 0, a.n, a.step, a.len};
+  else if (a.step != b.step && b.pieces == 1) b = Blocks{b.at, 1, 0, b.n, b.step, b.len};
   if (a.n == 1) a.step = b.step;
   if (b.n == 1) b.step = a.step;
   if (a.n == 1 && b.n == 1) a.step = b.step = a.block_bytes() + b.block_bytes();
-  if (a.step != b.step || a.step == 0) return true;
+  if (a.step != b.step) return true;
+  if (a.pieces == 1) a.gap = b.gap;
+  if (b.pieces == 1) b.gap = a.gap;
   // Block r of b begins at shift + (r - q) step from block q of a.
   const int64_t shift = static_cast<int64_t>(b.at - a.at);
   int64_t lo = (-b.block_bytes() - shift) / a.step - 1, hi = (a.block_bytes() - shift) / a.step + 1;
   if (lo < -(a.n - 1)) lo = -(a.n - 1);
   if (hi > b.n - 1) hi = b.n - 1;
-  if ((hi - lo + 1) * a.pieces > 4096) return true;
-  for (int64_t k = lo; k <= hi; ++k)
-    for (int64_t p = 0; p < a.pieces; ++p) {
-      const int64_t x = p * a.gap - (shift + k * a.step);  // a's piece, from the start of b's block
-      if (x + a.len <= 0 || x >= b.block_bytes()) continue;
-      if (b.pieces == 1 || b.gap == 0) return true;
-      for (int64_t q = x <= 0 ? 0 : x / b.gap; q < b.pieces && q * b.gap < x + a.len; ++q)
-        if (x < q * b.gap + b.len) return true;
+  const bool alike = a.gap == b.gap;  // then only the difference of two pieces' numbers counts
+  if ((hi - lo + 1) * (alike ? 1 : a.pieces) > 4096) return true;
+  for (int64_t k = lo; k <= hi; ++k) {
+    const int64_t d = shift + k * a.step;  // b's block, from the start of a's
+    if (alike) {
+      // piece q of b meets piece p of a where -b.len < d + (q - p) gap < a.len
+      const int64_t first = d - (a.pieces - 1) * a.gap;
+      if (step_between(a.pieces + b.pieces - 1, a.gap, -b.len - first, a.len - first)) return true;
+      continue;
     }
+    for (int64_t p = 0; p < a.pieces; ++p)
+      if (step_between(b.pieces, b.gap, p * a.gap - d - b.len, p * a.gap - d + a.len)) return true;
+  }
   return false;
 }
 
 inline bool rows_meet(const dora_rows* s, Extent o) {
   if (!s || s->rows == 0 || !o.at || !o.bytes) return false;
-  const Blocks a = blocks_of(s);
+  const Blocks a = blocks_read(s);
   if (!Extent(reinterpret_cast<void*>(a.at), static_cast<size_t>(a.bytes())).meets(o)) return false;
   // The vector against each run of the blocks that it could touch.
   const int64_t from = static_cast<int64_t>(o.at - a.at), to = from + static_cast<int64_t>(o.bytes);
-  if (a.n > 1 && a.step == 0) return true;
   int64_t lo = a.n > 1 ? (from - a.block_bytes()) / a.step - 1 : 0, hi = a.n > 1 ? to / a.step + 1 : 0;
   if (lo < 0) lo = 0;
   if (hi > a.n - 1) hi = a.n - 1;
-  if ((hi - lo + 1) * a.pieces > 4096) return true;
+  if (hi - lo > 4096) return true;  // a vector that long holds whole blocks
   for (int64_t k = lo; k <= hi; ++k)
-    for (int64_t p = 0; p < a.pieces; ++p) {
-      const int64_t x = k * a.step + p * a.gap;
-      if (x < to && from < x + a.len) return true;
-    }
+    if (step_between(a.pieces, a.gap, from - a.len - k * a.step, to - k * a.step)) return true;
   return false;
 }
 
