@@ -690,19 +690,22 @@ struct WideForward {
 };
 
 // Values that are not finite among keys that some rows do not see: 0 times them is NaN.  The rows that see them take
-// them here (an infinite or NaN sum is what p times them gives), and zeros stand in their place.
+// them here (an infinite or NaN sum is what p times them gives, NaN where p is 0 or NaN itself), and zeros stand in their
+// place.  alive[n] bit i: p of key 32 n + i is above 0.
 template <int D>
-__device__ __forceinline__ void take_odd(WideForward<D>& f, __bf16* vs, int end) {
+__device__ __forceinline__ void take_odd(WideForward<D>& f, __bf16* vs, int end, const uint32_t (&alive)[2]) {
   const int hi = (threadIdx.x & 63) >> 5;
-  for (int at = 0; at < min(end, kWideKeys); ++at)
+  for (int at = 0; at < min(end, kWideKeys); ++at) {
+    const bool counts = alive[at / 32] >> at % 32 & 1;
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
       for (int x = 0; x < 16; ++x) {
         const int d = 32 * dt + wide_place(x) + 4 * hi;
         const float v = static_cast<float>(vs[wide_at(at, d)]);
-        if (!(__builtin_fabsf(v) < INFINITY)) f.o[dt][x] += v;
+        if (!(__builtin_fabsf(v) < INFINITY)) f.o[dt][x] += counts ? v : NAN;
       }
+  }
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < kWideKeys * D / 8 / kThreads; ++i) {
@@ -720,7 +723,7 @@ __device__ __forceinline__ void wide_keys(const AttnArgs& a, WideForward<D>& f, 
                                           const WidePlaces& w, int end, bool masked, bool odd, bool idle) {
   const int hi = (threadIdx.x & 63) >> 5;
   if (idle) {
-    if (odd) take_odd<D>(f, vs, 0);
+    if (odd) take_odd<D>(f, vs, 0, {0u, 0u});
     return;
   }
   floatx16 s[2];
@@ -758,7 +761,17 @@ __device__ __forceinline__ void wide_keys(const AttnArgs& a, WideForward<D>& f, 
       s[n][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][i], a.c2, -ref));
       f.l += s[n][i];
     }
-  if (odd) take_odd<D>(f, vs, end);
+  if (odd) {
+    uint32_t alive[2] = {0u, 0u};
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) alive[n] |= s[n][i] > 0.f ? 1u << (wide_place(i) + 4 * hi) : 0u;
+      const auto halves = __builtin_amdgcn_permlane32_swap(alive[n], alive[n], false, false);
+      alive[n] = halves[0] | halves[1];
+    }
+    take_odd<D>(f, vs, end, alive);
+  }
 #pragma unroll
   for (int n = 0; n < 2; ++n)
 #pragma unroll
