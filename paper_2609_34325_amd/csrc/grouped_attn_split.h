@@ -47,10 +47,12 @@ inline Split forward_split(const Sizes& z, int32_t max_k) {
     // Every sequence is one tile: parts of the same number of keys, as many as fill the GPU once, 128 keys or more and at
     // most 32 a sequence, by the average.  A part's 64 keys take 1.3 us one after another, the parts' join 4 to 5: whole
     // sequences where the longest is short, 64 of 400 keys and 8 key heads of 128 25 us whole and 35 split, one of 512 12.5
-    // in two parts and 10 in four.  Where the longest is not known, an average can hide one that would be slow whole.
+    // in two parts and 10 in four.  Where the longest is not known, any one may have all the keys: whole only where those are few
+    // tiles.  (One list of 60000 among 500 of one key, 8 key heads of 128: 1268 us whole, 86 in parts; 100 of 100 keys 17 and
+    // 19; 64 of 120, 12 of 64, 7.4 and 12.8, the call's own launches: a caller who knows the longest has them whole.)
     const int64_t keys = z.total_k / z.B, want = std::max(z.total_k * z.Hk / kFill, keys / 32);
     const int64_t chunk = std::min<int64_t>(4096, std::max<int64_t>(128, (want + 63) / 64 * 64));
-    const bool whole = max_k > 0 ? max_k <= std::max<int64_t>(chunk, 256) : max_k == 0 && (keys <= 128 || z.total_k <= 512);
+    const bool whole = max_k > 0 ? max_k <= std::max<int64_t>(chunk, 256) : max_k == 0 && z.total_k <= 1024;
     // The workspace is sized for these parts: whole sequences are not cut again below, where a part keeps kTile rows.
     if (whole) return Split{1, 0, kTile, n};
     return Split{1, static_cast<int32_t>(chunk), static_cast<int32_t>(rows), tiles(z.total_k, z.B, chunk)};
