@@ -66,3 +66,73 @@ def test_one_long_list_among_short_ones(gpu, dtype, at):
     t, cu_q, cu_k = make([1] * 501, nk, 4, 2, 64, dtype, at)
     for max_k in (0, 60000):
         forward(gpu, t, cu_q, cu_k, 1, True, f"longest {max_k}", max_k=max_k)
+
+
+def both(gpu, nq, nk, H, Hk, D, dtype, causal, seed, what):
+    t, cu_q, cu_k = make(nq, nk, H, Hk, D, dtype, seed)
+    d, cq, ck, out, lse = forward(gpu, t, cu_q, cu_k, max(nq), causal, what)
+    *grads, st = gpu.dora_grouped_attn_backward(d["dout"], d["q"], d["k"], d["v"], out, lse, cq, max(nq), cu_k=ck, causal=causal)
+    assert int(st) == 0
+    want, bound = ref.attention(t["q"], t["k"], t["v"], cu_q, cu_k, causal, dout=t["dout"], out=out.cpu(), lse=lse.cpu())
+    for n, x in zip(("dq", "dk", "dv"), grads):
+        ref.check(x, want[n], bound[n], f"{what} {n}")
+
+
+def lengths(B, lo, hi, seed, empty=9):
+    """B lengths, tiles' own among them (one with a number of tiles that holds none beside it), every `empty`th 0."""
+    g = torch.Generator().manual_seed(seed)
+    n = torch.randint(lo, hi + 1, (B,), generator=g)
+    n[::5] = 64 if lo <= 64 <= hi else hi
+    n[1::7] = min(128, hi)
+    n[empty - 1::empty] = 0
+    return n.tolist()
+
+
+# sequences on both sides of a wave's 64 boundaries, of about one tile to four (whose numbers are turned), of the kernels of 64
+# and of 128 rows and keys
+@pytest.mark.parametrize("B", [63, 64, 65, 130])
+@pytest.mark.parametrize("dtype,D,lo,hi,causal", [(torch.bfloat16, 64, 20, 64, True), (torch.bfloat16, 64, 40, 140, False),
+                                                  (torch.bfloat16, 64, 150, 260, True), (torch.bfloat16, 128, 30, 128, True),
+                                                  (torch.bfloat16, 128, 90, 200, False), (torch.bfloat16, 32, 40, 140, True),
+                                                  (torch.float32, 32, 40, 140, False), (torch.float32, 64, 30, 100, True)])
+def test_many_sequences(gpu, B, dtype, D, lo, hi, causal):
+    lens = lengths(B, lo, hi, B + hi)
+    both(gpu, lens, lens, 2, 1 if hi < 150 else 2, D, dtype, causal, B, f"{B}")
+
+
+@pytest.mark.parametrize("B", [64, 66])
+@pytest.mark.parametrize("dtype,D", itertools.product(DTYPES, (64, 128)))
+def test_own_boundaries_of_many(gpu, B, dtype, D):
+    """Queries without keys, keys without queries, more of either, rows that see nothing."""
+    both(gpu, lengths(B, 1, 150, 1, 8), lengths(B, 1, 190, 2, 11), 3, 1, D, dtype, True, B, "causal")
+    both(gpu, lengths(B, 1, 70, 3, 8), lengths(B, 100, 250, 4, 11), 2, 2, D, dtype, False, B, "full")
+
+
+@pytest.mark.parametrize("B", [63, 64, 65, 130])
+@pytest.mark.parametrize("dtype,D,nq", [(torch.bfloat16, 128, 1), (torch.bfloat16, 64, 3), (torch.float32, 32, 1)])
+def test_new_tokens_of_many(gpu, B, dtype, D, nq):
+    """Their lists of keys in parts and joined: longer and shorter than a part, a part exactly, none; the longest known too."""
+    nk = lengths(B, 1, 900, B, 10)
+    nk[::13], nk[2::17] = [2000] * len(nk[::13]), [192] * len(nk[2::17])
+    t, cu_q, cu_k = make([nq] * B, nk, 4, 2, D, dtype, B)
+    for max_k in (0, 2000):
+        forward(gpu, t, cu_q, cu_k, nq, True, f"longest {max_k}", max_k=max_k)
+
+
+@pytest.mark.parametrize("dtype,D", itertools.product(DTYPES, (32, 64, 128)))
+def test_parts_of_rows_of_many(gpu, dtype, D):
+    """More than 64 sequences of few keys and many rows: dk and dv in parts of rows, joined."""
+    B = 66
+    nk = lengths(B, 1, 12, 5, 9)
+    both(gpu, [130] * B, nk, 8, 1, D, dtype, False, 6, "parts of rows")
+
+
+@pytest.mark.parametrize("dtype,D", itertools.product(DTYPES, (64, 128)))
+def test_parts_of_keys_of_many(gpu, dtype, D):
+    """More than 64 sequences of several tiles of rows and long lists of keys: the tiles' keys in parts, joined."""
+    B = 66
+    nq = lengths(B, 1, 70, 7, 9)
+    nk = [n + 1100 for n in lengths(B, 1, 100, 8, 9)]
+    nk[3], nk[11] = 0, 70
+    t, cu_q, cu_k = make(nq, nk, 1, 1, D, dtype, 9)
+    forward(gpu, t, cu_q, cu_k, max(nq), True, "parts of keys")
