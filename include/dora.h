@@ -793,8 +793,8 @@ int dora_grouped_attn_backward(const dora_rows* dout, const dora_rows* q, const 
  *
  *   x, a       HOST descriptions of matrices [T, C] (heads 1), read during the
  *              call; a NULL: h = x (then scale, gate, post_gamma and post_beta
- *              are NULL, and h_out may be).  16-byte aligned throughout, rows of
- *              16 .. 32768 bytes, a multiple of 16.
+ *              are NULL, and h_out may be).  16-byte aligned throughout, C at most
+ *              8192 and rows a multiple of 16 bytes.
  *   gamma, beta, scale, post_gamma, post_beta  fp32 [C]; gate fp32 [T]; each
  *              but gamma may be NULL (post_beta only without post_gamma too).
  *   eps        >= 0.

@@ -1186,8 +1186,8 @@ def dora_residual_norm(x: torch.Tensor, a: Optional[torch.Tensor], gamma: torch.
     """h = x + gate scale u and y = norm(h), u the branch's output a or (with
     post_gamma) its norm.
 
-    x, a: [T, C] bf16 or fp32, rows any distance apart; a None: the norm of x
-    alone.  gamma, beta, scale (layer scale), post_gamma, post_beta: fp32 [C];
+    x, a: [T, C] bf16 or fp32, C at most 8192, rows a multiple of 16 bytes and any
+    distance of such apart; a None: the norm of x alone.  gamma, beta, scale (layer scale), post_gamma, post_beta: fp32 [C];
     gate: fp32 [T], 0 drops a row's branch.  kind: "layer" or "rms".  h_out and
     y_out may be x or a.  Returns (h, y); h is x itself without a."""
     if stream is not None:
