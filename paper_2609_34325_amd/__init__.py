@@ -1092,8 +1092,9 @@ def dora_grouped_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: t
     128, bf16 or fp32, any strides of 16 bytes; cu_q, cu_k (cu_q when None):
     int32 [B + 1]; max_q: no sequence has more queries.  causal: query i of nq
     sees the keys j <= i + nk - nq, so one new token sees all.  max_k: no
-    sequence has more keys (0: not known); short lists then take one launch.  Returns (out
-    [total_q, H, D], lse [total_q, H] fp32 or None without keep_lse, dev_status)."""
+    sequence has more keys (0: not known); short lists then take one launch.
+    Returns (out [total_q, H, D], lse [total_q, H] fp32 or None without keep_lse,
+    dev_status)."""
     if stream is not None:
         with _in_stream(stream):
             return dora_grouped_attn(q, k, v, cu_q, max_q, cu_k, causal, softmax_scale, out, lse_out, keep_lse,
@@ -1187,9 +1188,10 @@ def dora_residual_norm(x: torch.Tensor, a: Optional[torch.Tensor], gamma: torch.
     post_gamma) its norm.
 
     x, a: [T, C] bf16 or fp32, C at most 8192, rows a multiple of 16 bytes and any
-    distance of such apart; a None: the norm of x alone.  gamma, beta, scale (layer scale), post_gamma, post_beta: fp32 [C];
-    gate: fp32 [T], 0 drops a row's branch.  kind: "layer" or "rms".  h_out and
-    y_out may be x or a.  Returns (h, y); h is x itself without a."""
+    distance of such apart; a None: the norm of x alone.  gamma, beta, scale (layer
+    scale), post_gamma, post_beta: fp32 [C]; gate: fp32 [T], 0 drops a row's branch.
+    kind: "layer" or "rms".  h_out and y_out may be x or a.  Returns (h, y); h is x
+    itself without a."""
     if stream is not None:
         with _in_stream(stream):
             return dora_residual_norm(x, a, gamma, beta, scale, gate, post_gamma, post_beta, kind, eps, h_out, y_out)

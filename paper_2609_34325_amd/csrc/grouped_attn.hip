@@ -17,8 +17,8 @@
 // Each forms P and dS for itself (seven products in place of five, eight for bf16
 // heads of 128), so that no sum goes through memory and results do not depend on
 // timing.  Eight packed sequences of up to 8192, 30497 rows, 32 query and 8 key
-// heads of 128, bf16, causal: forward 1.2 ms, grad_q 1.6, grad_kv 3.0; 660 to 700
-// TFLOP/s of seven products, 930 to 1000 of the ten that are formed, where a large
+// heads of 128, bf16, causal: forward 1.25 ms, grad_q 1.6, grad_kv 2.9 to 3.3; 650 to
+// 700 TFLOP/s of seven products, 930 to 1000 of the ten that are formed, where a large
 // library product reaches 1254 on the same card.  Sums of dq by atomics would save
 // three of the ten, and depend on timing.
 //
@@ -934,7 +934,8 @@ __device__ __forceinline__ float row_lse2(const AttnArgs& a, const Seq& s, int h
 // row has few keys (2^-9 of |dout||out|, and |out| falls as 1 / sqrt(keys)): 1.6 times the error of a form that rounds its
 // results alone, 1.4 without.  Where a tile's keys are staged at once (64, wide 128), delta is the sum of P dP over the sum
 // of P instead.  That sum is 1 but for lse's roundings, 2^-23 of its size: left out, dS of a row whose P is all on one key
-// keeps as much of dP (1e-4 of it at scores of 900), where it should vanish.
+// keeps as much of dP (1e-4 of it at scores of 900), where it should vanish.  S and dP are formed a second time for it: 128
+// sequences of 64, 8 heads of 64, backward 35.2 -> 36.6 us; 64 of 128, 16 on 4 of 128, 100 -> 106.
 __device__ __forceinline__ float mean_of(float sum, float weights) { return weights == 0.f ? 0.f : sum / weights; }
 
 // Keys whose dS counts, of `limit` that the row sees: of one key P is 1 whatever its score, and dS 0.
