@@ -136,3 +136,26 @@ def test_parts_of_keys_of_many(gpu, dtype, D):
     nk[3], nk[11] = 0, 70
     t, cu_q, cu_k = make(nq, nk, 1, 1, D, dtype, 9)
     forward(gpu, t, cu_q, cu_k, max(nq), True, "parts of keys")
+
+
+@pytest.mark.parametrize("dtype,D", itertools.product(DTYPES, (64, 128)))
+def test_heads_before_rows(gpu, dtype, D):
+    """q, k, v and their gradients as slices of [H, T, 3 D] tensors of thousands of rows: bit for bit the packed ones' results."""
+    H, lens = 3, [1500, 0, 700, 33]
+    t, cu, _ = make(lens, lens, H, H, D, dtype, 10)
+    d = {n: x.cuda() for n, x in t.items()}
+    c = torch.tensor(cu, dtype=torch.int32, device="cuda")
+    out, lse, _ = gpu.dora_grouped_attn(d["q"], d["k"], d["v"], c, 1500, causal=True)
+    grads = gpu.dora_grouped_attn_backward(d["dout"], d["q"], d["k"], d["v"], out, lse, c, 1500, causal=True)[:3]
+
+    def slices(x):
+        return [x[:, :, i * D:(i + 1) * D].transpose(0, 1) for i in range(3)]
+    qkv = slices(torch.full((H, cu[-1], 3 * D), 7.0, dtype=dtype, device="cuda"))
+    for x, n in zip(qkv, "qkv"):
+        x.copy_(d[n])
+    out2, lse2, _ = gpu.dora_grouped_attn(*qkv, c, 1500, causal=True)
+    assert torch.equal(out2, out) and torch.equal(lse2, lse)
+    into = slices(torch.full((H, cu[-1], 3 * D), 9.0, dtype=dtype, device="cuda"))
+    gpu.dora_grouped_attn_backward(d["dout"], *qkv, out, lse, c, 1500, causal=True, dq=into[0], dk=into[1], dv=into[2])
+    for x, want in zip(into, grads):
+        assert torch.equal(x, want)
